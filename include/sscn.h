@@ -248,6 +248,137 @@ SSCN_API sscn_status sscn_sgd_step(sscn_net* net, float* const* h_W32, void* con
                                    float* const* h_vW, float* const* h_vb, float lr, float momentum,
                                    float weight_decay, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators on plain arrays, without a net: layer norm, orthogonalised
+ * matrices, and the update that uses them.  The caller owns every buffer; the
+ * calls are asynchronous on `stream`, keep nothing between calls and can be
+ * captured into a graph.  A workspace is scratch during a call's kernels only:
+ * it may serve any number of calls and graphs, one at a time.  It must be
+ * 256-byte aligned.  dtype is an sscn_dtype.  Row r of an array with stride s
+ * starts s elements behind row r - 1 (s >= cols); elements between a row's end
+ * and the next row are neither read nor written.  Arrays must be aligned to
+ * their element type only. */
+
+/* Limits: rows of an array; columns of a layer norm; shorter and longer side of
+ * a matrix to orthogonalise; Newton-Schulz steps. */
+#define SSCN_MAX_ROWS 2147483647
+#define SSCN_NORM_MAX_COLS 1048576
+#define SSCN_ORTHO_MAX_SHORT 16384
+#define SSCN_ORTHO_MAX_LONG 1048576
+#define SSCN_ORTHO_MAX_STEPS 32
+
+/* Layer norm of every row of x [rows][cols] over its columns (the channels of an
+ * active site, or of the ground row: the norm works site by site, so inactive
+ * sites keep sharing one ground state):
+ *   mean = sum x / cols,  r = 1 / sqrt(sum (x - mean)^2 / cols + eps),
+ *   y = (x - mean) r gain + shift.
+ * x and y have type dtype, the arithmetic is float32; d_gain and d_shift are
+ * [cols] float32, each null for 1 and 0.  y may be x (same stride).  eps must be
+ * finite and > 0.  rows = 0 does nothing.  A row with a NaN or an infinity comes
+ * out as NaN and leaves the others alone. */
+SSCN_API sscn_status sscn_layer_norm_forward(int32_t dtype, const void* d_x, int64_t x_stride, int64_t rows,
+                                             int32_t cols, const float* d_gain, const float* d_shift, float eps,
+                                             void* d_y, int64_t y_stride, void* stream);
+
+/* Its backward pass from dy [rows][cols] (type dtype) and the forward's x, with
+ * h = (x - mean) r and t = dy gain:
+ *   dx = r (t - sum t / cols - h sum(t h) / cols)   (type dtype),
+ *   dgain = sum over rows of dy h,  dshift = sum over rows of dy   ([cols] float32).
+ * dgain and dshift are overwritten, each may be null; their sums are taken in an
+ * order that the shape alone decides.  dx may be dy or x (same stride).  With
+ * rows = 0 they are zero.  The workspace (needed when dgain or dshift is wanted
+ * and rows > 0) has sscn_layer_norm_workspace_bytes, which grows with rows. */
+SSCN_API sscn_status sscn_layer_norm_workspace_bytes(int32_t dtype, int64_t rows, int32_t cols, size_t* bytes);
+SSCN_API sscn_status sscn_layer_norm_backward(int32_t dtype, const void* d_dy, int64_t dy_stride, const void* d_x,
+                                              int64_t x_stride, int64_t rows, int32_t cols, const float* d_gain,
+                                              float eps, void* d_dx, int64_t dx_stride, float* d_dgain,
+                                              float* d_dshift, void* d_workspace, size_t workspace_bytes,
+                                              void* stream);
+
+/* One matrix for sscn_orthogonalize; in and out may be the same array. */
+typedef struct {
+  int64_t rows, cols;
+  const void* d_in;
+  int64_t in_stride;
+  void* d_out;
+  int64_t out_stride;
+} sscn_ortho_matrix;
+
+/* Orthogonalises n matrices (of any shapes, type dtype) by Newton-Schulz products:
+ *   X = in / |in|_F, transposed when rows > cols;
+ *   for each of `steps` steps with h_coef[3 s] = {a, b, c}:
+ *     A = X X^T,  X = a X + (b A + c A A) X;
+ *   out = X, transposed back.
+ * Every singular value s of X becomes a s + b s^3 + c s^5 per step; {3.4445,
+ * -4.7750, 2.0315} over five steps, as commonly used with Muon, brings them to
+ * about 0.7 .. 1.2.  X is float32 throughout and the products have float32
+ * accuracy whatever dtype is; the result is rounded once.  A zero matrix gives
+ * zeros, one with a NaN or an infinity NaN everywhere.  Coefficients must be
+ * finite and keep every singular value at most 3.5 and |b s^2 + c s^4| at most
+ * 200 (followed from [0, 1]), else SSCN_ERR_INVALID_ARGUMENT.  Matrices are
+ * worked on together: one call for many is faster than a call for each. */
+SSCN_API sscn_status sscn_orthogonalize_workspace_bytes(int32_t n, const sscn_ortho_matrix* h_matrices, size_t* bytes);
+SSCN_API sscn_status sscn_orthogonalize(int32_t dtype, int32_t n, const sscn_ortho_matrix* h_matrices, int32_t steps,
+                                        const float* h_coef, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* One parameter array for sscn_muon_update (contiguous, [rows][cols]). */
+typedef struct {
+  int64_t rows, cols;
+  float* d_w;        /* float32 master, updated in place                          */
+  void* d_w_store;   /* its copy in dtype, rewritten; null or equal to d_w: none   */
+  const float* d_g;  /* gradient                                                   */
+  float* d_v;        /* velocity, updated in place (zero before the first step)    */
+  float lr, weight_decay;
+  float scale;       /* factor of the orthogonal update (orthogonal != 0)          */
+  int32_t orthogonal;
+} sscn_muon_param;
+
+/* One update of n parameter arrays.  Where orthogonal != 0 (Muon):
+ *   v = momentum v + g;  u = nesterov ? g + momentum v : v;
+ *   w = w - lr (scale orthogonalise(u) + weight_decay w)
+ * with sscn_orthogonalize's steps and coefficients; elsewhere (biases, gains)
+ * sscn_sgd_step's rule: v = momentum v + (g + weight_decay w), w = w - lr v.
+ * No array may be named twice.  lr, weight_decay and momentum must be finite and
+ * >= 0, scale finite.  Without an orthogonal array, steps and h_coef are ignored
+ * and no workspace is needed. */
+SSCN_API sscn_status sscn_muon_workspace_bytes(int32_t n, const sscn_muon_param* h_params, size_t* bytes);
+SSCN_API sscn_status sscn_muon_update(int32_t dtype, int32_t n, const sscn_muon_param* h_params, float momentum,
+                                      int32_t nesterov, int32_t steps, const float* h_coef, void* d_workspace,
+                                      size_t workspace_bytes, void* stream);
+
+/* sscn_muon_update on a net's parameters, in the place of sscn_sgd_step: the same
+ * arrays, from the gradients of the last sscn_backward, with the same errors.
+ * Convolutions (and with softmax != 0 the softmax layer's matrix) take the
+ * orthogonal update with lr, weight_decay and scale = sqrt(max(1, cols / rows));
+ * the other arrays the SGD rule with lr_rest (weight_decay on the softmax
+ * layer's matrix, none on biases). */
+typedef struct {
+  float lr, lr_rest, momentum, weight_decay;
+  int32_t nesterov;
+  int32_t softmax;
+  int32_t steps;
+  const float* h_coef; /* [steps][3] */
+} sscn_muon_options;
+SSCN_API sscn_status sscn_net_muon_workspace_bytes(const sscn_net* net, const sscn_muon_options* options,
+                                                   size_t* bytes);
+SSCN_API sscn_status sscn_muon_step(sscn_net* net, float* const* h_W32, void* const* h_W, float* const* h_b,
+                                    float* const* h_vW, float* const* h_vb, const sscn_muon_options* options,
+                                    void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* Layer norm in front of the softmax layer: in every following pass each sample's
+ * top feature vector h_b (C_last values) becomes its layer norm with d_gain and
+ * d_shift, rounded to the storage dtype, before the last level's dropout and the
+ * softmax layer; sscn_backward also writes d_dgain and d_dshift.  All [C_last]
+ * float32.  The workspace has sscn_head_norm_workspace_bytes and stays untouched
+ * from sscn_forward through sscn_backward.  Null gain, shift, dgain, dshift and
+ * workspace switch the norm off; some of them null, or eps not finite and > 0, is
+ * SSCN_ERR_INVALID_ARGUMENT (a small or misaligned workspace
+ * SSCN_ERR_WORKSPACE).  A successful call ends the current pass, as
+ * sscn_set_dropout does. */
+SSCN_API sscn_status sscn_head_norm_workspace_bytes(const sscn_net* net, size_t* bytes);
+SSCN_API sscn_status sscn_set_head_norm(sscn_net* net, const float* d_gain, const float* d_shift, float* d_dgain,
+                                        float* d_dshift, float eps, void* d_workspace, size_t workspace_bytes);
+
 /* Online pen strokes -> sparse input with M = 9 features (Section 2.4): per
  * grid square the picture of the pen's path (feature 0, 1 where the pen went)
  * and an 8-bin histogram of its movement in the compass directions E, NE, N,
@@ -314,11 +445,11 @@ typedef enum {
   SSCN_KC_POOL_FWD = 4,
   SSCN_KC_POOL_BWD = 5,   /* routing through the windows, with the ground-row,
                              bias and ground-window sums of the conv below    */
-  SSCN_KC_HEAD = 6,       /* input scatter, weight packing, softmax, loss, scatter of dh */
+  SSCN_KC_HEAD = 6,       /* input scatter, weight packing, head norm, softmax, loss, scatter of dh */
   SSCN_KC_GROUND = 7,     /* bias and ground-window sums of a conv not under a
                              pooling layer; ground-row input gradient        */
   SSCN_KC_DROPOUT = 8,    /* dropped copies of the dropout levels' inputs      */
-  SSCN_KC_SGD = 9,        /* the parameter update of sscn_sgd_step             */
+  SSCN_KC_SGD = 9,        /* the parameter update of sscn_sgd_step, sscn_muon_step */
   SSCN_KC_CONV_NARROW = 10,/* convolution forward with few input channels (at most
                              32 products per output, e.g. the first layer of a
                              one-channel input) on the vector ALUs, with the

@@ -120,6 +120,16 @@ struct sscn_net {
   double rates[MAX_LAYERS] = {};
   uint64_t seed = 0;
   bool drop_on = false;  // the current pass applies dropout (a training pass with rates set)
+  // layer norm in front of the softmax layer, set by sscn_set_head_norm
+  const float* norm_gain = nullptr;  // null: none
+  const float* norm_shift = nullptr;
+  float* norm_dgain = nullptr;
+  float* norm_dshift = nullptr;
+  float norm_eps = 0.f;
+  void* hnorm = nullptr;      // [batch_max][Cp_top] normed rows (storage dtype)
+  float* hnorm_dy = nullptr;  // [batch_max][Cp_top] their gradient: split-K partials summed, dropout applied
+  float* hnorm_dx = nullptr;  // [batch_max][Cp_top] gradient of the rows below the norm
+  float* hnorm_part = nullptr;
   // kernel timing (HIP events around launcher calls of the selected classes)
   uint32_t tmask = 0;
   std::vector<hipEvent_t> ev_pool;
@@ -1081,14 +1091,30 @@ sscn_status sscn_forward(sscn_net* net, const void* d_feats, const void* const* 
   const LayerPlan& Lt = net->L[net->nlayers - 1];
   const ParamPlan& P = net->P[net->nconv];
   const DropArgs hdr = head_drop(net);
+  if (net->norm_gain) {  // one row per sample; its padding columns stay zero
+    NormArgs nm{};
+    nm.x = Lt.X;
+    nm.x_stride = Lt.Cp;
+    nm.rmap = net->head_rows;
+    nm.rows = net->batch;
+    nm.cols = Lt.C;
+    nm.gain = net->norm_gain;
+    nm.shift = net->norm_shift;
+    nm.eps = net->norm_eps;
+    nm.y = net->hnorm;
+    nm.y_stride = Lt.Cp;
+    nm.y_cols = Lt.Cp;
+    if (timed(net, SSCN_KC_HEAD, st, [&] { return launch_norm(net->bf16, nm, st); }) != hipSuccess) return SSCN_ERR_HIP;
+  }
   if (hdr.on && timed(net, SSCN_KC_DROPOUT, st, [&] {
-        return launch_head_drop(net->bf16, Lt.X, net->head_rows, net->batch, Lt.Cp, net->hdrop, hdr, st);
+        return launch_head_drop(net->bf16, net->norm_gain ? net->hnorm : Lt.X, net->norm_gain ? nullptr : net->head_rows,
+                                net->batch, Lt.Cp, net->hdrop, hdr, st);
       }) != hipSuccess)
     return SSCN_ERR_HIP;
   GemmArgs g{};
-  g.src = hdr.on ? net->hdrop : Lt.X;
+  g.src = hdr.on ? net->hdrop : net->norm_gain ? net->hnorm : Lt.X;
   g.src_stride = Lt.Cp;
-  g.rmap = hdr.on ? nullptr : net->head_rows;
+  g.rmap = hdr.on || net->norm_gain ? nullptr : net->head_rows;
   g.A = 1;
   g.cseg = Lt.Cp;
   g.K = Lt.Cp;
@@ -1168,6 +1194,36 @@ sscn_status sscn_backward(sscn_net* net, float* const* h_dW, float* const* h_db,
   hb.cp = Lt.Cp;
   hb.slope = net->slope;
   hb.drop = head_drop(net);
+  if (net->norm_gain) {  // through the dropout and the norm to the top rows' gradient
+    if (hb.ksplit > 1 || hb.drop.on) {
+      if (timed(net, SSCN_KC_HEAD, st, [&] { return launch_head_sum(hb, Lt.C, net->hnorm_dy, st); }) != hipSuccess)
+        return SSCN_ERR_HIP;
+      hb.dh_part = net->hnorm_dy;
+    }
+    NormBwdArgs nm{};
+    nm.dy = hb.dh_part;
+    nm.dy_stride = Lt.Cp;
+    nm.x = Lt.X;
+    nm.x_stride = Lt.Cp;
+    nm.rmap = net->head_rows;
+    nm.rows = net->batch;
+    nm.cols = Lt.C;
+    nm.gain = net->norm_gain;
+    nm.eps = net->norm_eps;
+    nm.dx = net->hnorm_dx;
+    nm.dx_stride = Lt.Cp;
+    nm.dx_cols = Lt.Cp;
+    nm.part = net->hnorm_part;
+    if (timed(net, SSCN_KC_HEAD, st, [&] {
+          return launch_norm_bwd(net->bf16, true, nm, net->norm_dgain, net->norm_dshift, st);
+        }) != hipSuccess)
+      return SSCN_ERR_HIP;
+    hb.dh_part = net->hnorm_dx;
+    hb.ksplit = 1;
+    hb.ks_stride = 0;
+    hb.dh_stride = Lt.Cp;
+    hb.drop = DropArgs{};
+  }
   hb.R = Lt.rules;
   hb.part = part_of(net, top);
   hb.PM = net->pool_parts;
@@ -1266,11 +1322,11 @@ sscn_status sscn_backward(sscn_net* net, float* const* h_dW, float* const* h_db,
   {
     WGradArgs& f = w[nw++];
     f = WGradArgs{};
-    const bool hd = head_drop(net).on;  // the softmax layer read its dropped input
-    f.src = hd ? net->hdrop : Lt.X;
+    const bool hd = head_drop(net).on, hn = net->norm_gain != nullptr;  // the softmax layer read its dropped or normed input
+    f.src = hd ? net->hdrop : hn ? net->hnorm : Lt.X;
     f.zero = zeros(net);
     f.src_stride = Lt.Cp;
-    f.rmap = hd ? nullptr : net->head_rows;
+    f.rmap = hd || hn ? nullptr : net->head_rows;
     f.A = 1;
     f.cseg = Lt.Cp;
     f.m_ones = P.m_ones;
@@ -1332,7 +1388,6 @@ sscn_status sscn_sgd_step(sscn_net* net, float* const* h_W32, void* const* h_W, 
   SgdArgs a;
   std::memset(&a, 0, sizeof(a));
   a.store_bf16 = net->bf16 ? 1 : 0;
-  a.lr = lr;
   a.momentum = momentum;
   int blocks = 0;
   auto add = [&](float* w, void* ws, const float* g, float* v, int64_t n, float wd) {
@@ -1343,6 +1398,7 @@ sscn_status sscn_sgd_step(sscn_net* net, float* const* h_W32, void* const* h_W, 
     J.v = v;
     J.n = n;
     J.wd = wd;
+    J.lr = lr;
     a.blk_beg[a.njobs] = blocks;
     blocks += (int)std::max<int64_t>(1, std::min<int64_t>(2048, (n + 255) / 256));
     ++a.njobs;
@@ -1360,6 +1416,112 @@ sscn_status sscn_sgd_step(sscn_net* net, float* const* h_W32, void* const* h_W, 
                  hipSuccess
              ? SSCN_OK
              : SSCN_ERR_HIP;
+}
+
+// The arrays of a Muon step: convolutions, the softmax layer's matrix, biases.
+static int muon_params(const sscn_net* net, const sscn_muon_options& o, sscn_muon_param* p) {
+  int n = 0;
+  for (int i = 0; i < net->nparams; ++i) {
+    const ParamPlan& P = net->P[i];
+    sscn_muon_param w{};
+    w.rows = (int64_t)P.A * P.c_in;
+    w.cols = P.c_out;
+    w.orthogonal = i < net->nconv || o.softmax;
+    w.lr = w.orthogonal ? o.lr : o.lr_rest;
+    w.weight_decay = o.weight_decay;
+    w.scale = (float)std::sqrt(std::max(1.0, (double)w.cols / (double)w.rows));
+    p[n++] = w;
+    sscn_muon_param b{};
+    b.rows = 1;
+    b.cols = P.c_out;
+    b.lr = o.lr_rest;
+    p[n++] = b;
+  }
+  return n;
+}
+
+sscn_status sscn_net_muon_workspace_bytes(const sscn_net* net, const sscn_muon_options* options, size_t* bytes) {
+  if (!net || !options || !bytes) return SSCN_ERR_INVALID_ARGUMENT;
+  sscn_muon_param p[2 * MAX_LAYERS];
+  return sscn_muon_workspace_bytes(muon_params(net, *options, p), p, bytes);
+}
+
+sscn_status sscn_muon_step(sscn_net* net, float* const* h_W32, void* const* h_W, float* const* h_b,
+                           float* const* h_vW, float* const* h_vb, const sscn_muon_options* options, void* d_ws,
+                           size_t ws_bytes, void* stream) {
+  if (!net || !h_W32 || !h_b || !h_vW || !h_vb || !options) return SSCN_ERR_INVALID_ARGUMENT;
+  if (!(options->lr >= 0.f) || !std::isfinite(options->lr) || !(options->lr_rest >= 0.f) ||
+      !std::isfinite(options->lr_rest) || !(options->momentum >= 0.f) || !std::isfinite(options->momentum) ||
+      !(options->weight_decay >= 0.f) || !std::isfinite(options->weight_decay))
+    return SSCN_ERR_INVALID_ARGUMENT;
+  if (!net->backwarded) return SSCN_ERR_BAD_STATE;
+  sscn_muon_param p[2 * MAX_LAYERS];
+  const int n = muon_params(net, *options, p);
+  for (int i = 0; i < net->nparams; ++i) {
+    if (!h_W32[i] || !h_b[i] || !h_vW[i] || !h_vb[i]) return SSCN_ERR_INVALID_ARGUMENT;
+    if (net->bf16 && (!h_W || !h_W[i])) return SSCN_ERR_INVALID_ARGUMENT;  // the forward reads the bf16 copy
+    sscn_muon_param &w = p[2 * i], &b = p[2 * i + 1];
+    w.d_w = h_W32[i];
+    w.d_w_store = h_W ? h_W[i] : nullptr;
+    w.d_g = net->dW[i];
+    w.d_v = h_vW[i];
+    b.d_w = h_b[i];
+    b.d_g = net->db[i];
+    b.d_v = h_vb[i];
+  }
+  sscn_status s = SSCN_OK;
+  const hipError_t e = timed(net, SSCN_KC_SGD, (hipStream_t)stream, [&] {
+    s = sscn_muon_update(net->bf16 ? SSCN_BF16 : SSCN_F32, n, p, options->momentum, options->nesterov, options->steps,
+                         options->h_coef, d_ws, ws_bytes, stream);
+    return hipSuccess;
+  });
+  return s != SSCN_OK ? s : e == hipSuccess ? SSCN_OK : SSCN_ERR_HIP;
+}
+
+// The head norm's buffers in its workspace.
+static size_t carve_head_norm(const sscn_net* net, void* base, void** rows, float** dy, float** dx, float** part) {
+  const LayerPlan& Lt = net->L[net->nlayers - 1];
+  Carver cv(base);
+  const size_t n = (size_t)net->d.batch_max * Lt.Cp;
+  void* r = cv.take(n * net->esz);
+  void* y = cv.take(n * 4);
+  void* x = cv.take(n * 4);
+  // (fewer samples may take as many partial rows, never more)
+  void* p = cv.take((size_t)norm_parts(net->bf16, net->d.batch_max, Lt.C) * Lt.C * 2 * sizeof(float));
+  if (rows) {
+    *rows = r;
+    *dy = (float*)y;
+    *dx = (float*)x;
+    *part = (float*)p;
+  }
+  return cv.off;
+}
+
+sscn_status sscn_head_norm_workspace_bytes(const sscn_net* net, size_t* bytes) {
+  if (!net || !bytes) return SSCN_ERR_INVALID_ARGUMENT;
+  *bytes = carve_head_norm(net, nullptr, nullptr, nullptr, nullptr, nullptr);
+  return SSCN_OK;
+}
+
+sscn_status sscn_set_head_norm(sscn_net* net, const float* d_gain, const float* d_shift, float* d_dgain,
+                               float* d_dshift, float eps, void* d_ws, size_t ws_bytes) {
+  if (!net) return SSCN_ERR_INVALID_ARGUMENT;
+  const bool off = !d_gain && !d_shift && !d_dgain && !d_dshift && !d_ws;
+  if (!off) {
+    if (!d_gain || !d_shift || !d_dgain || !d_dshift || !std::isfinite(eps) || !(eps > 0.f))
+      return SSCN_ERR_INVALID_ARGUMENT;
+    if (!d_ws || (uintptr_t)d_ws % 256 != 0 ||
+        ws_bytes < carve_head_norm(net, nullptr, nullptr, nullptr, nullptr, nullptr))
+      return SSCN_ERR_WORKSPACE;
+    carve_head_norm(net, d_ws, &net->hnorm, &net->hnorm_dy, &net->hnorm_dx, &net->hnorm_part);
+  }
+  net->norm_gain = d_gain;
+  net->norm_shift = d_shift;
+  net->norm_dgain = d_dgain;
+  net->norm_dshift = d_dshift;
+  net->norm_eps = eps;
+  net->forwarded = false;  // a backward pass must follow a forward pass with the same norm
+  return SSCN_OK;
 }
 
 static size_t encode_bytes(int64_t N, int64_t batch, int64_t max_sites, size_t* offs) {

@@ -40,8 +40,9 @@ __global__ void __launch_bounds__(256) k_dropout_rows(const T* X, T* Xd, int32_t
   }
 }
 
-// The softmax layer's input with dropout: hd[b] = X_top[head_rows[b]] times the
-// factors of row key b (every sample, the empty ones -- ground row -- included).
+// The softmax layer's input with dropout: hd[b] = X_top[head_rows[b]] (row b
+// without head_rows: normed rows) times the factors of row key b (every sample,
+// the empty ones -- ground row -- included).
 template <typename T>
 __global__ void __launch_bounds__(256) k_head_drop(const T* __restrict__ X_top, const int32_t* __restrict__ head_rows,
                                                    int32_t batch, int32_t cp, T* __restrict__ hd, DropArgs d) {
@@ -51,7 +52,7 @@ __global__ void __launch_bounds__(256) k_head_drop(const T* __restrict__ X_top, 
   for (int64_t t = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; t < total; t += (int64_t)gridDim.x * blockDim.x) {
     const int b = (int)(t / vpr);
     const int v = (int)(t - (int64_t)b * vpr);
-    Vec16 x = ((const Vec16*)(X_top + (int64_t)head_rows[b] * cp))[v];
+    Vec16 x = ((const Vec16*)(X_top + (int64_t)(head_rows ? head_rows[b] : b) * cp))[v];
 #pragma unroll
     for (int h = 0; h < VE / 4; ++h) {
       float f[4];

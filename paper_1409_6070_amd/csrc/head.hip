@@ -308,6 +308,26 @@ __global__ void __launch_bounds__(256) k_head_backward(HeadBwdArgs h, ExtraTask 
     h.part[((int64_t)k * h.cp + c) * h.PM + p] = ((red[0][k][cl] + red[1][k][cl]) + red[2][k][cl]) + red[3][k][cl];
 }
 
+// The softmax input's gradient as the norm in front of it takes it: split-K
+// partials added in split order, times the last level's dropout factors.
+__global__ void __launch_bounds__(256) k_head_sum(HeadBwdArgs h, int cols, float* __restrict__ dy) {
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (t >= (int64_t)h.batch * cols) return;
+  const int b = (int)(t / cols), c = (int)(t - (int64_t)b * cols);
+  float g = 0.f;
+#pragma unroll 4
+  for (int ks = 0; ks < h.ksplit; ++ks) g += h.dh_part[ks * h.ks_stride + (int64_t)b * h.dh_stride + c];
+  if (h.drop.on) g *= drop_factor(h.drop, (uint32_t)b, c);
+  dy[(int64_t)b * h.cp + c] = g;
+}
+
+hipError_t launch_head_sum(const HeadBwdArgs& h, int32_t cols, float* dy, hipStream_t st) {
+  const int64_t n = (int64_t)h.batch * cols;
+  if (n <= 0) return hipSuccess;
+  hipLaunchKernelGGL(k_head_sum, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, h, cols, dy);
+  return hipGetLastError();
+}
+
 // Partials (sample chunks of 8) of the head backward.
 int head_backward_parts(int32_t batch) { return std::max(1, (batch + 7) / 8); }
 

@@ -399,6 +399,8 @@ struct HeadBwdArgs {
   float* part;       // [(2 + AC) * cp * PM]
   int32_t PM;
 };
+// dy[b][c] = the split-K partials' sum of sample b times its dropout factor, c < cols (rows of h.cp)
+hipError_t launch_head_sum(const HeadBwdArgs& h, int32_t cols, float* dy, hipStream_t st);
 int head_backward_parts(int32_t batch);
 hipError_t launch_head_backward(bool bf16, const HeadBwdArgs& h, int32_t AC, hipStream_t st,
                                 const ExtraTask* extra = nullptr);
@@ -428,14 +430,87 @@ struct SgdJob {
   float* v;          // velocity
   int64_t n;
   float wd;          // weight decay
+  float lr;
 };
 struct SgdArgs {
   int32_t njobs;
   int32_t store_bf16;
-  float lr, momentum;
+  float momentum;
   int32_t blk_beg[MAX_SGD_JOBS + 1];
   SgdJob job[MAX_SGD_JOBS];
 };
 hipError_t launch_sgd(const SgdArgs& a, hipStream_t st);
+
+// layer_norm.hip: layer norm of rows over their columns
+struct NormArgs {
+  const void* x;
+  int64_t x_stride;     // elements between rows
+  const int32_t* rmap;  // row of x that row r reads (null: r)
+  int64_t rows;
+  int32_t cols;
+  const float* gain;    // [cols], null: 1
+  const float* shift;   // [cols], null: 0
+  float eps;
+  void* y;
+  int64_t y_stride;
+  int32_t y_cols;       // columns cols .. y_cols - 1 of y are set to zero
+};
+struct NormBwdArgs {
+  const void* dy;
+  int64_t dy_stride;
+  const void* x;
+  int64_t x_stride;
+  const int32_t* rmap;
+  int64_t rows;
+  int32_t cols;
+  const float* gain;
+  float eps;
+  void* dx;             // the type of dy
+  int64_t dx_stride;
+  int32_t dx_cols;      // columns cols .. dx_cols - 1 of dx are set to zero
+  float* part;          // [2][norm_parts][cols], null: no parameter gradients
+};
+// Partial rows of the parameter gradients (the backward kernel's workgroups).
+int64_t norm_parts(bool bf16, int64_t rows, int32_t cols);
+hipError_t launch_norm(bool bf16, const NormArgs& a, hipStream_t st);
+// f32_grads: dy and dx are float32 beside bf16 features.
+hipError_t launch_norm_bwd(bool bf16, bool f32_grads, const NormBwdArgs& a, float* dgain, float* dshift, hipStream_t st);
+
+// newton_schulz.hip: orthogonalised matrices, and the update that uses them
+constexpr int NS_MATS = 24;   // matrices of one group of launches
+constexpr int NS_SSQ = 1024;  // partial sums of a matrix's norm
+struct NsMat {
+  int32_t m, n;    // X: m <= n
+  int32_t mp, np;  // padded to the tile edge
+  int32_t tall;    // the caller's matrix is X transposed
+  int32_t nssq;
+  // workspace
+  float* X;        // [mp][np]
+  char* opX;       // operand with X's rows
+  char* opXt[2];   // operand with X's columns as rows, one step's read while the next's is written
+  char* opA;
+  char* opB;
+  double* ssq;
+  // the caller's
+  const void* u;   // matrix to orthogonalise, or gradient (float32)
+  int64_t u_stride;
+  void* o;         // result, or storage copy of the weights (may be null)
+  int64_t o_stride;
+  float* w;
+  float* v;
+  float scale, decay;  // w -= scale * orthogonal(u) + decay * w
+};
+struct NsArgs {
+  int32_t n;
+  int32_t parity;
+  int32_t nesterov;
+  float momentum;
+  float a, b, c;
+  int32_t beg[NS_MATS + 1];
+  NsMat mat[NS_MATS];
+};
+int ns_ssq_blocks(int64_t m, int64_t n);
+int ns_tile(int n, const int64_t* m);
+hipError_t launch_newton_schulz(NsArgs& a, int tile, bool bf16, bool muon, int steps, const float* coef, hipStream_t st);
 
 }  // namespace sscn

@@ -22,7 +22,7 @@ __global__ void __launch_bounds__(256) k_sgd(SgdArgs a) {
        i += nblk * blockDim.x) {
     const float w = J.w[i];
     const float v = a.momentum * J.v[i] + (J.g[i] + J.wd * w);
-    const float wn = w - a.lr * v;
+    const float wn = w - J.lr * v;
     J.v[i] = v;
     J.w[i] = wn;
     if (J.w_store) {

@@ -36,6 +36,9 @@ EXPORTED = [
     "sscn_timing_launches",
     "sscn_set_dropout", "sscn_philox4x32_10", "sscn_sgd_step", "sscn_encode_workspace_bytes", "sscn_encode_strokes",
     "sscn_encode_strokes_static",
+    "sscn_layer_norm_forward", "sscn_layer_norm_workspace_bytes", "sscn_layer_norm_backward",
+    "sscn_orthogonalize_workspace_bytes", "sscn_orthogonalize", "sscn_muon_workspace_bytes", "sscn_muon_update",
+    "sscn_net_muon_workspace_bytes", "sscn_muon_step", "sscn_head_norm_workspace_bytes", "sscn_set_head_norm",
 ]
 KERNEL_CLASSES = ["rulebook", "gather_gemm", "wgrad", "wgrad_reduce", "pool_fwd", "pool_bwd", "head", "ground",
                   "dropout", "sgd", "conv_narrow"]
@@ -63,6 +66,24 @@ class LayerView(ctypes.Structure):
     ]
 
 
+class OrthoMatrix(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("d_in", ctypes.c_void_p),
+                ("in_stride", ctypes.c_int64), ("d_out", ctypes.c_void_p), ("out_stride", ctypes.c_int64)]
+
+
+class MuonParam(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("d_w", ctypes.c_void_p),
+                ("d_w_store", ctypes.c_void_p), ("d_g", ctypes.c_void_p), ("d_v", ctypes.c_void_p),
+                ("lr", ctypes.c_float), ("weight_decay", ctypes.c_float), ("scale", ctypes.c_float),
+                ("orthogonal", ctypes.c_int32)]
+
+
+class MuonOptions(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_float), ("lr_rest", ctypes.c_float), ("momentum", ctypes.c_float),
+                ("weight_decay", ctypes.c_float), ("nesterov", ctypes.c_int32), ("softmax", ctypes.c_int32),
+                ("steps", ctypes.c_int32), ("h_coef", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -75,6 +96,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         raise RuntimeError(f"{path} is missing: build it with `python -m paper_1409_6070_amd.build`")
     lib = ctypes.CDLL(path)
     P, I32, VP, SZ = ctypes.POINTER, ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t
+    I64, F32 = ctypes.c_int64, ctypes.c_float
     sig = {
         "sscn_net_create": (I32, [P(NetDesc), P(VP)]),
         "sscn_net_destroy": (None, [VP]),
@@ -100,6 +122,17 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "sscn_encode_workspace_bytes": (I32, [I32, I32, I32, P(SZ)]),
         "sscn_encode_strokes": (I32, [I32, I32, VP, I32, VP, VP, I32, I32, VP, VP, I32, P(I32), VP, SZ, VP]),
         "sscn_encode_strokes_static": (I32, [I32, I32, VP, I32, VP, VP, I32, I32, VP, VP, I32, P(I32), VP]),
+        "sscn_layer_norm_forward": (I32, [I32, VP, I64, I64, I32, VP, VP, F32, VP, I64, VP]),
+        "sscn_layer_norm_workspace_bytes": (I32, [I32, I64, I32, P(SZ)]),
+        "sscn_layer_norm_backward": (I32, [I32, VP, I64, VP, I64, I64, I32, VP, F32, VP, I64, VP, VP, VP, SZ, VP]),
+        "sscn_orthogonalize_workspace_bytes": (I32, [I32, P(OrthoMatrix), P(SZ)]),
+        "sscn_orthogonalize": (I32, [I32, I32, P(OrthoMatrix), I32, P(F32), VP, SZ, VP]),
+        "sscn_muon_workspace_bytes": (I32, [I32, P(MuonParam), P(SZ)]),
+        "sscn_muon_update": (I32, [I32, I32, P(MuonParam), F32, I32, I32, P(F32), VP, SZ, VP]),
+        "sscn_net_muon_workspace_bytes": (I32, [VP, P(MuonOptions), P(SZ)]),
+        "sscn_muon_step": (I32, [VP, P(VP), P(VP), P(VP), P(VP), P(VP), P(MuonOptions), VP, SZ, VP]),
+        "sscn_head_norm_workspace_bytes": (I32, [VP, P(SZ)]),
+        "sscn_set_head_norm": (I32, [VP, VP, VP, VP, VP, F32, VP, SZ]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -274,8 +307,116 @@ def sscn_timing_launches(net, kernel_class: int, capacity: int, stream):
     return list(tags[:k]), list(ms[:k]), n.value
 
 
+def sscn_layer_norm_forward(dtype, d_x, x_stride, rows, cols, d_gain, d_shift, eps, d_y, y_stride, stream) -> None:
+    _check(load_library().sscn_layer_norm_forward(dtype, d_x, x_stride, rows, cols, d_gain, d_shift, eps, d_y, y_stride,
+                                                  stream), "sscn_layer_norm_forward")
+
+
+def sscn_layer_norm_workspace_bytes(dtype, rows, cols) -> int:
+    b = ctypes.c_size_t()
+    _check(load_library().sscn_layer_norm_workspace_bytes(dtype, rows, cols, ctypes.byref(b)),
+           "sscn_layer_norm_workspace_bytes")
+    return b.value
+
+
+def sscn_layer_norm_backward(dtype, d_dy, dy_stride, d_x, x_stride, rows, cols, d_gain, eps, d_dx, dx_stride, d_dgain,
+                             d_dshift, d_ws, ws_bytes, stream) -> None:
+    _check(load_library().sscn_layer_norm_backward(dtype, d_dy, dy_stride, d_x, x_stride, rows, cols, d_gain, eps, d_dx,
+                                                   dx_stride, d_dgain, d_dshift, d_ws, ws_bytes, stream),
+           "sscn_layer_norm_backward")
+
+
+def sscn_orthogonalize_workspace_bytes(matrices) -> int:
+    """matrices: a ctypes array of OrthoMatrix (rows and cols are read)."""
+    b = ctypes.c_size_t()
+    _check(load_library().sscn_orthogonalize_workspace_bytes(len(matrices), matrices, ctypes.byref(b)),
+           "sscn_orthogonalize_workspace_bytes")
+    return b.value
+
+
+def sscn_orthogonalize(dtype, matrices, steps, coef, d_ws, ws_bytes, stream) -> None:
+    _check(load_library().sscn_orthogonalize(dtype, len(matrices), matrices, steps, coef, d_ws, ws_bytes, stream),
+           "sscn_orthogonalize")
+
+
+def sscn_muon_workspace_bytes(params) -> int:
+    """params: a ctypes array of MuonParam (rows, cols and orthogonal are read)."""
+    b = ctypes.c_size_t()
+    _check(load_library().sscn_muon_workspace_bytes(len(params), params, ctypes.byref(b)), "sscn_muon_workspace_bytes")
+    return b.value
+
+
+def sscn_muon_update(dtype, params, momentum, nesterov, steps, coef, d_ws, ws_bytes, stream) -> None:
+    _check(load_library().sscn_muon_update(dtype, len(params), params, momentum, nesterov, steps, coef, d_ws, ws_bytes,
+                                           stream), "sscn_muon_update")
+
+
+def sscn_net_muon_workspace_bytes(net, options: MuonOptions) -> int:
+    b = ctypes.c_size_t()
+    _check(load_library().sscn_net_muon_workspace_bytes(net, ctypes.byref(options), ctypes.byref(b)),
+           "sscn_net_muon_workspace_bytes")
+    return b.value
+
+
+def sscn_muon_step(net, W32_ptrs, W_ptrs, b_ptrs, vW_ptrs, vb_ptrs, options: MuonOptions, d_ws, ws_bytes, stream) -> None:
+    _check(load_library().sscn_muon_step(net, _ptr_array(W32_ptrs), _ptr_array(W_ptrs) if W_ptrs is not None else None,
+                                         _ptr_array(b_ptrs), _ptr_array(vW_ptrs), _ptr_array(vb_ptrs),
+                                         ctypes.byref(options), d_ws, ws_bytes, stream), "sscn_muon_step")
+
+
+def sscn_head_norm_workspace_bytes(net) -> int:
+    b = ctypes.c_size_t()
+    _check(load_library().sscn_head_norm_workspace_bytes(net, ctypes.byref(b)), "sscn_head_norm_workspace_bytes")
+    return b.value
+
+
+def sscn_set_head_norm(net, d_gain, d_shift, d_dgain, d_dshift, eps, d_ws, ws_bytes) -> None:
+    _check(load_library().sscn_set_head_norm(net, d_gain, d_shift, d_dgain, d_dshift, eps, d_ws, ws_bytes),
+           "sscn_set_head_norm")
+
+
 # ---------------------------------------------------------------------------
 # convenience wrapper
+
+NORM_MAX_COLS = 1 << 20  # SSCN_NORM_MAX_COLS
+# coefficients (a, b, c) of the quintic commonly used with Muon
+MUON_COEF = (3.4445, -4.7750, 2.0315)
+_TYPES = {"f32": (SSCN_F32, torch.float32), "bf16": (SSCN_BF16, torch.bfloat16)}
+
+
+def _gpu_device(device) -> torch.device:
+    d = torch.device(device)
+    return torch.device("cuda", torch.cuda.current_device()) if d.type == "cuda" and d.index is None else d
+
+
+def _launch(device: torch.device, call):
+    """call(stream) on the device's current stream, with the device current."""
+    if device.index == torch.cuda.current_device():
+        return call(torch.cuda.current_stream(device).cuda_stream)
+    with torch.cuda.device(device):
+        return call(torch.cuda.current_stream(device).cuda_stream)
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _row_stride(t: torch.Tensor, what: str) -> int:
+    """Elements between the rows of a matrix whose rows are contiguous and do not overlap."""
+    rows, cols = t.shape
+    _need(cols <= 1 or t.stride(1) == 1, f"{what}: rows must be contiguous")
+    if rows <= 1:
+        return cols
+    _need(t.stride(0) >= cols, f"{what}: rows overlap")
+    return t.stride(0)
+
+
+def _coef_array(coef, steps):
+    """[steps][3] float32 from one triple for every step, or a triple per step."""
+    rows = [coef] * steps if not hasattr(coef[0], "__len__") else list(coef)
+    _need(len(rows) == steps and all(len(r) == 3 for r in rows), "coef: one (a, b, c), or one per step")
+    return (ctypes.c_float * max(3 * steps, 1))(*[x for r in rows for x in r])
 
 
 class SparseDeepCNet:
@@ -304,6 +445,8 @@ class SparseDeepCNet:
         self.loss = torch.empty(1, dtype=torch.float32, device=self.device)
         self.logits = None
         self._keep = []
+        self._muon_ws = None
+        self._norm_keep = None
 
     def __del__(self):
         h = getattr(self, "handle", None)
@@ -378,6 +521,43 @@ class SparseDeepCNet:
         sscn_sgd_step(self.handle, [t.data_ptr() for t in W32], [t.data_ptr() for t in W] if W is not None else None,
                       [t.data_ptr() for t in bs], [t.data_ptr() for t in vW], [t.data_ptr() for t in vb], lr,
                       momentum, weight_decay, _stream())
+
+    def muon_step(self, W32: Sequence[torch.Tensor], W: Optional[Sequence[torch.Tensor]], bs: Sequence[torch.Tensor],
+                  vW: Sequence[torch.Tensor], vb: Sequence[torch.Tensor], lr: float, lr_rest: float,
+                  momentum: float = 0.95, weight_decay: float = 0.0, nesterov: bool = True, softmax: bool = False,
+                  coef=MUON_COEF, steps: int = 5) -> None:
+        """Muon's update from the last backward's gradients, in the place of sgd_step: orthogonalised updates of
+        the convolutions (and with softmax=True of the softmax layer's matrix), momentum SGD with lr_rest elsewhere."""
+        for t in list(W32) + list(bs) + list(vW) + list(vb):
+            assert t.dtype == torch.float32 and t.is_contiguous()
+        if W is not None:
+            for t in W:
+                assert t.dtype == self.tdtype and t.is_contiguous()
+        arr = _coef_array(coef, steps)
+        opt = MuonOptions(lr, lr_rest, momentum, weight_decay, int(nesterov), int(softmax), steps, ctypes.addressof(arr))
+        need = sscn_net_muon_workspace_bytes(self.handle, opt)
+        if self._muon_ws is None or self._muon_ws.numel() < need:
+            self._muon_ws = torch.empty(max(need, 1), dtype=torch.uint8, device=self.device)
+        sscn_muon_step(self.handle, [t.data_ptr() for t in W32], [t.data_ptr() for t in W] if W is not None else None,
+                       [t.data_ptr() for t in bs], [t.data_ptr() for t in vW], [t.data_ptr() for t in vb], opt,
+                       self._muon_ws.data_ptr(), self._muon_ws.numel(), _stream())
+
+    def set_head_norm(self, gain: Optional[torch.Tensor], shift: Optional[torch.Tensor] = None, eps: float = 1e-5):
+        """Layer norm of the softmax layer's input with the given gain and shift ([C_last] float32, read by every
+        following pass); returns (dgain, dshift), which each backward overwrites. None switches it off."""
+        if gain is None:
+            sscn_set_head_norm(self.handle, None, None, None, None, 0.0, None, 0)
+            self._norm_keep = None
+            return None
+        c = self.param_shapes[-1][0]
+        for t in (gain, shift):
+            assert t.dtype == torch.float32 and t.is_contiguous() and t.numel() == c and t.device.type == "cuda"
+        ws = torch.empty(sscn_head_norm_workspace_bytes(self.handle), dtype=torch.uint8, device=self.device)
+        dgain, dshift = (torch.empty(c, dtype=torch.float32, device=self.device) for _ in range(2))
+        sscn_set_head_norm(self.handle, gain.data_ptr(), shift.data_ptr(), dgain.data_ptr(), dshift.data_ptr(), eps,
+                           ws.data_ptr(), ws.numel())
+        self._norm_keep = (gain, shift, dgain, dshift, ws)
+        return dgain, dshift
 
     def timing(self, classes: Sequence[str]) -> None:
         """Bracket launches of the named kernel classes with HIP events (empty: off)."""
@@ -463,3 +643,136 @@ class StrokeEncoder:
                                 batch, self.coords.data_ptr(), self.feats.data_ptr(), self.max_sites,
                                 self.ws.data_ptr(), self.ws_bytes, _stream())
         return self.coords[:n], self.feats[:n]
+
+
+class LayerNorm:
+    """Layer norm of feature rows [rows, cols] over their columns, through sscn_layer_norm_*; holds the backward
+    pass's workspace for up to rows_max rows. One stream at a time."""
+
+    def __init__(self, cols: int, rows_max: int, dtype: str = "bf16", eps: float = 1e-5, device: str = "cuda"):
+        if dtype not in _TYPES:
+            raise ValueError(dtype)
+        self.cols, self.rows_max, self.dtype, self.eps = cols, rows_max, dtype, eps
+        self.code, self.tdtype = _TYPES[dtype]
+        self.ws_bytes = sscn_layer_norm_workspace_bytes(self.code, rows_max, cols)
+        self.device = _gpu_device(device)
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
+
+    def _rows(self, t: torch.Tensor, rows: Optional[int], what: str) -> int:
+        _need(t.dtype == self.tdtype and t.device == self.device, f"{what}: {self.dtype} on {self.device}")
+        _need(t.dim() == 2 and t.shape[1] == self.cols and (rows is None or t.shape[0] == rows),
+              f"{what}: [{'rows' if rows is None else rows}, {self.cols}]")
+        return _row_stride(t, what)
+
+    def _param(self, t: Optional[torch.Tensor], what: str):
+        if t is None:
+            return None
+        _need(t.dtype == torch.float32 and t.device == self.device and t.is_contiguous() and t.numel() == self.cols,
+              f"{what}: [{self.cols}] float32 on {self.device}")
+        return t.data_ptr()
+
+    def forward(self, x: torch.Tensor, gain: Optional[torch.Tensor] = None, shift: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """out (may be x) or a new contiguous tensor; gain and shift [cols] float32, None for 1 and 0."""
+        xs = self._rows(x, None, "x")
+        rows = x.shape[0]
+        if out is None:
+            out = torch.empty(rows, self.cols, dtype=self.tdtype, device=self.device)
+        ys = self._rows(out, rows, "out")
+        g, s = self._param(gain, "gain"), self._param(shift, "shift")
+        _launch(self.device, lambda st: sscn_layer_norm_forward(
+            self.code, x.data_ptr(), xs, rows, self.cols, g, s, self.eps, out.data_ptr(), ys, st))
+        return out
+
+    def backward(self, dy: torch.Tensor, x: torch.Tensor, gain: Optional[torch.Tensor] = None,
+                 dx: Optional[torch.Tensor] = None):
+        """(dx, dgain, dshift) from the output's gradient and the forward's input; dx may be given (dy and x too)."""
+        xs = self._rows(x, None, "x")
+        rows = x.shape[0]
+        _need(rows <= self.rows_max, f"rows: at most {self.rows_max}")
+        if dx is None:
+            dx = torch.empty(rows, self.cols, dtype=self.tdtype, device=self.device)
+        ds, os = self._rows(dy, rows, "dy"), self._rows(dx, rows, "dx")
+        g = self._param(gain, "gain")
+        dgain = torch.empty(self.cols, dtype=torch.float32, device=self.device)
+        dshift = torch.empty(self.cols, dtype=torch.float32, device=self.device)
+        _launch(self.device, lambda st: sscn_layer_norm_backward(
+            self.code, dy.data_ptr(), ds, x.data_ptr(), xs, rows, self.cols, g, self.eps, dx.data_ptr(), os,
+            dgain.data_ptr(), dshift.data_ptr(), self.ws.data_ptr(), self.ws_bytes, st))
+        return dx, dgain, dshift
+
+
+class Orthogonalizer:
+    """Newton-Schulz orthogonalisation of matrices of fixed shapes, through sscn_orthogonalize; holds the workspace.
+    coef: (a, b, c) for every step, or one triple per step. One stream at a time."""
+
+    def __init__(self, shapes: Sequence, dtype: str = "bf16", coef=MUON_COEF, steps: int = 5, device: str = "cuda"):
+        if dtype not in _TYPES:
+            raise ValueError(dtype)
+        self.shapes = [(int(r), int(c)) for r, c in shapes]
+        self.code, self.tdtype = _TYPES[dtype]
+        self.steps, self.coef = steps, _coef_array(coef, steps)
+        self._mats = (OrthoMatrix * len(self.shapes))(*[OrthoMatrix(rows=r, cols=c) for r, c in self.shapes])
+        self.ws_bytes = sscn_orthogonalize_workspace_bytes(self._mats)
+        self.device = _gpu_device(device)
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
+
+    def orthogonalize(self, mats: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]] = None):
+        """out (may be mats) or new contiguous matrices, in the order of the shapes."""
+        if out is None:
+            out = [torch.empty(r, c, dtype=self.tdtype, device=self.device) for r, c in self.shapes]
+        _need(len(mats) == len(out) == len(self.shapes), f"{len(self.shapes)} matrices")
+        for m, i, o, shape in zip(self._mats, mats, out, self.shapes):
+            for t, what in ((i, "matrix"), (o, "out")):
+                _need(t.shape == shape and t.dtype == self.tdtype and t.device == self.device,
+                      f"{what}: {shape} {self.tdtype} on {self.device}")
+            m.d_in, m.in_stride = i.data_ptr(), _row_stride(i, "matrix")
+            m.d_out, m.out_stride = o.data_ptr(), _row_stride(o, "out")
+        _launch(self.device, lambda st: sscn_orthogonalize(self.code, self._mats, self.steps, self.coef,
+                                                           self.ws.data_ptr(), self.ws_bytes, st))
+        return out
+
+
+class Muon:
+    """Muon's update of parameter arrays of fixed shapes, through sscn_muon_update; holds the workspace. Matrices
+    take the orthogonalised update (orthogonal[i] says otherwise), vectors momentum SGD without weight decay.
+    dtype is that of the storage copies. One stream at a time."""
+
+    def __init__(self, shapes: Sequence, dtype: str = "bf16", coef=MUON_COEF, steps: int = 5,
+                 orthogonal: Optional[Sequence[bool]] = None, device: str = "cuda"):
+        if dtype not in _TYPES:
+            raise ValueError(dtype)
+        self.shapes = [tuple(int(n) for n in s) for s in shapes]
+        _need(all(len(s) in (1, 2) for s in self.shapes), "shapes: vectors and matrices")
+        orthogonal = [len(s) == 2 for s in self.shapes] if orthogonal is None else [bool(o) for o in orthogonal]
+        _need(len(orthogonal) == len(self.shapes), f"orthogonal: {len(self.shapes)} truth values")
+        self.code, self.tdtype = _TYPES[dtype]
+        self.steps, self.coef = steps, _coef_array(coef, steps)
+        self._params = (MuonParam * len(self.shapes))(*[
+            MuonParam(rows=s[0] if len(s) == 2 else 1, cols=s[-1], orthogonal=int(o),
+                      scale=max(1.0, s[-1] / s[0]) ** 0.5 if len(s) == 2 else 1.0)
+            for s, o in zip(self.shapes, orthogonal)])
+        self.ws_bytes = sscn_muon_workspace_bytes(self._params)
+        self.device = _gpu_device(device)
+        self.ws = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=self.device)
+
+    def step(self, W32: Sequence[torch.Tensor], W: Optional[Sequence[Optional[torch.Tensor]]],
+             grads: Sequence[torch.Tensor], vs: Sequence[torch.Tensor], lr: float, momentum: float = 0.95,
+             weight_decay: float = 0.0, nesterov: bool = True, lr_rest: Optional[float] = None) -> None:
+        """Updates the masters W32 and velocities vs in place and rewrites the copies W (None: no copies); lr_rest
+        (default lr) is the rate of the arrays that are not orthogonalised."""
+        n = len(self.shapes)
+        W = [None] * n if W is None else W
+        _need(len(W32) == len(W) == len(grads) == len(vs) == n, f"{n} arrays")
+        for p, s, w, c, g, v in zip(self._params, self.shapes, W32, W, grads, vs):
+            for t in (w, g, v):
+                _need(t.shape == s and t.dtype == torch.float32 and t.device == self.device and t.is_contiguous(),
+                      f"parameter: {s} float32 on {self.device}, contiguous")
+            _need(c is None or (c.shape == s and c.dtype == self.tdtype and c.device == self.device
+                                and c.is_contiguous()), f"copy: {s} {self.tdtype} on {self.device}, contiguous")
+            p.d_w, p.d_g, p.d_v = w.data_ptr(), g.data_ptr(), v.data_ptr()
+            p.d_w_store = None if c is None else c.data_ptr()
+            p.lr = lr if p.orthogonal or lr_rest is None else lr_rest
+            p.weight_decay = weight_decay if len(s) == 2 else 0.0
+        _launch(self.device, lambda st: sscn_muon_update(self.code, self._params, momentum, int(nesterov), self.steps,
+                                                         self.coef, self.ws.data_ptr(), self.ws_bytes, st))

@@ -1,0 +1,428 @@
+"""Newton-Schulz orthogonalisation and Muon's update on the GPU, against the formula in 64 bits.
+
+Bound of the orthogonalisation, as a 2-norm relative to the result.  Two sources of error, both propagated through
+the steps for the very matrix at hand, since the steps multiply an early error by the derivatives p'(s) that its
+singular values meet (up to 4 each):
+
+* float32 sums and roundings: the distance of the same steps computed here in float32;
+* operands split into two fp16 numbers: hi is off by at most 2^-11 of the entry, lo by at most 2^-11 of that, so the
+  operand by 2^-22 of the entry; the dropped lo lo is at most 2^-22 of the product.  Together at most 1.5 2^-22 of
+  each operand: the steps in 64 bits with every operand entry of every product off by that much, with random signs
+  (the largest distance of four trials).
+
+Three times their sum, and half a step of the result's type."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests.gpu_harness import log
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+MUON = (3.4445, -4.7750, 2.0315)
+
+
+@pytest.fixture(autouse=True, scope="module")
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_1409_6070_amd import sscn
+    sscn.load_library()
+
+
+def ns(u, dt, coef=MUON, steps=5, off=None):
+    """The formula in dtype dt on the CPU, with coefficients as float32 holds them; off: a generator of the signs
+    that put every product's operands off by 1.5 2^-22."""
+    def o(t):
+        if off is None:
+            return t
+        return t * (1 + 1.5 * 2.0 ** -22 * (2 * torch.randint(0, 2, t.shape, generator=off) - 1))
+    rows = [coef] * steps if not hasattr(coef[0], "__len__") else coef
+    x = u.double()
+    norm = x.norm()
+    x = (x / norm if norm > 0 else x).to(dt)
+    tall = x.shape[0] > x.shape[1]
+    x = x.t().contiguous() if tall else x
+    for r in rows:
+        a, b, c = (float(np.float32(v)) for v in r)
+        g = o(x) @ o(x).t()
+        x = a * x + o(b * g + c * (o(g) @ o(g))) @ o(x)
+    return x.t() if tall else x
+
+
+def _bound(u, dtype, coef=MUON, steps=5):
+    want = ns(u.cpu().float(), torch.float64, coef, steps)
+    f32 = ns(u.cpu().float(), torch.float32, coef, steps).double()
+    scale = max(want.norm().item(), 1e-300)
+    off32 = (f32 - want).norm().item() / scale
+    off22 = max((ns(u.cpu().float(), torch.float64, coef, steps, torch.Generator().manual_seed(k)) - want).norm().item()
+                for k in range(4 if u.numel() < 10 ** 6 else 1)) / scale
+    return want, 3 * (off32 + off22) + HALF[dtype]
+
+
+def _check(outs, mats, dtype, coef=MUON, steps=5):
+    for o, u in zip(outs, mats):
+        want, tol = _bound(u, dtype, coef, steps)
+        got = o.double().cpu()
+        assert torch.isfinite(got).all()
+        rel = (got - want).norm().item() / max(want.norm().item(), 1e-300)
+        log(f"  {tuple(u.shape)}: off {rel:.3g}, allowed {tol:.3g}")
+        assert rel <= tol
+
+
+def _rand(rows, cols, seed, dtype="f32", kind="gauss"):
+    g = torch.Generator().manual_seed(seed)
+    t = torch.randn(rows, cols, generator=g)
+    if kind == "spread":  # channels of differing size, a few strong directions
+        t = t * torch.exp(torch.randn(rows, 1, generator=g)) * torch.exp(torch.randn(1, cols, generator=g))
+        t = t + 3 * torch.randn(rows, 2, generator=g) @ torch.randn(2, cols, generator=g)
+    if kind == "rank":  # gradients of a batch of three
+        t = torch.randn(rows, 3, generator=g) @ torch.randn(3, cols, generator=g)
+    return t.to(torch.bfloat16 if dtype == "bf16" else torch.float32).cuda()
+
+
+# one row, one column, edges of the 32, 64 and 128 tiles, tall and wide; the largest take the 64 and 128 tiles
+SHAPES = [(1, 1), (1, 7), (7, 1), (2, 2), (9, 50), (31, 33), (32, 32), (33, 31), (64, 64), (65, 129), (100, 200), (200, 100),
+          (300, 300), (128, 1000), (1000, 128), (40, 5000), (300, 3755), (777, 777), (1433, 1500), (1500, 1433)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_one_matrix(shape, dtype):
+    from paper_1409_6070_amd.sscn import Orthogonalizer
+    u = _rand(*shape, seed=sum(shape), dtype=dtype, kind="spread")
+    log(f"[orthogonalize] {shape} {dtype}")
+    _check(Orthogonalizer([shape], dtype).orthogonalize([u]), [u], dtype)
+
+
+def test_large_matrix():
+    from paper_1409_6070_amd.sscn import Orthogonalizer
+    u = _rand(2900, 3011, 1)  # more 128-tiles than compute units
+    log("[orthogonalize] 2900 x 3011")
+    _check(Orthogonalizer([(2900, 3011)], "f32").orthogonalize([u]), [u], "f32")
+
+
+@pytest.mark.parametrize("kind", ["gauss", "spread", "rank"])
+def test_spectra(kind):
+    """Small and vanishing singular values: as exact as float32 products carry them."""
+    from paper_1409_6070_amd.sscn import Orthogonalizer
+    for shape in ((96, 96), (150, 400), (600, 200)):
+        u = _rand(*shape, seed=3, kind=kind)
+        log(f"[orthogonalize] {kind} {shape}")
+        _check(Orthogonalizer([shape], "f32").orthogonalize([u]), [u], "f32")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_matrices_equal_one_at_a_time_in_value(dtype):
+    """A list of 30 shapes (two groups) against the formula, and each alone within rounding of the list's."""
+    from paper_1409_6070_amd.sscn import Orthogonalizer
+    shapes = [(9 * (i % 5 + 1), 20 + 13 * i) for i in range(29)] + [(500, 260)]
+    mats = [_rand(*s, seed=i, dtype=dtype) for i, s in enumerate(shapes)]
+    log(f"[orthogonalize] list of {len(shapes)} {dtype}")
+    _check(Orthogonalizer(shapes, dtype).orthogonalize(mats), mats, dtype)
+
+
+def test_other_coefficients_and_step_counts():
+    from paper_1409_6070_amd.sscn import Orthogonalizer
+    u = _rand(70, 90, 4)
+    for coef, steps in (((1.5, -0.5, 0.0), 12), ((1.875, -1.25, 0.375), 9), (MUON, 1), (MUON, 2),
+                        ([(3.4445, -4.7750, 2.0315), (2.5, -2.0, 0.6), (1.5, -0.5, 0.0)], 3)):
+        log(f"[orthogonalize] {coef} x {steps}")
+        _check(Orthogonalizer([(70, 90)], "f32", coef=coef, steps=steps).orthogonalize([u]), [u], "f32", coef, steps)
+    o = Orthogonalizer([(70, 90)], "f32", coef=(1.5, -0.5, 0.0), steps=32).orthogonalize([u])[0].double().cpu()
+    assert (o @ o.t() - torch.eye(70, dtype=torch.float64)).abs().max() < 1e-5  # the cubic has converged
+
+
+@pytest.mark.parametrize("scale", [1e-38, 1e-30, 1e-8, 1.0, 1e18, 1e36])
+def test_the_size_of_a_matrix_does_not_matter(scale):
+    from paper_1409_6070_amd.sscn import Orthogonalizer
+    u = _rand(40, 60, 5) * scale
+    log(f"[orthogonalize] values of about {scale}")
+    _check(Orthogonalizer([(40, 60)], "f32").orthogonalize([u]), [u], "f32")
+
+
+def test_zero_and_bad_matrices_stay_alone():
+    from paper_1409_6070_amd.sscn import Orthogonalizer
+    shapes = [(40, 70)] * 4
+    mats = [_rand(40, 70, i) for i in range(4)]
+    plan = Orthogonalizer(shapes, "f32")
+    want = [o.clone() for o in plan.orthogonalize(mats)]
+    mats[1] = torch.zeros_like(mats[1])
+    mats[2] = mats[2].clone()
+    mats[2][39, 69] = float("nan")
+    mats[3] = mats[3].clone()
+    mats[3][0, 0] = float("inf")
+    got = plan.orthogonalize(mats)
+    assert torch.equal(got[0], want[0])
+    assert (got[1] == 0).all()
+    assert torch.isnan(got[2]).all() and torch.isnan(got[3]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_strides_in_place_and_guards(dtype):
+    from paper_1409_6070_amd.sscn import Orthogonalizer
+    tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    for shape, stride, start in (((50, 33), 37, 1), ((33, 50), 51, 3), ((129, 65), 65, 5)):
+        u = _rand(*shape, seed=6, dtype=dtype)
+        plan = Orthogonalizer([shape], dtype)
+        want = plan.orthogonalize([u])[0]
+        src = torch.full((start + shape[0] * stride + 9,), 7.5, dtype=tdt, device="cuda")
+        dst = src.clone()
+        vs, vd = (torch.as_strided(b, shape, (stride, 1), start) for b in (src, dst))
+        vs.copy_(u)
+        keep = src.clone()
+        plan.orthogonalize([vs], out=[vd])
+        assert torch.equal(vd, want) and torch.equal(src, keep)
+        mask = torch.ones_like(dst, dtype=torch.bool)
+        torch.as_strided(mask, shape, (stride, 1), start).fill_(False)
+        assert (dst[mask] == 7.5).all()
+        plan.orthogonalize([vs], out=[vs])
+        assert torch.equal(vs, want)
+
+
+def test_repeats_streams_and_graphs():
+    """The same bits every time: fresh and dirty workspace, another stream, a graph replayed between eager calls that
+    use the same workspace."""
+    from paper_1409_6070_amd.sscn import Orthogonalizer
+    shapes = [(200, 100), (64, 300), (9, 50)]
+    mats = [_rand(*s, seed=i) for i, s in enumerate(shapes)]
+    plan = Orthogonalizer(shapes, "f32")
+    want = [o.clone() for o in plan.orthogonalize(mats)]
+    plan.ws.fill_(0xFF)  # NaN everywhere in the workspace
+    assert all(torch.equal(a, b) for a, b in zip(plan.orthogonalize(mats), want))
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = plan.orthogonalize(mats)
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    out = [torch.empty_like(m) for m in mats]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan.orthogonalize(mats, out=out)
+    for i in range(4):
+        for m in mats:
+            m.add_(0.1 * i)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = plan.orthogonalize(mats)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), i
+
+
+def test_wrapper_refuses():
+    from paper_1409_6070_amd.sscn import Muon, Orthogonalizer, SSCNError
+    for bad in ([(0, 3)], [(20000, 20000)]):
+        with pytest.raises(SSCNError):
+            Orthogonalizer(bad)
+    with pytest.raises(ValueError):
+        Orthogonalizer([(3, 4)], "f16")
+    with pytest.raises(ValueError):
+        Orthogonalizer([(3, 4)], coef=[MUON] * 4, steps=5)
+    plan = Orthogonalizer([(8, 16)], "f32")
+    x = torch.randn(8, 16, device="cuda")
+    for mats in ([x, x], [], [x.bfloat16()], [x.cpu()], [x[:7]], [torch.randn(16, 8, device="cuda").t()],
+                 [x[:1].expand(8, 16)]):
+        with pytest.raises(ValueError):
+            plan.orthogonalize(mats)
+    with pytest.raises(SSCNError):
+        Orthogonalizer([(8, 16)], "f32", coef=(4.0, 0.0, 0.0)).orthogonalize([x])
+    with pytest.raises(ValueError):
+        Muon([(2, 3, 4)])
+    m = Muon([(8, 16), (16,)], "f32")
+    v = torch.zeros(16, device="cuda")
+    good = [[x, v], None, [x.clone(), v.clone()], [x.clone(), v.clone()]]
+    for i in (0, 2, 3):
+        for bad in ([x], [x, v, v], [x, v.double()], [x[:, :15], v], [x.t().contiguous().t(), v], [x.cpu(), v]):
+            with pytest.raises(ValueError):
+                m.step(*good[:i], bad, *good[i + 1:], lr=0.1)
+    with pytest.raises(ValueError):
+        m.step(good[0], [x.bfloat16(), None], *good[2:], lr=0.1)
+    with pytest.raises(SSCNError):
+        m.step(*good, lr=-0.1)
+
+
+# ---------------------------------------------------------------------------------------------------------
+# the update
+
+
+def _want_step(w, g, v, orthogonal, lr, momentum, wd, nesterov, scale):
+    """(w, tolerance of w, v): one update in 64 bits from float32 arrays."""
+    lr, momentum, wd = (float(np.float32(x)) for x in (lr, momentum, wd))
+    w, g, v = w.double().cpu(), g.double().cpu(), v.double().cpu()
+    if not orthogonal:
+        vn = momentum * v + (g + wd * w)
+        return w - lr * vn, 4 * U * (w.abs() + lr * (momentum * v.abs() + g.abs() + wd * w.abs())), vn
+    vn = momentum * v + g
+    u = g + momentum * vn if nesterov else vn
+    want, rel = _bound(u.float(), "f32")
+    # the float32 velocity and u are off by 3 u of their terms, which the steps (|p'| up to 4 each) enlarge at most by
+    # 4^5 = 1024 in norm: into the bound of the direction, as a share of its norm
+    terms = (momentum * v.abs() + g.abs()) * (1 + momentum) + g.abs()
+    rel = rel + 3 * U * 1024 * (terms.norm() / u.norm()).item() * (min(u.shape) ** 0.5 / want.norm().item())
+    tol_o = rel * want.norm().item()  # one entry may hold all of it
+    wn = w - lr * (scale * want + wd * w)
+    return wn, lr * scale * tol_o + 4 * U * (w.abs() + lr * (scale * want.abs() + wd * w.abs())), vn
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("nesterov", [True, False])
+def test_update_of_matrices_and_vectors(dtype, nesterov):
+    """Three steps of a list with tall, wide and single-row matrices, biases, and a matrix by the SGD rule."""
+    from paper_1409_6070_amd.sscn import Muon
+    shapes = [(9, 50), (50,), (200, 100), (100,), (300, 400), (1, 33), (70, 30), (1,)]
+    orth = [True, False, True, False, True, True, False, False]
+    tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    W = [_rand(s[0] if len(s) == 2 else 1, s[-1], i).reshape(s) for i, s in enumerate(shapes)]
+    V = [torch.zeros_like(w) for w in W]
+    C = [None if i in (3, 6) else torch.full(s, 7.0, dtype=tdt, device="cuda") for i, s in enumerate(shapes)]
+    plan = Muon(shapes, dtype, orthogonal=orth)
+    lr, mu, wd, rest = 0.02, 0.9, 0.1, 0.005
+    for k in range(3):
+        G = [_rand(s[0] if len(s) == 2 else 1, s[-1], 100 * k + i + 50).reshape(s) for i, s in enumerate(shapes)]
+        w0, v0 = [w.clone() for w in W], [v.clone() for v in V]
+        plan.step(W, C, G, V, lr=lr, momentum=mu, weight_decay=wd, nesterov=nesterov, lr_rest=rest)
+        torch.cuda.synchronize()
+        for i, s in enumerate(shapes):
+            scale = float(np.float32(max(1.0, s[-1] / s[0]) ** 0.5)) if len(s) == 2 else 1.0
+            want, tol, vn = _want_step(w0[i], G[i], v0[i], orth[i], lr if orth[i] else rest, mu,
+                                       wd if len(s) == 2 else 0.0, nesterov, scale)
+            got = W[i].double().cpu()
+            log(f"[muon] step {k} {s} {dtype}: at most {((got - want).abs() / (tol + 1e-30)).max():.3f} of the bound")
+            assert ((got - want).abs() <= tol + 1e-30).all()
+            assert ((V[i].double().cpu() - vn).abs() <= 4 * U * (mu * v0[i].double().cpu().abs() + G[i].double().cpu().abs()
+                                                                 + wd * w0[i].double().cpu().abs())).all()
+            if C[i] is not None:
+                assert torch.equal(C[i], W[i].to(tdt))  # the rounded master, bit for bit
+
+
+def test_update_without_matrices_is_the_sgd_rule():
+    """No workspace, no coefficients: a list longer than one launch holds."""
+    from paper_1409_6070_amd import sscn
+    n = 130
+    W, G, V = ([_rand(1, 10 + i, k * n + i).reshape(-1) for i in range(n)] for k in range(3))
+    W0, V0 = [w.clone() for w in W], [v.clone() for v in V]
+    arr = (sscn.MuonParam * n)(*[sscn.MuonParam(1, w.numel(), w.data_ptr(), None, g.data_ptr(), v.data_ptr(),
+                                                0.1 + 0.001 * i, 0.5, 0.0, 0)
+                                 for i, (w, g, v) in enumerate(zip(W, G, V))])
+    assert sscn.sscn_muon_workspace_bytes(arr) == 0
+    sscn.sscn_muon_update(sscn.SSCN_F32, arr, 0.9, 0, 0, None, None, 0, sscn._stream())
+    torch.cuda.synchronize()
+    for i in range(n):
+        want, tol, vn = _want_step(W0[i], G[i], V0[i], False, 0.1 + 0.001 * i, 0.9, 0.5, False, 0)
+        assert ((W[i].double().cpu() - want).abs() <= tol).all()
+
+
+def _net(dtype, arch="deepcnet", classes=40, seed=0):
+    from paper_1409_6070_amd.sscn import SparseDeepCNet
+    from workloads import he_params, random_labels
+    rng = np.random.default_rng(seed)
+    ell, k, c_in, batch = 3, 12, 2, 16
+    N = 3 * 2 ** ell
+    coords = np.concatenate([np.stack([np.full(30, b), *np.divmod(rng.choice(N * N, 30, replace=False), N)], 1)
+                             for b in range(batch)])
+    net = SparseDeepCNet(ell, k, c_in, classes, batch, len(coords), dtype, arch=arch)
+    feats = torch.tensor(rng.normal(size=(len(coords), c_in))).to(net.tdtype).cuda()
+    Ws, bs = he_params(ell, k, c_in, classes, 1, arch=arch)
+    W32 = [torch.tensor(w, dtype=torch.float32, device="cuda") for w in Ws]
+    b = [torch.tensor(v, dtype=torch.float32, device="cuda") for v in bs]
+    labels = torch.tensor(random_labels(batch, classes, 2), dtype=torch.int32, device="cuda")
+    net.rulebook_build(torch.tensor(coords, dtype=torch.int32, device="cuda"), batch)
+    return net, feats, W32, [w.to(net.tdtype) for w in W32], b, labels
+
+
+@pytest.mark.parametrize("dtype,arch,softmax", [("f32", "deepcnet", False), ("bf16", "deepcnet", True),
+                                                ("bf16", "deepcnin", False), ("f32", "deepcnin", True)])
+def test_muon_step_of_a_network(dtype, arch, softmax):
+    net, feats, W32, W, b, labels = _net(dtype, arch)
+    vW, vb = [torch.zeros_like(w) for w in W32], [torch.zeros_like(v) for v in b]
+    lr, rest, mu, wd = 0.03, 0.01, 0.95, 0.05
+    for k in range(2):
+        net.forward(feats, W, b, labels)
+        dW, db, _ = net.backward()
+        torch.cuda.synchronize()
+        keep = [[t.clone() for t in ts] for ts in (W32, dW, vW, b, db, vb)]
+        net.muon_step(W32, W, b, vW, vb, lr, rest, mu, wd, softmax=softmax)
+        torch.cuda.synchronize()
+        for i, w in enumerate(W32):
+            orth = softmax or i < len(W32) - 1
+            scale = float(np.float32(math.sqrt(max(1.0, w.shape[1] / w.shape[0]))))
+            want, tol, vn = _want_step(keep[0][i], keep[1][i], keep[2][i], orth, lr if orth else rest, mu, wd, True, scale)
+            log(f"[muon step] {dtype} {arch} step {k} matrix {i}")
+            assert ((w.double().cpu() - want).abs() <= tol + 1e-30).all()
+            assert torch.equal(W[i], w.to(net.tdtype))
+            want, tol, vn = _want_step(keep[3][i], keep[4][i], keep[5][i], False, rest, mu, 0.0, True, 0)
+            assert ((b[i].double().cpu() - want).abs() <= tol + 1e-30).all()
+
+
+def test_muon_step_needs_a_backward_and_has_its_times():
+    from paper_1409_6070_amd.sscn import SSCNError
+    net, feats, W32, W, b, labels = _net("bf16")
+    vW, vb = [torch.zeros_like(w) for w in W32], [torch.zeros_like(v) for v in b]
+    net.forward(feats, W, b, labels)
+    with pytest.raises(SSCNError) as e:
+        net.muon_step(W32, W, b, vW, vb, 0.02, 0.01)
+    assert e.value.name == "SSCN_ERR_BAD_STATE"
+    net.backward()
+    with pytest.raises(SSCNError) as e:
+        net.muon_step(W32, None, b, vW, vb, 0.02, 0.01)
+    assert e.value.name == "SSCN_ERR_INVALID_ARGUMENT"  # the bf16 copies
+    net.timing(["sgd"])
+    net.muon_step(W32, W, b, vW, vb, 0.02, 0.01)
+    n, ms = net.timing_collect("sgd")
+    net.timing([])
+    assert n == 1 and ms > 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_training_steps_with_a_head_norm_in_one_graph(dtype):
+    """A whole step (forward, backward, Muon on the matrices, the SGD rule on biases and the norm's gain and shift)
+    captured once and replayed gives what the eager calls give, bit for bit."""
+    from paper_1409_6070_amd.sscn import Muon
+    runs = []
+    for graphed in (False, True):
+        net, feats, W32, W, b, labels = _net(dtype)
+        c = W32[-1].shape[0]
+        gain, shift = torch.ones(c, device="cuda"), torch.zeros(c, device="cuda")
+        dgain, dshift = net.set_head_norm(gain, shift)
+        vW, vb = [torch.zeros_like(w) for w in W32], [torch.zeros_like(v) for v in b]
+        vn = [torch.zeros_like(gain), torch.zeros_like(shift)]
+        norms = Muon([(c,), (c,)], dtype)
+        net.forward(feats, W, b, labels)  # buffers and kernels are there before the capture
+        net.backward()
+
+        def step():
+            net.forward(feats, W, b, labels)
+            net.backward()
+            net.muon_step(W32, W, b, vW, vb, 0.02, 0.01)
+            norms.step([gain, shift], None, [dgain, dshift], vn, lr=0.01)
+
+        if graphed:
+            keep = [[t.clone() for t in ts] for ts in (W32, W, b, [gain, shift])]
+            step()  # the workspace of the update is allocated by the first step
+            torch.cuda.synchronize()
+            for ts, ks in zip((W32, W, b, [gain, shift]), keep):
+                for t, k in zip(ts, ks):
+                    t.copy_(k)
+            for t in (*vW, *vb, *vn):
+                t.zero_()
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                step()
+        got = []
+        for _ in range(4):
+            graph.replay() if graphed else step()
+            torch.cuda.synchronize()
+            got.append([net.loss.clone(), gain.clone(), shift.clone(), *[w.clone() for w in W32], *[v.clone() for v in vb]])
+        runs.append(got)
+    for k, (e, g) in enumerate(zip(*runs)):
+        assert all(torch.isfinite(t).all() for t in e)
+        for i, (p, q) in enumerate(zip(e, g)):
+            assert torch.equal(p, q), (k, i)
+    log(f"[training] {dtype}: losses {[float(r[0]) for r in runs[0]]}")

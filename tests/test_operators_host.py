@@ -1,0 +1,186 @@
+"""The host side of the layer norm, orthogonalisation and Muon calls: every refusal, and the workspace sizes
+(no kernel is launched)."""
+
+import ctypes
+import math
+
+import pytest
+
+from paper_1409_6070_amd import sscn
+
+FAKE = 1 << 20  # never dereferenced: every call below fails its host checks first
+COEF = (ctypes.c_float * 15)(*(sscn.MUON_COEF * 5))
+INVALID, BAD_STATE, WORKSPACE = 1, 5, 7
+
+
+def _fwd(dtype=0, x=FAKE, xs=8, rows=4, cols=8, eps=1e-5, y=FAKE, ys=8):
+    return sscn.load_library().sscn_layer_norm_forward(dtype, x, xs, rows, cols, None, None, eps, y, ys, None)
+
+
+def _bwd(dtype=0, dy=FAKE, ds=8, x=FAKE, xs=8, rows=4, cols=8, eps=1e-5, dx=FAKE, os=8, dg=FAKE, ws=FAKE, nb=1 << 20):
+    return sscn.load_library().sscn_layer_norm_backward(dtype, dy, ds, x, xs, rows, cols, None, eps, dx, os, dg, None,
+                                                        ws, nb, None)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(dtype=2), dict(dtype=-1), dict(x=None), dict(y=None), dict(rows=-1), dict(rows=1 << 31), dict(cols=0),
+    dict(cols=-3), dict(cols=sscn.NORM_MAX_COLS + 1, xs=1 << 21, ys=1 << 21), dict(xs=7), dict(ys=7), dict(xs=-8),
+    dict(eps=0.0), dict(eps=-1e-5), dict(eps=math.nan), dict(eps=math.inf)])
+def test_norm_forward_refuses(bad):
+    assert _fwd(**bad) == INVALID
+
+
+def test_norm_of_no_rows_is_nothing():
+    assert _fwd(rows=0, x=None, y=None) == 0
+
+
+@pytest.mark.parametrize("bad,status", [
+    (dict(dtype=2), INVALID), (dict(dy=None), INVALID), (dict(x=None), INVALID), (dict(dx=None), INVALID),
+    (dict(rows=-1), INVALID), (dict(cols=0), INVALID), (dict(ds=7), INVALID), (dict(xs=7), INVALID),
+    (dict(os=7), INVALID), (dict(eps=0.0), INVALID), (dict(ws=None), WORKSPACE), (dict(nb=63), WORKSPACE),
+    (dict(ws=FAKE + 128), WORKSPACE)])
+def test_norm_backward_refuses(bad, status):
+    assert _bwd(**bad) == status
+
+
+def test_norm_workspace_holds_two_rows_per_part_and_grows():
+    last = 0
+    for rows in (0, 1, 31, 32, 33, 1000, 10 ** 5, 10 ** 6):
+        n = sscn.sscn_layer_norm_workspace_bytes(1, rows, 100)
+        assert n >= 800 and n % 800 == 0 and n >= last
+        last = n
+    assert sscn.sscn_layer_norm_workspace_bytes(0, 2 ** 31 - 1, sscn.NORM_MAX_COLS) <= 1 << 28
+    for bad in ((2, 1, 1), (0, -1, 1), (0, 1, 0), (0, 1, sscn.NORM_MAX_COLS + 1)):
+        with pytest.raises(sscn.SSCNError):
+            sscn.sscn_layer_norm_workspace_bytes(*bad)
+
+
+def _mats(*shapes, **kw):
+    return (sscn.OrthoMatrix * max(len(shapes), 1))(*[
+        sscn.OrthoMatrix(r, c, kw.get("d_in", FAKE), kw.get("si", c), kw.get("d_out", FAKE), kw.get("so", c))
+        for r, c in shapes])
+
+
+def _ortho(mats, n=None, dtype=0, steps=5, coef=COEF, ws=FAKE, nb=1 << 40):
+    return sscn.load_library().sscn_orthogonalize(dtype, len(mats) if n is None else n, mats, steps, coef, ws, nb, None)
+
+
+def test_orthogonalize_refuses():
+    good = _mats((5, 7), (9, 3))
+    need = sscn.sscn_orthogonalize_workspace_bytes(good)
+    assert need > 0
+    assert _ortho(good, dtype=2) == INVALID
+    assert _ortho(good, n=-1) == INVALID
+    assert _ortho(None, n=1) == INVALID
+    assert _ortho(good, steps=0) == INVALID
+    assert _ortho(good, steps=33, coef=(ctypes.c_float * 99)(*([1.5, -0.5, 0.0] * 33))) == INVALID
+    assert _ortho(good, coef=None) == INVALID
+    assert _ortho(good, ws=None) == WORKSPACE
+    assert _ortho(good, nb=need - 1) == WORKSPACE
+    assert _ortho(good, ws=FAKE + 64) == WORKSPACE
+    for shape in ((0, 4), (4, 0), (-1, 4), (16385, 16385), (1, (1 << 20) + 1), ((1 << 20) + 1, 1)):
+        assert _ortho(_mats(shape)) == INVALID, shape
+    for kw in (dict(d_in=None), dict(d_out=None), dict(si=6), dict(so=6), dict(si=-7)):
+        assert _ortho(_mats((5, 7), **kw)) == INVALID, kw
+    assert _ortho(good, n=0, ws=None, nb=0) == 0  # nothing to do
+
+
+@pytest.mark.parametrize("row,ok", [
+    ((3.4445, -4.7750, 2.0315), True), ((1.5, -0.5, 0.0), True), ((1.0, 0.0, 0.0), True), ((15 / 8, -10 / 8, 3 / 8), True),
+    ((3.6, 0.0, 0.0), False),        # singular values up to 3.6
+    ((1.0, 3.0, 0.0), False),        # 1 + 3
+    ((0.0, 250.0, -250.0), False),   # b s^2 + c s^4 stays below 200, the singular value does not
+    ((20.0, -75.0, 55.5), False),    # zero at the end of the range, 2.7 .. inside it
+    ((math.nan, 0.0, 0.0), False), ((1.0, math.inf, 0.0), False)])
+def test_coefficients_are_followed_over_the_whole_range(row, ok):
+    """The largest |p(s)| of each step over [0, hi], against a dense scan here."""
+    coef = (ctypes.c_float * 3)(*row)
+    want = WORKSPACE if ok else INVALID  # good coefficients get as far as the missing workspace
+    assert _ortho(_mats((5, 7)), steps=1, coef=coef, ws=None) == want
+    if all(math.isfinite(v) for v in row):
+        a, b, c = list(coef)
+        s = [i / 20000 for i in range(20001)]
+        worst = max(abs(a * x + b * x ** 3 + c * x ** 5) for x in s)
+        assert ok == (worst <= 3.5 and max(abs(b * x ** 2 + c * x ** 4) for x in s) <= 200)
+
+
+def test_coefficients_are_followed_through_the_steps():
+    grow = (1.5, 0.0, 0.0)  # 1.5^3 < 3.5 < 1.5^4
+    for steps, ok in ((3, True), (4, False)):
+        coef = (ctypes.c_float * (3 * steps))(*(grow * steps))
+        assert _ortho(_mats((5, 7)), steps=steps, coef=coef, ws=None) == (WORKSPACE if ok else INVALID)
+
+
+def _param(rows=6, cols=4, orthogonal=1, w=FAKE, g=FAKE, v=FAKE, lr=0.1, wd=0.0, scale=1.0):
+    return sscn.MuonParam(rows, cols, w, None, g, v, lr, wd, scale, orthogonal)
+
+
+def _update(*params, n=None, dtype=0, momentum=0.9, steps=5, coef=COEF, ws=FAKE, nb=1 << 40):
+    arr = (sscn.MuonParam * max(len(params), 1))(*params)
+    return sscn.load_library().sscn_muon_update(dtype, len(params) if n is None else n, arr, momentum, 1, steps, coef, ws,
+                                                nb, None)
+
+
+def test_muon_update_refuses():
+    for kw in (dict(w=None), dict(g=None), dict(v=None), dict(lr=-0.1), dict(lr=math.nan), dict(wd=-1.0),
+               dict(wd=math.inf), dict(scale=math.nan), dict(rows=0), dict(cols=0), dict(rows=16385, cols=16385),
+               dict(rows=-1, orthogonal=0), dict(cols=1 << 31, orthogonal=0)):
+        assert _update(_param(**kw)) == INVALID, kw
+    for kw in (dict(dtype=2), dict(momentum=-0.1), dict(momentum=math.nan), dict(steps=0), dict(coef=None), dict(n=-1)):
+        assert _update(_param(), **kw) == INVALID, kw
+    need = sscn.sscn_muon_workspace_bytes((sscn.MuonParam * 1)(_param()))
+    assert _update(_param(), nb=need - 1) == WORKSPACE
+    assert _update(_param(), ws=None) == WORKSPACE
+    assert _update(_param(), ws=FAKE + 8) == WORKSPACE
+    assert _update(n=0, ws=None, nb=0, steps=0, coef=None) == 0
+
+
+def test_muon_workspace_covers_its_largest_group():
+    """Matrices go 24 at a time, vectors need none, a permutation of equal matrices changes nothing."""
+    def need(*params):
+        return sscn.sscn_muon_workspace_bytes((sscn.MuonParam * len(params))(*params))
+
+    one, vec = _param(64, 32), _param(1, 500, 0)
+    assert need(vec, vec) == 0
+    assert need(one, vec) == need(one)
+    assert need(*([one] * 24)) == need(*([one] * 25)) == need(*([one] * 70))
+    assert need(*([one] * 24)) == 24 * need(one)
+    mats = _mats(*([(64, 32)] * 30))
+    assert sscn.sscn_orthogonalize_workspace_bytes(mats) == need(*([one] * 30))
+
+
+def test_net_calls_refuse():
+    lib = sscn.load_library()
+    h = sscn.sscn_net_create(sscn.NetDesc(2, 3, 9, 4, 4, 100, sscn.SSCN_BF16))
+    try:
+        opt = sscn.MuonOptions(0.1, 0.1, 0.9, 0.0, 1, 0, 5, ctypes.addressof(COEF))
+        need = sscn.sscn_net_muon_workspace_bytes(h, opt)
+        assert need > 0
+        opt.softmax = 1
+        assert sscn.sscn_net_muon_workspace_bytes(h, opt) > need
+        ptrs = (ctypes.c_void_p * 4)(*([FAKE] * 4))
+        args = [h, ptrs, ptrs, ptrs, ptrs, ptrs, ctypes.byref(opt), FAKE, 1 << 40, None]
+        assert lib.sscn_muon_step(*args) == BAD_STATE  # no backward yet
+        for i in (0, 1, 3, 4, 5, 6):
+            assert lib.sscn_muon_step(*args[:i], None, *args[i + 1:]) == INVALID, i
+        for field in ("lr", "lr_rest", "momentum", "weight_decay"):
+            for bad in (-1.0, math.nan, math.inf):
+                keep = getattr(opt, field)
+                setattr(opt, field, bad)
+                assert lib.sscn_muon_step(*args) == INVALID, field
+                setattr(opt, field, keep)
+        n = sscn.sscn_head_norm_workspace_bytes(h)
+        assert n >= 4 * 3 * 9  # batch_max rows of the top layer's nine channels
+        good = [h, FAKE, FAKE, FAKE, FAKE, 1e-5, FAKE, n]
+        for i in (1, 2, 3, 4):
+            assert lib.sscn_set_head_norm(*good[:i], None, *good[i + 1:]) == INVALID
+        for eps in (0.0, -1.0, math.nan, math.inf):
+            assert lib.sscn_set_head_norm(*good[:5], eps, FAKE, n) == INVALID
+        assert lib.sscn_set_head_norm(*good[:6], None, n) == WORKSPACE
+        assert lib.sscn_set_head_norm(*good[:6], FAKE, n - 1) == WORKSPACE
+        assert lib.sscn_set_head_norm(*good[:6], FAKE + 4, n) == WORKSPACE
+        assert lib.sscn_set_head_norm(None, *good[1:]) == INVALID
+        assert lib.sscn_set_head_norm(*good) == 0
+        assert lib.sscn_set_head_norm(h, None, None, None, None, 0.0, None, 0) == 0
+    finally:
+        sscn.sscn_net_destroy(h)
