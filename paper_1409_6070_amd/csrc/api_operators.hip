@@ -2,6 +2,7 @@
 // matrices and the update that uses them.  Host code only: argument checks,
 // workspace layout, launches on the caller's stream.
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 
@@ -68,13 +69,13 @@ bool coefficients_ok(int32_t steps, const float* coef) {
   return true;
 }
 
-// Workspace of one matrix with tiles of edge T; sets its pointers when base is not null.
-size_t carve_matrix(NsMat& M, int64_t rows, int64_t cols, int T, char* base) {
+// Workspace of one matrix; sets its pointers when base is not null.
+size_t carve_matrix(NsMat& M, int64_t rows, int64_t cols, char* base) {
   M.tall = rows > cols;
   M.m = (int32_t)std::min(rows, cols);
   M.n = (int32_t)std::max(rows, cols);
-  M.mp = (int32_t)round_up(M.m, T);
-  M.np = (int32_t)round_up(M.n, T);
+  M.mp = (int32_t)round_up(M.m, 32);
+  M.np = (int32_t)round_up(M.n, 32);
   size_t off = 0;
   auto take = [&](size_t bytes) {
     char* p = base ? base + off : nullptr;
@@ -84,8 +85,8 @@ size_t carve_matrix(NsMat& M, int64_t rows, int64_t cols, int T, char* base) {
   const size_t x = (size_t)M.mp * M.np * 4, g = (size_t)M.mp * M.mp * 4;
   M.X = (float*)take(x);
   M.opX = take(x);
-  M.opXt[0] = take(x);
-  M.opXt[1] = take(x);
+  M.opXt = take(x);
+  M.opXt_next = take(x);
   M.opA = take(g);
   M.opB = take(g);
   M.ssq = (double*)take(NS_SSQ * sizeof(double));
@@ -98,17 +99,11 @@ size_t group_bytes(int32_t n, Shape&& shape) {
   size_t most = 0;
   for (int32_t g = 0; g < n; g += NS_MATS) {
     const int k = std::min(NS_MATS, n - g);
-    int64_t m[NS_MATS];
-    for (int j = 0; j < k; ++j) {
-      const auto s = shape(g + j);
-      m[j] = std::min(s.first, s.second);
-    }
-    const int T = ns_tile(k, m);
     size_t sum = 0;
     for (int j = 0; j < k; ++j) {
       NsMat M{};
       const auto s = shape(g + j);
-      sum += carve_matrix(M, s.first, s.second, T, nullptr);
+      sum += carve_matrix(M, s.first, s.second, nullptr);
     }
     most = std::max(most, sum);
   }
@@ -120,22 +115,18 @@ hipError_t run_groups(int32_t n, Shape&& shape, Fill&& fill, NsArgs& a, bool bf1
                       const float* coef, void* d_ws, hipStream_t st) {
   for (int32_t g = 0; g < n; g += NS_MATS) {
     const int k = std::min(NS_MATS, n - g);
-    int64_t m[NS_MATS];
-    for (int j = 0; j < k; ++j) {
-      const auto s = shape(g + j);
-      m[j] = std::min(s.first, s.second);
-    }
-    const int T = ns_tile(k, m);
     char* at = (char*)d_ws;
     a.n = k;
     for (int j = 0; j < k; ++j) {
       NsMat& M = a.mat[j];
       M = NsMat{};
       const auto s = shape(g + j);
-      at += carve_matrix(M, s.first, s.second, T, at);
+      at += carve_matrix(M, s.first, s.second, at);
       fill(g + j, M);
     }
-    const hipError_t e = launch_newton_schulz(a, T, bf16, muon, steps, coef, st);
+    // the longest sums start first
+    std::stable_sort(a.mat, a.mat + k, [](const NsMat& x, const NsMat& y) { return x.n > y.n; });
+    const hipError_t e = launch_newton_schulz(a, bf16, muon, steps, coef, st);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

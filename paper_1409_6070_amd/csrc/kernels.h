@@ -481,13 +481,14 @@ constexpr int NS_MATS = 24;   // matrices of one group of launches
 constexpr int NS_SSQ = 1024;  // partial sums of a matrix's norm
 struct NsMat {
   int32_t m, n;    // X: m <= n
-  int32_t mp, np;  // padded to the tile edge
+  int32_t mp, np;  // padded to multiples of 32
   int32_t tall;    // the caller's matrix is X transposed
   int32_t nssq;
   // workspace
   float* X;        // [mp][np]
   char* opX;       // operand with X's rows
-  char* opXt[2];   // operand with X's columns as rows, one step's read while the next's is written
+  char* opXt;      // operand with X's columns as rows
+  char* opXt_next; // the next step's, written while opXt is read
   char* opA;
   char* opB;
   double* ssq;
@@ -502,15 +503,12 @@ struct NsMat {
 };
 struct NsArgs {
   int32_t n;
-  int32_t parity;
   int32_t nesterov;
   float momentum;
   float a, b, c;
   int32_t beg[NS_MATS + 1];
   NsMat mat[NS_MATS];
 };
-int ns_ssq_blocks(int64_t m, int64_t n);
-int ns_tile(int n, const int64_t* m);
-hipError_t launch_newton_schulz(NsArgs& a, int tile, bool bf16, bool muon, int steps, const float* coef, hipStream_t st);
+hipError_t launch_newton_schulz(NsArgs& a, bool bf16, bool muon, int steps, const float* coef, hipStream_t st);
 
 }  // namespace sscn

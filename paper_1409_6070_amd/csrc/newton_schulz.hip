@@ -22,7 +22,10 @@
 // its lo plane, lane l's 16 bytes being row l % 16, k 8 (l / 16) .. + 7.  One wave
 // moves a plane with one 16-byte load per lane straight into LDS and reads it
 // back the same way: contiguous everywhere, no bank conflicts, no swizzle.  Rows
-// and columns are padded with zeros to the tile edge, so no product checks bounds.
+// and columns are padded with zeros to multiples of 32.
+
+#include <atomic>
+#include <type_traits>
 
 #include "common.h"
 #include "kernels.h"
@@ -50,8 +53,9 @@ __device__ inline void wait_loads() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
 }
 
-// One 16-byte load per lane into LDS: lane l's bytes land at lds + 16 l.  The
-// compiler does not see it; wait_loads and the barriers' fences order it.
+// One 16-byte load per lane into LDS: lane l's bytes, lane_off + off into the buffer,
+// land at lds + 16 l (lds and off uniform over the wave).  The compiler does not see
+// it; wait_loads and the barriers' fences order it.
 __device__ inline void load_plane(u32x4 rsrc, uint32_t lds, uint32_t lane_off, uint32_t off) {
   asm volatile(
       "s_mov_b32 m0, %0\n\t"
@@ -83,12 +87,6 @@ __device__ inline void store_split(char* at, const float (&v)[8], float s) {
   *(f16x8*)(at + BLOCK / 2) = lo;
 }
 
-__device__ inline void load_split(const char* at, float (&v)[8], float inv) {
-  const f16x8 hi = *(const f16x8*)at, lo = *(const f16x8*)(at + BLOCK / 2);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = ((float)hi[e] + (float)lo[e]) * inv;
-}
-
 // Address of lane l's part of block (rb, kb) of an operand with kblocks blocks a row.
 __device__ inline int64_t block_at(int rb, int kb, int kblocks) { return ((int64_t)rb * kblocks + kb) * BLOCK; }
 
@@ -98,103 +96,129 @@ __device__ inline int find_mat(const NsArgs& a, int t) {
   return j;
 }
 
+// Products take 256 x 128 tiles where that makes NS_LARGE of them, 64 x 64 tiles where
+// that makes NS_MID, else 32 x 32.
+constexpr int NS_LARGE = 100, NS_MID = 160;
+
+// Sum over the workgroup's 256 threads, in all of them (red: four doubles).
+__device__ inline double block_sum(double s, double* red) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
 // ---------------------------------------------------------------------------
 // |u|_F^2 as partial sums in float64 (any float32 matrix's fits), and for Muon
-// the velocity: v <- mu v + g.  NS_SSQ workgroups at most per matrix.
+// the velocity: v <- mu v + g.  NS_SSQ workgroups at most per matrix; the loads of
+// eight elements a thread are in flight together.
 
 template <typename T, bool MUON>
 __global__ void __launch_bounds__(256) k_ns_begin(NsArgs a) {
+  constexpr int U = 8;
   const int j = find_mat(a, blockIdx.x);
-  const NsMat& M = a.mat[j];
+  const NsMat M = a.mat[j];
   const int blk = blockIdx.x - a.beg[j], nblk = a.beg[j + 1] - a.beg[j];
-  const int64_t rows = M.tall ? M.n : M.m, cols = M.tall ? M.m : M.n;
+  const int64_t rows = M.tall ? M.n : M.m, cols = M.tall ? M.m : M.n, total = rows * cols;
   double s = 0.0;
-  if constexpr (MUON) {
-    const float* g = (const float*)M.u;
-    for (int64_t i = (int64_t)blk * 256 + threadIdx.x; i < rows * cols; i += (int64_t)nblk * 256) {
-      const float gi = g[i], v = a.momentum * M.v[i] + gi;
-      M.v[i] = v;
-      const float u = a.nesterov ? a.momentum * v + gi : v;
-      s += (double)u * u;
+  if (MUON || M.u_stride == cols) {
+    const T* u = (const T*)M.u;
+    const int64_t step = (int64_t)nblk * 256;
+    for (int64_t i0 = (int64_t)blk * 256 + threadIdx.x; i0 < total; i0 += U * step) {
+      float x[U], v[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {  // (past the end: the last element, not used)
+        const int64_t i = std::min(i0 + k * step, total - 1);
+        x[k] = Elem<T>::to_f32(u[i]);
+        if constexpr (MUON) v[k] = M.v[i];
+      }
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int64_t i = i0 + k * step;
+        if constexpr (MUON) {
+          v[k] = a.momentum * v[k] + x[k];
+          if (i < total) M.v[i] = v[k];
+          x[k] = a.nesterov ? a.momentum * v[k] + x[k] : v[k];
+        }
+        s += i < total ? (double)x[k] * x[k] : 0.0;
+      }
     }
   } else {
     const T* u = (const T*)M.u;
     int tx = 256;  // threads along a row: short rows go several at a time
     while (tx / 2 >= cols) tx /= 2;
-    for (int64_t r = (int64_t)blk * (256 / tx) + threadIdx.x / tx; r < rows; r += (int64_t)nblk * (256 / tx))
-#pragma unroll 4
-      for (int64_t c = threadIdx.x % tx; c < cols; c += tx) {
-        const double x = Elem<T>::to_f32(u[r * M.u_stride + c]);
-        s += x * x;
+    const int64_t step = (int64_t)nblk * (256 / tx);
+    for (int64_t c = threadIdx.x % tx; c < cols; c += tx)
+      for (int64_t r0 = (int64_t)blk * (256 / tx) + threadIdx.x / tx; r0 < rows; r0 += U * step) {
+        float x[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) x[k] = Elem<T>::to_f32(u[std::min(r0 + k * step, rows - 1) * M.u_stride + c]);
+#pragma unroll
+        for (int k = 0; k < U; ++k) s += r0 + k * step < rows ? (double)x[k] * x[k] : 0.0;
       }
   }
-  __shared__ double red[256];
-  red[threadIdx.x] = s;
-  __syncthreads();
-  for (int w = 128; w > 0; w >>= 1) {
-    if ((int)threadIdx.x < w) red[threadIdx.x] += red[threadIdx.x + w];
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) M.ssq[blk] = red[0];
+  __shared__ double red[4];
+  s = block_sum(s, red);
+  if (threadIdx.x == 0) M.ssq[blk] = s;
 }
 
-// X = u / |u|_F in float32 and as both operands; a wave per 32 x 32 tile.
+// X = u / |u|_F in float32 and as both operands; a wave per 32 x 32 tile, whose
+// values are on their way while the norm's partial sums are added.
 template <typename T, bool MUON>
 __global__ void __launch_bounds__(256) k_ns_convert(NsArgs a) {
   const int j = find_mat(a, blockIdx.x);
-  const NsMat& M = a.mat[j];
-  __shared__ double red[256];
+  const NsMat M = a.mat[j];
+  __shared__ double red[4];
   __shared__ float tile[4][32][36];
-  double ss = 0.0;
-  for (int k = threadIdx.x; k < M.nssq; k += 256) ss += M.ssq[k];
-  red[threadIdx.x] = ss;
-  __syncthreads();
-  for (int w = 128; w > 0; w >>= 1) {
-    if ((int)threadIdx.x < w) red[threadIdx.x] += red[threadIdx.x + w];
-    __syncthreads();
-  }
-  const double inv = red[0] == 0.0 ? 0.0 : 1.0 / sqrt(red[0]);  // (a zero matrix stays zero)
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int tn = M.np / 32, t = (blockIdx.x - a.beg[j]) * 4 + wave;
   const bool live = t < (M.mp / 32) * tn;
-  const int i0 = t / tn * 32, j0 = t % tn * 32;
-  if (live) {
-    // lanes along the caller's rows
-    const int q = lane & 31;
-#pragma unroll 8
-    for (int p = lane >> 5; p < 32; p += 2) {
-      const int i = i0 + (M.tall ? q : p), c = j0 + (M.tall ? p : q);
-      float x = 0.f;
-      if (i < M.m && c < M.n) {
-        const int64_t r = M.tall ? c : i, k = M.tall ? i : c;
-        if constexpr (MUON) {
-          const int64_t at = r * (M.tall ? M.m : M.n) + k;
-          const float v = M.v[at];
-          x = a.nesterov ? a.momentum * v + ((const float*)M.u)[at] : v;
-        } else {
-          x = Elem<T>::to_f32(((const T*)M.u)[r * M.u_stride + k]);
-        }
-        x = (float)((double)x * inv);
-      }
-      tile[wave][i - i0][c - j0] = x;
+  const int i0 = live ? t / tn * 32 : 0, j0 = live ? t % tn * 32 : 0;
+  // lanes along the caller's rows; outside the matrix a lane reads its nearest element
+  const int64_t stride = MUON ? (M.tall ? M.m : M.n) : M.u_stride;
+  const int r0 = M.tall ? j0 : i0, c = (M.tall ? i0 : j0) + (lane & 31), p0 = lane >> 5;
+  const int rows = M.tall ? M.n : M.m, cols = M.tall ? M.m : M.n;
+  const int64_t at0 = std::min(c, cols - 1);
+  float x[16], v[16];
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const int64_t at = std::min(r0 + p0 + 2 * k, rows - 1) * stride + at0;
+    if constexpr (MUON) {
+      v[k] = M.v[at];
+      x[k] = ((const float*)M.u)[at];
+    } else {
+      x[k] = Elem<T>::to_f32(((const T*)M.u)[at]);
     }
+  }
+  double ss = 0.0;
+  for (int k = threadIdx.x; k < M.nssq; k += 256) ss += M.ssq[k];
+  ss = block_sum(ss, red);
+  const double inv = ss == 0.0 ? 0.0 : 1.0 / sqrt(ss);  // (a zero matrix stays zero)
+  // the padding stays zero, beside a matrix whose norm is NaN or infinite too
+  float* to = M.tall ? &tile[wave][lane & 31][p0] : &tile[wave][p0][lane & 31];
+  const int ts = M.tall ? 2 : 2 * 36;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    if constexpr (MUON) x[k] = a.nesterov ? a.momentum * v[k] + x[k] : v[k];
+    to[k * ts] = c < cols && r0 + p0 + 2 * k < rows ? (float)((double)x[k] * inv) : 0.f;
   }
   __syncthreads();
   if (!live) return;
   const int r16 = lane & 15, k8 = lane >> 4;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    float v[8];
+    float w[8];
     const int i = h * 16 + r16;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = tile[wave][i][k8 * 8 + e];
+    for (int e = 0; e < 8; ++e) w[e] = tile[wave][i][k8 * 8 + e];
     float* X = M.X + (int64_t)(i0 + i) * M.np + j0 + k8 * 8;
-    *(f32x4*)X = f32x4{v[0], v[1], v[2], v[3]};
-    *(f32x4*)(X + 4) = f32x4{v[4], v[5], v[6], v[7]};
-    store_split(M.opX + block_at(i0 / 16 + h, j0 / 32, M.np / 32) + lane * 16, v, SX);
+    *(f32x4*)X = f32x4{w[0], w[1], w[2], w[3]};
+    *(f32x4*)(X + 4) = f32x4{w[4], w[5], w[6], w[7]};
+    store_split(M.opX + block_at(i0 / 16 + h, j0 / 32, M.np / 32) + lane * 16, w, SX);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = tile[wave][k8 * 8 + e][h * 16 + r16];
-    store_split(M.opXt[0] + block_at(j0 / 16 + h, i0 / 32, M.mp / 32) + lane * 16, v, SX);
+    for (int e = 0; e < 8; ++e) w[e] = tile[wave][k8 * 8 + e][h * 16 + r16];
+    store_split(M.opXt + block_at(j0 / 16 + h, i0 / 32, M.mp / 32) + lane * 16, w, SX);
   }
 }
 
@@ -203,233 +227,542 @@ __global__ void __launch_bounds__(256) k_ns_convert(NsArgs a) {
 
 enum NsKind { NS_GRAM, NS_POLY, NS_APPLY, NS_ORTHO, NS_MUON };
 
-// T x T result tiles of four waves (2 x 2), KB blocks of k per slab, NST slabs in LDS.
-template <int T, int KB, int NST>
-struct NsTile {
-  static constexpr int RB = T / 16;                     // row blocks of an operand's tile
-  static constexpr int FT = T / 32;                     // 16 x 16 results per wave and side
-  static constexpr int SLAB = 2 * RB * KB * BLOCK;      // bytes
-  static constexpr int LPW = SLAB / 1024 / 4;           // planes a wave loads per slab
-  static constexpr int CS = T + 4;                      // floats per row of the staged result
-  static constexpr int LDS = NST * SLAB > T * CS * 4 ? NST * SLAB : T * CS * 4;
-  static_assert(SLAB % 4096 == 0, "planes are dealt to four waves");
+constexpr bool symmetric(int kind) { return kind == NS_GRAM || kind == NS_POLY; }
+
+// A TM x TN result tile: its matrix, place and operands.
+template <int TM, int TN, int KIND>
+struct NsWork {
+  static_assert(TM % TN == 0, "a tile row is one or several tile columns high");
+  NsMat M;
+  int ti, tj;       // tile row and column
+  int kblocks;
+  const char *P, *Q;  // first block of the tile's rows in each operand
+  int pr, qr;         // row blocks of each inside the padded matrix (a last tile has fewer)
+
+  // false: no tile for this workgroup.  Workgroup b runs on XCD b % 8: each XCD takes
+  // an eighth of every matrix's tiles, consecutive ones, whose operands its L2 shares.
+  __device__ inline bool find(const NsArgs& a) {
+    const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
+    const int j = find_mat(a, slot);
+    M = a.mat[j];
+    const int per = a.beg[j + 1] - a.beg[j], t = xcd * per + slot - a.beg[j];
+    const int tm = (M.mp + TM - 1) / TM;
+    if constexpr (symmetric(KIND)) {  // tiles that reach the diagonal or lie below it
+      constexpr int R = TM / TN;
+      ti = 0;  // R (1 + 2 + .. + ti) tiles in the rows above
+      ti = (int)((sqrtf(8.f / R * (float)t + 1.f) - 1.f) * 0.5f);
+      while (R * ti * (ti + 1) / 2 > t) --ti;
+      while (R * (ti + 1) * (ti + 2) / 2 <= t) ++ti;
+      tj = t - R * ti * (ti + 1) / 2;
+    } else {
+      const int tn = (M.np + TN - 1) / TN;
+      ti = t / tn;
+      tj = t - ti * tn;
+    }
+    ti = __builtin_amdgcn_readfirstlane(ti);
+    tj = __builtin_amdgcn_readfirstlane(tj);
+    const int mp = M.mp, cols = symmetric(KIND) ? mp : M.np;
+    if (ti >= tm || tj * TN >= cols) return false;
+    kblocks = (KIND == NS_GRAM ? M.np : mp) / 32;
+    P = KIND == NS_GRAM ? M.opX : KIND == NS_POLY ? M.opA : M.opB;
+    Q = KIND == NS_GRAM ? M.opX : KIND == NS_POLY ? M.opA : M.opXt;
+    P += block_at(ti * (TM / 16), 0, kblocks);
+    Q += block_at(tj * (TN / 16), 0, kblocks);
+    pr = min(TM, mp - ti * TM) / 16;
+    qr = min(TN, cols - tj * TN) / 16;
+    return true;
+  }
+
+  // Of a symmetric result, the part of row block rb: 1 below the diagonal's squares
+  // of edge TN (stored, and mirrored), 0 on it (stored), -1 above (another's mirror).
+  __device__ inline int side(int rb) const {
+    if constexpr (!symmetric(KIND)) return 1;
+    const int d = ti * (TM / TN) + rb * 16 / TN - tj;
+    return d > 0 ? 1 : d == 0 ? 0 : -1;
+  }
 };
 
-template <int T, int KB, int NST, int KIND, typename TO>
-__global__ void __launch_bounds__(256) k_ns_product(NsArgs a) {
-  using C = NsTile<T, KB, NST>;
-  constexpr int FT = C::FT, RB = C::RB;
-  constexpr bool SYM = KIND == NS_GRAM || KIND == NS_POLY;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
-  // consecutive tiles on one XCD, whose L2 they share
-  const int total = a.beg[a.n], per = (total + 7) / 8;
-  const int tix = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per || tix >= total) return;
-  const int j = find_mat(a, tix);
-  const NsMat& M = a.mat[j];
-  int t = tix - a.beg[j], ti, tj;
-  if constexpr (SYM) {  // tiles on and below the diagonal
-    ti = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
-    while (ti * (ti + 1) / 2 > t) --ti;
-    while ((ti + 1) * (ti + 2) / 2 <= t) ++ti;
-    tj = t - ti * (ti + 1) / 2;
-  } else {
-    ti = t / (M.np / T);
-    tj = t - ti * (M.np / T);
-  }
-  ti = __builtin_amdgcn_readfirstlane(ti);
-  tj = __builtin_amdgcn_readfirstlane(tj);
-  const int kblocks = (KIND == NS_GRAM ? M.np : M.mp) / 32;
-  const char* P = KIND == NS_GRAM ? M.opX : KIND == NS_POLY ? M.opA : M.opB;
-  const char* Q = KIND == NS_GRAM ? M.opX : KIND == NS_POLY ? M.opA : M.opXt[a.parity];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int wm = wave >> 1, wn = wave & 1;
-  const uint32_t span = (uint32_t)RB * (uint32_t)kblocks * BLOCK;  // a row tile of an operand
-  const u32x4 rs = wave < 2 ? plane_rsrc(P + (int64_t)ti * span, span) : plane_rsrc(Q + (int64_t)tj * span, span);
-  const uint32_t lds0 = lds_offset(smem);
-  const uint32_t lane_off = (uint32_t)lane * 16u;
-  // waves 0 and 1 load P's planes of a slab, 2 and 3 Q's
-  auto issue = [&](int s, int st) {
+// What the epilogue reads at a 16 x 32 block beside the sums, lane l's part (row
+// l % 16, columns 8 (l / 16) .. + 7): A's planes (POLY), X's values (APPLY and the
+// last ones), 16 bytes at each of two addresses.
+template <class W, int KIND>
+__device__ inline const char* beside_at(const W& w, int row16, int col32, int lane, int half) {
+  if constexpr (KIND == NS_POLY)
+    return w.M.opA + block_at(row16, col32, w.M.mp / 32) + lane * 16 + half * (BLOCK / 2);
+  else
+    return (const char*)(w.M.X + (int64_t)(row16 * 16 + (lane & 15)) * w.M.np + col32 * 32 + (lane >> 4) * 8 + half * 4);
+}
+
+// ... straight into LDS (2 KiB at lds), waited for with wait_loads.
+template <class W, int KIND>
+__device__ inline void load_beside(const W& w, int row16, int col32, int lane, uint32_t lds) {
 #pragma unroll
-    for (int i = 0; i < C::LPW; ++i) {
-      const int p = wave * C::LPW + i;                 // plane within the slab
-      const int q = p % (RB * KB * 2);                 // within its operand
-      const int rb = q / (KB * 2), rest = q % (KB * 2);  // row block, then (k block, plane): contiguous
-      load_plane(rs, lds0 + (uint32_t)(st * C::SLAB + p * 1024), lane_off,
-                 (uint32_t)((rb * kblocks + s * KB) * BLOCK + rest * 1024));
+  for (int h = 0; h < 2; ++h)
+    asm volatile(
+        "s_mov_b32 m0, %0\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dwordx4 %1, off" ::"s"(lds + h * 1024),
+        "v"(beside_at<W, KIND>(w, row16, col32, lane, h))
+        : "m0");
+}
+
+template <int KIND>
+__device__ inline void beside_values(u32x4 p, u32x4 q, float (&x)[8]) {
+  if constexpr (KIND == NS_POLY) {
+    const f16x8 hi = __builtin_bit_cast(f16x8, p), lo = __builtin_bit_cast(f16x8, q);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = ((float)hi[e] + (float)lo[e]) * (1.f / SA);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = __uint_as_float(p[e]);
+      x[4 + e] = __uint_as_float(q[e]);
     }
-  };
-  f32x4 acc[FT][FT];
+  }
+}
+
+// Eight consecutive elements of a row of the caller's array, from column c on, of
+// which the first n exist (n <= 0: none); addresses aligned to one element.
+template <typename T>
+struct Run8 {
+  T e[8];
+};
+template <typename T>
+__device__ inline Run8<T> load_run(const T* p, int n) {
+  Run8<T> r;
+  if (n >= 8) {
+    __builtin_memcpy(&r, p, sizeof(r));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.e[e] = e < n ? p[e] : T(0);
+  }
+  return r;
+}
+template <typename T>
+__device__ inline void store_run(T* p, const float (&v)[8], int n) {
+  Run8<T> r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r.e[e] = Elem<T>::from_f32(v[e]);
+  if (n >= 8) {
+    __builtin_memcpy(p, &r, sizeof(r));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) p[e] = r.e[e];
+  }
+}
+
+// Row `row` of the caller's matrix, columns c .. c + 7: the orthogonal matrix, or the
+// weights it updates (their old values in `old`).
+template <int KIND, typename TO>
+__device__ inline void store_result(const NsMat& M, int row, int c, const float (&o)[8], const Run8<float>& old) {
+  const int rows = M.tall ? M.n : M.m, cols = M.tall ? M.m : M.n;
+  const int n = row < rows ? cols - c : 0;
+  if constexpr (KIND == NS_ORTHO) {
+    store_run<TO>((TO*)M.o + (int64_t)row * M.o_stride + c, o, n);
+  } else {
+    float w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = old.e[e] - (M.scale * o[e] + M.decay * old.e[e]);
+    const int64_t at = (int64_t)row * cols + c;
+    store_run<float>(M.w + at, w, n);
+    if (M.o) store_run<TO>((TO*)M.o + at, w, n);
+  }
+}
+template <int KIND>
+__device__ inline Run8<float> load_weights(const NsMat& M, int row, int c) {
+  if constexpr (KIND != NS_MUON) return Run8<float>{};
+  const int rows = M.tall ? M.n : M.m, cols = M.tall ? M.m : M.n;
+  return load_run<float>(M.w + (int64_t)row * cols + c, row < rows ? cols - c : 0);
+}
+
+// The tile's sums, staged in LDS as PARTS partial tiles [TM][TN + 4], to the result:
+// first along the rows, then along the columns, in blocks of 16 x 32 dealt to NW
+// waves, GROUP blocks at a time whose reads are in flight together.  With PRE,
+// `beside` holds what load_beside brought for each block.
+template <int TM, int TN, int KIND, typename TO, int NW, int PARTS, int GROUP, bool PRE>
+__device__ inline void finish_tile(const NsArgs& a, const NsWork<TM, TN, KIND>& w, float* Cs, int wave, int lane,
+                                   const char* beside) {
+  using W = NsWork<TM, TN, KIND>;
+  constexpr int CS = TN + 4;
+  constexpr float unscale = KIND == NS_GRAM ? 1.f / (SX * SX) : KIND == NS_POLY ? 1.f / (SA * SA) : 1.f / (SB * SX);
+  constexpr bool LAST = KIND == NS_ORTHO || KIND == NS_MUON;
+  const NsMat& M = w.M;
+  const int l16 = lane & 15, g4 = lane >> 4;
+  {
+    constexpr int KB = TN / 32, NB = TM / 16 * KB, PER = (NB + NW - 1) / NW, G = GROUP < PER ? GROUP : PER;
+    const int row0 = w.ti * (TM / 16), col0 = w.tj * KB;
+#pragma unroll 1
+    for (int n0 = 0; n0 < PER; n0 += G) {
+      u32x4 bes[G][2];
+      Run8<float> old[G];
+#pragma unroll
+      for (int g = 0; g < G; ++g) {  // (blocks outside the matrix: the nearest one, not used)
+        const int b = min(wave + (n0 + g) * NW, NB - 1), rb = min(b / KB, w.pr - 1), kb = min(b % KB, w.qr / 2 - 1);
+        if constexpr (KIND != NS_GRAM) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            bes[g][h] = *(const u32x4*)(PRE ? beside + (rb * KB + kb) * 2048 + h * 1024 + lane * 16
+                                            : beside_at<W, KIND>(w, row0 + rb, col0 + kb, lane, h));
+        }
+        if (KIND == NS_MUON && !M.tall)
+          old[g] = load_weights<KIND>(M, (row0 + rb) * 16 + l16, (col0 + kb) * 32 + g4 * 8);
+      }
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const int b = wave + (n0 + g) * NW, rb = b / KB, kb = b % KB;
+        if (n0 + g >= PER || b >= NB || rb >= w.pr || 2 * kb >= w.qr || w.side(rb) < 0) continue;
+        float* c = Cs + (rb * 16 + l16) * CS + kb * 32 + g4 * 8;
+        float v[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          f32x4 s = *(const f32x4*)(c + 4 * h);
+#pragma unroll
+          for (int p = 1; p < PARTS; ++p) s += *(const f32x4*)(c + 4 * h + p * TM * CS);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[4 * h + e] = s[e] * unscale;
+        }
+        float x[8];
+        if constexpr (KIND != NS_GRAM) beside_values<KIND>(bes[g][0], bes[g][1], x);
+        if constexpr (KIND == NS_GRAM) {
+          store_split(M.opA + block_at(row0 + rb, col0 + kb, M.mp / 32) + lane * 16, v, SA);
+        } else if constexpr (KIND == NS_POLY) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = a.b * x[e] + a.c * v[e];
+          store_split(M.opB + block_at(row0 + rb, col0 + kb, M.mp / 32) + lane * 16, v, SB);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = a.a * x[e] + v[e];
+          if constexpr (KIND == NS_APPLY) {
+            float* X = M.X + (int64_t)((row0 + rb) * 16 + l16) * M.np + (col0 + kb) * 32 + g4 * 8;
+            *(f32x4*)X = *(const f32x4*)v;
+            *(f32x4*)(X + 4) = *(const f32x4*)(v + 4);
+            store_split(M.opX + block_at(row0 + rb, col0 + kb, M.np / 32) + lane * 16, v, SX);
+          } else if (!M.tall) {
+            store_result<KIND, TO>(M, (row0 + rb) * 16 + l16, (col0 + kb) * 32 + g4 * 8, v, old[g]);
+          }
+        }
+        *(f32x4*)c = *(const f32x4*)v;
+        *(f32x4*)(c + 4) = *(const f32x4*)(v + 4);
+      }
+    }
+  }
+  if (LAST && !M.tall) return;
+  __syncthreads();
+  // the mirrored part of a symmetric result, X's other operand, or a tall result
+  constexpr int KB = TM / 32, NB = TN / 16 * KB, PER = (NB + NW - 1) / NW, G = GROUP < PER ? GROUP : PER;
+  const int row0 = w.tj * (TN / 16), col0 = w.ti * KB;
+#pragma unroll 1
+  for (int n0 = 0; n0 < PER; n0 += G) {
+    Run8<float> old[G];
+    if constexpr (KIND == NS_MUON) {
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const int b = min(wave + (n0 + g) * NW, NB - 1), rb = min(b / KB, w.qr - 1), kb = min(b % KB, w.pr / 2 - 1);
+        old[g] = load_weights<KIND>(M, (row0 + rb) * 16 + l16, (col0 + kb) * 32 + g4 * 8);
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int b = wave + (n0 + g) * NW, rb = b / KB, kb = b % KB;
+      if (n0 + g >= PER || b >= NB || rb >= w.qr || 2 * kb >= w.pr || w.side(2 * kb) <= 0) continue;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = Cs[(kb * 32 + g4 * 8 + e) * CS + rb * 16 + l16];
+      if constexpr (LAST) {
+        store_result<KIND, TO>(M, (row0 + rb) * 16 + l16, (col0 + kb) * 32 + g4 * 8, v, old[g]);
+      } else {
+        char* op = KIND == NS_GRAM ? M.opA : KIND == NS_POLY ? M.opB : M.opXt_next;
+        constexpr float scale = KIND == NS_GRAM ? SA : KIND == NS_POLY ? SB : SX;
+        store_split(op + block_at(row0 + rb, col0 + kb, M.mp / 32) + lane * 16, v, scale);
+      }
+    }
+  }
+}
+
+// Blocks of both operands in registers.
+template <int FT>
+struct NsOperands {
+  f16x8 ph[FT], pl[FT], qh[FT], ql[FT];
+};
+
+// One 16 x 32 by 32 x 16 product of split operands, smallest terms first.
+template <int FT>
+__device__ inline void mma_block(const f16x8 (&ph)[FT], const f16x8 (&pl)[FT], const f16x8 (&qh)[FT],
+                                 const f16x8 (&ql)[FT], f32x4 (&acc)[FT][FT]) {
 #pragma unroll
   for (int i = 0; i < FT; ++i)
 #pragma unroll
-    for (int k = 0; k < FT; ++k) acc[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int nsl = kblocks / KB;
+    for (int k = 0; k < FT; ++k) acc[i][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl[i], qh[k], acc[i][k], 0, 0, 0);
 #pragma unroll
-  for (int p = 0; p < NST - 1; ++p)
-    if (p < nsl) issue(p, p);
-  for (int s = 0; s < nsl; ++s) {
-    // this wave's loads of slab s have landed once only those of the slabs after
-    // it are outstanding; the barrier makes it every wave's
-    asm volatile("" ::: "memory");
-    if constexpr (NST == 3) {
-      if (s + 1 < nsl) wait_loads<C::LPW>(); else wait_loads<0>();
-    } else {
-      wait_loads<0>();
-    }
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    if (s + NST - 1 < nsl) issue(s + NST - 1, (s + NST - 1) % NST);
-    const char* Ps = smem + (s % NST) * C::SLAB;
-    const char* Qs = Ps + RB * KB * BLOCK;
+  for (int i = 0; i < FT; ++i)
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      f16x8 ph[FT], pl[FT], qh[FT], ql[FT];
+    for (int k = 0; k < FT; ++k) acc[i][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph[i], ql[k], acc[i][k], 0, 0, 0);
 #pragma unroll
-      for (int i = 0; i < FT; ++i) {
-        const char* pp = Ps + ((wm * FT + i) * KB + kb) * BLOCK + lane * 16;
-        const char* qp = Qs + ((wn * FT + i) * KB + kb) * BLOCK + lane * 16;
-        ph[i] = *(const f16x8*)pp;
-        pl[i] = *(const f16x8*)(pp + BLOCK / 2);
-        qh[i] = *(const f16x8*)qp;
-        ql[i] = *(const f16x8*)(qp + BLOCK / 2);
-      }
+  for (int i = 0; i < FT; ++i)
 #pragma unroll
-      for (int i = 0; i < FT; ++i)
-#pragma unroll
-        for (int k = 0; k < FT; ++k) acc[i][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl[i], qh[k], acc[i][k], 0, 0, 0);
-#pragma unroll
-      for (int i = 0; i < FT; ++i)
-#pragma unroll
-        for (int k = 0; k < FT; ++k) acc[i][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph[i], ql[k], acc[i][k], 0, 0, 0);
-#pragma unroll
-      for (int i = 0; i < FT; ++i)
-#pragma unroll
-        for (int k = 0; k < FT; ++k) acc[i][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph[i], qh[k], acc[i][k], 0, 0, 0);
-    }
-  }
-  asm volatile("" ::: "memory");
-  __syncthreads();  // every wave done with the slabs before the result is staged over them
+    for (int k = 0; k < FT; ++k) acc[i][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph[i], qh[k], acc[i][k], 0, 0, 0);
+}
 
-  constexpr float unscale = KIND == NS_GRAM ? 1.f / (SX * SX) : KIND == NS_POLY ? 1.f / (SA * SA) : 1.f / (SB * SX);
-  float* Cs = (float*)smem;
+// Result lane l of a 16 x 16 block holds rows 4 (l / 16) .. + 3 of column l % 16.
+template <int FT, int CS>
+__device__ inline void stage_tile(float* Cs, const f32x4 (&acc)[FT][FT], int lane) {
   const int l16 = lane & 15, g4 = lane >> 4;
 #pragma unroll
   for (int i = 0; i < FT; ++i)
 #pragma unroll
     for (int k = 0; k < FT; ++k)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        Cs[(wm * (T / 2) + i * 16 + g4 * 4 + r) * C::CS + wn * (T / 2) + k * 16 + l16] = acc[i][k][r] * unscale;
-  __syncthreads();
-  // along the rows: lane l takes row l % 16, columns 8 (l / 16) .. of a 16 x 32 block
-  constexpr int NB = RB * (T / 32);
-  for (int b = wave; b < NB; b += 4) {
-    const int rb = b / (T / 32), kb = b % (T / 32);
-    float* c = Cs + (rb * 16 + l16) * C::CS + kb * 32 + g4 * 8;
-    float v[8];
-    *(f32x4*)v = *(const f32x4*)c;
-    *(f32x4*)(v + 4) = *(const f32x4*)(c + 4);
-    if constexpr (KIND == NS_GRAM) {
-      store_split(M.opA + block_at(ti * RB + rb, tj * (T / 32) + kb, M.mp / 32) + lane * 16, v, SA);
-    } else if constexpr (KIND == NS_POLY) {
-      const int64_t at = block_at(ti * RB + rb, tj * (T / 32) + kb, M.mp / 32) + lane * 16;
-      float x[8];
-      load_split(M.opA + at, x, 1.f / SA);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = a.b * x[e] + a.c * v[e];
-      store_split(M.opB + at, v, SB);
-    } else {
-      float* X = M.X + (int64_t)(ti * T + rb * 16 + l16) * M.np + tj * T + kb * 32 + g4 * 8;
-      const f32x4 x0 = *(const f32x4*)X, x1 = *(const f32x4*)(X + 4);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[e] = a.a * x0[e] + v[e];
-        v[4 + e] = a.a * x1[e] + v[4 + e];
-      }
-      if constexpr (KIND == NS_APPLY) {
-        *(f32x4*)X = *(const f32x4*)v;
-        *(f32x4*)(X + 4) = *(const f32x4*)(v + 4);
-        store_split(M.opX + block_at(ti * RB + rb, tj * (T / 32) + kb, M.np / 32) + lane * 16, v, SX);
-      }
-    }
-    if constexpr (KIND != NS_GRAM) {
-      *(f32x4*)c = *(const f32x4*)v;
-      *(f32x4*)(c + 4) = *(const f32x4*)(v + 4);
-    }
-  }
-  if constexpr (SYM)
-    if (ti == tj) return;  // a diagonal tile is its own mirror
-  __syncthreads();
-  if constexpr (KIND == NS_ORTHO || KIND == NS_MUON) {
-    // to the caller's matrix, lanes along its rows
-    const int64_t ld = M.tall ? M.m : M.n;
-    for (int q = threadIdx.x; q < T * T; q += 256) {
-      const int il = M.tall ? q % T : q / T, jl = M.tall ? q / T : q % T;
-      const int i = ti * T + il, k = tj * T + jl;
-      if (i >= M.m || k >= M.n) continue;
-      const int64_t r = M.tall ? k : i, c = M.tall ? i : k;
-      const float o = Cs[il * C::CS + jl];
-      if constexpr (KIND == NS_ORTHO) {
-        ((TO*)M.o)[r * M.o_stride + c] = Elem<TO>::from_f32(o);
-      } else {
-        const int64_t at = r * ld + c;
-        const float w = M.w[at], wn = w - (M.scale * o + M.decay * w);
-        M.w[at] = wn;
-        if (M.o) ((TO*)M.o)[at] = Elem<TO>::from_f32(wn);
-      }
-    }
-    return;
-  }
-  // along the columns: the mirrored part of a symmetric result, or X's other operand
-  char* op = KIND == NS_GRAM ? M.opA : KIND == NS_POLY ? M.opB : M.opXt[a.parity ^ 1];
-  constexpr float scale = KIND == NS_GRAM ? SA : KIND == NS_POLY ? SB : SX;
-  for (int b = wave; b < NB; b += 4) {
-    const int rb = b / (T / 32), kb = b % (T / 32);
-    float v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = Cs[(kb * 32 + g4 * 8 + e) * C::CS + rb * 16 + l16];
-    store_split(op + block_at(tj * RB + rb, ti * (T / 32) + kb, M.mp / 32) + lane * 16, v, scale);
-  }
+      for (int r = 0; r < 4; ++r) Cs[(i * 16 + g4 * 4 + r) * CS + k * 16 + l16] = acc[i][k][r];
 }
 
-template <int T, int KB, int NST, int KIND, typename TO>
-hipError_t run_product(NsArgs& a, hipStream_t st) {
-  using C = NsTile<T, KB, NST>;
-  static_assert(C::LDS <= 160 * 1024, "LDS of a compute unit");
-  int tiles = 0;
-  for (int j = 0; j < a.n; ++j) {
-    a.beg[j] = tiles;
-    const int tm = a.mat[j].mp / T;
-    tiles += KIND == NS_GRAM || KIND == NS_POLY ? tm * (tm + 1) / 2 : tm * (a.mat[j].np / T);
+// Large products: TM x TN tiles, a wave for each 64 x 64 of them, operands through a
+// ring of NST LDS slabs of 32 k.
+template <int TM, int TN, int NST>
+struct NsTile {
+  static constexpr int PB = TM / 16, QB = TN / 16, FT = 4;
+  static constexpr int NW = (TM / 64) * (TN / 64);
+  static constexpr int SLAB = (PB + QB) * BLOCK;    // bytes
+  static constexpr int LPW = SLAB / 1024 / NW;      // planes a wave loads per slab
+  static constexpr int CS = TN + 4;                 // floats per row of the staged result
+  static constexpr int LDS = NST * SLAB > TM * CS * 4 ? NST * SLAB : TM * CS * 4;
+  static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
+  static_assert(SLAB % (1024 * NW) == 0, "planes are dealt evenly");
+};
+
+template <int TM, int TN, int NST, int KIND, typename TO>
+__global__ void __launch_bounds__((NsTile<TM, TN, NST>::NW * 64)) k_ns_tiles(NsArgs a) {
+  using C = NsTile<TM, TN, NST>;
+  constexpr int FT = C::FT;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  NsWork<TM, TN, KIND> w;
+  if (!w.find(a)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wm = wave / (TN / 64), wn = wave % (TN / 64);
+  const u32x4 rp = plane_rsrc(w.P, (uint32_t)w.pr * (uint32_t)w.kblocks * BLOCK);
+  const u32x4 rq = plane_rsrc(w.Q, (uint32_t)w.qr * (uint32_t)w.kblocks * BLOCK);
+  const uint32_t lds0 = lds_offset(smem), lane_off = (uint32_t)lane * 16u;
+  auto issue_one = [&](int s, int st, int i) {
+    const int p = wave * C::LPW + i;  // plane within the slab: P's, then Q's
+    const bool of_q = p >= C::PB * 2;
+    const int q = of_q ? p - C::PB * 2 : p;
+    // (row blocks past the matrix: the last one again, its results are dropped)
+    const int rb = min(q / 2, (of_q ? w.qr : w.pr) - 1);
+    load_plane(of_q ? rq : rp, lds0 + (uint32_t)(st * C::SLAB + p * 1024), lane_off,
+               (uint32_t)((rb * w.kblocks + s) * BLOCK + (q % 2) * 1024));
+  };
+  auto issue = [&](int s, int st) {
+#pragma unroll
+    for (int i = 0; i < C::LPW; ++i) issue_one(s, st, i);
+  };
+  f32x4 acc[FT][FT];
+#pragma unroll
+  for (int i = 0; i < FT; ++i)
+#pragma unroll
+    for (int k = 0; k < FT; ++k) acc[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // (slabs behind the last one: the last one again, not used)
+  const int nsl = w.kblocks;
+#pragma unroll
+  for (int p = 0; p < NST; ++p) issue(min(p, nsl - 1), p);
+  // Slab s lies in registers when its turn comes: it is read out of LDS while slab
+  // s - 1 is multiplied, and the stage it leaves is refilled with slab s + NST.
+  // Reads and loads are dealt between the products, since a wave that issues them
+  // in a row waits for LDS and feeds no product meanwhile.
+  NsOperands<FT> ring[2];
+  auto read_one = [&](NsOperands<FT>& o, int st, int n) {
+    const char* Ps = smem + st * C::SLAB + lane * 16 + wm * FT * BLOCK;
+    const char* Qs = smem + st * C::SLAB + lane * 16 + (C::PB + wn * FT) * BLOCK;
+    const int i = n % FT;
+    if (n < FT) o.pl[i] = *(const f16x8*)(Ps + i * BLOCK + BLOCK / 2);
+    else if (n < 2 * FT) o.qh[i] = *(const f16x8*)(Qs + i * BLOCK);
+    else if (n < 3 * FT) o.ph[i] = *(const f16x8*)(Ps + i * BLOCK);
+    else o.ql[i] = *(const f16x8*)(Qs + i * BLOCK + BLOCK / 2);
+  };
+  // this wave's loads of slab s have landed once only those behind it are
+  // outstanding; the barrier makes it every wave's, and says that every wave's
+  // reads of the slab before it are done
+  auto arrive = [&](auto behind) {
+    asm volatile("" ::: "memory");
+    wait_loads<decltype(behind)::value * C::LPW>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  static_assert(NST == 3 && C::LPW <= 2 * FT, "the waits and the dealing of loads below");
+  arrive(std::integral_constant<int, 2>{});
+#pragma unroll
+  for (int n = 0; n < 4 * FT; ++n) read_one(ring[0], 0, n);
+  constexpr int GROUPS = 4 * FT, PER = 3 * FT * FT / GROUPS;
+  auto products = [&](const NsOperands<FT>& now, int g) {  // smallest terms first
+#pragma unroll
+    for (int q = g * PER; q < (g + 1) * PER; ++q) {
+      const int i = q % (FT * FT) / FT, k = q % FT, t = q / (FT * FT);
+      acc[i][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(t == 0 ? now.pl[i] : now.ph[i], t == 1 ? now.ql[k] : now.qh[k],
+                                                         acc[i][k], 0, 0, 0);
+    }
+  };
+  auto step = [&](int s, const NsOperands<FT>& now, NsOperands<FT>& next, int from, int to) {
+    arrive(std::integral_constant<int, 1>{});
+    const int slab = min(s + NST, nsl - 1);
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+      products(now, g);
+      read_one(next, from, g);
+      if (g % 2 == 0 && g / 2 < C::LPW) issue_one(slab, to, g / 2);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  int st = 0;  // stage of slab s
+  int s = 0;
+#pragma unroll 1
+  for (; s + 1 < nsl; s += 2) {
+    const int st1 = st == 2 ? 0 : st + 1, st2 = st1 == 2 ? 0 : st1 + 1;
+    step(s, ring[0], ring[1], st1, st);
+    step(s + 1, ring[1], ring[0], st2, st1);
+    st = st2;
   }
-  a.beg[a.n] = tiles;
-  const auto kern = k_ns_product<T, KB, NST, KIND, TO>;
-  if (C::LDS > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
+  if (s < nsl)
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) products(ring[0], g);
+  wait_loads<0>();
+  asm volatile("" ::: "memory");
+  __syncthreads();  // every wave done with the slabs before the result is staged over them
+  float* Cs = (float*)smem;
+  stage_tile<FT, C::CS>(Cs + wm * 64 * C::CS + wn * 64, acc, lane);
+  __syncthreads();
+  finish_tile<TM, TN, KIND, TO, C::NW, 1, 8, false>(a, w, Cs, wave, lane, nullptr);
+}
+
+// Small products: a T x T tile per workgroup, K dealt to its NW waves in runs of
+// blocks, each wave loading its operands straight into registers (a load is one
+// contiguous plane), DEPTH blocks ahead; the waves' sums meet in LDS, where what the
+// epilogue reads beside them has arrived meanwhile.  No barrier before that: such a
+// product is bound by latencies, not by the matrix cores.
+template <int T, int NW, int DEPTH, int KIND, typename TO>
+__global__ void __launch_bounds__(NW * 64) k_ns_direct(NsArgs a) {
+  using W = NsWork<T, T, KIND>;
+  constexpr int FT = T / 16, CS = T + 4, NB = FT * (T / 32);
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  W w;
+  if (!w.find(a)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int k0 = w.kblocks * wave / NW, k1 = w.kblocks * (wave + 1) / NW;
+  auto load = [&](int kb) {
+    NsOperands<FT> o;
+    kb = min(kb, w.kblocks - 1);  // (behind the last block: loaded again, not used)
+#pragma unroll
+    for (int i = 0; i < FT; ++i) {
+      // row blocks past the matrix: the last one again, its results are dropped
+      const char* p = w.P + block_at(min(i, w.pr - 1), kb, w.kblocks) + lane * 16;
+      const char* q = w.Q + block_at(min(i, w.qr - 1), kb, w.kblocks) + lane * 16;
+      o.ph[i] = *(const f16x8*)p;
+      o.pl[i] = *(const f16x8*)(p + BLOCK / 2);
+      o.qh[i] = *(const f16x8*)q;
+      o.ql[i] = *(const f16x8*)(q + BLOCK / 2);
+    }
+    return o;
+  };
+  NsOperands<FT> ring[DEPTH];
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d) ring[d] = load(k0 + d);
+  char* beside = smem + NW * T * CS * 4;
+  if constexpr (KIND != NS_GRAM)
+    for (int b = wave; b < NB; b += NW) {
+      const int rb = b / (T / 32), kb = b % (T / 32);
+      if (rb < w.pr && 2 * kb < w.qr)
+        load_beside<W, KIND>(w, w.ti * FT + rb, w.tj * (T / 32) + kb, lane, lds_offset(beside + b * 2048));
+    }
+  f32x4 acc[FT][FT];
+#pragma unroll
+  for (int i = 0; i < FT; ++i)
+#pragma unroll
+    for (int k = 0; k < FT; ++k) acc[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // (no copies and no loads under a condition: either would wait for every load)
+  int kb = k0;
+  for (; kb + DEPTH <= k1; kb += DEPTH)
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      mma_block<FT>(ring[d].ph, ring[d].pl, ring[d].qh, ring[d].ql, acc);
+      ring[d] = load(kb + DEPTH + d);
+    }
+#pragma unroll
+  for (int d = 0; d < DEPTH - 1; ++d)
+    if (kb + d < k1) mma_block<FT>(ring[d].ph, ring[d].pl, ring[d].qh, ring[d].ql, acc);
+  float* Cs = (float*)smem;
+  stage_tile<FT, CS>(Cs + wave * T * CS, acc, lane);
+  asm volatile("" ::: "memory");
+  wait_loads<0>();
+  __syncthreads();
+  finish_tile<T, T, KIND, TO, NW, NW, 2, true>(a, w, Cs, wave, lane, beside);
+}
+
+// ---------------------------------------------------------------------------
+// host
+
+// TM x TN tiles of one product over the group; with `slots`, a.beg gets each matrix's
+// range of workgroups per XCD.
+int64_t count_tiles(NsArgs& a, int kind, int TM, int TN, bool slots) {
+  int64_t all = 0, beg = 0;
+  for (int j = 0; j < a.n; ++j) {
+    const int64_t tm = (a.mat[j].mp + TM - 1) / TM, tn = (a.mat[j].np + TN - 1) / TN;
+    // (a last tile row that ends early has tiles past the diagonal: they find nothing to do)
+    const int64_t tiles = symmetric(kind) ? TM / TN * (tm * (tm + 1) / 2) : tm * tn;
+    if (slots) a.beg[j] = (int32_t)beg;
+    all += tiles;
+    beg += (tiles + 7) / 8;
+  }
+  if (slots) a.beg[a.n] = (int32_t)beg;
+  return all;
+}
+
+// LDS of k_ns_direct: the waves' partial tiles, and what lies beside the result.
+constexpr int direct_lds(int T, int waves) { return waves * T * (T + 4) * 4 + (T / 16) * (T / 32) * 2048; }
+
+template <auto KERN>
+hipError_t launch_tiles(int threads, int lds, const NsArgs& a, hipStream_t st) {
+  if (lds > 64 * 1024) {  // once per kernel and device: the call costs as much as a launch
+    static std::atomic<uint64_t> allowed{0};
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+    if (e == hipSuccess && !(allowed.load(std::memory_order_relaxed) & bit)) {
+      e = hipFuncSetAttribute((const void*)KERN, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+      if (e == hipSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
+    }
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(kern, dim3((tiles + 7) / 8 * 8), dim3(256), C::LDS, st, a);
+  hipLaunchKernelGGL(KERN, dim3(8 * a.beg[a.n]), dim3(threads), lds, st, a);
   return hipGetLastError();
 }
 
-template <int T, int KB, int NST>
-hipError_t run_steps(NsArgs& a, bool bf16, bool muon, int steps, const float* coef, hipStream_t st) {
+template <int KIND, typename TO>
+hipError_t run_product(NsArgs& a, hipStream_t st) {
+  if (count_tiles(a, KIND, 256, 128, false) >= NS_LARGE) {
+    count_tiles(a, KIND, 256, 128, true);
+    using C = NsTile<256, 128, 3>;
+    return launch_tiles<k_ns_tiles<256, 128, 3, KIND, TO>>(C::NW * 64, C::LDS, a, st);
+  }
+  if (count_tiles(a, KIND, 64, 64, false) >= NS_MID) {
+    count_tiles(a, KIND, 64, 64, true);
+    return launch_tiles<k_ns_direct<64, 4, 2, KIND, TO>>(256, direct_lds(64, 4), a, st);
+  }
+  count_tiles(a, KIND, 32, 32, true);
+  // (X X^T has the longest sums, B X the most tiles)
+  constexpr int NW = symmetric(KIND) ? 8 : 4;
+  return launch_tiles<k_ns_direct<32, NW, 3, KIND, TO>>(NW * 64, direct_lds(32, NW), a, st);
+}
+
+template <typename TO, bool MUON>
+hipError_t run_steps(NsArgs& a, int steps, const float* coef, hipStream_t st) {
   for (int s = 0; s < steps; ++s) {
     a.a = coef[3 * s];
     a.b = coef[3 * s + 1];
     a.c = coef[3 * s + 2];
-    a.parity = s & 1;
-    hipError_t e = run_product<T, KB, NST, NS_GRAM, float>(a, st);
-    if (e == hipSuccess) e = run_product<T, KB, NST, NS_POLY, float>(a, st);
+    hipError_t e = run_product<NS_GRAM, float>(a, st);
+    if (e == hipSuccess) e = run_product<NS_POLY, float>(a, st);
+    if (e == hipSuccess)
+      e = s + 1 < steps ? run_product<NS_APPLY, float>(a, st) : run_product<MUON ? NS_MUON : NS_ORTHO, TO>(a, st);
     if (e != hipSuccess) return e;
-    if (s + 1 < steps)
-      e = run_product<T, KB, NST, NS_APPLY, float>(a, st);
-    else if (muon)
-      e = bf16 ? run_product<T, KB, NST, NS_MUON, __bf16>(a, st) : run_product<T, KB, NST, NS_MUON, float>(a, st);
-    else
-      e = bf16 ? run_product<T, KB, NST, NS_ORTHO, __bf16>(a, st) : run_product<T, KB, NST, NS_ORTHO, float>(a, st);
-    if (e != hipSuccess) return e;
+    for (int j = 0; j < a.n; ++j) std::swap(a.mat[j].opXt, a.mat[j].opXt_next);
   }
   return hipSuccess;
 }
@@ -439,7 +772,7 @@ hipError_t run_begin(NsArgs& a, hipStream_t st) {
   int blocks = 0;
   for (int j = 0; j < a.n; ++j) {
     a.beg[j] = blocks;
-    a.mat[j].nssq = ns_ssq_blocks(a.mat[j].m, a.mat[j].n);
+    a.mat[j].nssq = (int)std::max<int64_t>(1, std::min<int64_t>(NS_SSQ, (int64_t)a.mat[j].m * a.mat[j].n / 2048));
     blocks += a.mat[j].nssq;
   }
   a.beg[a.n] = blocks;
@@ -458,33 +791,12 @@ hipError_t run_begin(NsArgs& a, hipStream_t st) {
 
 }  // namespace
 
-int ns_ssq_blocks(int64_t m, int64_t n) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>(NS_SSQ, m * n / 2048));
-}
-
-// The edge of the result tiles for a group of matrices: the largest of 128, 64 and
-// 32 whose products X X^T fill the compute units.
-int ns_tile(int n, const int64_t* m) {
-  for (int T : {128, 64}) {
-    int64_t tiles = 0;
-    for (int j = 0; j < n; ++j) {
-      const int64_t tm = (m[j] + T - 1) / T;
-      tiles += tm * (tm + 1) / 2;
-    }
-    if (tiles >= 256) return T;
-  }
-  return 32;
-}
-
-hipError_t launch_newton_schulz(NsArgs& a, int tile, bool bf16, bool muon, int steps, const float* coef, hipStream_t st) {
+hipError_t launch_newton_schulz(NsArgs& a, bool bf16, bool muon, int steps, const float* coef, hipStream_t st) {
   hipError_t e = muon ? run_begin<float, true>(a, st)
                  : bf16 ? run_begin<__bf16, false>(a, st) : run_begin<float, false>(a, st);
   if (e != hipSuccess) return e;
-  switch (tile) {
-    case 128: return run_steps<128, 1, 2>(a, bf16, muon, steps, coef, st);
-    case 64: return run_steps<64, 1, 3>(a, bf16, muon, steps, coef, st);
-    default: return run_steps<32, 1, 3>(a, bf16, muon, steps, coef, st);
-  }
+  if (muon) return bf16 ? run_steps<__bf16, true>(a, steps, coef, st) : run_steps<float, true>(a, steps, coef, st);
+  return bf16 ? run_steps<__bf16, false>(a, steps, coef, st) : run_steps<float, false>(a, steps, coef, st);
 }
 
 }  // namespace sscn
