@@ -93,20 +93,33 @@ size_t carve_matrix(NsMat& M, int64_t rows, int64_t cols, char* base) {
   return off;
 }
 
-// Matrices go through the launches in groups of NS_MATS; the groups share the workspace.
+// Matrices go through the launches in groups of NS_MATS, which share the workspace.
+// Carves a group's part of it, the matrices with the longest sums first, and calls
+// fill(index, matrix) for each; returns the bytes.
+template <class Shape, class Fill>
+size_t carve_group(NsArgs& a, int32_t first, int k, Shape&& shape, Fill&& fill, char* base) {
+  size_t off = 0;
+  a.n = k;
+  for (int j = 0; j < k; ++j) {
+    NsMat& M = a.mat[j];
+    M = NsMat{};
+    const auto s = shape(first + j);
+    off += carve_matrix(M, s.first, s.second, base ? base + off : nullptr);
+    fill(first + j, M);
+  }
+  std::stable_sort(a.mat, a.mat + k, [](const NsMat& x, const NsMat& y) { return x.n > y.n; });
+  a.count = (int32_t*)(base ? base + off : nullptr);
+  off += aligned256(NS_COUNT * sizeof(int32_t));
+  a.part = (float*)(base ? base + off : nullptr);
+  return off + aligned256(ns_part_bytes(a));
+}
+
 template <class Shape>
 size_t group_bytes(int32_t n, Shape&& shape) {
   size_t most = 0;
-  for (int32_t g = 0; g < n; g += NS_MATS) {
-    const int k = std::min(NS_MATS, n - g);
-    size_t sum = 0;
-    for (int j = 0; j < k; ++j) {
-      NsMat M{};
-      const auto s = shape(g + j);
-      sum += carve_matrix(M, s.first, s.second, nullptr);
-    }
-    most = std::max(most, sum);
-  }
+  NsArgs a;
+  for (int32_t g = 0; g < n; g += NS_MATS)
+    most = std::max(most, carve_group(a, g, std::min(NS_MATS, n - g), shape, [](int32_t, NsMat&) {}, nullptr));
   return most;
 }
 
@@ -114,18 +127,7 @@ template <class Shape, class Fill>
 hipError_t run_groups(int32_t n, Shape&& shape, Fill&& fill, NsArgs& a, bool bf16, bool muon, int32_t steps,
                       const float* coef, void* d_ws, hipStream_t st) {
   for (int32_t g = 0; g < n; g += NS_MATS) {
-    const int k = std::min(NS_MATS, n - g);
-    char* at = (char*)d_ws;
-    a.n = k;
-    for (int j = 0; j < k; ++j) {
-      NsMat& M = a.mat[j];
-      M = NsMat{};
-      const auto s = shape(g + j);
-      at += carve_matrix(M, s.first, s.second, at);
-      fill(g + j, M);
-    }
-    // the longest sums start first
-    std::stable_sort(a.mat, a.mat + k, [](const NsMat& x, const NsMat& y) { return x.n > y.n; });
+    carve_group(a, g, std::min(NS_MATS, n - g), shape, fill, (char*)d_ws);
     const hipError_t e = launch_newton_schulz(a, bf16, muon, steps, coef, st);
     if (e != hipSuccess) return e;
   }

@@ -484,6 +484,9 @@ struct NsMat {
   int32_t mp, np;  // padded to multiples of 32
   int32_t tall;    // the caller's matrix is X transposed
   int32_t nssq;
+  // of the product at hand: tiles before `whole` are one workgroup's, the others are
+  // summed by `parts` workgroups each, whose partial tiles and counters start here
+  int32_t whole, parts, slot, counter;
   // workspace
   float* X;        // [mp][np]
   char* opX;       // operand with X's rows
@@ -506,9 +509,14 @@ struct NsArgs {
   int32_t nesterov;
   float momentum;
   float a, b, c;
+  float* part;     // partial tiles
+  int32_t* count;  // [NS_COUNT] finished parts of each divided tile, zero between products
   int32_t beg[NS_MATS + 1];
   NsMat mat[NS_MATS];
 };
+constexpr int NS_COUNT = 1024;
+// Bytes of partial tiles that the group's products need (m, n, mp, np set).
+size_t ns_part_bytes(NsArgs& a);
 hipError_t launch_newton_schulz(NsArgs& a, bool bf16, bool muon, int steps, const float* coef, hipStream_t st);
 
 }  // namespace sscn

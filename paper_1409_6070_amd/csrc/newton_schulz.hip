@@ -96,9 +96,12 @@ __device__ inline int find_mat(const NsArgs& a, int t) {
   return j;
 }
 
-// Products take 256 x 128 tiles where that makes NS_LARGE of them, 64 x 64 tiles where
-// that makes NS_MID, else 32 x 32.
-constexpr int NS_LARGE = 100, NS_MID = 160;
+// Products with at least NS_BIG slabs of 128 x 128 x 32 per compute unit go through LDS:
+// in 256 x 128 tiles where their last round has NS_FULL workgroups or can be divided,
+// else in 128 x 128 tiles, two workgroups a compute unit.  Smaller ones go straight into
+// registers, in 64 x 64 tiles where those make two per compute unit, else in 32 x 32.
+constexpr int NS_CUS = 256, NS_BIG = 30, NS_FULL = 192;
+constexpr int NS_PARTS = 16;  // workgroups that share a tile, at most
 
 // Sum over the workgroup's 256 threads, in all of them (red: four doubles).
 __device__ inline double block_sum(double s, double* red) {
@@ -117,6 +120,8 @@ __device__ inline double block_sum(double s, double* red) {
 template <typename T, bool MUON>
 __global__ void __launch_bounds__(256) k_ns_begin(NsArgs a) {
   constexpr int U = 8;
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < NS_COUNT; i += 256) a.count[i] = 0;
   const int j = find_mat(a, blockIdx.x);
   const NsMat M = a.mat[j];
   const int blk = blockIdx.x - a.beg[j], nblk = a.beg[j + 1] - a.beg[j];
@@ -235,18 +240,34 @@ struct NsWork {
   static_assert(TM % TN == 0, "a tile row is one or several tile columns high");
   NsMat M;
   int ti, tj;       // tile row and column
-  int kblocks;
+  int kblocks;        // blocks of k in the operands' rows
+  int k0, k1;         // those of this workgroup
+  int part, parts;    // which of the workgroups that share the tile
+  int slot, counter;  // the tile's first partial tile, its counter
   const char *P, *Q;  // first block of the tile's rows in each operand
   int pr, qr;         // row blocks of each inside the padded matrix (a last tile has fewer)
 
   // false: no tile for this workgroup.  Workgroup b runs on XCD b % 8: each XCD takes
   // an eighth of every matrix's tiles, consecutive ones, whose operands its L2 shares.
   __device__ inline bool find(const NsArgs& a) {
-    const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
-    const int j = find_mat(a, slot);
+    const int xcd = blockIdx.x & 7, slot_of_xcd = blockIdx.x >> 3;
+    const int j = find_mat(a, slot_of_xcd);
     M = a.mat[j];
-    const int per = a.beg[j + 1] - a.beg[j], t = xcd * per + slot - a.beg[j];
-    const int tm = (M.mp + TM - 1) / TM;
+    const int tm = (M.mp + TM - 1) / TM, whole = (M.whole + 7) / 8;
+    int t = slot_of_xcd - a.beg[j];
+    part = 0;
+    parts = 1;
+    if (t < whole) {
+      t += xcd * whole;
+      if (t >= M.whole) return false;
+    } else {
+      const int r = xcd * (a.beg[j + 1] - a.beg[j] - whole) + t - whole, q = r / M.parts;
+      t = M.whole + q;
+      part = r - q * M.parts;
+      parts = M.parts;
+      slot = M.slot + q * M.parts;
+      counter = M.counter + q;
+    }
     if constexpr (symmetric(KIND)) {  // tiles that reach the diagonal or lie below it
       constexpr int R = TM / TN;
       ti = 0;  // R (1 + 2 + .. + ti) tiles in the rows above
@@ -264,6 +285,8 @@ struct NsWork {
     const int mp = M.mp, cols = symmetric(KIND) ? mp : M.np;
     if (ti >= tm || tj * TN >= cols) return false;
     kblocks = (KIND == NS_GRAM ? M.np : mp) / 32;
+    k0 = kblocks * part / parts;
+    k1 = kblocks * (part + 1) / parts;
     P = KIND == NS_GRAM ? M.opX : KIND == NS_POLY ? M.opA : M.opB;
     Q = KIND == NS_GRAM ? M.opX : KIND == NS_POLY ? M.opA : M.opXt;
     P += block_at(ti * (TM / 16), 0, kblocks);
@@ -374,6 +397,47 @@ __device__ inline Run8<float> load_weights(const NsMat& M, int row, int c) {
   if constexpr (KIND != NS_MUON) return Run8<float>{};
   const int rows = M.tall ? M.n : M.m, cols = M.tall ? M.m : M.n;
   return load_run<float>(M.w + (int64_t)row * cols + c, row < rows ? cols - c : 0);
+}
+
+// A tile that several workgroups share: each stores its sums (staged in LDS) as a
+// partial tile; the last one to finish adds them all in their order, back into LDS,
+// and returns true.  Released with the counter, acquired by
+// the last.
+template <int TM, int TN, int NT, class W>
+__device__ inline bool join_parts(const NsArgs& a, const W& w, float* Cs) {
+  constexpr int CS = TN + 4, V = TM * TN / 4;
+  static_assert(V % NT == 0, "whole vectors per thread");
+  __shared__ int last;
+  f32x4* out = (f32x4*)(a.part + (int64_t)(w.slot + w.part) * (TM * TN));
+  for (int i = threadIdx.x; i < V; i += NT)
+    out[i] = *(const f32x4*)(Cs + i / (TN / 4) * CS + i % (TN / 4) * 4);
+  __syncthreads();
+  if (threadIdx.x == 0)
+    last = __hip_atomic_fetch_add(a.count + w.counter, 1, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT) == w.parts - 1;
+  __syncthreads();
+  if (!last) return false;
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+  const f32x4* in = (const f32x4*)(a.part + (int64_t)w.slot * (TM * TN)) + threadIdx.x;
+  constexpr int N = V / NT;  // a part's loads are in flight together
+  f32x4 sum[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) sum[i] = in[i * NT];
+#pragma unroll 1
+  for (int p = 1; p < w.parts; ++p) {
+    f32x4 more[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) more[i] = in[(int64_t)p * V + i * NT];
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] += more[i];
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int at = threadIdx.x + i * NT;
+    *(f32x4*)(Cs + at / (TN / 4) * CS + at % (TN / 4) * 4) = sum[i];
+  }
+  if (threadIdx.x == 0) __hip_atomic_store(a.count + w.counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  return true;
 }
 
 // The tile's sums, staged in LDS as PARTS partial tiles [TM][TN + 4], to the result:
@@ -531,7 +595,7 @@ struct NsTile {
 };
 
 template <int TM, int TN, int NST, int KIND, typename TO>
-__global__ void __launch_bounds__((NsTile<TM, TN, NST>::NW * 64)) k_ns_tiles(NsArgs a) {
+__global__ void __launch_bounds__((NsTile<TM, TN, NST>::NW * 64), 2) k_ns_tiles(NsArgs a) {
   using C = NsTile<TM, TN, NST>;
   constexpr int FT = C::FT;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -549,7 +613,7 @@ __global__ void __launch_bounds__((NsTile<TM, TN, NST>::NW * 64)) k_ns_tiles(NsA
     // (row blocks past the matrix: the last one again, its results are dropped)
     const int rb = min(q / 2, (of_q ? w.qr : w.pr) - 1);
     load_plane(of_q ? rq : rp, lds0 + (uint32_t)(st * C::SLAB + p * 1024), lane_off,
-               (uint32_t)((rb * w.kblocks + s) * BLOCK + (q % 2) * 1024));
+               (uint32_t)((rb * w.kblocks + w.k0 + s) * BLOCK + (q % 2) * 1024));
   };
   auto issue = [&](int s, int st) {
 #pragma unroll
@@ -561,7 +625,7 @@ __global__ void __launch_bounds__((NsTile<TM, TN, NST>::NW * 64)) k_ns_tiles(NsA
 #pragma unroll
     for (int k = 0; k < FT; ++k) acc[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
   // (slabs behind the last one: the last one again, not used)
-  const int nsl = w.kblocks;
+  const int nsl = w.k1 - w.k0;
 #pragma unroll
   for (int p = 0; p < NST; ++p) issue(min(p, nsl - 1), p);
   // Slab s lies in registers when its turn comes: it is read out of LDS while slab
@@ -587,8 +651,8 @@ __global__ void __launch_bounds__((NsTile<TM, TN, NST>::NW * 64)) k_ns_tiles(NsA
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  static_assert(NST == 3 && C::LPW <= 2 * FT, "the waits and the dealing of loads below");
-  arrive(std::integral_constant<int, 2>{});
+  static_assert(NST >= 2 && C::LPW <= 2 * FT, "the waits and the dealing of loads below");
+  arrive(std::integral_constant<int, NST - 1>{});
 #pragma unroll
   for (int n = 0; n < 4 * FT; ++n) read_one(ring[0], 0, n);
   constexpr int GROUPS = 4 * FT, PER = 3 * FT * FT / GROUPS;
@@ -601,7 +665,7 @@ __global__ void __launch_bounds__((NsTile<TM, TN, NST>::NW * 64)) k_ns_tiles(NsA
     }
   };
   auto step = [&](int s, const NsOperands<FT>& now, NsOperands<FT>& next, int from, int to) {
-    arrive(std::integral_constant<int, 1>{});
+    arrive(std::integral_constant<int, NST - 2>{});
     const int slab = min(s + NST, nsl - 1);
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
@@ -615,7 +679,7 @@ __global__ void __launch_bounds__((NsTile<TM, TN, NST>::NW * 64)) k_ns_tiles(NsA
   int s = 0;
 #pragma unroll 1
   for (; s + 1 < nsl; s += 2) {
-    const int st1 = st == 2 ? 0 : st + 1, st2 = st1 == 2 ? 0 : st1 + 1;
+    const int st1 = st == NST - 1 ? 0 : st + 1, st2 = st1 == NST - 1 ? 0 : st1 + 1;
     step(s, ring[0], ring[1], st1, st);
     step(s + 1, ring[1], ring[0], st2, st1);
     st = st2;
@@ -629,6 +693,7 @@ __global__ void __launch_bounds__((NsTile<TM, TN, NST>::NW * 64)) k_ns_tiles(NsA
   float* Cs = (float*)smem;
   stage_tile<FT, C::CS>(Cs + wm * 64 * C::CS + wn * 64, acc, lane);
   __syncthreads();
+  if (w.parts > 1 && !join_parts<TM, TN, C::NW * 64>(a, w, Cs)) return;
   finish_tile<TM, TN, KIND, TO, C::NW, 1, 8, false>(a, w, Cs, wave, lane, nullptr);
 }
 
@@ -698,20 +763,94 @@ __global__ void __launch_bounds__(NW * 64) k_ns_direct(NsArgs a) {
 // ---------------------------------------------------------------------------
 // host
 
-// TM x TN tiles of one product over the group; with `slots`, a.beg gets each matrix's
-// range of workgroups per XCD.
-int64_t count_tiles(NsArgs& a, int kind, int TM, int TN, bool slots) {
-  int64_t all = 0, beg = 0;
+// The kernels of a product.
+enum NsPlan { NS_256, NS_128, NS_64, NS_32 };
+struct NsShape {
+  int tm, tn;
+  int min_k;  // blocks of k that a part of a divided tile has at least; 0: tiles are not divided
+};
+constexpr NsShape NS_SHAPE[] = {{256, 128, 16}, {128, 128, 12}, {64, 64, 0}, {32, 32, 0}};
+
+int64_t tiles_of(const NsMat& M, int kind, const NsShape& s) {
+  const int64_t tm = (M.mp + s.tm - 1) / s.tm, tn = (M.np + s.tn - 1) / s.tn;
+  // (a last tile row that ends early has tiles past the diagonal: they find nothing to do)
+  return symmetric(kind) ? s.tm / s.tn * (tm * (tm + 1) / 2) : tm * tn;
+}
+
+int64_t k_of(const NsMat& M, int kind) { return (kind == NS_GRAM ? M.np : M.mp) / 32; }
+
+// How many workgroups can share a tile of the last round of 256 x 128 tiles, which has
+// `rest` tiles: they are the last matrix's.
+int64_t last_round_parts(const NsMat& last, int kind, int64_t rest) {
+  if (rest == 0 || rest > tiles_of(last, kind, NS_SHAPE[NS_256])) return 1;
+  return std::max<int64_t>(1, std::min<int64_t>({NS_PARTS, NS_CUS / rest, k_of(last, kind) / NS_SHAPE[NS_256].min_k}));
+}
+
+// Which kernel a product over the group takes.
+NsPlan plan_product(const NsArgs& a, int kind) {
+  int64_t t256 = 0, t64 = 0, slabs = 0;
   for (int j = 0; j < a.n; ++j) {
-    const int64_t tm = (a.mat[j].mp + TM - 1) / TM, tn = (a.mat[j].np + TN - 1) / TN;
-    // (a last tile row that ends early has tiles past the diagonal: they find nothing to do)
-    const int64_t tiles = symmetric(kind) ? TM / TN * (tm * (tm + 1) / 2) : tm * tn;
-    if (slots) a.beg[j] = (int32_t)beg;
-    all += tiles;
-    beg += (tiles + 7) / 8;
+    t256 += tiles_of(a.mat[j], kind, NS_SHAPE[NS_256]);
+    t64 += tiles_of(a.mat[j], kind, NS_SHAPE[NS_64]);
+    slabs += tiles_of(a.mat[j], kind, NS_SHAPE[NS_128]) * k_of(a.mat[j], kind);
   }
-  if (slots) a.beg[a.n] = (int32_t)beg;
-  return all;
+  if (slabs < NS_BIG * NS_CUS) return t64 >= 2 * NS_CUS ? NS_64 : NS_32;
+  const int64_t rest = t256 % NS_CUS;
+  return rest == 0 || rest >= NS_FULL || (t256 > NS_CUS && last_round_parts(a.mat[a.n - 1], kind, rest) > 1) ? NS_256
+                                                                                                         : NS_128;
+}
+
+// Deals the tiles of a product to workgroups, and the k of a tile to several where the
+// tiles alone would leave compute units idle: all tiles of a product that has fewer than
+// compute units, or those of its last round.  Sets a.beg (workgroups per XCD) and the
+// matrices' parts; returns the partial tiles.
+int64_t deal_tiles(NsArgs& a, int kind, NsPlan plan) {
+  const NsShape& s = NS_SHAPE[plan];
+  int64_t all = 0, work = 0, most_k = 0;
+  for (int j = 0; j < a.n; ++j) {
+    const int64_t t = tiles_of(a.mat[j], kind, s), k = k_of(a.mat[j], kind);
+    a.mat[j].whole = (int32_t)t;
+    a.mat[j].parts = 1;
+    all += t;
+    work += t * k;
+    most_k = std::max(most_k, k);
+  }
+  if (s.min_k == 0) {
+  } else if (all < NS_CUS) {
+    auto parts = [&](const NsMat& M, int64_t len) {
+      return std::min<int64_t>(NS_PARTS, (k_of(M, kind) + len - 1) / len);
+    };
+    int64_t len = std::max<int64_t>(s.min_k, (work + NS_CUS - 1) / NS_CUS);
+    for (; len < most_k; len += std::max<int64_t>(1, len / 16)) {
+      int64_t items = 0;
+      for (int j = 0; j < a.n; ++j) items += a.mat[j].whole * parts(a.mat[j], len);
+      if (items <= NS_CUS) break;
+    }
+    for (int j = 0; j < a.n; ++j) {
+      a.mat[j].parts = (int32_t)parts(a.mat[j], len);
+      if (a.mat[j].parts > 1) a.mat[j].whole = 0;
+    }
+  } else if (plan == NS_256) {
+    NsMat& M = a.mat[a.n - 1];
+    const int64_t rest = all % NS_CUS, p = last_round_parts(M, kind, rest);
+    if (p > 1) {
+      M.whole -= (int32_t)rest;
+      M.parts = (int32_t)p;
+    }
+  }
+  int64_t beg = 0, slots = 0, counters = 0;
+  for (int j = 0; j < a.n; ++j) {
+    NsMat& M = a.mat[j];
+    const int64_t divided = tiles_of(M, kind, s) - M.whole;
+    M.slot = (int32_t)slots;
+    M.counter = (int32_t)counters;
+    a.beg[j] = (int32_t)beg;
+    beg += (M.whole + 7) / 8 + (divided * M.parts + 7) / 8;
+    slots += divided * M.parts;
+    counters += divided;
+  }
+  a.beg[a.n] = (int32_t)beg;
+  return slots;  // (divided tiles are fewer than compute units, so than NS_COUNT)
 }
 
 // LDS of k_ns_direct: the waves' partial tiles, and what lies beside the result.
@@ -736,19 +875,24 @@ hipError_t launch_tiles(int threads, int lds, const NsArgs& a, hipStream_t st) {
 
 template <int KIND, typename TO>
 hipError_t run_product(NsArgs& a, hipStream_t st) {
-  if (count_tiles(a, KIND, 256, 128, false) >= NS_LARGE) {
-    count_tiles(a, KIND, 256, 128, true);
-    using C = NsTile<256, 128, 3>;
-    return launch_tiles<k_ns_tiles<256, 128, 3, KIND, TO>>(C::NW * 64, C::LDS, a, st);
+  const NsPlan plan = plan_product(a, KIND);
+  deal_tiles(a, KIND, plan);
+  switch (plan) {
+    case NS_256: {
+      using C = NsTile<256, 128, 3>;
+      return launch_tiles<k_ns_tiles<256, 128, 3, KIND, TO>>(C::NW * 64, C::LDS, a, st);
+    }
+    case NS_128: {
+      using C = NsTile<128, 128, 2>;
+      return launch_tiles<k_ns_tiles<128, 128, 2, KIND, TO>>(C::NW * 64, C::LDS, a, st);
+    }
+    case NS_64:
+      return launch_tiles<k_ns_direct<64, 4, 2, KIND, TO>>(256, direct_lds(64, 4), a, st);
+    default: {
+      constexpr int NW = symmetric(KIND) ? 8 : 4;  // (X X^T has the longest sums, B X the most tiles)
+      return launch_tiles<k_ns_direct<32, NW, 3, KIND, TO>>(NW * 64, direct_lds(32, NW), a, st);
+    }
   }
-  if (count_tiles(a, KIND, 64, 64, false) >= NS_MID) {
-    count_tiles(a, KIND, 64, 64, true);
-    return launch_tiles<k_ns_direct<64, 4, 2, KIND, TO>>(256, direct_lds(64, 4), a, st);
-  }
-  count_tiles(a, KIND, 32, 32, true);
-  // (X X^T has the longest sums, B X the most tiles)
-  constexpr int NW = symmetric(KIND) ? 8 : 4;
-  return launch_tiles<k_ns_direct<32, NW, 3, KIND, TO>>(NW * 64, direct_lds(32, NW), a, st);
 }
 
 template <typename TO, bool MUON>
@@ -790,6 +934,15 @@ hipError_t run_begin(NsArgs& a, hipStream_t st) {
 }
 
 }  // namespace
+
+size_t ns_part_bytes(NsArgs& a) {
+  int64_t most = 0;
+  for (const int kind : {NS_GRAM, NS_POLY, NS_APPLY}) {
+    const NsPlan plan = plan_product(a, kind);
+    most = std::max(most, deal_tiles(a, kind, plan) * NS_SHAPE[plan].tm * NS_SHAPE[plan].tn);
+  }
+  return (size_t)most * sizeof(float);
+}
 
 hipError_t launch_newton_schulz(NsArgs& a, bool bf16, bool muon, int steps, const float* coef, hipStream_t st) {
   hipError_t e = muon ? run_begin<float, true>(a, st)

@@ -144,7 +144,7 @@ def test_muon_workspace_covers_its_largest_group():
     assert need(vec, vec) == 0
     assert need(one, vec) == need(one)
     assert need(*([one] * 24)) == need(*([one] * 25)) == need(*([one] * 70))
-    assert need(*([one] * 24)) == 24 * need(one)
+    assert need(one) < need(*([one] * 24)) <= 24 * need(one)  # a group shares its counters
     mats = _mats(*([(64, 32)] * 30))
     assert sscn.sscn_orthogonalize_workspace_bytes(mats) == need(*([one] * 30))
 
