@@ -45,6 +45,20 @@ __device__ inline void store_pack(T* p, const float (&f)[V]) {
   __builtin_memcpy(p, &v, sizeof(v));
 }
 
+// Makes the compiler convert a bf16 pack anew behind this point instead of keeping
+// its float32 values, which take twice the registers (rows of NV > 1 vectors a
+// thread, where registers limit the waves).
+template <int NV, typename T, int V>
+__device__ inline void keep_packed(Pack<T, V>& p) {
+  if constexpr (NV > 1 && sizeof(T) == 2 && V % 2 == 0) {
+    uint32_t w[V / 2];
+    __builtin_memcpy(w, &p, sizeof(p));
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) asm volatile("" : "+v"(w[i]));
+    __builtin_memcpy(&p, w, sizeof(p));
+  }
+}
+
 template <int CTRL>
 __device__ inline float add_dpp(float v) {
   return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
@@ -125,35 +139,36 @@ __global__ void __launch_bounds__(threads_of(TPR)) k_norm(NormArgs a) {
   }
   const float rc = 1.f / (float)a.cols;
   const int64_t step = (int64_t)gridDim.x * RPB;
-  Pack<T, V> raw[NV];
-  auto fetch = [&](int64_t r) {
+  Pack<T, V> raw[NV], next[NV];
+  auto fetch = [&](Pack<T, V>(&to)[NV], int64_t r) {
     const T* x = (const T*)a.x + (a.rmap ? (int64_t)a.rmap[r] : r) * a.x_stride;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-      if (skip[i] < V) raw[i] = load_pack<T, V>(x + col[i]);
+      if (skip[i] < V) to[i] = load_pack<T, V>(x + col[i]);
   };
   int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
-  if (r < a.rows) fetch(r);
+  if (r < a.rows) fetch(next, r);
   for (; r < a.rows; r += step) {
-    float f[NV][V];
+    // the row stays as loaded and is converted wherever it is used
     float s[1] = {0.f};
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+      raw[i] = next[i];
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        f[i][e] = skip[i] < V ? Elem<T>::to_f32(raw[i].e[e]) : 0.f;
-        s[0] += e >= skip[i] ? f[i][e] : 0.f;
-      }
-    if (r + step < a.rows) fetch(r + step);  // in flight while this row is reduced
+      for (int e = 0; e < V; ++e) s[0] += e >= skip[i] ? Elem<T>::to_f32(raw[i].e[e]) : 0.f;
+    }
+    if (r + step < a.rows) fetch(next, r + step);  // in flight while this row is reduced
     row_sums<TPR, 1>(s, red[0]);
     const float mean = s[0] * rc;
     s[0] = 0.f;
 #pragma unroll
+    for (int i = 0; i < NV; ++i) keep_packed<NV>(raw[i]);
+#pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        f[i][e] -= mean;
-        s[0] += e >= skip[i] ? f[i][e] * f[i][e] : 0.f;
+        const float f = Elem<T>::to_f32(raw[i].e[e]) - mean;
+        s[0] += e >= skip[i] ? f * f : 0.f;
       }
     row_sums<TPR, 1>(s, red[1]);
     const float rs = 1.f / sqrtf(s[0] * rc + a.eps);
@@ -161,9 +176,11 @@ __global__ void __launch_bounds__(threads_of(TPR)) k_norm(NormArgs a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if (skip[i] >= V) continue;
+      keep_packed<NV>(raw[i]);
+      float f[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) f[i][e] = f[i][e] * rs * gain[i][e] + shift[i][e];
-      store_pack<T, V>(y + col[i], f[i]);
+      for (int e = 0; e < V; ++e) f[e] = (Elem<T>::to_f32(raw[i].e[e]) - mean) * rs * gain[i][e] + shift[i][e];
+      store_pack<T, V>(y + col[i], f);
     }
     for (int c = a.cols + t; c < a.y_cols; c += TPR) y[c] = Elem<T>::from_f32(0.f);
   }
@@ -217,45 +234,47 @@ __global__ void __launch_bounds__(threads_of(TPR)) k_norm_bwd(NormBwdArgs a) {
   }
   const float rc = 1.f / (float)a.cols;
   const int64_t step = (int64_t)gridDim.x * RPB;
-  Pack<T, V> rx[NV];
-  Pack<TD, V> rd[NV];
+  Pack<T, V> x[NV], nx[NV];
+  Pack<TD, V> d[NV], nd[NV];
   auto fetch = [&](int64_t r) {
-    const T* x = (const T*)a.x + (a.rmap ? (int64_t)a.rmap[r] : r) * a.x_stride;
-    const TD* d = (const TD*)a.dy + r * a.dy_stride;
+    const T* px = (const T*)a.x + (a.rmap ? (int64_t)a.rmap[r] : r) * a.x_stride;
+    const TD* pd = (const TD*)a.dy + r * a.dy_stride;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (skip[i] < V) {
-        rx[i] = load_pack<T, V>(x + col[i]);
-        rd[i] = load_pack<TD, V>(d + col[i]);
+        nx[i] = load_pack<T, V>(px + col[i]);
+        nd[i] = load_pack<TD, V>(pd + col[i]);
       }
   };
   int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
   if (r < a.rows) fetch(r);
   for (; r < a.rows; r += step) {
-    float f[NV][V], d[NV][V];
+    // both rows stay as loaded and are converted wherever they are used: fewer
+    // registers, so more rows of other workgroups in flight
     float s[1] = {0.f};
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+      x[i] = nx[i];
+      d[i] = nd[i];
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        f[i][e] = skip[i] < V ? Elem<T>::to_f32(rx[i].e[e]) : 0.f;
-        d[i][e] = skip[i] < V ? Elem<TD>::to_f32(rd[i].e[e]) : 0.f;
-        s[0] += e >= skip[i] ? f[i][e] : 0.f;
-      }
+      for (int e = 0; e < V; ++e) s[0] += e >= skip[i] ? Elem<T>::to_f32(x[i].e[e]) : 0.f;
+    }
     if (r + step < a.rows) fetch(r + step);
     row_sums<TPR, 1>(s, red[0]);
     const float mean = s[0] * rc;
     float q[3] = {0.f, 0.f, 0.f};
 #pragma unroll
+    for (int i = 0; i < NV; ++i) keep_packed<NV>(x[i]);
+#pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        f[i][e] -= mean;
-        const float tt = d[i][e] * gain[i][e];
+        const float f = Elem<T>::to_f32(x[i].e[e]) - mean;
+        const float tt = Elem<TD>::to_f32(d[i].e[e]) * gain[i][e];
         const bool in = e >= skip[i];
-        q[0] += in ? f[i][e] * f[i][e] : 0.f;
+        q[0] += in ? f * f : 0.f;
         q[1] += in ? tt : 0.f;
-        q[2] += in ? tt * f[i][e] : 0.f;
+        q[2] += in ? tt * f : 0.f;
       }
     row_sums<TPR, 3>(q, red[1]);
     const float rs = 1.f / sqrtf(q[0] * rc + a.eps);
@@ -264,13 +283,15 @@ __global__ void __launch_bounds__(threads_of(TPR)) k_norm_bwd(NormBwdArgs a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if (skip[i] >= V) continue;
+      keep_packed<NV>(x[i]);
+      keep_packed<NV>(d[i]);
       float o[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const float h = f[i][e] * rs;
-        o[e] = rs * (d[i][e] * gain[i][e] - m1 - h * m2);
-        dg[i][e] += d[i][e] * h;
-        ds[i][e] += d[i][e];
+        const float h = (Elem<T>::to_f32(x[i].e[e]) - mean) * rs, g = Elem<TD>::to_f32(d[i].e[e]);
+        o[e] = rs * (g * gain[i][e] - m1 - h * m2);
+        dg[i][e] += g * h;
+        ds[i][e] += g;
       }
       store_pack<TD, V>(dx + col[i], o);
     }
@@ -311,8 +332,9 @@ __global__ void __launch_bounds__(threads_of(TPR)) k_norm_bwd(NormBwdArgs a) {
   }
 }
 
-template <typename T, typename TD>
+template <typename T>
 __global__ void __launch_bounds__(1024) k_norm_bwd_long(NormBwdArgs a) {
+  using TD = T;
   __shared__ float red[2][48];
   const float rc = 1.f / (float)a.cols;
   float* pg = a.part ? a.part + (int64_t)blockIdx.x * a.cols : nullptr;
@@ -377,9 +399,11 @@ struct NormShape {
   int rpb() const { return tpr == 0 ? 1 : threads_of(tpr) / tpr; }
 };
 
-NormShape norm_shape(int ve, int cols) {
+// two: rows of up to 64 vectors in half the lanes, two vectors a lane.
+NormShape norm_shape(int ve, int cols, bool two) {
   if (cols < ve) return {8, 1, true};
   const int nvec = (cols + ve - 1) / ve;
+  if (two && nvec > 8 && nvec <= 64) return {nvec <= 16 ? 8 : nvec <= 32 ? 16 : 32, 2, false};
   if (nvec <= 8) return {8, 1, false};
   if (nvec <= 16) return {16, 1, false};
   if (nvec <= 32) return {32, 1, false};
@@ -392,12 +416,18 @@ NormShape norm_shape(int ve, int cols) {
   return {0, 0, false};
 }
 
+// float32 gradients of bf16 rows come from the softmax layer only, whose input has at
+// most 256 vectors a row
+constexpr int HEAD_VECS = 256;
+
 int64_t row_blocks(const NormShape& s, int64_t rows) { return (rows + s.rpb() - 1) / s.rpb(); }
 
 template <typename T>
 hipError_t norm_fwd(const NormArgs& a, hipStream_t st) {
   constexpr int VE = Elem<T>::VE;
-  const NormShape s = norm_shape(VE, a.cols);
+  // where rows abound, more bytes in flight (200001 rows of 100 bf16: 18.8 us with two
+  // vectors a lane, 21.1 with one; a single row of 300: 7.7 with one, 8.3 with two)
+  const NormShape s = norm_shape(VE, a.cols, a.rows >= 8192);
   const int grid = (int)std::min<int64_t>(row_blocks(s, a.rows), s.tpr == 0 || s.tpr == 1024 ? 512 : s.tpr == 512 ? 1024 : 2048);
 #define SSCN_NORM(V, TPR, NV) \
   case TPR * 8 + NV: hipLaunchKernelGGL((k_norm<T, V, TPR, NV>), dim3(grid), dim3(threads_of(TPR)), 0, st, a); break
@@ -408,8 +438,11 @@ hipError_t norm_fwd(const NormArgs& a, hipStream_t st) {
   else
     switch (s.tpr * 8 + s.nv) {
       SSCN_NORM(VE, 8, 1);
+      SSCN_NORM(VE, 8, 2);
       SSCN_NORM(VE, 16, 1);
+      SSCN_NORM(VE, 16, 2);
       SSCN_NORM(VE, 32, 1);
+      SSCN_NORM(VE, 32, 2);
       SSCN_NORM(VE, 64, 1);
       SSCN_NORM(VE, 64, 2);
       SSCN_NORM(VE, 256, 1);
@@ -425,12 +458,21 @@ hipError_t norm_fwd(const NormArgs& a, hipStream_t st) {
 template <typename T, typename TD>
 hipError_t norm_bwd(const NormBwdArgs& a, int grid, hipStream_t st) {
   constexpr int VE = Elem<T>::VE;
-  const NormShape s = norm_shape(VE, a.cols);
-#define SSCN_NORM(V, TPR, NV) \
-  case TPR * 8 + NV: hipLaunchKernelGGL((k_norm_bwd<T, TD, V, TPR, NV>), dim3(grid), dim3(threads_of(TPR)), 0, st, a); break
-  if (s.tpr == 0)
-    hipLaunchKernelGGL((k_norm_bwd_long<T, TD>), dim3(grid), dim3(1024), 0, st, a);
-  else if (s.scalar)
+  const NormShape s = norm_shape(VE, a.cols, false);
+#define SSCN_NORM(V, TPR, NV)                                                                                     \
+  case TPR * 8 + NV:                                                                                              \
+    if constexpr (sizeof(T) == sizeof(TD) || TPR * NV <= HEAD_VECS)                                               \
+      hipLaunchKernelGGL((k_norm_bwd<T, TD, V, TPR, NV>), dim3(grid), dim3(threads_of(TPR)), 0, st, a);           \
+    else                                                                                                          \
+      return hipErrorInvalidValue;                                                                                \
+    break
+  if (sizeof(T) != sizeof(TD) && (s.tpr == 0 || s.tpr * s.nv > HEAD_VECS)) return hipErrorInvalidValue;
+  if constexpr (sizeof(T) == sizeof(TD))
+    if (s.tpr == 0) {
+      hipLaunchKernelGGL(k_norm_bwd_long<T>, dim3(grid), dim3(1024), 0, st, a);
+      return hipGetLastError();
+    }
+  if (s.scalar)
     hipLaunchKernelGGL((k_norm_bwd<T, TD, 1, 8, 1>), dim3(grid), dim3(256), 0, st, a);
   else
     switch (s.tpr * 8 + s.nv) {
@@ -452,8 +494,11 @@ hipError_t norm_bwd(const NormBwdArgs& a, int grid, hipStream_t st) {
 }  // namespace
 
 int64_t norm_parts(bool bf16, int64_t rows, int32_t cols) {
-  const NormShape s = norm_shape(bf16 ? 8 : 4, cols);
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(1024, ((int64_t)1 << 25) / cols));
+  // (one vector a lane: its sums double the registers; 200001 rows of 100 bf16: 30.5 us, 33.3 with two)
+  const NormShape s = norm_shape(bf16 ? 8 : 4, cols, false);
+  // as many workgroups as the compute units hold at once: 16 waves each
+  const int64_t fill = s.tpr == 0 || s.tpr == 1024 ? 256 : s.tpr == 512 ? 512 : 1024;
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(fill, ((int64_t)1 << 25) / cols));
   return std::max<int64_t>(1, std::min(row_blocks(s, rows), most));
 }
 

@@ -389,12 +389,17 @@ def _gpu_device(device) -> torch.device:
     return torch.device("cuda", torch.cuda.current_device()) if d.type == "cuda" and d.index is None else d
 
 
-def _launch(device: torch.device, call):
-    """call(stream) on the device's current stream, with the device current."""
+# the current stream's handle; the public way to it costs 2 us a call, as much as a launch
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _launch(device: torch.device, call, *args):
+    """call(stream, ...) on the device's current stream, with the device current."""
     if device.index == torch.cuda.current_device():
-        return call(torch.cuda.current_stream(device).cuda_stream)
+        return call(_raw_stream(device.index), *args)
     with torch.cuda.device(device):
-        return call(torch.cuda.current_stream(device).cuda_stream)
+        return call(_raw_stream(device.index), *args)
 
 
 def _need(ok: bool, what: str):
@@ -405,10 +410,12 @@ def _need(ok: bool, what: str):
 def _row_stride(t: torch.Tensor, what: str) -> int:
     """Elements between the rows of a matrix whose rows are contiguous and do not overlap."""
     rows, cols = t.shape
-    _need(cols <= 1 or t.stride(1) == 1, f"{what}: rows must be contiguous")
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: rows must be contiguous")
     if rows <= 1:
         return cols
-    _need(t.stride(0) >= cols, f"{what}: rows overlap")
+    if t.stride(0) < cols:
+        raise ValueError(f"{what}: rows overlap")
     return t.stride(0)
 
 
@@ -657,49 +664,63 @@ class LayerNorm:
         self.ws_bytes = sscn_layer_norm_workspace_bytes(self.code, rows_max, cols)
         self.device = _gpu_device(device)
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
+        self.ws_ptr = self.ws.data_ptr()
 
-    def _rows(self, t: torch.Tensor, rows: Optional[int], what: str) -> int:
-        _need(t.dtype == self.tdtype and t.device == self.device, f"{what}: {self.dtype} on {self.device}")
-        _need(t.dim() == 2 and t.shape[1] == self.cols and (rows is None or t.shape[0] == rows),
-              f"{what}: [{'rows' if rows is None else rows}, {self.cols}]")
-        return _row_stride(t, what)
+    # (messages are made only where they are raised: the calls below are a few microseconds long)
+    def _rows(self, t: torch.Tensor, what: str):
+        """(rows, elements between rows) of a matrix for this norm."""
+        if t.dtype != self.tdtype or t.device != self.device or t.dim() != 2 or t.shape[1] != self.cols:
+            raise ValueError(f"{what}: [rows, {self.cols}] {self.dtype} on {self.device}")
+        if t.is_contiguous():
+            return t.shape[0], self.cols
+        return t.shape[0], _row_stride(t, what)
 
     def _param(self, t: Optional[torch.Tensor], what: str):
         if t is None:
             return None
-        _need(t.dtype == torch.float32 and t.device == self.device and t.is_contiguous() and t.numel() == self.cols,
-              f"{what}: [{self.cols}] float32 on {self.device}")
+        if t.dtype != torch.float32 or t.device != self.device or t.numel() != self.cols or not t.is_contiguous():
+            raise ValueError(f"{what}: [{self.cols}] float32 on {self.device}")
         return t.data_ptr()
 
     def forward(self, x: torch.Tensor, gain: Optional[torch.Tensor] = None, shift: Optional[torch.Tensor] = None,
                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """out (may be x) or a new contiguous tensor; gain and shift [cols] float32, None for 1 and 0."""
-        xs = self._rows(x, None, "x")
-        rows = x.shape[0]
+        rows, xs = self._rows(x, "x")
         if out is None:
-            out = torch.empty(rows, self.cols, dtype=self.tdtype, device=self.device)
-        ys = self._rows(out, rows, "out")
+            out, ys = torch.empty((rows, self.cols), dtype=self.tdtype, device=self.device), self.cols
+        else:
+            n, ys = self._rows(out, "out")
+            _need(n == rows, "out: as many rows as x")
         g, s = self._param(gain, "gain"), self._param(shift, "shift")
-        _launch(self.device, lambda st: sscn_layer_norm_forward(
-            self.code, x.data_ptr(), xs, rows, self.cols, g, s, self.eps, out.data_ptr(), ys, st))
+        _launch(self.device, self._forward, x.data_ptr(), xs, rows, g, s, out.data_ptr(), ys)
         return out
+
+    def _forward(self, stream, x, xs, rows, g, s, y, ys):
+        sscn_layer_norm_forward(self.code, x, xs, rows, self.cols, g, s, self.eps, y, ys, stream)
 
     def backward(self, dy: torch.Tensor, x: torch.Tensor, gain: Optional[torch.Tensor] = None,
                  dx: Optional[torch.Tensor] = None):
         """(dx, dgain, dshift) from the output's gradient and the forward's input; dx may be given (dy and x too)."""
-        xs = self._rows(x, None, "x")
-        rows = x.shape[0]
-        _need(rows <= self.rows_max, f"rows: at most {self.rows_max}")
+        rows, xs = self._rows(x, "x")
+        n, ds = self._rows(dy, "dy")
+        _need(n == rows, "dy: as many rows as x")
+        if rows > self.rows_max:
+            raise ValueError(f"rows: at most {self.rows_max}")
         if dx is None:
-            dx = torch.empty(rows, self.cols, dtype=self.tdtype, device=self.device)
-        ds, os = self._rows(dy, rows, "dy"), self._rows(dx, rows, "dx")
+            dx, os = torch.empty((rows, self.cols), dtype=self.tdtype, device=self.device), self.cols
+        else:
+            n, os = self._rows(dx, "dx")
+            _need(n == rows, "dx: as many rows as x")
         g = self._param(gain, "gain")
         dgain = torch.empty(self.cols, dtype=torch.float32, device=self.device)
         dshift = torch.empty(self.cols, dtype=torch.float32, device=self.device)
-        _launch(self.device, lambda st: sscn_layer_norm_backward(
-            self.code, dy.data_ptr(), ds, x.data_ptr(), xs, rows, self.cols, g, self.eps, dx.data_ptr(), os,
-            dgain.data_ptr(), dshift.data_ptr(), self.ws.data_ptr(), self.ws_bytes, st))
+        _launch(self.device, self._backward, dy.data_ptr(), ds, x.data_ptr(), xs, rows, g, dx.data_ptr(), os,
+                dgain.data_ptr(), dshift.data_ptr())
         return dx, dgain, dshift
+
+    def _backward(self, stream, dy, ds, x, xs, rows, g, dx, os, dgain, dshift):
+        sscn_layer_norm_backward(self.code, dy, ds, x, xs, rows, self.cols, g, self.eps, dx, os, dgain, dshift,
+                                 self.ws_ptr, self.ws_bytes, stream)
 
 
 class Orthogonalizer:
@@ -724,8 +745,8 @@ class Orthogonalizer:
         _need(len(mats) == len(out) == len(self.shapes), f"{len(self.shapes)} matrices")
         for m, i, o, shape in zip(self._mats, mats, out, self.shapes):
             for t, what in ((i, "matrix"), (o, "out")):
-                _need(t.shape == shape and t.dtype == self.tdtype and t.device == self.device,
-                      f"{what}: {shape} {self.tdtype} on {self.device}")
+                if t.shape != shape or t.dtype != self.tdtype or t.device != self.device:
+                    raise ValueError(f"{what}: {shape} {self.tdtype} on {self.device}")
             m.d_in, m.in_stride = i.data_ptr(), _row_stride(i, "matrix")
             m.d_out, m.out_stride = o.data_ptr(), _row_stride(o, "out")
         _launch(self.device, lambda st: sscn_orthogonalize(self.code, self._mats, self.steps, self.coef,
@@ -766,10 +787,11 @@ class Muon:
         _need(len(W32) == len(W) == len(grads) == len(vs) == n, f"{n} arrays")
         for p, s, w, c, g, v in zip(self._params, self.shapes, W32, W, grads, vs):
             for t in (w, g, v):
-                _need(t.shape == s and t.dtype == torch.float32 and t.device == self.device and t.is_contiguous(),
-                      f"parameter: {s} float32 on {self.device}, contiguous")
-            _need(c is None or (c.shape == s and c.dtype == self.tdtype and c.device == self.device
-                                and c.is_contiguous()), f"copy: {s} {self.tdtype} on {self.device}, contiguous")
+                if t.shape != s or t.dtype != torch.float32 or t.device != self.device or not t.is_contiguous():
+                    raise ValueError(f"parameter: {s} float32 on {self.device}, contiguous")
+            if c is not None and (c.shape != s or c.dtype != self.tdtype or c.device != self.device
+                                  or not c.is_contiguous()):
+                raise ValueError(f"copy: {s} {self.tdtype} on {self.device}, contiguous")
             p.d_w, p.d_g, p.d_v = w.data_ptr(), g.data_ptr(), v.data_ptr()
             p.d_w_store = None if c is None else c.data_ptr()
             p.lr = lr if p.orthogonal or lr_rest is None else lr_rest
