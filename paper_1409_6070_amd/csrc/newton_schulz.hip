@@ -96,11 +96,12 @@ __device__ inline int find_mat(const NsArgs& a, int t) {
   return j;
 }
 
-// Products with at least NS_BIG slabs of 128 x 128 x 32 per compute unit go through LDS:
+// Products with at least NS_BIG (X X^T, A A) or NS_BIG_APPLY (B X: more tiles, shorter
+// sums) slabs of 128 x 128 x 32 per compute unit go through LDS:
 // in 256 x 128 tiles where their last round has NS_FULL workgroups or can be divided,
 // else in 128 x 128 tiles, two workgroups a compute unit.  Smaller ones go straight into
 // registers, in 64 x 64 tiles where those make two per compute unit, else in 32 x 32.
-constexpr int NS_CUS = 256, NS_BIG = 30, NS_FULL = 192;
+constexpr int NS_CUS = 256, NS_BIG = 30, NS_BIG_APPLY = 5, NS_FULL = 192;
 constexpr int NS_PARTS = 16;  // workgroups that share a tile, at most
 
 // Sum over the workgroup's 256 threads, in all of them (red: four doubles).
@@ -728,7 +729,8 @@ __global__ void __launch_bounds__(NW * 64) k_ns_direct(NsArgs a) {
   };
   NsOperands<FT> ring[DEPTH];
 #pragma unroll
-  for (int d = 0; d < DEPTH; ++d) ring[d] = load(k0 + d);
+  for (int d = 0; d < DEPTH; ++d)  // (X X^T: its waves have more blocks than DEPTH, as a rule)
+    if (d == 0 || KIND == NS_GRAM || k0 + d < k1) ring[d] = load(k0 + d);
   char* beside = smem + NW * T * CS * 4;
   if constexpr (KIND != NS_GRAM)
     for (int b = wave; b < NB; b += NW) {
@@ -794,7 +796,7 @@ NsPlan plan_product(const NsArgs& a, int kind) {
     t64 += tiles_of(a.mat[j], kind, NS_SHAPE[NS_64]);
     slabs += tiles_of(a.mat[j], kind, NS_SHAPE[NS_128]) * k_of(a.mat[j], kind);
   }
-  if (slabs < NS_BIG * NS_CUS) return t64 >= 2 * NS_CUS ? NS_64 : NS_32;
+  if (slabs < (symmetric(kind) ? NS_BIG : NS_BIG_APPLY) * NS_CUS) return t64 >= 2 * NS_CUS ? NS_64 : NS_32;
   const int64_t rest = t256 % NS_CUS;
   return rest == 0 || rest >= NS_FULL || (t256 > NS_CUS && last_round_parts(a.mat[a.n - 1], kind, rest) > 1) ? NS_256
                                                                                                          : NS_128;
