@@ -32,7 +32,7 @@
 
 namespace sscn {
 
-static_assert(sizeof(NsArgs) <= 4096, "kernel arguments must fit the 4 KiB argument segment");
+static_assert(sizeof(NsArgs) + 128 <= 4096, "kernel arguments must fit the 4 KiB argument segment");
 
 namespace {
 
@@ -763,6 +763,177 @@ __global__ void __launch_bounds__(NW * 64) k_ns_direct(NsArgs a) {
 }
 
 // ---------------------------------------------------------------------------
+// A small matrix, all steps in one workgroup: X stays in registers in float32 (wave w
+// holds the 16 x 16 blocks w, w + 8, .. of it, as the matrix cores leave them), its
+// operands, A and B in LDS.  A list of such matrices is one launch of a few
+// microseconds a step, where 3 launches a step cost 5 each.
+
+constexpr int SMALL_M = 64, SMALL_ELEMS = 8192, SMALL_STEPS = 8;
+constexpr int SMALL_XB = SMALL_ELEMS / 256 / 8, SMALL_AB = SMALL_M * SMALL_M / 256 / 8;  // blocks a wave holds
+constexpr int SMALL_LDS = 2 * SMALL_ELEMS * 4 + 2 * SMALL_M * SMALL_M * 4;
+
+struct NsCoef {
+  int32_t steps;
+  float c[3 * SMALL_STEPS];
+};
+
+// Block (bi, bj) of a result, lane l's part rows 4 (l / 16) .. of column l % 16, as the
+// operand whose rows are the result's columns: four consecutive k, 8 bytes a plane.
+__device__ inline void put_columns(char* op, int bi, int bj, int kblocks, int lane, f32x4 v, float s) {
+  typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+  f16x4 hi, lo;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float x = v[e] * s;
+    hi[e] = (_Float16)x;
+    lo[e] = (_Float16)(x - (float)hi[e]);
+  }
+  const int k = (bi & 1) * 16 + (lane >> 4) * 4;  // within a block of 32
+  char* at = op + block_at(bj, bi >> 1, kblocks) + ((k >> 3) * 16 + (lane & 15)) * 16 + (k & 7) * 2;
+  *(f16x4*)at = hi;
+  *(f16x4*)(at + BLOCK / 2) = lo;
+}
+
+// ... and as the operand with the result's rows.
+__device__ inline void put_rows(char* op, int bi, int bj, int kblocks, int lane, f32x4 v, float s) {
+  const int k = (bj & 1) * 16 + (lane & 15);
+  char* at = op + block_at(bi, bj >> 1, kblocks) + ((k >> 3) * 16 + (lane >> 4) * 4) * 16 + (k & 7) * 2;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float x = v[e] * s;
+    const _Float16 hi = (_Float16)x;
+    *(_Float16*)(at + e * 16) = hi;
+    *(_Float16*)(at + e * 16 + BLOCK / 2) = (_Float16)(x - (float)hi);
+  }
+}
+
+__device__ inline f32x4 small_product(const char* P, int bi, const char* Q, int bj, int kblocks, int lane) {
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int kb = 0; kb < kblocks; ++kb) {
+    const char* p = P + block_at(bi, kb, kblocks) + lane * 16;
+    const char* q = Q + block_at(bj, kb, kblocks) + lane * 16;
+    const f16x8 ph = *(const f16x8*)p, pl = *(const f16x8*)(p + BLOCK / 2);
+    const f16x8 qh = *(const f16x8*)q, ql = *(const f16x8*)(q + BLOCK / 2);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl, qh, acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph, ql, acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph, qh, acc, 0, 0, 0);
+  }
+  return acc;
+}
+
+template <typename T, typename TO, bool MUON>
+__global__ void __launch_bounds__(512) k_ns_small(NsArgs a, NsCoef coef) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  __shared__ double red[8];
+  const NsMat M = a.mat[blockIdx.x];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int mb = M.mp / 16, nb = M.np / 16, mk = M.mp / 32, nk = M.np / 32;
+  const int xblocks = mb * nb, ablocks = mb * mb;
+  char* opX = smem;
+  char* opXt = opX + M.mp * M.np * 4;
+  char* opA = opXt + M.mp * M.np * 4;
+  char* opB = opA + M.mp * M.mp * 4;
+  // element (i, k) of X in the caller's array
+  const int64_t stride = MUON ? (M.tall ? M.m : M.n) : M.u_stride;
+  const auto at = [&](int i, int k, int64_t ld) { return M.tall ? (int64_t)k * ld + i : (int64_t)i * ld + k; };
+  f32x4 x[SMALL_XB];
+  double ss = 0.0;
+#pragma unroll
+  for (int n = 0; n < SMALL_XB; ++n) {
+    const int t = wave + 8 * n, bi = t / nb, bj = t - bi * nb;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = bi * 16 + (lane >> 4) * 4 + e, k = bj * 16 + (lane & 15);
+      const bool in = t < xblocks && i < M.m && k < M.n;
+      const int64_t q = at(min(i, M.m - 1), min(k, M.n - 1), stride);  // (outside: an element that is read, not used)
+      float u = Elem<T>::to_f32(((const T*)M.u)[q]);
+      if constexpr (MUON) {
+        const float v = a.momentum * M.v[q] + u;
+        if (in) M.v[q] = v;
+        u = a.nesterov ? a.momentum * v + u : v;
+      }
+      x[n][e] = in ? u : 0.f;
+      ss += (double)x[n][e] * x[n][e];
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) ss += __shfl_xor(ss, d, 64);
+  if (lane == 0) red[wave] = ss;
+  __syncthreads();
+  ss = 0.0;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) ss += red[w];
+  const double inv = ss == 0.0 ? 0.0 : 1.0 / sqrt(ss);
+  const auto put_x = [&]() {
+#pragma unroll
+    for (int n = 0; n < SMALL_XB; ++n) {
+      const int t = wave + 8 * n, bi = t / nb, bj = t - bi * nb;
+      if (t >= xblocks) break;
+      put_rows(opX, bi, bj, nk, lane, x[n], SX);
+      put_columns(opXt, bi, bj, mk, lane, x[n], SX);
+    }
+  };
+#pragma unroll
+  for (int n = 0; n < SMALL_XB; ++n) {
+    const int t = wave + 8 * n, bi = t / nb, bj = t - bi * nb;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {  // (the padding stays zero beside a norm that is NaN or infinite)
+      const bool in = bi * 16 + (lane >> 4) * 4 + e < M.m && bj * 16 + (lane & 15) < M.n;
+      x[n][e] = in ? (float)((double)x[n][e] * inv) : 0.f;
+    }
+  }
+  put_x();
+  __syncthreads();
+  for (int s = 0; s < coef.steps; ++s) {
+    const float ca = coef.c[3 * s], cb = coef.c[3 * s + 1], cc = coef.c[3 * s + 2];
+    f32x4 A[SMALL_AB];
+#pragma unroll
+    for (int n = 0; n < SMALL_AB; ++n) {
+      const int t = wave + 8 * n, bi = t / mb, bj = t - bi * mb;
+      if (t >= ablocks) break;
+      A[n] = small_product(opX, bi, opX, bj, nk, lane) * (1.f / (SX * SX));
+      put_columns(opA, bi, bj, mk, lane, A[n], SA);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < SMALL_AB; ++n) {
+      const int t = wave + 8 * n, bi = t / mb, bj = t - bi * mb;
+      if (t >= ablocks) break;
+      const f32x4 B = cb * A[n] + cc * (small_product(opA, bi, opA, bj, mk, lane) * (1.f / (SA * SA)));
+      put_columns(opB, bi, bj, mk, lane, B, SB);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < SMALL_XB; ++n) {
+      const int t = wave + 8 * n, bi = t / nb, bj = t - bi * nb;
+      if (t >= xblocks) break;
+      x[n] = ca * x[n] + small_product(opB, bi, opXt, bj, mk, lane) * (1.f / (SB * SX));
+    }
+    if (s + 1 == coef.steps) break;
+    __syncthreads();  // every wave done with X's operands
+    put_x();
+    __syncthreads();
+  }
+#pragma unroll
+  for (int n = 0; n < SMALL_XB; ++n) {
+    const int t = wave + 8 * n, bi = t / nb, bj = t - bi * nb;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = bi * 16 + (lane >> 4) * 4 + e, k = bj * 16 + (lane & 15);
+      if (t >= xblocks || i >= M.m || k >= M.n) continue;
+      if constexpr (MUON) {
+        const int64_t q = at(i, k, stride);
+        const float w = M.w[q], wn = w - (M.scale * x[n][e] + M.decay * w);
+        M.w[q] = wn;
+        if (M.o) ((TO*)M.o)[q] = Elem<TO>::from_f32(wn);
+      } else {
+        ((TO*)M.o)[at(i, k, M.o_stride)] = Elem<TO>::from_f32(x[n][e]);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
 // host
 
 // The kernels of a product.
@@ -858,19 +1029,26 @@ int64_t deal_tiles(NsArgs& a, int kind, NsPlan plan) {
 // LDS of k_ns_direct: the waves' partial tiles, and what lies beside the result.
 constexpr int direct_lds(int T, int waves) { return waves * T * (T + 4) * 4 + (T / 16) * (T / 32) * 2048; }
 
+// Allows a kernel its LDS: once per kernel and device, since the call costs as much as
+// a launch.
+template <auto KERN>
+hipError_t allow_lds(int lds) {
+  static std::atomic<uint64_t> allowed{0};
+  if (lds <= 64 * 1024) return hipSuccess;
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (e == hipSuccess && !(allowed.load(std::memory_order_relaxed) & bit)) {
+    e = hipFuncSetAttribute((const void*)KERN, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e == hipSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
+  }
+  return e;
+}
+
 template <auto KERN>
 hipError_t launch_tiles(int threads, int lds, const NsArgs& a, hipStream_t st) {
-  if (lds > 64 * 1024) {  // once per kernel and device: the call costs as much as a launch
-    static std::atomic<uint64_t> allowed{0};
-    int dev = 0;
-    hipError_t e = hipGetDevice(&dev);
-    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
-    if (e == hipSuccess && !(allowed.load(std::memory_order_relaxed) & bit)) {
-      e = hipFuncSetAttribute((const void*)KERN, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-      if (e == hipSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
-    }
-    if (e != hipSuccess) return e;
-  }
+  const hipError_t e = allow_lds<KERN>(lds);
+  if (e != hipSuccess) return e;
   hipLaunchKernelGGL(KERN, dim3(8 * a.beg[a.n]), dim3(threads), lds, st, a);
   return hipGetLastError();
 }
@@ -946,7 +1124,24 @@ size_t ns_part_bytes(NsArgs& a) {
   return (size_t)most * sizeof(float);
 }
 
+template <typename T, typename TO, bool MUON>
+static hipError_t run_small(const NsArgs& a, const NsCoef& c, hipStream_t st) {
+  const hipError_t e = allow_lds<k_ns_small<T, TO, MUON>>(SMALL_LDS);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((k_ns_small<T, TO, MUON>), dim3(a.n), dim3(512), SMALL_LDS, st, a, c);
+  return hipGetLastError();
+}
+
 hipError_t launch_newton_schulz(NsArgs& a, bool bf16, bool muon, int steps, const float* coef, hipStream_t st) {
+  bool small = steps <= SMALL_STEPS;
+  for (int j = 0; j < a.n; ++j) small = small && a.mat[j].mp <= SMALL_M && (int64_t)a.mat[j].mp * a.mat[j].np <= SMALL_ELEMS;
+  if (small) {
+    NsCoef c{};
+    c.steps = steps;
+    for (int i = 0; i < 3 * steps; ++i) c.c[i] = coef[i];
+    if (muon) return bf16 ? run_small<float, __bf16, true>(a, c, st) : run_small<float, float, true>(a, c, st);
+    return bf16 ? run_small<__bf16, __bf16, false>(a, c, st) : run_small<float, float, false>(a, c, st);
+  }
   hipError_t e = muon ? run_begin<float, true>(a, st)
                  : bf16 ? run_begin<__bf16, false>(a, st) : run_begin<float, false>(a, st);
   if (e != hipSuccess) return e;

@@ -136,7 +136,8 @@ def test_long_rows(cols, dtype):
     _check(300 if cols < 20000 else 5, cols, dtype, 0)
 
 
-@pytest.mark.parametrize("rows,cols,dtype", [(1000, 9, "f32"), (40000, 50, "bf16"), (33001, 100, "f32"), (9001, 300, "bf16"),
+@pytest.mark.parametrize("rows,cols,dtype", [(1000, 9, "f32"), (40000, 50, "bf16"), (20000, 100, "bf16"), (8193, 61, "f32"),
+                                             (8192, 511, "bf16"), (33001, 100, "f32"), (9001, 300, "bf16"),
                                              (5000, 1024, "f32"), (2500, 4099, "f32"), (1500, 8192, "bf16")])
 def test_many_rows(rows, cols, dtype):
     _check(rows, cols, dtype, 0)

@@ -127,6 +127,29 @@ def test_many_matrices_equal_one_at_a_time_in_value(dtype):
     _check(Orthogonalizer(shapes, dtype).orthogonalize(mats), mats, dtype)
 
 
+# matrices that one workgroup holds (short side to 64, 8192 padded elements), their borders, and lists of them
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(64, 128), (128, 64), (63, 127), (32, 256), (256, 31), (5, 250), (33, 97), (48, 48), (64, 129),
+                                   (32, 257), (65, 65)], ids=str)
+def test_small_matrices(shape, dtype):
+    from paper_1409_6070_amd.sscn import Orthogonalizer
+    mats = [_rand(*shape, seed=sum(shape) + i, dtype=dtype, kind=k) for i, k in enumerate(("gauss", "spread"))]
+    log(f"[orthogonalize] small {shape} {dtype}")
+    _check(Orthogonalizer([shape] * 2, dtype).orthogonalize(mats), mats, dtype)
+
+
+def test_a_list_of_small_matrices_and_more_steps_than_one_launch_takes():
+    from paper_1409_6070_amd.sscn import Orthogonalizer
+    shapes = [(9, 16), (16, 9), (64, 32), (1, 200), (64, 24), (40, 60)] * 5
+    mats = [_rand(*s, seed=i) for i, s in enumerate(shapes)]
+    log("[orthogonalize] 30 small matrices")
+    _check(Orthogonalizer(shapes, "f32").orthogonalize(mats), mats, "f32")
+    for steps in (8, 9, 12):
+        log(f"[orthogonalize] small, {steps} steps")
+        plan = Orthogonalizer([(40, 60)], "f32", coef=(1.5, -0.5, 0.0), steps=steps)
+        _check(plan.orthogonalize([mats[5]]), [mats[5]], "f32", (1.5, -0.5, 0.0), steps)
+
+
 def test_other_coefficients_and_step_counts():
     from paper_1409_6070_amd.sscn import Orthogonalizer
     u = _rand(70, 90, 4)
@@ -270,12 +293,16 @@ def _want_step(w, g, v, orthogonal, lr, momentum, wd, nesterov, scale):
     return wn, lr * scale * tol_o + 4 * U * (w.abs() + lr * (scale * want.abs() + wd * w.abs())), vn
 
 
+MIXED = [(9, 50), (50,), (200, 100), (100,), (300, 400), (1, 33), (70, 30), (1,)]
+SMALL = [(9, 50), (50,), (120, 60), (100,), (60, 90), (1, 33), (70, 30), (1,)]
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("nesterov", [True, False])
-def test_update_of_matrices_and_vectors(dtype, nesterov):
+@pytest.mark.parametrize("shapes", [MIXED, SMALL], ids=["mixed", "small"])
+def test_update_of_matrices_and_vectors(shapes, dtype, nesterov):
     """Three steps of a list with tall, wide and single-row matrices, biases, and a matrix by the SGD rule."""
     from paper_1409_6070_amd.sscn import Muon
-    shapes = [(9, 50), (50,), (200, 100), (100,), (300, 400), (1, 33), (70, 30), (1,)]
     orth = [True, False, True, False, True, True, False, False]
     tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
     W = [_rand(s[0] if len(s) == 2 else 1, s[-1], i).reshape(s) for i, s in enumerate(shapes)]
