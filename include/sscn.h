@@ -295,7 +295,8 @@ SSCN_API sscn_status sscn_layer_norm_backward(int32_t dtype, const void* d_dy, i
                                               float* d_dshift, void* d_workspace, size_t workspace_bytes,
                                               void* stream);
 
-/* One matrix for sscn_orthogonalize; in and out may be the same array. */
+/* One matrix for sscn_orthogonalize; in and out may be the same array (same
+ * stride); an output may not overlap anything else that the call names. */
 typedef struct {
   int64_t rows, cols;
   const void* d_in;

@@ -85,8 +85,8 @@ size_t carve_matrix(NsMat& M, int64_t rows, int64_t cols, char* base) {
   const size_t x = (size_t)M.mp * M.np * 4, g = (size_t)M.mp * M.mp * 4;
   M.X = (float*)take(x);
   M.opX = take(x);
-  M.opXt = take(x);
-  M.opXt_next = take(x);
+  M.opXt[0] = take(x);
+  M.opXt[1] = take(x);
   M.opA = take(g);
   M.opB = take(g);
   M.ssq = (double*)take(NS_SSQ * sizeof(double));
@@ -97,38 +97,40 @@ size_t carve_matrix(NsMat& M, int64_t rows, int64_t cols, char* base) {
 // Carves a group's part of it, the matrices with the longest sums first, and calls
 // fill(index, matrix) for each; returns the bytes.
 template <class Shape, class Fill>
-size_t carve_group(NsArgs& a, int32_t first, int k, Shape&& shape, Fill&& fill, char* base) {
+size_t carve_group(NsGroup& g, int32_t first, int k, Shape&& shape, Fill&& fill, char* base) {
   size_t off = 0;
-  a.n = k;
+  g.a.n = k;
   for (int j = 0; j < k; ++j) {
-    NsMat& M = a.mat[j];
+    NsMat& M = g.t.mat[j];
     M = NsMat{};
     const auto s = shape(first + j);
     off += carve_matrix(M, s.first, s.second, base ? base + off : nullptr);
     fill(first + j, M);
   }
-  std::stable_sort(a.mat, a.mat + k, [](const NsMat& x, const NsMat& y) { return x.n > y.n; });
-  a.count = (int32_t*)(base ? base + off : nullptr);
+  std::stable_sort(g.t.mat, g.t.mat + k, [](const NsMat& x, const NsMat& y) { return x.n > y.n; });
+  g.a.table = (const NsTable*)(base ? base + off : nullptr);
+  off += aligned256(sizeof(NsTable));
+  g.a.count = (int32_t*)(base ? base + off : nullptr);
   off += aligned256(NS_COUNT * sizeof(int32_t));
-  a.part = (float*)(base ? base + off : nullptr);
-  return off + aligned256(ns_part_bytes(a));
+  g.a.part = (float*)(base ? base + off : nullptr);
+  return off + aligned256(ns_part_bytes(g));
 }
 
 template <class Shape>
 size_t group_bytes(int32_t n, Shape&& shape) {
   size_t most = 0;
-  NsArgs a;
-  for (int32_t g = 0; g < n; g += NS_MATS)
-    most = std::max(most, carve_group(a, g, std::min(NS_MATS, n - g), shape, [](int32_t, NsMat&) {}, nullptr));
+  NsGroup g{};
+  for (int32_t i = 0; i < n; i += NS_MATS)
+    most = std::max(most, carve_group(g, i, std::min(NS_MATS, n - i), shape, [](int32_t, NsMat&) {}, nullptr));
   return most;
 }
 
 template <class Shape, class Fill>
-hipError_t run_groups(int32_t n, Shape&& shape, Fill&& fill, NsArgs& a, bool bf16, bool muon, int32_t steps,
+hipError_t run_groups(int32_t n, Shape&& shape, Fill&& fill, NsGroup& g, bool bf16, bool muon, int32_t steps,
                       const float* coef, void* d_ws, hipStream_t st) {
-  for (int32_t g = 0; g < n; g += NS_MATS) {
-    carve_group(a, g, std::min(NS_MATS, n - g), shape, fill, (char*)d_ws);
-    const hipError_t e = launch_newton_schulz(a, bf16, muon, steps, coef, st);
+  for (int32_t i = 0; i < n; i += NS_MATS) {
+    carve_group(g, i, std::min(NS_MATS, n - i), shape, fill, (char*)d_ws);
+    const hipError_t e = launch_newton_schulz(g, bf16, muon, steps, coef, st);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -217,8 +219,7 @@ sscn_status sscn_orthogonalize(int32_t dtype, int32_t n, const sscn_ortho_matrix
       return SSCN_ERR_INVALID_ARGUMENT;
   }
   if (bad_workspace(d_workspace, workspace_bytes, need)) return SSCN_ERR_WORKSPACE;
-  NsArgs a;
-  std::memset((void*)&a, 0, sizeof(a));
+  NsGroup g{};
   return of_hip(run_groups(
       n, [&](int32_t i) { return std::make_pair(h_matrices[i].rows, h_matrices[i].cols); },
       [&](int32_t i, NsMat& M) {
@@ -227,7 +228,7 @@ sscn_status sscn_orthogonalize(int32_t dtype, int32_t n, const sscn_ortho_matrix
         M.o = h_matrices[i].d_out;
         M.o_stride = h_matrices[i].out_stride;
       },
-      a, dtype == SSCN_BF16, false, steps, h_coef, d_workspace, (hipStream_t)stream));
+      g, dtype == SSCN_BF16, false, steps, h_coef, d_workspace, (hipStream_t)stream));
 }
 
 sscn_status sscn_muon_workspace_bytes(int32_t n, const sscn_muon_param* h_params, size_t* bytes) {
@@ -281,10 +282,9 @@ sscn_status sscn_muon_update(int32_t dtype, int32_t n, const sscn_muon_param* h_
     sgd.blk_beg[0] = 0;
     return e;
   };
-  NsArgs a;
-  std::memset((void*)&a, 0, sizeof(a));
-  a.momentum = momentum;
-  a.nesterov = nesterov != 0;
+  NsGroup g{};
+  g.a.momentum = momentum;
+  g.a.nesterov = nesterov != 0;
   const sscn_muon_param* group[NS_MATS];
   int k = 0;
   auto flush_group = [&]() {
@@ -299,7 +299,7 @@ sscn_status sscn_muon_update(int32_t dtype, int32_t n, const sscn_muon_param* h_
           M.scale = p.lr * p.scale;
           M.decay = p.lr * p.weight_decay;
         },
-        a, dtype == SSCN_BF16, true, steps, h_coef, d_workspace, st);
+        g, dtype == SSCN_BF16, true, steps, h_coef, d_workspace, st);
     k = 0;
     return e;
   };

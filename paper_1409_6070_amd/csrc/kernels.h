@@ -484,14 +484,10 @@ struct NsMat {
   int32_t mp, np;  // padded to multiples of 32
   int32_t tall;    // the caller's matrix is X transposed
   int32_t nssq;
-  // of the product at hand: tiles before `whole` are one workgroup's, the others are
-  // summed by `parts` workgroups each, whose partial tiles and counters start here
-  int32_t whole, parts, slot, counter;
   // workspace
   float* X;        // [mp][np]
   char* opX;       // operand with X's rows
-  char* opXt;      // operand with X's columns as rows
-  char* opXt_next; // the next step's, written while opXt is read
+  char* opXt[2];   // operand with X's columns as rows: step s reads [s % 2] and writes the other
   char* opA;
   char* opB;
   double* ssq;
@@ -504,19 +500,36 @@ struct NsMat {
   float* v;
   float scale, decay;  // w -= scale * orthogonal(u) + decay * w
 };
+// The group's matrices: copied into the workspace by the first launch, so that the
+// others' arguments stay small (1000 x 300: 77 us of host time a call; 102 with 3.8 KB
+// of arguments in each of its 17 launches).
+struct NsTable {
+  NsMat mat[NS_MATS];
+};
+// Of one product: a matrix's tiles before `whole` are one workgroup's, the others are
+// summed by `parts` workgroups each, whose partial tiles and counters start here.
+struct NsDeal {
+  int32_t whole, parts, slot, counter;
+};
 struct NsArgs {
   int32_t n;
+  int32_t step;
   int32_t nesterov;
   float momentum;
   float a, b, c;
+  const NsTable* table;
   float* part;     // partial tiles
   int32_t* count;  // [NS_COUNT] finished parts of each divided tile, zero between products
   int32_t beg[NS_MATS + 1];
-  NsMat mat[NS_MATS];
+  NsDeal deal[NS_MATS];
 };
 constexpr int NS_COUNT = 1024;
+struct NsGroup {
+  NsArgs a;
+  NsTable t;
+};
 // Bytes of partial tiles that the group's products need (m, n, mp, np set).
-size_t ns_part_bytes(NsArgs& a);
-hipError_t launch_newton_schulz(NsArgs& a, bool bf16, bool muon, int steps, const float* coef, hipStream_t st);
+size_t ns_part_bytes(NsGroup& g);
+hipError_t launch_newton_schulz(NsGroup& g, bool bf16, bool muon, int steps, const float* coef, hipStream_t st);
 
 }  // namespace sscn

@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(1024) k_norm_params(const float* __restrict__ 
   const float* p = part + (blockIdx.y ? (int64_t)parts * cols : 0);
   float v = 0.f;
   if (c < cols)
-#pragma unroll 8
+#pragma unroll 16
     for (int k = sl; k < parts; k += 16) v += p[(int64_t)k * cols + c];
   red[sl][threadIdx.x & 63] = v;
   __syncthreads();

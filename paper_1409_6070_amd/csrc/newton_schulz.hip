@@ -32,7 +32,7 @@
 
 namespace sscn {
 
-static_assert(sizeof(NsArgs) + 128 <= 4096, "kernel arguments must fit the 4 KiB argument segment");
+static_assert(sizeof(NsGroup) + 128 <= 4096, "kernel arguments must fit the 4 KiB argument segment");
 
 namespace {
 
@@ -96,12 +96,14 @@ __device__ inline int find_mat(const NsArgs& a, int t) {
   return j;
 }
 
-// Products with at least NS_BIG (X X^T, A A) or NS_BIG_APPLY (B X: more tiles, shorter
-// sums) slabs of 128 x 128 x 32 per compute unit go through LDS:
-// in 256 x 128 tiles where their last round has NS_FULL workgroups or can be divided,
-// else in 128 x 128 tiles, two workgroups a compute unit.  Smaller ones go straight into
-// registers, in 64 x 64 tiles where those make two per compute unit, else in 32 x 32.
-constexpr int NS_CUS = 256, NS_BIG = 30, NS_BIG_APPLY = 5, NS_FULL = 192;
+// The kernels of a product, by its 128 x 128 tiles, their slabs of 32 k per compute unit
+// and its 64 x 64 tiles (plan_product).  Measured, us, 128 / 64 / 32 tiles:
+//   X X^T  1500 x 1500 (14 slabs, 300 tiles of 64)  33.9 / 32.0 / 37.0;  2047 x 822 (7, 91)  28.2 / 20.6 / 15.0;
+//          DeepCNet(6,100) with softmax (23, 312)  44.7 / 37.7 / 38.5
+//   B X    400 x 1600 four times (208 tiles of 128)  23.2 / 30.3 / 30.4;  DeepCNiN(5,50)
+//          with softmax (about 180)  20.2 / 24.0 / 21.0;  1000 x 600 three times (120; 480 of 64)
+//          34.2 / 24.0 / 23.0;  2047 x 822 (112; 416)  35.4 / 25.9 / 33.3;  DeepCNet(5,50) (65; 216)  19.0 / 10.4 / 9.7
+constexpr int NS_CUS = 256, NS_SLABS = 30, NS_SLABS_APPLY = 20, NS_TILES_APPLY = 160, NS_TILES_64 = 256, NS_FULL = 192;
 constexpr int NS_PARTS = 16;  // workgroups that share a tile, at most
 
 // Sum over the workgroup's 256 threads, in all of them (red: four doubles).
@@ -118,13 +120,21 @@ __device__ inline double block_sum(double s, double* red) {
 // the velocity: v <- mu v + g.  NS_SSQ workgroups at most per matrix; the loads of
 // eight elements a thread are in flight together.
 
+// The first launch of a group: it also copies the table and clears the counters.
+
 template <typename T, bool MUON>
-__global__ void __launch_bounds__(256) k_ns_begin(NsArgs a) {
+__global__ void __launch_bounds__(256) k_ns_begin(NsArgs a, NsTable t) {
   constexpr int U = 8;
-  if (blockIdx.x == 0)
+  if (blockIdx.x == 0) {
     for (int i = threadIdx.x; i < NS_COUNT; i += 256) a.count[i] = 0;
+    // from the argument segment, where t lies behind a
+    constexpr int AT = (sizeof(NsArgs) + alignof(NsTable) - 1) / alignof(NsTable) * alignof(NsTable);
+    const auto* from = (const __attribute__((address_space(4))) uint32_t*)(
+        (const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr() + AT);
+    for (int i = threadIdx.x; i < (int)(sizeof(NsTable) / 4); i += 256) ((uint32_t*)a.table)[i] = from[i];
+  }
   const int j = find_mat(a, blockIdx.x);
-  const NsMat M = a.mat[j];
+  const NsMat M = t.mat[j];
   const int blk = blockIdx.x - a.beg[j], nblk = a.beg[j + 1] - a.beg[j];
   const int64_t rows = M.tall ? M.n : M.m, cols = M.tall ? M.m : M.n, total = rows * cols;
   double s = 0.0;
@@ -174,7 +184,7 @@ __global__ void __launch_bounds__(256) k_ns_begin(NsArgs a) {
 template <typename T, bool MUON>
 __global__ void __launch_bounds__(256) k_ns_convert(NsArgs a) {
   const int j = find_mat(a, blockIdx.x);
-  const NsMat M = a.mat[j];
+  const NsMat M = a.table->mat[j];
   __shared__ double red[4];
   __shared__ float tile[4][32][36];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -224,7 +234,7 @@ __global__ void __launch_bounds__(256) k_ns_convert(NsArgs a) {
     store_split(M.opX + block_at(i0 / 16 + h, j0 / 32, M.np / 32) + lane * 16, w, SX);
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[e] = tile[wave][k8 * 8 + e][h * 16 + r16];
-    store_split(M.opXt + block_at(j0 / 16 + h, i0 / 32, M.mp / 32) + lane * 16, w, SX);
+    store_split(M.opXt[0] + block_at(j0 / 16 + h, i0 / 32, M.mp / 32) + lane * 16, w, SX);
   }
 }
 
@@ -246,6 +256,7 @@ struct NsWork {
   int part, parts;    // which of the workgroups that share the tile
   int slot, counter;  // the tile's first partial tile, its counter
   const char *P, *Q;  // first block of the tile's rows in each operand
+  char *Xt, *Xt_next; // this step's operand with X's columns, and the next one's
   int pr, qr;         // row blocks of each inside the padded matrix (a last tile has fewer)
 
   // false: no tile for this workgroup.  Workgroup b runs on XCD b % 8: each XCD takes
@@ -253,21 +264,24 @@ struct NsWork {
   __device__ inline bool find(const NsArgs& a) {
     const int xcd = blockIdx.x & 7, slot_of_xcd = blockIdx.x >> 3;
     const int j = find_mat(a, slot_of_xcd);
-    M = a.mat[j];
-    const int tm = (M.mp + TM - 1) / TM, whole = (M.whole + 7) / 8;
+    M = a.table->mat[j];
+    const NsDeal D = a.deal[j];
+    Xt = a.step % 2 ? M.opXt[1] : M.opXt[0];
+    Xt_next = a.step % 2 ? M.opXt[0] : M.opXt[1];
+    const int tm = (M.mp + TM - 1) / TM, whole = (D.whole + 7) / 8;
     int t = slot_of_xcd - a.beg[j];
     part = 0;
     parts = 1;
     if (t < whole) {
       t += xcd * whole;
-      if (t >= M.whole) return false;
+      if (t >= D.whole) return false;
     } else {
-      const int r = xcd * (a.beg[j + 1] - a.beg[j] - whole) + t - whole, q = r / M.parts;
-      t = M.whole + q;
-      part = r - q * M.parts;
-      parts = M.parts;
-      slot = M.slot + q * M.parts;
-      counter = M.counter + q;
+      const int r = xcd * (a.beg[j + 1] - a.beg[j] - whole) + t - whole, q = r / D.parts;
+      t = D.whole + q;
+      part = r - q * D.parts;
+      parts = D.parts;
+      slot = D.slot + q * D.parts;
+      counter = D.counter + q;
     }
     if constexpr (symmetric(KIND)) {  // tiles that reach the diagonal or lie below it
       constexpr int R = TM / TN;
@@ -289,7 +303,7 @@ struct NsWork {
     k0 = kblocks * part / parts;
     k1 = kblocks * (part + 1) / parts;
     P = KIND == NS_GRAM ? M.opX : KIND == NS_POLY ? M.opA : M.opB;
-    Q = KIND == NS_GRAM ? M.opX : KIND == NS_POLY ? M.opA : M.opXt;
+    Q = KIND == NS_GRAM ? M.opX : KIND == NS_POLY ? M.opA : Xt;
     P += block_at(ti * (TM / 16), 0, kblocks);
     Q += block_at(tj * (TN / 16), 0, kblocks);
     pr = min(TM, mp - ti * TM) / 16;
@@ -537,7 +551,7 @@ __device__ inline void finish_tile(const NsArgs& a, const NsWork<TM, TN, KIND>& 
       if constexpr (LAST) {
         store_result<KIND, TO>(M, (row0 + rb) * 16 + l16, (col0 + kb) * 32 + g4 * 8, v, old[g]);
       } else {
-        char* op = KIND == NS_GRAM ? M.opA : KIND == NS_POLY ? M.opB : M.opXt_next;
+        char* op = KIND == NS_GRAM ? M.opA : KIND == NS_POLY ? M.opB : w.Xt_next;
         constexpr float scale = KIND == NS_GRAM ? SA : KIND == NS_POLY ? SB : SX;
         store_split(op + block_at(row0 + rb, col0 + kb, M.mp / 32) + lane * 16, v, scale);
       }
@@ -822,10 +836,10 @@ __device__ inline f32x4 small_product(const char* P, int bi, const char* Q, int 
 }
 
 template <typename T, typename TO, bool MUON>
-__global__ void __launch_bounds__(512) k_ns_small(NsArgs a, NsCoef coef) {
+__global__ void __launch_bounds__(512) k_ns_small(NsArgs a, NsTable t, NsCoef coef) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   __shared__ double red[8];
-  const NsMat M = a.mat[blockIdx.x];
+  const NsMat M = t.mat[blockIdx.x];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int mb = M.mp / 16, nb = M.np / 16, mk = M.mp / 32, nk = M.np / 32;
   const int xblocks = mb * nb, ablocks = mb * mb;
@@ -959,17 +973,24 @@ int64_t last_round_parts(const NsMat& last, int kind, int64_t rest) {
   return std::max<int64_t>(1, std::min<int64_t>({NS_PARTS, NS_CUS / rest, k_of(last, kind) / NS_SHAPE[NS_256].min_k}));
 }
 
-// Which kernel a product over the group takes.
-NsPlan plan_product(const NsArgs& a, int kind) {
-  int64_t t256 = 0, t64 = 0, slabs = 0;
-  for (int j = 0; j < a.n; ++j) {
-    t256 += tiles_of(a.mat[j], kind, NS_SHAPE[NS_256]);
-    t64 += tiles_of(a.mat[j], kind, NS_SHAPE[NS_64]);
-    slabs += tiles_of(a.mat[j], kind, NS_SHAPE[NS_128]) * k_of(a.mat[j], kind);
+// Which kernel a product over the group takes: through LDS where it has work for that
+// (X X^T, A A: slabs; B X, whose sums are short: tiles), in 256 x 128 tiles if their last
+// round has NS_FULL workgroups or can be divided, else in 128 x 128 tiles, two
+// workgroups a compute unit; straight into registers otherwise.
+NsPlan plan_product(const NsGroup& g, int kind) {
+  int64_t t256 = 0, t128 = 0, t64 = 0, slabs = 0;
+  for (int j = 0; j < g.a.n; ++j) {
+    const int64_t t = tiles_of(g.t.mat[j], kind, NS_SHAPE[NS_128]);
+    t256 += tiles_of(g.t.mat[j], kind, NS_SHAPE[NS_256]);
+    t128 += t;
+    t64 += tiles_of(g.t.mat[j], kind, NS_SHAPE[NS_64]);
+    slabs += t * k_of(g.t.mat[j], kind);
   }
-  if (slabs < (symmetric(kind) ? NS_BIG : NS_BIG_APPLY) * NS_CUS) return t64 >= 2 * NS_CUS ? NS_64 : NS_32;
+  const bool lds = symmetric(kind) ? slabs >= NS_SLABS * NS_CUS
+                                   : slabs >= NS_SLABS_APPLY * NS_CUS || t128 >= NS_TILES_APPLY;
+  if (!lds) return t64 >= NS_TILES_64 ? NS_64 : NS_32;
   const int64_t rest = t256 % NS_CUS;
-  return rest == 0 || rest >= NS_FULL || (t256 > NS_CUS && last_round_parts(a.mat[a.n - 1], kind, rest) > 1) ? NS_256
+  return rest == 0 || rest >= NS_FULL || (t256 > NS_CUS && last_round_parts(g.t.mat[g.a.n - 1], kind, rest) > 1) ? NS_256
                                                                                                          : NS_128;
 }
 
@@ -977,13 +998,14 @@ NsPlan plan_product(const NsArgs& a, int kind) {
 // tiles alone would leave compute units idle: all tiles of a product that has fewer than
 // compute units, or those of its last round.  Sets a.beg (workgroups per XCD) and the
 // matrices' parts; returns the partial tiles.
-int64_t deal_tiles(NsArgs& a, int kind, NsPlan plan) {
+int64_t deal_tiles(NsGroup& g, int kind, NsPlan plan) {
+  NsArgs& a = g.a;
+  const NsMat* mat = g.t.mat;
   const NsShape& s = NS_SHAPE[plan];
   int64_t all = 0, work = 0, most_k = 0;
   for (int j = 0; j < a.n; ++j) {
-    const int64_t t = tiles_of(a.mat[j], kind, s), k = k_of(a.mat[j], kind);
-    a.mat[j].whole = (int32_t)t;
-    a.mat[j].parts = 1;
+    const int64_t t = tiles_of(mat[j], kind, s), k = k_of(mat[j], kind);
+    a.deal[j] = NsDeal{(int32_t)t, 1, 0, 0};
     all += t;
     work += t * k;
     most_k = std::max(most_k, k);
@@ -996,30 +1018,29 @@ int64_t deal_tiles(NsArgs& a, int kind, NsPlan plan) {
     int64_t len = std::max<int64_t>(s.min_k, (work + NS_CUS - 1) / NS_CUS);
     for (; len < most_k; len += std::max<int64_t>(1, len / 16)) {
       int64_t items = 0;
-      for (int j = 0; j < a.n; ++j) items += a.mat[j].whole * parts(a.mat[j], len);
+      for (int j = 0; j < a.n; ++j) items += a.deal[j].whole * parts(mat[j], len);
       if (items <= NS_CUS) break;
     }
     for (int j = 0; j < a.n; ++j) {
-      a.mat[j].parts = (int32_t)parts(a.mat[j], len);
-      if (a.mat[j].parts > 1) a.mat[j].whole = 0;
+      a.deal[j].parts = (int32_t)parts(mat[j], len);
+      if (a.deal[j].parts > 1) a.deal[j].whole = 0;
     }
   } else if (plan == NS_256) {
-    NsMat& M = a.mat[a.n - 1];
-    const int64_t rest = all % NS_CUS, p = last_round_parts(M, kind, rest);
+    const int64_t rest = all % NS_CUS, p = last_round_parts(mat[a.n - 1], kind, rest);
     if (p > 1) {
-      M.whole -= (int32_t)rest;
-      M.parts = (int32_t)p;
+      a.deal[a.n - 1].whole -= (int32_t)rest;
+      a.deal[a.n - 1].parts = (int32_t)p;
     }
   }
   int64_t beg = 0, slots = 0, counters = 0;
   for (int j = 0; j < a.n; ++j) {
-    NsMat& M = a.mat[j];
-    const int64_t divided = tiles_of(M, kind, s) - M.whole;
-    M.slot = (int32_t)slots;
-    M.counter = (int32_t)counters;
+    NsDeal& D = a.deal[j];
+    const int64_t divided = tiles_of(mat[j], kind, s) - D.whole;
+    D.slot = (int32_t)slots;
+    D.counter = (int32_t)counters;
     a.beg[j] = (int32_t)beg;
-    beg += (M.whole + 7) / 8 + (divided * M.parts + 7) / 8;
-    slots += divided * M.parts;
+    beg += (D.whole + 7) / 8 + (divided * D.parts + 7) / 8;
+    slots += divided * D.parts;
     counters += divided;
   }
   a.beg[a.n] = (int32_t)beg;
@@ -1054,9 +1075,10 @@ hipError_t launch_tiles(int threads, int lds, const NsArgs& a, hipStream_t st) {
 }
 
 template <int KIND, typename TO>
-hipError_t run_product(NsArgs& a, hipStream_t st) {
-  const NsPlan plan = plan_product(a, KIND);
-  deal_tiles(a, KIND, plan);
+hipError_t run_product(NsGroup& g, hipStream_t st) {
+  const NsPlan plan = plan_product(g, KIND);
+  deal_tiles(g, KIND, plan);
+  const NsArgs& a = g.a;
   switch (plan) {
     case NS_256: {
       using C = NsTile<256, 128, 3>;
@@ -1076,37 +1098,40 @@ hipError_t run_product(NsArgs& a, hipStream_t st) {
 }
 
 template <typename TO, bool MUON>
-hipError_t run_steps(NsArgs& a, int steps, const float* coef, hipStream_t st) {
+hipError_t run_steps(NsGroup& g, int steps, const float* coef, hipStream_t st) {
+  NsArgs& a = g.a;
   for (int s = 0; s < steps; ++s) {
     a.a = coef[3 * s];
     a.b = coef[3 * s + 1];
     a.c = coef[3 * s + 2];
-    hipError_t e = run_product<NS_GRAM, float>(a, st);
-    if (e == hipSuccess) e = run_product<NS_POLY, float>(a, st);
+    a.step = s;
+    hipError_t e = run_product<NS_GRAM, float>(g, st);
+    if (e == hipSuccess) e = run_product<NS_POLY, float>(g, st);
     if (e == hipSuccess)
-      e = s + 1 < steps ? run_product<NS_APPLY, float>(a, st) : run_product<MUON ? NS_MUON : NS_ORTHO, TO>(a, st);
+      e = s + 1 < steps ? run_product<NS_APPLY, float>(g, st) : run_product<MUON ? NS_MUON : NS_ORTHO, TO>(g, st);
     if (e != hipSuccess) return e;
-    for (int j = 0; j < a.n; ++j) std::swap(a.mat[j].opXt, a.mat[j].opXt_next);
   }
   return hipSuccess;
 }
 
 template <typename T, bool MUON>
-hipError_t run_begin(NsArgs& a, hipStream_t st) {
+hipError_t run_begin(NsGroup& g, hipStream_t st) {
+  NsArgs& a = g.a;
+  NsMat* mat = g.t.mat;
   int blocks = 0;
   for (int j = 0; j < a.n; ++j) {
     a.beg[j] = blocks;
-    a.mat[j].nssq = (int)std::max<int64_t>(1, std::min<int64_t>(NS_SSQ, (int64_t)a.mat[j].m * a.mat[j].n / 2048));
-    blocks += a.mat[j].nssq;
+    mat[j].nssq = (int)std::max<int64_t>(1, std::min<int64_t>(NS_SSQ, (int64_t)mat[j].m * mat[j].n / 2048));
+    blocks += mat[j].nssq;
   }
   a.beg[a.n] = blocks;
-  hipLaunchKernelGGL((k_ns_begin<T, MUON>), dim3(blocks), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((k_ns_begin<T, MUON>), dim3(blocks), dim3(256), 0, st, a, g.t);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   blocks = 0;
   for (int j = 0; j < a.n; ++j) {
     a.beg[j] = blocks;
-    blocks += (a.mat[j].mp / 32 * (a.mat[j].np / 32) + 3) / 4;
+    blocks += (mat[j].mp / 32 * (mat[j].np / 32) + 3) / 4;
   }
   a.beg[a.n] = blocks;
   hipLaunchKernelGGL((k_ns_convert<T, MUON>), dim3(blocks), dim3(256), 0, st, a);
@@ -1115,38 +1140,39 @@ hipError_t run_begin(NsArgs& a, hipStream_t st) {
 
 }  // namespace
 
-size_t ns_part_bytes(NsArgs& a) {
+size_t ns_part_bytes(NsGroup& g) {
   int64_t most = 0;
   for (const int kind : {NS_GRAM, NS_POLY, NS_APPLY}) {
-    const NsPlan plan = plan_product(a, kind);
-    most = std::max(most, deal_tiles(a, kind, plan) * NS_SHAPE[plan].tm * NS_SHAPE[plan].tn);
+    const NsPlan plan = plan_product(g, kind);
+    most = std::max(most, deal_tiles(g, kind, plan) * NS_SHAPE[plan].tm * NS_SHAPE[plan].tn);
   }
   return (size_t)most * sizeof(float);
 }
 
 template <typename T, typename TO, bool MUON>
-static hipError_t run_small(const NsArgs& a, const NsCoef& c, hipStream_t st) {
+static hipError_t run_small(const NsGroup& g, const NsCoef& c, hipStream_t st) {
   const hipError_t e = allow_lds<k_ns_small<T, TO, MUON>>(SMALL_LDS);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_ns_small<T, TO, MUON>), dim3(a.n), dim3(512), SMALL_LDS, st, a, c);
+  hipLaunchKernelGGL((k_ns_small<T, TO, MUON>), dim3(g.a.n), dim3(512), SMALL_LDS, st, g.a, g.t, c);
   return hipGetLastError();
 }
 
-hipError_t launch_newton_schulz(NsArgs& a, bool bf16, bool muon, int steps, const float* coef, hipStream_t st) {
+hipError_t launch_newton_schulz(NsGroup& g, bool bf16, bool muon, int steps, const float* coef, hipStream_t st) {
   bool small = steps <= SMALL_STEPS;
-  for (int j = 0; j < a.n; ++j) small = small && a.mat[j].mp <= SMALL_M && (int64_t)a.mat[j].mp * a.mat[j].np <= SMALL_ELEMS;
+  for (int j = 0; j < g.a.n; ++j)
+    small = small && g.t.mat[j].mp <= SMALL_M && (int64_t)g.t.mat[j].mp * g.t.mat[j].np <= SMALL_ELEMS;
   if (small) {
     NsCoef c{};
     c.steps = steps;
     for (int i = 0; i < 3 * steps; ++i) c.c[i] = coef[i];
-    if (muon) return bf16 ? run_small<float, __bf16, true>(a, c, st) : run_small<float, float, true>(a, c, st);
-    return bf16 ? run_small<__bf16, __bf16, false>(a, c, st) : run_small<float, float, false>(a, c, st);
+    if (muon) return bf16 ? run_small<float, __bf16, true>(g, c, st) : run_small<float, float, true>(g, c, st);
+    return bf16 ? run_small<__bf16, __bf16, false>(g, c, st) : run_small<float, float, false>(g, c, st);
   }
-  hipError_t e = muon ? run_begin<float, true>(a, st)
-                 : bf16 ? run_begin<__bf16, false>(a, st) : run_begin<float, false>(a, st);
+  hipError_t e = muon ? run_begin<float, true>(g, st)
+                 : bf16 ? run_begin<__bf16, false>(g, st) : run_begin<float, false>(g, st);
   if (e != hipSuccess) return e;
-  if (muon) return bf16 ? run_steps<__bf16, true>(a, steps, coef, st) : run_steps<float, true>(a, steps, coef, st);
-  return bf16 ? run_steps<__bf16, false>(a, steps, coef, st) : run_steps<float, false>(a, steps, coef, st);
+  if (muon) return bf16 ? run_steps<__bf16, true>(g, steps, coef, st) : run_steps<float, true>(g, steps, coef, st);
+  return bf16 ? run_steps<__bf16, false>(g, steps, coef, st) : run_steps<float, false>(g, steps, coef, st);
 }
 
 }  // namespace sscn

@@ -712,8 +712,7 @@ class LayerNorm:
             n, os = self._rows(dx, "dx")
             _need(n == rows, "dx: as many rows as x")
         g = self._param(gain, "gain")
-        dgain = torch.empty(self.cols, dtype=torch.float32, device=self.device)
-        dshift = torch.empty(self.cols, dtype=torch.float32, device=self.device)
+        dgain, dshift = torch.empty((2, self.cols), dtype=torch.float32, device=self.device).unbind(0)
         _launch(self.device, self._backward, dy.data_ptr(), ds, x.data_ptr(), xs, rows, g, dx.data_ptr(), os,
                 dgain.data_ptr(), dshift.data_ptr())
         return dx, dgain, dshift

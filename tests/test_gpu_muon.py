@@ -36,12 +36,12 @@ def _need_gpu():
 
 
 def ns(u, dt, coef=MUON, steps=5, off=None):
-    """The formula in dtype dt on the CPU, with coefficients as float32 holds them; off: a generator of the signs
+    """The formula in dtype dt where u lies, with coefficients as float32 holds them; off: a generator of the signs
     that put every product's operands off by 1.5 2^-22."""
     def o(t):
         if off is None:
             return t
-        return t * (1 + 1.5 * 2.0 ** -22 * (2 * torch.randint(0, 2, t.shape, generator=off) - 1))
+        return t * (1 + 1.5 * 2.0 ** -22 * (2 * torch.randint(0, 2, t.shape, generator=off, device=t.device) - 1))
     rows = [coef] * steps if not hasattr(coef[0], "__len__") else coef
     x = u.double()
     norm = x.norm()
@@ -56,13 +56,15 @@ def ns(u, dt, coef=MUON, steps=5, off=None):
 
 
 def _bound(u, dtype, coef=MUON, steps=5):
-    want = ns(u.cpu().float(), torch.float64, coef, steps)
-    f32 = ns(u.cpu().float(), torch.float32, coef, steps).double()
+    # (large matrices: on the GPU, by the library's products)
+    u = (u.cpu() if u.numel() < 4 * 10 ** 6 else u).float()
+    want = ns(u, torch.float64, coef, steps)
+    f32 = ns(u, torch.float32, coef, steps).double()
     scale = max(want.norm().item(), 1e-300)
     off32 = (f32 - want).norm().item() / scale
-    off22 = max((ns(u.cpu().float(), torch.float64, coef, steps, torch.Generator().manual_seed(k)) - want).norm().item()
+    off22 = max((ns(u, torch.float64, coef, steps, torch.Generator(u.device).manual_seed(k)) - want).norm().item()
                 for k in range(4 if u.numel() < 10 ** 6 else 1)) / scale
-    return want, 3 * (off32 + off22) + HALF[dtype]
+    return want.cpu(), 3 * (off32 + off22) + HALF[dtype]
 
 
 def _check(outs, mats, dtype, coef=MUON, steps=5):
@@ -100,11 +102,41 @@ def test_one_matrix(shape, dtype):
     _check(Orthogonalizer([shape], dtype).orthogonalize([u]), [u], dtype)
 
 
-def test_large_matrix():
+# 128-tiles in one round; tiles divided over k (X X^T and A A) and a divided last round of 256-tiles (B X), tall and
+# wide; a long sum divided sixteen times
+@pytest.mark.parametrize("shape", [(2900, 3011), (2100, 3900), (3900, 2100), (520, 40000)], ids=str)
+def test_large_matrices(shape):
+    """Against the formula, and the same bits again from a workspace full of NaN: partial sums are added in one order."""
     from paper_1409_6070_amd.sscn import Orthogonalizer
-    u = _rand(2900, 3011, 1)  # more 128-tiles than compute units
-    log("[orthogonalize] 2900 x 3011")
-    _check(Orthogonalizer([(2900, 3011)], "f32").orthogonalize([u]), [u], "f32")
+    u = _rand(*shape, 1)
+    log(f"[orthogonalize] {shape}")
+    plan = Orthogonalizer([shape], "f32")
+    out = plan.orthogonalize([u])
+    _check(out, [u], "f32")
+    plan.ws.fill_(0xFF)
+    assert torch.equal(plan.orthogonalize([u])[0], out[0])
+
+
+def test_large_matrices_of_several_sizes_update():
+    """A list whose products divide some tiles, through the update: masters, copies, velocities."""
+    from paper_1409_6070_amd.sscn import Muon
+    shapes = [(1200, 9000), (700, 300), (2000, 1300)]
+    W = [_rand(*s, seed=i) * 0.02 for i, s in enumerate(shapes)]
+    G = [_rand(*s, seed=10 + i) for i, s in enumerate(shapes)]
+    V = [torch.zeros_like(w) for w in W]
+    C = [torch.zeros_like(w, dtype=torch.bfloat16) for w in W]
+    w0 = [w.clone() for w in W]
+    Muon(shapes, "bf16").step(W, C, G, V, lr=0.02, momentum=0.9, weight_decay=0.1, nesterov=False)
+    for w, c, g, v, b in zip(W, C, G, V, w0):
+        assert torch.equal(v, g) and torch.equal(c, w.bfloat16())
+        scale = max(1.0, w.shape[1] / w.shape[0]) ** 0.5
+        want, rel = _bound(g, "f32")
+        got = (b.double() * (1 - 0.02 * 0.1) - w.double()).cpu() / (0.02 * scale)
+        # the update as the weights show it: rounded to half a step of weights of about 0.02 and of lr, wd and scale
+        off = (got - want).norm().item() / want.norm().item()
+        tol = rel + 8 * U * (b.double().norm().item() / (0.02 * scale)) / want.norm().item() + 8 * U
+        log(f"[muon] {tuple(w.shape)}: off {off:.3g}, allowed {tol:.3g}")
+        assert off <= tol
 
 
 @pytest.mark.parametrize("kind", ["gauss", "spread", "rank"])
