@@ -453,7 +453,7 @@ class SparseDeepCNet:
         self.logits = None
         self._keep = []
         self._muon_ws = None
-        self._norm_keep = None
+        self._norm_bufs = self._norm_keep = None
 
     def __del__(self):
         h = getattr(self, "handle", None)
@@ -542,28 +542,30 @@ class SparseDeepCNet:
                 assert t.dtype == self.tdtype and t.is_contiguous()
         arr = _coef_array(coef, steps)
         opt = MuonOptions(lr, lr_rest, momentum, weight_decay, int(nesterov), int(softmax), steps, ctypes.addressof(arr))
-        need = sscn_net_muon_workspace_bytes(self.handle, opt)
-        if self._muon_ws is None or self._muon_ws.numel() < need:
-            self._muon_ws = torch.empty(max(need, 1), dtype=torch.uint8, device=self.device)
+        if self._muon_ws is None:  # for either choice of softmax: a captured step keeps pointing at it
+            need = max(sscn_net_muon_workspace_bytes(self.handle, MuonOptions(softmax=s)) for s in (0, 1))
+            self._muon_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         sscn_muon_step(self.handle, [t.data_ptr() for t in W32], [t.data_ptr() for t in W] if W is not None else None,
                        [t.data_ptr() for t in bs], [t.data_ptr() for t in vW], [t.data_ptr() for t in vb], opt,
                        self._muon_ws.data_ptr(), self._muon_ws.numel(), _stream())
 
     def set_head_norm(self, gain: Optional[torch.Tensor], shift: Optional[torch.Tensor] = None, eps: float = 1e-5):
         """Layer norm of the softmax layer's input with the given gain and shift ([C_last] float32, read by every
-        following pass); returns (dgain, dshift), which each backward overwrites. None switches it off."""
+        following pass); returns (dgain, dshift), which each backward overwrites: the same two tensors at every
+        call, so that a pass captured before keeps its buffers. None switches it off."""
         if gain is None:
             sscn_set_head_norm(self.handle, None, None, None, None, 0.0, None, 0)
-            self._norm_keep = None
             return None
         c = self.param_shapes[-1][0]
         for t in (gain, shift):
-            assert t.dtype == torch.float32 and t.is_contiguous() and t.numel() == c and t.device.type == "cuda"
-        ws = torch.empty(sscn_head_norm_workspace_bytes(self.handle), dtype=torch.uint8, device=self.device)
-        dgain, dshift = (torch.empty(c, dtype=torch.float32, device=self.device) for _ in range(2))
+            assert t is not None and t.dtype == torch.float32 and t.is_contiguous() and t.numel() == c and t.device.type == "cuda"
+        if self._norm_bufs is None:
+            ws = torch.empty(sscn_head_norm_workspace_bytes(self.handle), dtype=torch.uint8, device=self.device)
+            self._norm_bufs = [ws] + [torch.empty(c, dtype=torch.float32, device=self.device) for _ in range(2)]
+        ws, dgain, dshift = self._norm_bufs
         sscn_set_head_norm(self.handle, gain.data_ptr(), shift.data_ptr(), dgain.data_ptr(), dshift.data_ptr(), eps,
                            ws.data_ptr(), ws.numel())
-        self._norm_keep = (gain, shift, dgain, dshift, ws)
+        self._norm_keep = (gain, shift)
         return dgain, dshift
 
     def timing(self, classes: Sequence[str]) -> None:
@@ -654,7 +656,7 @@ class StrokeEncoder:
 
 class LayerNorm:
     """Layer norm of feature rows [rows, cols] over their columns, through sscn_layer_norm_*; holds the backward
-    pass's workspace for up to rows_max rows. One stream at a time."""
+    pass's workspace for up to rows_max rows. One stream at a time, and kept until its calls have run."""
 
     def __init__(self, cols: int, rows_max: int, dtype: str = "bf16", eps: float = 1e-5, device: str = "cuda"):
         if dtype not in _TYPES:
@@ -724,7 +726,8 @@ class LayerNorm:
 
 class Orthogonalizer:
     """Newton-Schulz orthogonalisation of matrices of fixed shapes, through sscn_orthogonalize; holds the workspace.
-    coef: (a, b, c) for every step, or one triple per step. One stream at a time."""
+    coef: (a, b, c) for every step, or one triple per step. One stream at a time, and kept until its calls have
+    run."""
 
     def __init__(self, shapes: Sequence, dtype: str = "bf16", coef=MUON_COEF, steps: int = 5, device: str = "cuda"):
         if dtype not in _TYPES:
@@ -742,12 +745,15 @@ class Orthogonalizer:
         if out is None:
             out = [torch.empty(r, c, dtype=self.tdtype, device=self.device) for r, c in self.shapes]
         _need(len(mats) == len(out) == len(self.shapes), f"{len(self.shapes)} matrices")
-        for m, i, o, shape in zip(self._mats, mats, out, self.shapes):
+        ins, outs = [t.data_ptr() for t in mats], [t.data_ptr() for t in out]
+        apart = {i for i, o in zip(ins, outs) if i != o}
+        _need(len(set(outs)) == len(outs) and apart.isdisjoint(outs), "out: each its own array, or its own matrix")
+        for m, i, o, shape, a, b in zip(self._mats, mats, out, self.shapes, ins, outs):
             for t, what in ((i, "matrix"), (o, "out")):
                 if t.shape != shape or t.dtype != self.tdtype or t.device != self.device:
                     raise ValueError(f"{what}: {shape} {self.tdtype} on {self.device}")
-            m.d_in, m.in_stride = i.data_ptr(), _row_stride(i, "matrix")
-            m.d_out, m.out_stride = o.data_ptr(), _row_stride(o, "out")
+            m.d_in, m.in_stride = a, _row_stride(i, "matrix")
+            m.d_out, m.out_stride = b, _row_stride(o, "out")
         _launch(self.device, lambda st: sscn_orthogonalize(self.code, self._mats, self.steps, self.coef,
                                                            self.ws.data_ptr(), self.ws_bytes, st))
         return out
@@ -756,7 +762,7 @@ class Orthogonalizer:
 class Muon:
     """Muon's update of parameter arrays of fixed shapes, through sscn_muon_update; holds the workspace. Matrices
     take the orthogonalised update (orthogonal[i] says otherwise), vectors momentum SGD without weight decay.
-    dtype is that of the storage copies. One stream at a time."""
+    dtype is that of the storage copies. One stream at a time, and kept until its calls have run."""
 
     def __init__(self, shapes: Sequence, dtype: str = "bf16", coef=MUON_COEF, steps: int = 5,
                  orthogonal: Optional[Sequence[bool]] = None, device: str = "cuda"):
@@ -795,5 +801,6 @@ class Muon:
             p.d_w_store = None if c is None else c.data_ptr()
             p.lr = lr if p.orthogonal or lr_rest is None else lr_rest
             p.weight_decay = weight_decay if len(s) == 2 else 0.0
+        _need(len({p.d_w for p in self._params}) == n, "an array is named twice")
         _launch(self.device, lambda st: sscn_muon_update(self.code, self._params, momentum, int(nesterov), self.steps,
                                                          self.coef, self.ws.data_ptr(), self.ws_bytes, st))

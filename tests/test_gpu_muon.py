@@ -302,6 +302,23 @@ def test_wrapper_refuses():
         m.step(*good, lr=-0.1)
 
 
+def test_outputs_that_would_race_are_refused():
+    """An output named twice, or another matrix's input; a parameter array named twice."""
+    from paper_1409_6070_amd.sscn import Muon, Orthogonalizer
+    plan = Orthogonalizer([(8, 16)] * 2, "f32")
+    x, y, o = (torch.randn(8, 16, device="cuda") for _ in range(3))
+    for mats, out in (([x, y], [o, o]), ([x, y], [y, x]), ([x, y], [o, x]), ([x, x], [x, o]), ([x, x], [x, x])):
+        with pytest.raises(ValueError):
+            plan.orthogonalize(mats, out=out)
+    a, b = plan.orthogonalize([x, x])  # an input may be named twice
+    assert torch.equal(a, b)
+    plan.orthogonalize([x, y], out=[x, y])
+    assert torch.equal(x, a)
+    m = Muon([(8, 16)] * 2, "f32")
+    with pytest.raises(ValueError):
+        m.step([x, x], None, [y, y], [a, b], lr=0.1)
+
+
 # ---------------------------------------------------------------------------------------------------------
 # the update
 
@@ -485,3 +502,49 @@ def test_training_steps_with_a_head_norm_in_one_graph(dtype):
         for i, (p, q) in enumerate(zip(e, g)):
             assert torch.equal(p, q), (k, i)
     log(f"[training] {dtype}: losses {[float(r[0]) for r in runs[0]]}")
+
+
+def test_buffers_of_a_captured_step_outlive_other_choices():
+    """A captured step keeps its workspaces when eager steps after it choose differently: its replays give what they
+    gave before."""
+    net, feats, W32, W, b, labels = _net("f32")
+    c = W32[-1].shape[0]
+    gain, shift = torch.ones(c, device="cuda"), torch.zeros(c, device="cuda")
+    grads = net.set_head_norm(gain, shift)
+    vW, vb = [torch.zeros_like(w) for w in W32], [torch.zeros_like(v) for v in b]
+    keep = [[t.clone() for t in ts] for ts in (W32, b)]
+
+    def reset():
+        for ts, ks in zip((W32, b), keep):
+            for t, k in zip(ts, ks):
+                t.copy_(k)
+        for t in (*vW, *vb):
+            t.zero_()
+
+    def step(softmax):
+        net.forward(feats, W, b, labels)
+        net.backward()
+        net.muon_step(W32, W, b, vW, vb, 0.02, 0.01, softmax=softmax)
+
+    step(False)
+    reset()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(False)
+    want = None
+    for i in range(3):
+        reset()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (*W32, *b, *grads)]
+        want = got if want is None else want
+        assert all(torch.equal(p, q) for p, q in zip(got, want)), i
+        reset()
+        ws = net._muon_ws.data_ptr()
+        step(True)
+        net.set_head_norm(None)
+        step(True)
+        again = net.set_head_norm(gain, shift)
+        assert net._muon_ws.data_ptr() == ws and all(p is q for p, q in zip(again, grads))
+        torch.cuda.synchronize()
