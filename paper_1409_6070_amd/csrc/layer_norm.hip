@@ -121,6 +121,10 @@ __device__ inline int vec_col(int t, int i, int cols, int& skip) {
 
 constexpr int threads_of(int tpr) { return tpr < 256 ? 256 : tpr; }
 
+// Forward.  The next row's loads are in flight while a row is reduced; what bounds it
+// is memory: 200001 x 100 bf16 in 104-element rows 18.9 us (80 MB, 4.2 TB/s; the caches
+// hold part of it), 20011 x 4099 float32 124 .. 129 us (656 MB, 5.1 TB/s: a large copy
+// reaches 4.9), a single row 2.7 us of which the launch is 2.4.
 template <typename T, int V, int TPR, int NV>
 __global__ void __launch_bounds__(threads_of(TPR)) k_norm(NormArgs a) {
   constexpr int NT = threads_of(TPR), RPB = NT / TPR;
@@ -215,7 +219,9 @@ __global__ void __launch_bounds__(1024) k_norm_long(NormArgs a) {
 
 // Backward.  Each thread also sums dy h and dy of its columns over the rows it
 // meets; a workgroup writes one partial row of each (part[block][cols], then the
-// same for dshift), which k_norm_params adds in block order.
+// same for dshift), which k_norm_params adds in a fixed order: no atomics.  Memory-bound:
+// 16384 x 8192 bf16 takes 172 us and the parameters' sums 7 (805 MB, 4.7 TB/s; 201 before
+// the rows stayed packed in registers), 200001 x 100 bf16 25 and 5 (120 MB, 4.8 TB/s).
 template <typename T, typename TD, int V, int TPR, int NV>
 __global__ void __launch_bounds__(threads_of(TPR)) k_norm_bwd(NormBwdArgs a) {
   constexpr int NT = threads_of(TPR), RPB = NT / TPR;
@@ -332,6 +338,9 @@ __global__ void __launch_bounds__(threads_of(TPR)) k_norm_bwd(NormBwdArgs a) {
   }
 }
 
+// Rows too long for registers: x and dy are read once per pass, and a thread adds its
+// columns' parameter sums to the workgroup's partial row in memory (each column is one
+// thread's, so rows are added in order).
 template <typename T>
 __global__ void __launch_bounds__(1024) k_norm_bwd_long(NormBwdArgs a) {
   using TD = T;
@@ -373,7 +382,8 @@ __global__ void __launch_bounds__(1024) k_norm_bwd_long(NormBwdArgs a) {
 }
 
 // dgain (blockIdx.y = 0) and dshift (1): the partials of 64 columns, in 16
-// interleaved slices combined in order.
+// interleaved slices combined in order, 16 loads of a slice in flight: 1024 partial
+// rows of 100 columns take 5.4 us (latency), 512 of 8192 columns 7.0.
 __global__ void __launch_bounds__(1024) k_norm_params(const float* __restrict__ part, int parts, int cols, float* dgain,
                                                       float* dshift) {
   __shared__ float red[16][64];

@@ -10,8 +10,9 @@
 // Precision.  X is kept in float32.  A product's operands are split into two
 // fp16 numbers each, hi + lo (22 bits; powers of two keep them in fp16's range),
 // and multiplied on the fp16 matrix cores as hi hi + hi lo + lo hi with float32
-// sums: three times the matrix work of a plain fp16 product, and still a fifth of
-// the time of float32 MFMA.  A small singular value is carried from step to step
+// sums: three times the matrix work of a plain fp16 product, which the fp16 cores
+// still do at five times the rate of float32 MFMA (4096 x 4096: 387 TFLOP/s of the
+// formula's operations; a library's float32 product reaches 154).  A small singular value is carried from step to step
 // by a X alone (B's rows along it are small), which is float32 throughout: the
 // result is as near to the formula's as a float32 computation's, where operands
 // of fewer bits lose the small singular values, whose errors every step
@@ -118,10 +119,11 @@ __device__ inline double block_sum(double s, double* red) {
 // ---------------------------------------------------------------------------
 // |u|_F^2 as partial sums in float64 (any float32 matrix's fits), and for Muon
 // the velocity: v <- mu v + g.  NS_SSQ workgroups at most per matrix; the loads of
-// eight elements a thread are in flight together.
-
+// eight elements a thread are in flight together.  Memory-bound where the matrix is
+// large (4096 x 4096: 15.3 us, 4.4 TB/s), else one load's latency and the launch
+// (1000 x 300: 3.7 us).
+//
 // The first launch of a group: it also copies the table and clears the counters.
-
 template <typename T, bool MUON>
 __global__ void __launch_bounds__(256) k_ns_begin(NsArgs a, NsTable t) {
   constexpr int U = 8;
@@ -180,7 +182,9 @@ __global__ void __launch_bounds__(256) k_ns_begin(NsArgs a, NsTable t) {
 }
 
 // X = u / |u|_F in float32 and as both operands; a wave per 32 x 32 tile, whose
-// values are on their way while the norm's partial sums are added.
+// values are on their way while the norm's partial sums are added (7 us instead of
+// 13 at 1000 x 300).  Reads 4 bytes an element and writes 12: 4096 x 4096 takes
+// 46 us, 5.8 TB/s.
 template <typename T, bool MUON>
 __global__ void __launch_bounds__(256) k_ns_convert(NsArgs a) {
   const int j = find_mat(a, blockIdx.x);
@@ -416,8 +420,8 @@ __device__ inline Run8<float> load_weights(const NsMat& M, int row, int c) {
 
 // A tile that several workgroups share: each stores its sums (staged in LDS) as a
 // partial tile; the last one to finish adds them all in their order, back into LDS,
-// and returns true.  Released with the counter, acquired by
-// the last.
+// and returns true.  Every wave's stores are in L2 before the barrier; thread 0 then
+// releases them with the counter, and the last acquires.
 template <int TM, int TN, int NT, class W>
 __device__ inline bool join_parts(const NsArgs& a, const W& w, float* Cs) {
   constexpr int CS = TN + 4, V = TM * TN / 4;
@@ -426,6 +430,8 @@ __device__ inline bool join_parts(const NsArgs& a, const W& w, float* Cs) {
   f32x4* out = (f32x4*)(a.part + (int64_t)(w.slot + w.part) * (TM * TN));
   for (int i = threadIdx.x; i < V; i += NT)
     out[i] = *(const f32x4*)(Cs + i / (TN / 4) * CS + i % (TN / 4) * 4);
+  asm volatile("" ::: "memory");
+  wait_loads<0>();  // (vmcnt counts stores too; the barrier alone waits for none of them)
   __syncthreads();
   if (threadIdx.x == 0)
     last = __hip_atomic_fetch_add(a.count + w.counter, 1, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT) == w.parts - 1;
@@ -596,7 +602,15 @@ __device__ inline void stage_tile(float* Cs, const f32x4 (&acc)[FT][FT], int lan
 }
 
 // Large products: TM x TN tiles, a wave for each 64 x 64 of them, operands through a
-// ring of NST LDS slabs of 32 k.
+// ring of NST LDS slabs of 32 k.  Bound by the matrix cores: 4096 x 4096 takes 192 us
+// for X X^T, 199 for A A and 327 for B X, which is 1.14, 1.10 and 1.26 PFLOP/s of fp16
+// products (a loop of nothing but such products on random numbers reaches 1.7 here,
+// its clock held down by power; a library's fp16 product of this size 1.1).  A slab of
+// a 256 x 128 tile takes 1800 cycles where its products take 1536, the rest of a
+// launch is the epilogue: every workgroup writes its results at the same time.
+// 128 x 128 tiles with two workgroups a compute unit hide one's epilogue behind the
+// other's products, but read 1.5 times as much from L2: for last rounds that would
+// leave compute units idle (eight of 1024 x 1024: 288 tiles of 256 x 128).
 template <int TM, int TN, int NST>
 struct NsTile {
   static constexpr int PB = TM / 16, QB = TN / 16, FT = 4;
@@ -716,7 +730,9 @@ __global__ void __launch_bounds__((NsTile<TM, TN, NST>::NW * 64), 2) k_ns_tiles(
 // blocks, each wave loading its operands straight into registers (a load is one
 // contiguous plane), DEPTH blocks ahead; the waves' sums meet in LDS, where what the
 // epilogue reads beside them has arrived meanwhile.  No barrier before that: such a
-// product is bound by latencies, not by the matrix cores.
+// product is bound by latencies, not by the matrix cores.  1000 x 300 takes 7.0 us for
+// X X^T, 4.1 for A A and 9.0 for B X, of which an empty launch is 2.4 and the operands'
+// way from another XCD's writes (through memory) 1.2.
 template <int T, int NW, int DEPTH, int KIND, typename TO>
 __global__ void __launch_bounds__(NW * 64) k_ns_direct(NsArgs a) {
   using W = NsWork<T, T, KIND>;
@@ -779,8 +795,9 @@ __global__ void __launch_bounds__(NW * 64) k_ns_direct(NsArgs a) {
 // ---------------------------------------------------------------------------
 // A small matrix, all steps in one workgroup: X stays in registers in float32 (wave w
 // holds the 16 x 16 blocks w, w + 8, .. of it, as the matrix cores leave them), its
-// operands, A and B in LDS.  A list of such matrices is one launch of a few
-// microseconds a step, where 3 launches a step cost 5 each.
+// operands, A and B in LDS.  Five steps take 9.5 us for 9 x 50, 16.4 for 64 x 64 and
+// 22.4 for 64 x 128 (20 of these 41.4: a workgroup each); 65 x 65, just too large, takes
+// 65 in its 17 launches.
 
 constexpr int SMALL_M = 64, SMALL_ELEMS = 8192, SMALL_STEPS = 8;
 constexpr int SMALL_XB = SMALL_ELEMS / 256 / 8, SMALL_AB = SMALL_M * SMALL_M / 256 / 8;  // blocks a wave holds
