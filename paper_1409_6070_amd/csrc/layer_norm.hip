@@ -427,7 +427,7 @@ NormShape norm_shape(int ve, int cols, bool two) {
 }
 
 // float32 gradients of bf16 rows come from the softmax layer only, whose input has at
-// most 256 vectors a row
+// most 256 vectors a row (sscn_net_create refuses wider layers)
 constexpr int HEAD_VECS = 256;
 
 int64_t row_blocks(const NormShape& s, int64_t rows) { return (rows + s.rpb() - 1) / s.rpb(); }

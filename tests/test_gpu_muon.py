@@ -218,6 +218,39 @@ def test_zero_and_bad_matrices_stay_alone():
     assert torch.isnan(got[2]).all() and torch.isnan(got[3]).all()
 
 
+@pytest.mark.parametrize("shape", [(200, 300), (700, 650), (1600, 1700)], ids=str)
+def test_zero_and_bad_matrices_of_many_tiles_stay_alone(shape):
+    """The same beside each other in one launch of products, whose tiles some workgroups share."""
+    from paper_1409_6070_amd.sscn import Orthogonalizer
+    mats = [_rand(*shape, i) for i in range(4)]
+    plan = Orthogonalizer([shape] * 4, "f32")
+    want = [o.clone() for o in plan.orthogonalize(mats)]
+    mats[1] = torch.zeros_like(mats[1])
+    mats[2] = mats[2].clone()
+    mats[2][shape[0] - 1, shape[1] - 1] = float("nan")
+    mats[3] = mats[3].clone()
+    mats[3][0, 0] = float("-inf")
+    got = plan.orthogonalize(mats)
+    assert torch.equal(got[0], want[0])
+    assert (got[1] == 0).all()
+    assert torch.isnan(got[2]).all() and torch.isnan(got[3]).all()
+    mats = [mats[0]] * 4  # nothing of it stays in the workspace
+    assert all(torch.equal(o, want[0]) for o in plan.orthogonalize(mats))
+
+
+@pytest.mark.parametrize("shape", [(5, 60), (5, 2000)], ids=str)
+def test_offsets_past_32_bits(shape):
+    from paper_1409_6070_amd.sscn import Orthogonalizer
+    stride = (1 << 30) + 3
+    u = _rand(*shape, seed=1, dtype="bf16")
+    far = torch.as_strided(torch.empty((shape[0] - 1) * stride + shape[1], dtype=torch.bfloat16, device="cuda"), shape,
+                           (stride, 1))
+    far.copy_(u)
+    plan = Orthogonalizer([shape], "bf16")
+    want = plan.orthogonalize([u])[0]
+    assert torch.equal(plan.orthogonalize([far], out=[far])[0], want)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_strides_in_place_and_guards(dtype):
     from paper_1409_6070_amd.sscn import Orthogonalizer
