@@ -91,6 +91,30 @@ __device__ inline void store_split(char* at, const float (&v)[8], float s) {
 // Address of lane l's part of block (rb, kb) of an operand with kblocks blocks a row.
 __device__ inline int64_t block_at(int rb, int kb, int kblocks) { return ((int64_t)rb * kblocks + kb) * BLOCK; }
 
+// Matrix j, its pointers known to be global memory's.  Out of a table in memory the
+// compiler takes them for flat ones, whose loads share a counter with LDS and return in
+// any order: it then waits for all of them wherever one is needed.
+template <typename T>
+__device__ inline T* global_pointer(T* const& p) {
+  return (T*)*(__attribute__((address_space(1))) T* const*)&p;
+}
+__device__ inline NsMat matrix(const NsTable* t, int j) {
+  const NsMat& from = t->mat[j];
+  NsMat M = from;
+  M.X = global_pointer(from.X);
+  M.opX = global_pointer(from.opX);
+  M.opXt[0] = global_pointer(from.opXt[0]);
+  M.opXt[1] = global_pointer(from.opXt[1]);
+  M.opA = global_pointer(from.opA);
+  M.opB = global_pointer(from.opB);
+  M.ssq = global_pointer(from.ssq);
+  M.u = global_pointer(from.u);
+  M.o = global_pointer(from.o);
+  M.w = global_pointer(from.w);
+  M.v = global_pointer(from.v);
+  return M;
+}
+
 __device__ inline int find_mat(const NsArgs& a, int t) {
   int j = 0;
   while (j + 1 < a.n && t >= a.beg[j + 1]) ++j;
@@ -136,7 +160,7 @@ __global__ void __launch_bounds__(256) k_ns_begin(NsArgs a, NsTable t) {
     for (int i = threadIdx.x; i < (int)(sizeof(NsTable) / 4); i += 256) ((uint32_t*)a.table)[i] = from[i];
   }
   const int j = find_mat(a, blockIdx.x);
-  const NsMat M = t.mat[j];
+  const NsMat M = matrix(&t, j);
   const int blk = blockIdx.x - a.beg[j], nblk = a.beg[j + 1] - a.beg[j];
   const int64_t rows = M.tall ? M.n : M.m, cols = M.tall ? M.m : M.n, total = rows * cols;
   double s = 0.0;
@@ -188,7 +212,7 @@ __global__ void __launch_bounds__(256) k_ns_begin(NsArgs a, NsTable t) {
 template <typename T, bool MUON>
 __global__ void __launch_bounds__(256) k_ns_convert(NsArgs a) {
   const int j = find_mat(a, blockIdx.x);
-  const NsMat M = a.table->mat[j];
+  const NsMat M = matrix(a.table, j);
   __shared__ double red[4];
   __shared__ float tile[4][32][36];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -268,7 +292,7 @@ struct NsWork {
   __device__ inline bool find(const NsArgs& a) {
     const int xcd = blockIdx.x & 7, slot_of_xcd = blockIdx.x >> 3;
     const int j = find_mat(a, slot_of_xcd);
-    M = a.table->mat[j];
+    M = matrix(a.table, j);
     const NsDeal D = a.deal[j];
     Xt = a.step % 2 ? M.opXt[1] : M.opXt[0];
     Xt_next = a.step % 2 ? M.opXt[0] : M.opXt[1];
@@ -744,7 +768,6 @@ __global__ void __launch_bounds__(NW * 64) k_ns_direct(NsArgs a) {
   const int k0 = w.kblocks * wave / NW, k1 = w.kblocks * (wave + 1) / NW;
   auto load = [&](int kb) {
     NsOperands<FT> o;
-    kb = min(kb, w.kblocks - 1);  // (behind the last block: loaded again, not used)
 #pragma unroll
     for (int i = 0; i < FT; ++i) {
       // row blocks past the matrix: the last one again, its results are dropped
@@ -757,33 +780,55 @@ __global__ void __launch_bounds__(NW * 64) k_ns_direct(NsArgs a) {
     }
     return o;
   };
-  NsOperands<FT> ring[DEPTH];
-#pragma unroll
-  for (int d = 0; d < DEPTH; ++d)  // (X X^T: its waves have more blocks than DEPTH, as a rule)
-    if (d == 0 || KIND == NS_GRAM || k0 + d < k1) ring[d] = load(k0 + d);
   char* beside = smem + NW * T * CS * 4;
-  if constexpr (KIND != NS_GRAM)
-    for (int b = wave; b < NB; b += NW) {
-      const int rb = b / (T / 32), kb = b % (T / 32);
-      if (rb < w.pr && 2 * kb < w.qr)
-        load_beside<W, KIND>(w, w.ti * FT + rb, w.tj * (T / 32) + kb, lane, lds_offset(beside + b * 2048));
-    }
+  auto load_besides = [&]() {
+    if constexpr (KIND != NS_GRAM)
+      for (int b = wave; b < NB; b += NW) {
+        const int rb = b / (T / 32), kb = b % (T / 32);
+        if (rb < w.pr && 2 * kb < w.qr)
+          load_beside<W, KIND>(w, w.ti * FT + rb, w.tj * (T / 32) + kb, lane, lds_offset(beside + b * 2048));
+      }
+  };
   f32x4 acc[FT][FT];
 #pragma unroll
   for (int i = 0; i < FT; ++i)
 #pragma unroll
     for (int k = 0; k < FT; ++k) acc[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
-  // (no copies and no loads under a condition: either would wait for every load)
+  NsOperands<FT> ring[DEPTH];
   int kb = k0;
-  for (; kb + DEPTH <= k1; kb += DEPTH)
+  auto multiply = [&](int d) { mma_block<FT>(ring[d].ph, ring[d].pl, ring[d].qh, ring[d].ql, acc); };
+  if (k1 - k0 >= DEPTH) {
+    // In the loop nothing is loaded under a condition or out of order: a wait for a
+    // block would wait for younger ones too.
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) {
-      mma_block<FT>(ring[d].ph, ring[d].pl, ring[d].qh, ring[d].ql, acc);
-      ring[d] = load(kb + DEPTH + d);
+      ring[d] = load(k0 + d);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    load_besides();
+    for (; kb + 2 * DEPTH <= k1; kb += DEPTH)
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) {
+        multiply(d);
+        ring[d] = load(kb + DEPTH + d);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      multiply(d);
+      if (kb + DEPTH + d < k1) ring[d] = load(kb + DEPTH + d);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    kb += DEPTH;
+  } else {
+#pragma unroll
+    for (int d = 0; d < DEPTH - 1; ++d)
+      if (k0 + d < k1) ring[d] = load(k0 + d);
+    load_besides();
+  }
 #pragma unroll
   for (int d = 0; d < DEPTH - 1; ++d)
-    if (kb + d < k1) mma_block<FT>(ring[d].ph, ring[d].pl, ring[d].qh, ring[d].ql, acc);
+    if (kb + d < k1) multiply(d);
   float* Cs = (float*)smem;
   stage_tile<FT, CS>(Cs + wave * T * CS, acc, lane);
   asm volatile("" ::: "memory");
@@ -856,7 +901,7 @@ template <typename T, typename TO, bool MUON>
 __global__ void __launch_bounds__(512) k_ns_small(NsArgs a, NsTable t, NsCoef coef) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   __shared__ double red[8];
-  const NsMat M = t.mat[blockIdx.x];
+  const NsMat M = matrix(&t, blockIdx.x);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int mb = M.mp / 16, nb = M.np / 16, mk = M.mp / 32, nk = M.np / 32;
   const int xblocks = mb * nb, ablocks = mb * mb;
@@ -1064,8 +1109,11 @@ int64_t deal_tiles(NsGroup& g, int kind, NsPlan plan) {
   return slots;  // (divided tiles are fewer than compute units, so than NS_COUNT)
 }
 
-// LDS of k_ns_direct: the waves' partial tiles, and what lies beside the result.
-constexpr int direct_lds(int T, int waves) { return waves * T * (T + 4) * 4 + (T / 16) * (T / 32) * 2048; }
+// LDS of k_ns_direct: the waves' partial tiles, and what lies beside the result (nothing
+// for X X^T, which so has room for two 64 x 64 tiles a compute unit).
+constexpr int direct_lds(int T, int waves, int kind) {
+  return waves * T * (T + 4) * 4 + (kind == NS_GRAM ? 0 : (T / 16) * (T / 32) * 2048);
+}
 
 // Allows a kernel its LDS: once per kernel and device, since the call costs as much as
 // a launch.
@@ -1106,10 +1154,10 @@ hipError_t run_product(NsGroup& g, hipStream_t st) {
       return launch_tiles<k_ns_tiles<128, 128, 2, KIND, TO>>(C::NW * 64, C::LDS, a, st);
     }
     case NS_64:
-      return launch_tiles<k_ns_direct<64, 4, 2, KIND, TO>>(256, direct_lds(64, 4), a, st);
+      return launch_tiles<k_ns_direct<64, 4, 2, KIND, TO>>(256, direct_lds(64, 4, KIND), a, st);
     default: {
       constexpr int NW = symmetric(KIND) ? 8 : 4;  // (X X^T has the longest sums, B X the most tiles)
-      return launch_tiles<k_ns_direct<32, NW, 3, KIND, TO>>(NW * 64, direct_lds(32, NW), a, st);
+      return launch_tiles<k_ns_direct<32, NW, 3, KIND, TO>>(NW * 64, direct_lds(32, NW, KIND), a, st);
     }
   }
 }
