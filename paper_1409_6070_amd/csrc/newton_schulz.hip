@@ -758,7 +758,7 @@ __global__ void __launch_bounds__((NsTile<TM, TN, NST>::NW * 64), 2) k_ns_tiles(
 // X X^T, 4.1 for A A and 9.0 for B X, of which an empty launch is 2.4 and the operands'
 // way from another XCD's writes (through memory) 1.2.
 template <int T, int NW, int DEPTH, int KIND, typename TO>
-__global__ void __launch_bounds__(NW * 64) k_ns_direct(NsArgs a) {
+__global__ void __launch_bounds__((NW * 64), (NW == 8 ? 4 : 1)) k_ns_direct(NsArgs a) {
   using W = NsWork<T, T, KIND>;
   constexpr int FT = T / 16, CS = T + 4, NB = FT * (T / 32);
   extern __shared__ __attribute__((aligned(1024))) char smem[];
