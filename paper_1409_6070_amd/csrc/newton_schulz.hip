@@ -123,11 +123,14 @@ __device__ inline int find_mat(const NsArgs& a, int t) {
 
 // The kernels of a product, by its 128 x 128 tiles, their slabs of 32 k per compute unit
 // and its 64 x 64 tiles (plan_product).  Measured, us, 128 / 64 / 32 tiles:
-//   X X^T  1500 x 1500 (14 slabs, 300 tiles of 64)  33.9 / 32.0 / 37.0;  2047 x 822 (7, 91)  28.2 / 20.6 / 15.0;
-//          DeepCNet(6,100) with softmax (23, 312)  44.7 / 37.7 / 38.5
-//   B X    400 x 1600 four times (208 tiles of 128)  23.2 / 30.3 / 30.4;  DeepCNiN(5,50)
-//          with softmax (about 180)  20.2 / 24.0 / 21.0;  1000 x 600 three times (120; 480 of 64)
-//          34.2 / 24.0 / 23.0;  2047 x 822 (112; 416)  35.4 / 25.9 / 33.3;  DeepCNet(5,50) (65; 216)  19.0 / 10.4 / 9.7
+//   X X^T  2100 x 3900 (73 slabs)  76 / 86 / -;  2048 x 2048 (34)  44 / 46 / -;  1800 x 1900 (28)
+//          41.7 / 31.6 / -;  DeepCNet(6,100) with softmax (23, 312 tiles of 64)  39.7 / 35.5 / 35.6;
+//          1500 x 1500 (14, 300)  31.7 / 21.0 / 33.4;  1000 x 600 three times (6, 165)  24.8 / 14.0 /
+//          12.5;  DeepCNiN(5,50) with softmax (160)  27.3 / 23.2 / 14.7;  1000 x 300 (15)  17.0 / 10.0 / 6.3
+//   B X    1500 x 1500 (26 slabs)  36.5 / 42.5 / 63.9;  1300 x 1300 (19)  38.2 / 28.8 / -;
+//          400 x 1600 four times (208 tiles of 128)  21.2 / 28.0 / 23.4;  700 x 3755 (180)  24.4 / 32.4 /
+//          38.9;  1000 x 600 three times (120; 480 of 64)  32.8 / 22.5 / 20.4;  2047 x 822 (112; 416)  34.4 /
+//          24.0 / 30.0;  DeepCNet(5,50) (65; 216)  17.8 / 11.0 / 9.0
 constexpr int NS_CUS = 256, NS_SLABS = 30, NS_SLABS_APPLY = 20, NS_TILES_APPLY = 160, NS_TILES_64 = 256, NS_FULL = 192;
 constexpr int NS_PARTS = 16;  // workgroups that share a tile, at most
 
@@ -1037,8 +1040,7 @@ int64_t last_round_parts(const NsMat& last, int kind, int64_t rest) {
 
 // Which kernel a product over the group takes: through LDS where it has work for that
 // (X X^T, A A: slabs; B X, whose sums are short: tiles), in 256 x 128 tiles if their last
-// round has NS_FULL workgroups or can be divided, else in 128 x 128 tiles, two
-// workgroups a compute unit; straight into registers otherwise.
+// round has NS_FULL workgroups or can be divided, else in 128 x 128 tiles; straight into registers otherwise.
 NsPlan plan_product(const NsGroup& g, int kind) {
   int64_t t256 = 0, t128 = 0, t64 = 0, slabs = 0;
   for (int j = 0; j < g.a.n; ++j) {
@@ -1150,6 +1152,12 @@ hipError_t run_product(NsGroup& g, hipStream_t st) {
       return launch_tiles<k_ns_tiles<256, 128, 3, KIND, TO>>(C::NW * 64, C::LDS, a, st);
     }
     case NS_128: {
+      // alone on its compute unit a workgroup keeps one more slab in flight (X X^T of
+      // 2100 x 3900: 76 us with three stages, 96 with two; 2047 x 8000: 139 and 195)
+      if (8 * a.beg[a.n] <= NS_CUS + 8 * a.n) {
+        using C = NsTile<128, 128, 3>;
+        return launch_tiles<k_ns_tiles<128, 128, 3, KIND, TO>>(C::NW * 64, C::LDS, a, st);
+      }
       using C = NsTile<128, 128, 2>;
       return launch_tiles<k_ns_tiles<128, 128, 2, KIND, TO>>(C::NW * 64, C::LDS, a, st);
     }
