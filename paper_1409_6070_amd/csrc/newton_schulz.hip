@@ -1152,9 +1152,11 @@ hipError_t run_product(NsGroup& g, hipStream_t st) {
       return launch_tiles<k_ns_tiles<256, 128, 3, KIND, TO>>(C::NW * 64, C::LDS, a, st);
     }
     case NS_128: {
-      // alone on its compute unit a workgroup keeps one more slab in flight (X X^T of
-      // 2100 x 3900: 76 us with three stages, 96 with two; 2047 x 8000: 139 and 195)
-      if (8 * a.beg[a.n] <= NS_CUS + 8 * a.n) {
+      // Alone on its compute unit a workgroup keeps one more slab in flight (X X^T of
+      // 2100 x 3900: 76 us with three stages, 96 with two; 2047 x 8000: 139 and 195).
+      // Three stages leave no room for a second workgroup (eight of 1024 x 1024, 288
+      // tiles: 50 and 47).
+      if (8 * a.beg[a.n] <= NS_CUS) {
         using C = NsTile<128, 128, 3>;
         return launch_tiles<k_ns_tiles<128, 128, 3, KIND, TO>>(C::NW * 64, C::LDS, a, st);
       }
