@@ -635,9 +635,9 @@ __device__ inline void stage_tile(float* Cs, const f32x4 (&acc)[FT][FT], int lan
 // its clock held down by power; a library's fp16 product of this size 1.1).  A slab of
 // a 256 x 128 tile takes 1800 cycles where its products take 1536, the rest of a
 // launch is the epilogue: every workgroup writes its results at the same time.
-// 128 x 128 tiles with two workgroups a compute unit hide one's epilogue behind the
-// other's products, but read 1.5 times as much from L2: for last rounds that would
-// leave compute units idle (eight of 1024 x 1024: 288 tiles of 256 x 128).
+// 128 x 128 tiles read 1.5 times as much from L2: for products whose last round of
+// larger ones would leave compute units idle, or that have few tiles (eight of
+// 1024 x 1024, X X^T: 288 tiles, two workgroups a compute unit, 47 us).
 template <int TM, int TN, int NST>
 struct NsTile {
   static constexpr int PB = TM / 16, QB = TN / 16, FT = 4;
@@ -757,9 +757,10 @@ __global__ void __launch_bounds__((NsTile<TM, TN, NST>::NW * 64), 2) k_ns_tiles(
 // blocks, each wave loading its operands straight into registers (a load is one
 // contiguous plane), DEPTH blocks ahead; the waves' sums meet in LDS, where what the
 // epilogue reads beside them has arrived meanwhile.  No barrier before that: such a
-// product is bound by latencies, not by the matrix cores.  1000 x 300 takes 7.0 us for
-// X X^T, 4.1 for A A and 9.0 for B X, of which an empty launch is 2.4 and the operands'
-// way from another XCD's writes (through memory) 1.2.
+// product is bound by latencies, not by the matrix cores.  1000 x 300 takes 6.3 us for
+// X X^T, 4.7 for A A and 8.1 for B X, of which an empty launch is 2.4 and the operands'
+// way from another XCD's writes (through memory) 1.2.  With many tiles their operands'
+// way out of L2 bounds it: DeepCNet(6,100)'s matrices with softmax 35.5 us for X X^T.
 template <int T, int NW, int DEPTH, int KIND, typename TO>
 __global__ void __launch_bounds__((NW * 64), (NW == 8 ? 4 : 1)) k_ns_direct(NsArgs a) {
   using W = NsWork<T, T, KIND>;
