@@ -124,14 +124,16 @@ __device__ inline int find_mat(const NsArgs& a, int t) {
 // The kernels of a product, by its 128 x 128 tiles, their slabs of 32 k per compute unit
 // and its 64 x 64 tiles (plan_product).  Measured, us, 128 / 64 / 32 tiles:
 //   X X^T  2100 x 3900 (73 slabs)  76 / 86 / -;  2048 x 2048 (34)  44 / 46 / -;  1800 x 1900 (28)
-//          41.7 / 31.6 / -;  DeepCNet(6,100) with softmax (23, 312 tiles of 64)  39.7 / 35.5 / 35.6;
-//          1500 x 1500 (14, 300)  31.7 / 21.0 / 33.4;  1000 x 600 three times (6, 165)  24.8 / 14.0 /
-//          12.5;  DeepCNiN(5,50) with softmax (160)  27.3 / 23.2 / 14.7;  1000 x 300 (15)  17.0 / 10.0 / 6.3
-//   B X    1500 x 1500 (26 slabs)  36.5 / 42.5 / 63.9;  1300 x 1300 (19)  38.2 / 28.8 / -;
+//          41.7 / 31.5 / -;  DeepCNet(6,100) with softmax (23, 312 tiles of 64)  39.7 / 35.5 / 35.6;
+//          1500 x 1500 (14, 300)  31.7 / 21.0 / 33.4;  1300 x 1300 (231)  27.1 / 14.0 / 23.4;
+//          1100 x 1100 (171)  - / 12.0 / 14.2;  1000 x 600 three times (165)  24.8 / 14.0 / 12.5;
+//          DeepCNiN(5,50) with softmax (160)  27.3 / 23.0 / 14.7;  1000 x 300 (15)  17.0 / 10.0 / 6.3
+//   B X    1500 x 1500 (26 slabs)  36.5 / 42.5 / 63.9;  1300 x 1300 (19)  38.2 / 25.4 / 43.5;
 //          400 x 1600 four times (208 tiles of 128)  21.2 / 28.0 / 23.4;  700 x 3755 (180)  24.4 / 32.4 /
-//          38.9;  1000 x 600 three times (120; 480 of 64)  32.8 / 22.5 / 20.4;  2047 x 822 (112; 416)  34.4 /
-//          24.0 / 30.0;  DeepCNet(5,50) (65; 216)  17.8 / 11.0 / 9.0
-constexpr int NS_CUS = 256, NS_SLABS = 30, NS_SLABS_APPLY = 20, NS_TILES_APPLY = 160, NS_TILES_64 = 256, NS_FULL = 192;
+//          38.9;  1000 x 600 three times (120; 480 of 64)  32.8 / 18.8 / 20.4;  2047 x 822 (112; 416)  34.4 /
+//          20.9 / 30.0;  1000 x 1000 (64; 256)  - / 14.0 / 19.4;  DeepCNet(5,50) (65; 216)  17.8 / 11.4 / 9.4
+constexpr int NS_CUS = 256, NS_SLABS = 30, NS_SLABS_APPLY = 20, NS_TILES_APPLY = 160, NS_TILES_64 = 170,
+              NS_TILES_64_APPLY = 256, NS_FULL = 192;
 constexpr int NS_PARTS = 16;  // workgroups that share a tile, at most
 
 // Sum over the workgroup's 256 threads, in all of them (red: four doubles).
@@ -617,7 +619,7 @@ __device__ inline void mma_block(const f16x8 (&ph)[FT], const f16x8 (&pl)[FT], c
 }
 
 // Result lane l of a 16 x 16 block holds rows 4 (l / 16) .. + 3 of column l % 16.
-template <int FT, int CS>
+template <int FT, int CS, bool ADD = false>
 __device__ inline void stage_tile(float* Cs, const f32x4 (&acc)[FT][FT], int lane) {
   const int l16 = lane & 15, g4 = lane >> 4;
 #pragma unroll
@@ -625,7 +627,10 @@ __device__ inline void stage_tile(float* Cs, const f32x4 (&acc)[FT][FT], int lan
 #pragma unroll
     for (int k = 0; k < FT; ++k)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) Cs[(i * 16 + g4 * 4 + r) * CS + k * 16 + l16] = acc[i][k][r];
+      for (int r = 0; r < 4; ++r) {
+        float& c = Cs[(i * 16 + g4 * 4 + r) * CS + k * 16 + l16];
+        c = ADD ? c + acc[i][k][r] : acc[i][k][r];
+      }
 }
 
 // Large products: TM x TN tiles, a wave for each 64 x 64 of them, operands through a
@@ -761,6 +766,11 @@ __global__ void __launch_bounds__((NsTile<TM, TN, NST>::NW * 64), 2) k_ns_tiles(
 // X X^T, 4.7 for A A and 8.1 for B X, of which an empty launch is 2.4 and the operands'
 // way from another XCD's writes (through memory) 1.2.  With many tiles their operands'
 // way out of L2 bounds it: DeepCNet(6,100)'s matrices with softmax 35.5 us for X X^T.
+// The partial tiles that its waves stage in LDS: of 64 x 64, where something lies beside
+// them, the second half of the waves first, to which the first half then adds, so that two
+// workgroups fit a compute unit (B X of 1000 x 600 three times: 18.8 us, else 22.5).
+constexpr int direct_parts(int T, int waves, int kind) { return T == 64 && kind != NS_GRAM ? waves / 2 : waves; }
+
 template <int T, int NW, int DEPTH, int KIND, typename TO>
 __global__ void __launch_bounds__((NW * 64), (NW == 8 ? 4 : 1)) k_ns_direct(NsArgs a) {
   using W = NsWork<T, T, KIND>;
@@ -784,7 +794,7 @@ __global__ void __launch_bounds__((NW * 64), (NW == 8 ? 4 : 1)) k_ns_direct(NsAr
     }
     return o;
   };
-  char* beside = smem + NW * T * CS * 4;
+  char* beside = smem + direct_parts(T, NW, KIND) * T * CS * 4;
   auto load_besides = [&]() {
     if constexpr (KIND != NS_GRAM)
       for (int b = wave; b < NB; b += NW) {
@@ -834,11 +844,16 @@ __global__ void __launch_bounds__((NW * 64), (NW == 8 ? 4 : 1)) k_ns_direct(NsAr
   for (int d = 0; d < DEPTH - 1; ++d)
     if (kb + d < k1) multiply(d);
   float* Cs = (float*)smem;
-  stage_tile<FT, CS>(Cs + wave * T * CS, acc, lane);
+  constexpr int PARTS = direct_parts(T, NW, KIND);
+  if (wave >= NW - PARTS) stage_tile<FT, CS>(Cs + (wave - (NW - PARTS)) * T * CS, acc, lane);
+  if constexpr (PARTS < NW) {
+    __syncthreads();
+    if (wave < PARTS) stage_tile<FT, CS, true>(Cs + wave * T * CS, acc, lane);
+  }
   asm volatile("" ::: "memory");
   wait_loads<0>();
   __syncthreads();
-  finish_tile<T, T, KIND, TO, NW, NW, 2, true>(a, w, Cs, wave, lane, beside);
+  finish_tile<T, T, KIND, TO, NW, PARTS, 2, true>(a, w, Cs, wave, lane, beside);
 }
 
 // ---------------------------------------------------------------------------
@@ -1053,7 +1068,7 @@ NsPlan plan_product(const NsGroup& g, int kind) {
   }
   const bool lds = symmetric(kind) ? slabs >= NS_SLABS * NS_CUS
                                    : slabs >= NS_SLABS_APPLY * NS_CUS || t128 >= NS_TILES_APPLY;
-  if (!lds) return t64 >= NS_TILES_64 ? NS_64 : NS_32;
+  if (!lds) return t64 >= (symmetric(kind) ? NS_TILES_64 : NS_TILES_64_APPLY) ? NS_64 : NS_32;
   const int64_t rest = t256 % NS_CUS;
   return rest == 0 || rest >= NS_FULL || (t256 > NS_CUS && last_round_parts(g.t.mat[g.a.n - 1], kind, rest) > 1) ? NS_256
                                                                                                          : NS_128;
@@ -1112,10 +1127,9 @@ int64_t deal_tiles(NsGroup& g, int kind, NsPlan plan) {
   return slots;  // (divided tiles are fewer than compute units, so than NS_COUNT)
 }
 
-// LDS of k_ns_direct: the waves' partial tiles, and what lies beside the result (nothing
-// for X X^T, which so has room for two 64 x 64 tiles a compute unit).
+// LDS of k_ns_direct: the waves' partial tiles, and what lies beside the result.
 constexpr int direct_lds(int T, int waves, int kind) {
-  return waves * T * (T + 4) * 4 + (kind == NS_GRAM ? 0 : (T / 16) * (T / 32) * 2048);
+  return direct_parts(T, waves, kind) * T * (T + 4) * 4 + (kind == NS_GRAM ? 0 : (T / 16) * (T / 32) * 2048);
 }
 
 // Allows a kernel its LDS: once per kernel and device, since the call costs as much as
