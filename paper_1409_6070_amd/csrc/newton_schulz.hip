@@ -459,11 +459,16 @@ __device__ inline bool join_parts(const NsArgs& a, const W& w, float* Cs) {
   f32x4* out = (f32x4*)(a.part + (int64_t)(w.slot + w.part) * (TM * TN));
   for (int i = threadIdx.x; i < V; i += NT)
     out[i] = *(const f32x4*)(Cs + i / (TN / 4) * CS + i % (TN / 4) * 4);
-  asm volatile("" ::: "memory");
-  wait_loads<0>();  // (vmcnt counts stores too; the barrier alone waits for none of them)
+  // Waits in asm, for the stores (the barrier alone waits for none) and for the write-back:
+  // behind a wait that it knows of the compiler takes nothing to be outstanding, and
+  // leaves out its own between the write-back and the counter.
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (threadIdx.x == 0)
-    last = __hip_atomic_fetch_add(a.count + w.counter, 1, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT) == w.parts - 1;
+  if (threadIdx.x == 0) {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    last = __hip_atomic_fetch_add(a.count + w.counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == w.parts - 1;
+  }
   __syncthreads();
   if (!last) return false;
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
