@@ -53,15 +53,14 @@ bool coefficients_ok(int32_t steps, const float* coef) {
       most = std::max(most, std::fabs(a + p) * std::sqrt(q));
     };
     at(end);
-    if (c != 0.0) {
-      at(-b / (2.0 * c));
-      const double d = 9.0 * b * b - 20.0 * a * c;  // a + 3 b q + 5 c q^2 = 0
-      if (d >= 0.0) {
-        at((-3.0 * b + std::sqrt(d)) / (10.0 * c));
-        at((-3.0 * b - std::sqrt(d)) / (10.0 * c));
-      }
-    } else if (b != 0.0) {
-      at(-a / (3.0 * b));
+    if (c != 0.0) at(-b / (2.0 * c));
+    // a + 3 b q + 5 c q^2 = 0, its roots without a difference of nearly equal numbers:
+    // where c is too small to matter the cubic's extremum is still one of them
+    const double d = 9.0 * b * b - 20.0 * a * c;
+    if (d >= 0.0) {
+      const double t = -0.5 * (3.0 * b + std::copysign(std::sqrt(d), b));
+      if (c != 0.0) at(t / (5.0 * c));
+      if (t != 0.0) at(a / t);
     }
     if (!ok || !(most <= 3.5)) return false;
     hi = most;

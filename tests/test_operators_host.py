@@ -184,3 +184,28 @@ def test_net_calls_refuse():
         assert lib.sscn_set_head_norm(h, None, None, None, None, 0.0, None, 0) == 0
     finally:
         sscn.sscn_net_destroy(h)
+
+
+def _dense(rows):
+    """(largest singular value after a step, largest |b s^2 + c s^4|) over the steps, on a dense scan of [0, hi]."""
+    hi, most, inner = 1.0, 0.0, 0.0
+    for a, b, c in rows:
+        s = [hi * i / 20000 for i in range(20001)]
+        inner = max(inner, max(abs(b * x ** 2 + c * x ** 4) for x in s))
+        hi = max(abs(a * x + b * x ** 3 + c * x ** 5) for x in s)
+        most = max(most, hi)
+    return most, inner
+
+
+@pytest.mark.parametrize("rows", [
+    [(100.0, -100.0, 1e-20)], [(100.0, -100.0, 1e-14)], [(10.0, -10.0, 1e-18)], [(9.5, -9.5, 1e-17)], [(9.5, -9.5, -1e-17)],
+    [(9.0, -9.0, 1e-17)], [(9.0, -9.0, -1e-17)], [(9.0, -9.0, 1e-30)],
+    [(100.0, -100.0, 1e-20), (1.0, 0.0, 0.0)], [(1.0, 0.0, 0.0), (100.0, -100.0, 1e-20)],
+    [(9.0, -9.0, 1e-17), (1.05, 0.0, 0.0)], [(9.0, -9.0, 1e-17), (1.0, 0.0, 0.0)],
+    [(-100.0, 100.0, 1e-20)], [(1e-20, -3.0, 1e-20)], [(0.0, 0.0, 1e-20)], [(0.0, 0.0, 0.0), (2.0, 0.0, 0.0)]], ids=str)
+def test_an_extremum_inside_the_range_is_found_for_any_coefficients(rows):
+    """A fifth-power coefficient too small to matter must not hide where the cubic turns."""
+    coef = (ctypes.c_float * (3 * len(rows)))(*[x for r in rows for x in r])
+    most, inner = _dense([list(coef)[3 * k: 3 * k + 3] for k in range(len(rows))])
+    want = WORKSPACE if most <= 3.5 and inner <= 200 else INVALID
+    assert _ortho(_mats((5, 7)), steps=len(rows), coef=coef, ws=None) == want
