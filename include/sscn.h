@@ -312,11 +312,16 @@ typedef struct {
  *   out = X, transposed back.
  * Every singular value s of X becomes a s + b s^3 + c s^5 per step; {3.4445,
  * -4.7750, 2.0315} over five steps, as commonly used with Muon, brings them to
- * about 0.7 .. 1.2.  X is float32 throughout and the products have float32
- * accuracy whatever dtype is; the result is rounded once.  A zero matrix gives
- * zeros, one with a NaN or an infinity NaN everywhere.  Coefficients must be
- * finite and keep every singular value at most 3.5 and |b s^2 + c s^4| at most
- * 200 (followed from [0, 1]), else SSCN_ERR_INVALID_ARGUMENT.  Matrices are
+ * about 0.7 .. 1.2.  X and all sums are float32 whatever dtype is; the result is
+ * rounded once.  An entry of a product's operand (X, A, B = b A + c A A) is held
+ * to 2^-22 of itself or to 2^-39 of the largest value that the coefficients let
+ * the operand reach, whichever is more: relative to the whole matrix the result
+ * is as exact as with float32 products, but a row or column of less than about
+ * 1e-5 of the others' size loses accuracy relative to itself, in proportion.
+ * A zero matrix gives zeros, one with a NaN or an infinity NaN everywhere.
+ * Coefficients must be finite and keep every singular value at most 3.5 and
+ * |b s^2 + c s^4| at most 200 (followed from [0, 1]), else
+ * SSCN_ERR_INVALID_ARGUMENT.  Matrices are
  * worked on together: one call for many is faster than a call for each. */
 SSCN_API sscn_status sscn_orthogonalize_workspace_bytes(int32_t n, const sscn_ortho_matrix* h_matrices, size_t* bytes);
 SSCN_API sscn_status sscn_orthogonalize(int32_t dtype, int32_t n, const sscn_ortho_matrix* h_matrices, int32_t steps,

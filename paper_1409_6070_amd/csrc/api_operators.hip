@@ -34,22 +34,27 @@ bool shape_ok(int64_t rows, int64_t cols) {
   return rows >= 1 && cols >= 1 && std::min(rows, cols) <= SSCN_ORTHO_MAX_SHORT && std::max(rows, cols) <= SSCN_ORTHO_MAX_LONG;
 }
 
-// Whether the iteration keeps every singular value that starts in [0, 1] where the
-// planes of newton_schulz.hip hold it.  Each step's largest |p(s)| and
-// |b s^2 + c s^4| over [0, hi] lie at hi or where the derivative is zero.
-bool coefficients_ok(int32_t steps, const float* coef) {
+// The exponent of two that brings values up to `most` within NS_PLANE.
+int32_t plane_exponent(double most) {
+  return most > 0.0 ? (int32_t)std::min(60.0, std::floor(std::log2(NS_PLANE / most))) : 0;
+}
+
+// Follows the singular values that start in [0, 1] through the steps.  Each step's
+// largest |p(s)| and |b s^2 + c s^4| over [0, hi] lie at hi or where the derivative is
+// zero; entries of X, A and B are at most hi, hi^2 and the latter.  Sets out[0 .. steps - 1]
+// and returns true if X stays within 3.5 and B within 200.
+bool follow_steps(int32_t steps, const float* coef, NsStep (&out)[SSCN_ORTHO_MAX_STEPS]) {
   if (steps < 1 || steps > SSCN_ORTHO_MAX_STEPS || !coef) return false;
   double hi = 1.0;
   for (int k = 0; k < steps; ++k) {
     const double a = coef[3 * k], b = coef[3 * k + 1], c = coef[3 * k + 2];
     if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
-    double most = 0.0;
+    double most = 0.0, inner = 0.0;
     const double end = hi * hi;
-    bool ok = true;
     auto at = [&](double q) {  // q = s^2
       if (!(q >= 0.0 && q <= end)) return;
       const double p = b * q + c * q * q;
-      ok = ok && std::fabs(p) <= 200.0;
+      inner = std::max(inner, std::fabs(p));
       most = std::max(most, std::fabs(a + p) * std::sqrt(q));
     };
     at(end);
@@ -62,7 +67,9 @@ bool coefficients_ok(int32_t steps, const float* coef) {
       if (c != 0.0) at(t / (5.0 * c));
       if (t != 0.0) at(a / t);
     }
-    if (!ok || !(most <= 3.5)) return false;
+    if (!(inner <= 200.0) || !(most <= 3.5)) return false;
+    out[k] = NsStep{coef[3 * k], coef[3 * k + 1], coef[3 * k + 2], plane_exponent(hi), plane_exponent(end),
+                    plane_exponent(inner)};
     hi = most;
   }
   return true;
@@ -126,10 +133,10 @@ size_t group_bytes(int32_t n, Shape&& shape) {
 
 template <class Shape, class Fill>
 hipError_t run_groups(int32_t n, Shape&& shape, Fill&& fill, NsGroup& g, bool bf16, bool muon, int32_t steps,
-                      const float* coef, void* d_ws, hipStream_t st) {
+                      const NsStep* step, void* d_ws, hipStream_t st) {
   for (int32_t i = 0; i < n; i += NS_MATS) {
     carve_group(g, i, std::min(NS_MATS, n - i), shape, fill, (char*)d_ws);
-    const hipError_t e = launch_newton_schulz(g, bf16, muon, steps, coef, st);
+    const hipError_t e = launch_newton_schulz(g, bf16, muon, steps, step, st);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -209,7 +216,8 @@ sscn_status sscn_orthogonalize_workspace_bytes(int32_t n, const sscn_ortho_matri
 sscn_status sscn_orthogonalize(int32_t dtype, int32_t n, const sscn_ortho_matrix* h_matrices, int32_t steps,
                                const float* h_coef, void* d_workspace, size_t workspace_bytes, void* stream) {
   size_t need = 0;
-  if (!known_dtype(dtype) || !coefficients_ok(steps, h_coef)) return SSCN_ERR_INVALID_ARGUMENT;
+  NsStep step[SSCN_ORTHO_MAX_STEPS];
+  if (!known_dtype(dtype) || !follow_steps(steps, h_coef, step)) return SSCN_ERR_INVALID_ARGUMENT;
   const sscn_status s = sscn_orthogonalize_workspace_bytes(n, h_matrices, &need);
   if (s != SSCN_OK) return s;
   for (int32_t i = 0; i < n; ++i) {
@@ -227,7 +235,7 @@ sscn_status sscn_orthogonalize(int32_t dtype, int32_t n, const sscn_ortho_matrix
         M.o = h_matrices[i].d_out;
         M.o_stride = h_matrices[i].out_stride;
       },
-      g, dtype == SSCN_BF16, false, steps, h_coef, d_workspace, (hipStream_t)stream));
+      g, dtype == SSCN_BF16, false, steps, step, d_workspace, (hipStream_t)stream));
 }
 
 sscn_status sscn_muon_workspace_bytes(int32_t n, const sscn_muon_param* h_params, size_t* bytes) {
@@ -268,7 +276,8 @@ sscn_status sscn_muon_update(int32_t dtype, int32_t n, const sscn_muon_param* h_
       return SSCN_ERR_INVALID_ARGUMENT;
     any = any || p.orthogonal;
   }
-  if (any && !coefficients_ok(steps, h_coef)) return SSCN_ERR_INVALID_ARGUMENT;
+  NsStep step[SSCN_ORTHO_MAX_STEPS];
+  if (any && !follow_steps(steps, h_coef, step)) return SSCN_ERR_INVALID_ARGUMENT;
   if (bad_workspace(d_workspace, workspace_bytes, need)) return SSCN_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
   SgdArgs sgd;
@@ -298,7 +307,7 @@ sscn_status sscn_muon_update(int32_t dtype, int32_t n, const sscn_muon_param* h_
           M.scale = p.lr * p.scale;
           M.decay = p.lr * p.weight_decay;
         },
-        g, dtype == SSCN_BF16, true, steps, h_coef, d_workspace, st);
+        g, dtype == SSCN_BF16, true, steps, step, d_workspace, st);
     k = 0;
     return e;
   };

@@ -516,7 +516,10 @@ struct NsArgs {
   int32_t step;
   int32_t nesterov;
   float momentum;
-  float a, b, c;
+  // Of one product: result = of_sum times its sums + of_beside times what lies beside them
+  // (the step's coefficients, and the planes' powers of two undone), stored in planes
+  // times scale.
+  float of_sum, of_beside, scale;
   const NsTable* table;
   float* part;     // partial tiles
   int32_t* count;  // [NS_COUNT] finished parts of each divided tile, zero between products
@@ -528,8 +531,15 @@ struct NsGroup {
   NsArgs a;
   NsTable t;
 };
+// One step's coefficients, and the exponents of two by which the planes of X, A and B
+// are scaled in it: the largest that keep what they may hold within NS_PLANE.
+struct NsStep {
+  float a, b, c;
+  int32_t ex, ea, eb;
+};
+constexpr double NS_PLANE = 51200.0;  // fp16 ends at 65504: room for what roundings add to the singular values
 // Bytes of partial tiles that the group's products need (m, n, mp, np set).
 size_t ns_part_bytes(NsGroup& g);
-hipError_t launch_newton_schulz(NsGroup& g, bool bf16, bool muon, int steps, const float* coef, hipStream_t st);
+hipError_t launch_newton_schulz(NsGroup& g, bool bf16, bool muon, int steps, const NsStep* step, hipStream_t st);
 
 }  // namespace sscn

@@ -7,16 +7,22 @@
 // The odd polynomial p(s) = a s + b s^3 + c s^5 acts on X's singular values and
 // leaves its singular vectors: a few steps bring all but the smallest near 1.
 //
-// Precision.  X is kept in float32.  A product's operands are split into two
-// fp16 numbers each, hi + lo (22 bits; powers of two keep them in fp16's range),
-// and multiplied on the fp16 matrix cores as hi hi + hi lo + lo hi with float32
-// sums: three times the matrix work of a plain fp16 product, which the fp16 cores
-// still do at five times the rate of float32 MFMA (4096 x 4096: 387 TFLOP/s of the
-// formula's operations; a library's float32 product reaches 154).  A small singular value is carried from step to step
-// by a X alone (B's rows along it are small), which is float32 throughout: the
-// result is as near to the formula's as a float32 computation's, where operands
-// of fewer bits lose the small singular values, whose errors every step
-// multiplies by a (about 3.4).
+// Precision.  X is kept in float32.  A product's operands, A and B among them, are
+// split into two fp16 numbers each, hi + lo, and multiplied on the fp16 matrix cores
+// as hi hi + hi lo + lo hi with float32 sums: three times the matrix work of a plain
+// fp16 product, which the fp16 cores still do at five times the rate of float32 MFMA
+// (4096 x 4096: 387 TFLOP/s of the formula's operations; a library's float32 product
+// reaches 154).  An operand is scaled by the power of two that brings the largest value
+// it may hold near fp16's end (NsStep).  An entry is then off by 2^-22 of itself or,
+// where its lo part falls below fp16's smallest step, by 2^-39 of that largest value.
+// A small singular value is carried from step to step by a X alone (B's rows along it
+// are small), which is float32 throughout: relative to the matrix the result is as
+// near to the formula's as a float32 computation's, where operands of fewer bits lose
+// the small singular values, whose errors every step multiplies by a (about 3.4).  A
+// row or column far smaller than the others is less exact relative to itself, since the
+// scales are the matrix's: every second row (column) of 300 x 1000 at 1e-4 of the others
+// is off by 1.7e-7 (1.3e-6), at 1e-6 by 1.4e-6 (3.5e-5); float32 products 2.9e-7 (2.3e-6)
+// at either.
 //
 // Layout.  An operand with R rows of K values is stored as the matrix cores read
 // it: blocks of 16 rows x 32 k, row-block major, a block's hi plane of 1 KiB then
@@ -39,11 +45,6 @@ namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-// Powers of two that the planes carry.  The entry points admit coefficients that
-// keep X's singular values at most 3.5, so entries of A at most 12.25, and those of
-// B at most 200: all below fp16's 65504, with lo parts above its smallest steps.
-constexpr float SX = 256.f, SA = 4096.f, SB = 256.f;
 
 constexpr int BLOCK = 2048;  // bytes of a 16 x 32 block, both planes
 
@@ -264,10 +265,10 @@ __global__ void __launch_bounds__(256) k_ns_convert(NsArgs a) {
     float* X = M.X + (int64_t)(i0 + i) * M.np + j0 + k8 * 8;
     *(f32x4*)X = f32x4{w[0], w[1], w[2], w[3]};
     *(f32x4*)(X + 4) = f32x4{w[4], w[5], w[6], w[7]};
-    store_split(M.opX + block_at(i0 / 16 + h, j0 / 32, M.np / 32) + lane * 16, w, SX);
+    store_split(M.opX + block_at(i0 / 16 + h, j0 / 32, M.np / 32) + lane * 16, w, a.scale);
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[e] = tile[wave][k8 * 8 + e][h * 16 + r16];
-    store_split(M.opXt[0] + block_at(j0 / 16 + h, i0 / 32, M.mp / 32) + lane * 16, w, SX);
+    store_split(M.opXt[0] + block_at(j0 / 16 + h, i0 / 32, M.mp / 32) + lane * 16, w, a.scale);
   }
 }
 
@@ -382,7 +383,7 @@ __device__ inline void beside_values(u32x4 p, u32x4 q, float (&x)[8]) {
   if constexpr (KIND == NS_POLY) {
     const f16x8 hi = __builtin_bit_cast(f16x8, p), lo = __builtin_bit_cast(f16x8, q);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = ((float)hi[e] + (float)lo[e]) * (1.f / SA);
+    for (int e = 0; e < 8; ++e) x[e] = (float)hi[e] + (float)lo[e];
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -504,7 +505,6 @@ __device__ inline void finish_tile(const NsArgs& a, const NsWork<TM, TN, KIND>& 
                                    const char* beside) {
   using W = NsWork<TM, TN, KIND>;
   constexpr int CS = TN + 4;
-  constexpr float unscale = KIND == NS_GRAM ? 1.f / (SX * SX) : KIND == NS_POLY ? 1.f / (SA * SA) : 1.f / (SB * SX);
   constexpr bool LAST = KIND == NS_ORTHO || KIND == NS_MUON;
   const NsMat& M = w.M;
   const int l16 = lane & 15, g4 = lane >> 4;
@@ -539,24 +539,24 @@ __device__ inline void finish_tile(const NsArgs& a, const NsWork<TM, TN, KIND>& 
 #pragma unroll
           for (int p = 1; p < PARTS; ++p) s += *(const f32x4*)(c + 4 * h + p * TM * CS);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[4 * h + e] = s[e] * unscale;
+          for (int e = 0; e < 4; ++e) v[4 * h + e] = s[e] * a.of_sum;
         }
         float x[8];
-        if constexpr (KIND != NS_GRAM) beside_values<KIND>(bes[g][0], bes[g][1], x);
+        if constexpr (KIND != NS_GRAM) {
+          beside_values<KIND>(bes[g][0], bes[g][1], x);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = fmaf(a.of_beside, x[e], v[e]);
+        }
         if constexpr (KIND == NS_GRAM) {
-          store_split(M.opA + block_at(row0 + rb, col0 + kb, M.mp / 32) + lane * 16, v, SA);
+          store_split(M.opA + block_at(row0 + rb, col0 + kb, M.mp / 32) + lane * 16, v, a.scale);
         } else if constexpr (KIND == NS_POLY) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = a.b * x[e] + a.c * v[e];
-          store_split(M.opB + block_at(row0 + rb, col0 + kb, M.mp / 32) + lane * 16, v, SB);
+          store_split(M.opB + block_at(row0 + rb, col0 + kb, M.mp / 32) + lane * 16, v, a.scale);
         } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = a.a * x[e] + v[e];
           if constexpr (KIND == NS_APPLY) {
             float* X = M.X + (int64_t)((row0 + rb) * 16 + l16) * M.np + (col0 + kb) * 32 + g4 * 8;
             *(f32x4*)X = *(const f32x4*)v;
             *(f32x4*)(X + 4) = *(const f32x4*)(v + 4);
-            store_split(M.opX + block_at(row0 + rb, col0 + kb, M.np / 32) + lane * 16, v, SX);
+            store_split(M.opX + block_at(row0 + rb, col0 + kb, M.np / 32) + lane * 16, v, a.scale);
           } else if (!M.tall) {
             store_result<KIND, TO>(M, (row0 + rb) * 16 + l16, (col0 + kb) * 32 + g4 * 8, v, old[g]);
           }
@@ -592,8 +592,7 @@ __device__ inline void finish_tile(const NsArgs& a, const NsWork<TM, TN, KIND>& 
         store_result<KIND, TO>(M, (row0 + rb) * 16 + l16, (col0 + kb) * 32 + g4 * 8, v, old[g]);
       } else {
         char* op = KIND == NS_GRAM ? M.opA : KIND == NS_POLY ? M.opB : w.Xt_next;
-        constexpr float scale = KIND == NS_GRAM ? SA : KIND == NS_POLY ? SB : SX;
-        store_split(op + block_at(row0 + rb, col0 + kb, M.mp / 32) + lane * 16, v, scale);
+        store_split(op + block_at(row0 + rb, col0 + kb, M.mp / 32) + lane * 16, v, a.scale);
       }
     }
   }
@@ -875,7 +874,9 @@ constexpr int SMALL_LDS = 2 * SMALL_ELEMS * 4 + 2 * SMALL_M * SMALL_M * 4;
 struct NsCoef {
   int32_t steps;
   float c[3 * SMALL_STEPS];
+  int8_t ex[SMALL_STEPS], ea[SMALL_STEPS], eb[SMALL_STEPS];  // NsStep's
 };
+static_assert(sizeof(NsArgs) + sizeof(NsTable) + sizeof(NsCoef) <= 4096, "kernel arguments");
 
 // Block (bi, bj) of a result, lane l's part rows 4 (l / 16) .. of column l % 16, as the
 // operand whose rows are the result's columns: four consecutive k, 8 bytes a plane.
@@ -964,13 +965,13 @@ __global__ void __launch_bounds__(512) k_ns_small(NsArgs a, NsTable t, NsCoef co
 #pragma unroll
   for (int w = 0; w < 8; ++w) ss += red[w];
   const double inv = ss == 0.0 ? 0.0 : 1.0 / sqrt(ss);
-  const auto put_x = [&]() {
+  const auto put_x = [&](float sx) {
 #pragma unroll
     for (int n = 0; n < SMALL_XB; ++n) {
       const int t = wave + 8 * n, bi = t / nb, bj = t - bi * nb;
       if (t >= xblocks) break;
-      put_rows(opX, bi, bj, nk, lane, x[n], SX);
-      put_columns(opXt, bi, bj, mk, lane, x[n], SX);
+      put_rows(opX, bi, bj, nk, lane, x[n], sx);
+      put_columns(opXt, bi, bj, mk, lane, x[n], sx);
     }
   };
 #pragma unroll
@@ -982,36 +983,39 @@ __global__ void __launch_bounds__(512) k_ns_small(NsArgs a, NsTable t, NsCoef co
       x[n][e] = in ? (float)((double)x[n][e] * inv) : 0.f;
     }
   }
-  put_x();
+  put_x(ldexpf(1.f, coef.ex[0]));
   __syncthreads();
   for (int s = 0; s < coef.steps; ++s) {
     const float ca = coef.c[3 * s], cb = coef.c[3 * s + 1], cc = coef.c[3 * s + 2];
+    const int ex = coef.ex[s], ea = coef.ea[s], eb = coef.eb[s];
+    const float sa = ldexpf(1.f, ea), sb = ldexpf(1.f, eb);
+    const float from_xx = ldexpf(1.f, -2 * ex), from_aa = ldexpf(1.f, -2 * ea), from_bx = ldexpf(1.f, -eb - ex);
     f32x4 A[SMALL_AB];
 #pragma unroll
     for (int n = 0; n < SMALL_AB; ++n) {
       const int t = wave + 8 * n, bi = t / mb, bj = t - bi * mb;
       if (t >= ablocks) break;
-      A[n] = small_product(opX, bi, opX, bj, nk, lane) * (1.f / (SX * SX));
-      put_columns(opA, bi, bj, mk, lane, A[n], SA);
+      A[n] = small_product(opX, bi, opX, bj, nk, lane) * from_xx;
+      put_columns(opA, bi, bj, mk, lane, A[n], sa);
     }
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < SMALL_AB; ++n) {
       const int t = wave + 8 * n, bi = t / mb, bj = t - bi * mb;
       if (t >= ablocks) break;
-      const f32x4 B = cb * A[n] + cc * (small_product(opA, bi, opA, bj, mk, lane) * (1.f / (SA * SA)));
-      put_columns(opB, bi, bj, mk, lane, B, SB);
+      const f32x4 B = cb * A[n] + cc * (small_product(opA, bi, opA, bj, mk, lane) * from_aa);
+      put_columns(opB, bi, bj, mk, lane, B, sb);
     }
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < SMALL_XB; ++n) {
       const int t = wave + 8 * n, bi = t / nb, bj = t - bi * nb;
       if (t >= xblocks) break;
-      x[n] = ca * x[n] + small_product(opB, bi, opXt, bj, mk, lane) * (1.f / (SB * SX));
+      x[n] = ca * x[n] + small_product(opB, bi, opXt, bj, mk, lane) * from_bx;
     }
     if (s + 1 == coef.steps) break;
     __syncthreads();  // every wave done with X's operands
-    put_x();
+    put_x(ldexpf(1.f, coef.ex[s + 1]));
     __syncthreads();
   }
 #pragma unroll
@@ -1193,15 +1197,22 @@ hipError_t run_product(NsGroup& g, hipStream_t st) {
 }
 
 template <typename TO, bool MUON>
-hipError_t run_steps(NsGroup& g, int steps, const float* coef, hipStream_t st) {
+hipError_t run_steps(NsGroup& g, int steps, const NsStep* step, hipStream_t st) {
   NsArgs& a = g.a;
   for (int s = 0; s < steps; ++s) {
-    a.a = coef[3 * s];
-    a.b = coef[3 * s + 1];
-    a.c = coef[3 * s + 2];
+    const NsStep& S = step[s];
     a.step = s;
+    // (powers of two: nothing is rounded)
+    a.of_sum = ldexpf(1.f, -2 * S.ex);
+    a.scale = ldexpf(1.f, S.ea);
     hipError_t e = run_product<NS_GRAM, float>(g, st);
+    a.of_sum = ldexpf(S.c, -2 * S.ea);
+    a.of_beside = ldexpf(S.b, -S.ea);
+    a.scale = ldexpf(1.f, S.eb);
     if (e == hipSuccess) e = run_product<NS_POLY, float>(g, st);
+    a.of_sum = ldexpf(1.f, -S.eb - S.ex);
+    a.of_beside = S.a;
+    a.scale = s + 1 < steps ? ldexpf(1.f, step[s + 1].ex) : 1.f;
     if (e == hipSuccess)
       e = s + 1 < steps ? run_product<NS_APPLY, float>(g, st) : run_product<MUON ? NS_MUON : NS_ORTHO, TO>(g, st);
     if (e != hipSuccess) return e;
@@ -1210,8 +1221,9 @@ hipError_t run_steps(NsGroup& g, int steps, const float* coef, hipStream_t st) {
 }
 
 template <typename T, bool MUON>
-hipError_t run_begin(NsGroup& g, hipStream_t st) {
+hipError_t run_begin(NsGroup& g, const NsStep& first, hipStream_t st) {
   NsArgs& a = g.a;
+  a.scale = ldexpf(1.f, first.ex);
   NsMat* mat = g.t.mat;
   int blocks = 0;
   for (int j = 0; j < a.n; ++j) {
@@ -1252,22 +1264,29 @@ static hipError_t run_small(const NsGroup& g, const NsCoef& c, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_newton_schulz(NsGroup& g, bool bf16, bool muon, int steps, const float* coef, hipStream_t st) {
+hipError_t launch_newton_schulz(NsGroup& g, bool bf16, bool muon, int steps, const NsStep* step, hipStream_t st) {
   bool small = steps <= SMALL_STEPS;
   for (int j = 0; j < g.a.n; ++j)
     small = small && g.t.mat[j].mp <= SMALL_M && (int64_t)g.t.mat[j].mp * g.t.mat[j].np <= SMALL_ELEMS;
   if (small) {
     NsCoef c{};
     c.steps = steps;
-    for (int i = 0; i < 3 * steps; ++i) c.c[i] = coef[i];
+    for (int i = 0; i < steps; ++i) {
+      c.c[3 * i] = step[i].a;
+      c.c[3 * i + 1] = step[i].b;
+      c.c[3 * i + 2] = step[i].c;
+      c.ex[i] = (int8_t)step[i].ex;
+      c.ea[i] = (int8_t)step[i].ea;
+      c.eb[i] = (int8_t)step[i].eb;
+    }
     if (muon) return bf16 ? run_small<float, __bf16, true>(g, c, st) : run_small<float, float, true>(g, c, st);
     return bf16 ? run_small<__bf16, __bf16, false>(g, c, st) : run_small<float, float, false>(g, c, st);
   }
-  hipError_t e = muon ? run_begin<float, true>(g, st)
-                 : bf16 ? run_begin<__bf16, false>(g, st) : run_begin<float, false>(g, st);
+  hipError_t e = muon ? run_begin<float, true>(g, step[0], st)
+                 : bf16 ? run_begin<__bf16, false>(g, step[0], st) : run_begin<float, false>(g, step[0], st);
   if (e != hipSuccess) return e;
-  if (muon) return bf16 ? run_steps<__bf16, true>(g, steps, coef, st) : run_steps<float, true>(g, steps, coef, st);
-  return bf16 ? run_steps<__bf16, false>(g, steps, coef, st) : run_steps<float, false>(g, steps, coef, st);
+  if (muon) return bf16 ? run_steps<__bf16, true>(g, steps, step, st) : run_steps<float, true>(g, steps, step, st);
+  return bf16 ? run_steps<__bf16, false>(g, steps, step, st) : run_steps<float, false>(g, steps, step, st);
 }
 
 }  // namespace sscn

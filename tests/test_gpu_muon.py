@@ -581,3 +581,82 @@ def test_buffers_of_a_captured_step_outlive_other_choices():
         again = net.set_head_norm(gain, shift)
         assert net._muon_ws.data_ptr() == ws and all(p is q for p, q in zip(again, grads))
         torch.cuda.synchronize()
+
+
+def _largest(rows):
+    """Largest values that X, A and B = b A + c A A may hold in each step: dense scans of [0, hi]."""
+    hi, out = 1.0, []
+    for a, b, c in ((float(np.float32(v)) for v in r) for r in rows):
+        s = np.linspace(0.0, hi, 20001)
+        out.append((hi, hi * hi, np.abs(b * s ** 2 + c * s ** 4).max()))
+        hi = np.abs(a * s + b * s ** 3 + c * s ** 5).max()
+    return out
+
+
+def _ns_held(u, rows, gen):
+    """The formula in 64 bits with every operand's entries off, in a random direction, by what the interface states:
+    1.5 2^-22 of themselves (the dropped product of the lo parts included) or 2^-39 of the operand's largest value."""
+    def o(t, most):
+        sign = 2 * torch.randint(0, 2, t.shape, generator=gen, device=t.device) - 1
+        return t + sign * torch.clamp(1.5 * 2.0 ** -22 * t.abs(), min=2.0 ** -39 * most)
+    x = u.double() / u.double().norm()
+    for (a, b, c), (hx, ha, hb) in zip(((float(np.float32(v)) for v in r) for r in rows), _largest(rows)):
+        g = o(x, hx) @ o(x, hx).t().contiguous()
+        x = a * x + o(b * o(g, ha) + c * (o(g, ha) @ o(g, ha).t().contiguous()), hb) @ o(x, hx)
+    return x
+
+
+# by each kernel: one workgroup, 32 and 64 wide register tiles, tiles in LDS; other coefficients: smaller and larger values
+@pytest.mark.parametrize("size", [1e-3, 1e-4, 1e-5, 1e-6, 1e-8])
+@pytest.mark.parametrize("axis", [0, 1], ids=["rows", "columns"])
+@pytest.mark.parametrize("shape,coef", [((48, 100), MUON), ((300, 1000), MUON), ((1100, 1150), MUON), ((1433, 1500), MUON),
+                                        ((300, 1000), (1.5, -0.5, 0.0)), ((300, 1000), (2.0, -0.2, 0.0))], ids=str)
+def test_small_rows_and_columns_relative_to_themselves(shape, coef, axis, size):
+    """Every second row or column of another size: their error, relative to themselves alone.  Bound: three times the
+    distance of the steps in float32 plus that of the steps with operands held as the interface states, both taken
+    over these rows or columns."""
+    from paper_1409_6070_amd.sscn import Orthogonalizer
+    rows = [coef] * 5
+    at = [slice(None)] * 2
+    at[axis] = slice(0, None, 2)
+    at = tuple(at)
+    u = _rand(*shape, seed=7)
+    u[at] *= size
+    want = ns(u, torch.float64, coef)[at]
+    norm = want.norm().item()
+    off32 = (ns(u, torch.float32, coef).double()[at] - want).norm().item() / norm
+    held = max((_ns_held(u, rows, torch.Generator(u.device).manual_seed(k))[at] - want).norm().item()
+               for k in range(3)) / norm
+    got = Orthogonalizer([shape], "f32", coef=coef).orthogonalize([u])[0].double()[at]
+    off = (got - want).norm().item() / norm
+    log(f"[orthogonalize] {shape} {coef} {'columns' if axis else 'rows'} of {size}: off {off:.3g} (float32 {off32:.3g}), "
+        f"allowed {3 * (off32 + held):.3g}")
+    assert off <= 3 * (off32 + held)
+
+
+# singular values that end just below where the planes' powers of two change (1.25^2 = 1.5625 = 51200 / 2^15), and at 3.5
+REACH = [[(1.5624, 0.0, 0.0), (0.9, 0.0, 0.0)], [(1.2499, 0.0, 0.0), (0.9, 0.1, 0.0)], [(1.2501, 0.0, 0.0), (0.9, 0.1, 0.0)],
+         [(3.499, 0.0, 0.0), (0.9, -0.05, 0.0)], [(17.4, -69.6, 55.68), (0.25, -0.02, 0.001)], [(1e-9, 0.0, 0.0), (3e4, 0.0, 0.0)],
+         [(1.0, 0.7812, 0.7812), (0.5, 0.0, 0.0)], [(1.0, 0.0, 0.0)]]
+
+
+@pytest.mark.parametrize("shape", [(1, 1), (40, 60), (300, 1000), (1433, 1500)], ids=str)
+@pytest.mark.parametrize("rows", REACH, ids=str)
+def test_values_that_reach_the_ends_of_the_planes(rows, shape):
+    """One entry alone is its own singular value, 1 before the first step: what the coefficients were followed for.
+    Bound: a step's relative error of s is |s p'(s) / p(s)| times the last one's, and ten roundings of the terms' sizes,
+    of which those of B s hold 2^-21."""
+    from paper_1409_6070_amd.sscn import Orthogonalizer
+    u = torch.zeros(shape, device="cuda")
+    u[shape[0] // 2, shape[1] // 3] = -7.0
+    s, rel = 1.0, 2 * U
+    for a, b, c in ((float(np.float32(v)) for v in r) for r in rows):
+        terms = abs(a) + 2 ** 3 * (abs(b) * s ** 2 + abs(c) * s ** 4)
+        p = a + b * s ** 2 + c * s ** 4
+        rel = abs((a + 3 * b * s ** 2 + 5 * c * s ** 4) / p) * rel + 10 * U * terms / abs(p)
+        s *= p
+    got = Orthogonalizer([shape], "f32", coef=rows, steps=len(rows)).orthogonalize([u])[0].double().cpu()
+    want = torch.zeros(shape, dtype=torch.float64)
+    want[shape[0] // 2, shape[1] // 3] = -s
+    log(f"[orthogonalize] {shape} {rows}: {got.min().item():.9g}, {-s:.9g} within {rel:.2g}")
+    assert (got - want).abs().max() <= rel * abs(s)
