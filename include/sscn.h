@@ -259,8 +259,9 @@ SSCN_API sscn_status sscn_sgd_step(sscn_net* net, float* const* h_W32, void* con
  * and the next row are neither read nor written.  Arrays must be aligned to
  * their element type only. */
 
-/* Limits: rows of an array; columns of a layer norm; shorter and longer side of
- * a matrix to orthogonalise; Newton-Schulz steps. */
+/* Limits: rows of an array (whose last element lies at most 2^60 elements behind
+ * its first, with strides up to 2^31); columns of a layer norm; shorter and longer
+ * side of a matrix to orthogonalise; Newton-Schulz steps. */
 #define SSCN_MAX_ROWS 2147483647
 #define SSCN_NORM_MAX_COLS 1048576
 #define SSCN_ORTHO_MAX_SHORT 16384

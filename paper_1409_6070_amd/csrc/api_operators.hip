@@ -20,9 +20,13 @@ size_t aligned256(size_t n) { return (n + 255) / 256 * 256; }
 
 sscn_status of_hip(hipError_t e) { return e == hipSuccess ? SSCN_OK : SSCN_ERR_HIP; }
 
-// rows x cols elements with `stride` elements between rows, addressable in 63 bits of bytes
+// Elements from an array's first to its last, at most: their bytes fit 63 bits.
+constexpr int64_t MAX_SPAN = (int64_t)1 << 60;
+
+// rows x cols elements with `stride` elements between rows (both below 2^32: no overflow here)
 bool rows_ok(int64_t rows, int64_t cols, int64_t stride) {
-  return rows >= 0 && rows <= SSCN_MAX_ROWS && stride >= cols && stride <= ((int64_t)1 << 31);
+  return rows >= 0 && rows <= SSCN_MAX_ROWS && stride >= cols && stride <= ((int64_t)1 << 31) &&
+         (rows <= 1 || (rows - 1) * stride + cols <= MAX_SPAN);
 }
 
 bool norm_ok(int32_t dtype, int64_t rows, int32_t cols, float eps) {
@@ -251,7 +255,8 @@ sscn_status sscn_muon_workspace_bytes(int32_t n, const sscn_muon_param* h_params
         if (!shape_ok(p.rows, p.cols)) return SSCN_ERR_INVALID_ARGUMENT;
         shape[k][0] = p.rows;
         shape[k++][1] = p.cols;
-      } else if (p.rows < 1 || p.cols < 1 || p.rows > SSCN_MAX_ROWS || p.cols > SSCN_MAX_ROWS) {
+      } else if (p.rows < 1 || p.cols < 1 || p.rows > SSCN_MAX_ROWS || p.cols > SSCN_MAX_ROWS ||
+                 p.rows * p.cols > MAX_SPAN) {
         return SSCN_ERR_INVALID_ARGUMENT;
       }
     }

@@ -209,3 +209,13 @@ def test_an_extremum_inside_the_range_is_found_for_any_coefficients(rows):
     most, inner = _dense([list(coef)[3 * k: 3 * k + 3] for k in range(len(rows))])
     want = WORKSPACE if most <= 3.5 and inner <= 200 else INVALID
     assert _ortho(_mats((5, 7)), steps=len(rows), coef=coef, ws=None) == want
+
+
+def test_arrays_past_the_address_space_are_refused():
+    """2^31 rows 2^31 elements apart: byte offsets would pass 63 bits."""
+    top, far = (1 << 31) - 1, 1 << 31
+    assert _fwd(rows=top, xs=far) == INVALID and _fwd(rows=top, ys=far) == INVALID
+    for kw in (dict(ds=far), dict(xs=far), dict(os=far)):
+        assert _bwd(rows=top, nb=0, **kw) == INVALID, kw  # (fewer bytes than any workspace: nothing is launched)
+        assert _bwd(rows=1 << 28, nb=0, **kw) == WORKSPACE, kw  # 2^61 bytes
+    assert _update(_param(top, top, 0)) == INVALID
