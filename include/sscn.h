@@ -345,8 +345,9 @@ typedef struct {
  *   w = w - lr (scale orthogonalise(u) + weight_decay w)
  * with sscn_orthogonalize's steps and coefficients; elsewhere (biases, gains)
  * sscn_sgd_step's rule: v = momentum v + (g + weight_decay w), w = w - lr v.
- * No array may be named twice.  lr, weight_decay and momentum must be finite and
- * >= 0, scale finite.  Without an orthogonal array, steps and h_coef are ignored
+ * No array that is written (masters, velocities, copies, the workspace) may
+ * overlap another one, else SSCN_ERR_INVALID_ARGUMENT; gradients may be shared.
+ * lr, weight_decay and momentum must be finite and >= 0, scale finite.  Without an orthogonal array, steps and h_coef are ignored
  * and no workspace is needed. */
 SSCN_API sscn_status sscn_muon_workspace_bytes(int32_t n, const sscn_muon_param* h_params, size_t* bytes);
 SSCN_API sscn_status sscn_muon_update(int32_t dtype, int32_t n, const sscn_muon_param* h_params, float momentum,

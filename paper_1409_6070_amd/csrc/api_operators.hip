@@ -5,10 +5,13 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <memory>
+#include <new>
 
 #include "sscn.h"
 #include "common.h"
 #include "kernels.h"
+#include "spans.h"
 
 using namespace sscn;
 
@@ -150,6 +153,21 @@ bool bad_workspace(const void* ws, size_t have, size_t need) {
   return need > 0 && (!ws || have < need || (uintptr_t)ws % 256 != 0);
 }
 
+// Refuses arrays of which one that is written overlaps another: fill(list) sets at most
+// `most` of them and returns how many.
+template <class Fill>
+sscn_status apart(int64_t most, Fill&& fill) {
+  Span few[64];
+  std::unique_ptr<Span[]> many;
+  Span* list = few;
+  if (most > 64) {
+    many.reset(new (std::nothrow) Span[most]);
+    if (!many) return SSCN_ERR_INVALID_ARGUMENT;
+    list = many.get();
+  }
+  return outputs_overlap(list, fill(list)) ? SSCN_ERR_INVALID_ARGUMENT : SSCN_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -284,6 +302,21 @@ sscn_status sscn_muon_update(int32_t dtype, int32_t n, const sscn_muon_param* h_
   NsStep step[SSCN_ORTHO_MAX_STEPS];
   if (any && !follow_steps(steps, h_coef, step)) return SSCN_ERR_INVALID_ARGUMENT;
   if (bad_workspace(d_workspace, workspace_bytes, need)) return SSCN_ERR_WORKSPACE;
+  const sscn_status overlap = apart((int64_t)n * 4 + 1, [&](Span* list) {
+    int64_t k = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      const sscn_muon_param& p = h_params[i];
+      const int64_t bytes = p.rows * p.cols * 4;
+      list[k++] = span(p.d_w, 1, bytes, 0, true);
+      list[k++] = span(p.d_v, 1, bytes, 0, true);
+      list[k++] = span(p.d_g, 1, bytes, 0, false);
+      if (p.d_w_store && p.d_w_store != (void*)p.d_w)
+        list[k++] = span(p.d_w_store, 1, dtype == SSCN_BF16 ? bytes / 2 : bytes, 0, true);
+    }
+    if (need) list[k++] = span(d_workspace, 1, (int64_t)need, 0, true);
+    return k;
+  });
+  if (overlap != SSCN_OK) return overlap;
   hipStream_t st = (hipStream_t)stream;
   SgdArgs sgd;
   std::memset((void*)&sgd, 0, sizeof(sgd));

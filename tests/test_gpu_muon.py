@@ -660,3 +660,23 @@ def test_values_that_reach_the_ends_of_the_planes(rows, shape):
     want[shape[0] // 2, shape[1] // 3] = -s
     log(f"[orthogonalize] {shape} {rows}: {got.min().item():.9g}, {-s:.9g} within {rel:.2g}")
     assert (got - want).abs().max() <= rel * abs(s)
+
+
+def test_update_refuses_overlapping_arrays_and_shares_gradients():
+    from paper_1409_6070_amd.sscn import Muon, SSCNError
+    m = Muon([(8, 16), (8, 16), (16,)], "f32")
+    mat = lambda: torch.randn(8, 16, device="cuda")  # noqa: E731
+    W, G, V, C = [mat(), mat(), mat()[0]], [mat(), mat(), mat()[0]], [mat(), mat(), mat()[0]], [mat(), mat(), mat()[0]]
+    keep = [t.clone() for t in W + V + C]
+    pair = torch.randn(12, 16, device="cuda")
+    for w, c, g, v in ((W, C, G, [V[0], V[0], V[2]]), (W, [C[0], C[0], C[2]], G, V), (W, C, [V[1], G[1], G[2]], V),
+                       (W, C, G, [pair[:8], pair[4:], V[2]]), (W, [C[0], W[0], C[2]], G, V), (W, C, G, [V[0], V[1], C[0][3]])):
+        with pytest.raises(SSCNError) as e:
+            m.step(w, c, g, v, lr=0.1)
+        assert e.value.name == "SSCN_ERR_INVALID_ARGUMENT"
+    assert all(torch.equal(a, b) for a, b in zip(W + V + C, keep))
+    w0, v0 = [w.clone() for w in W], [v.clone() for v in V]
+    m.step(W, C, [G[0], G[0], G[0][5]], V, lr=0.1)  # one gradient for all
+    m.step(w0, [w0[0], None, w0[2]], [G[0].clone(), G[0].clone(), G[0][5].clone()], v0, lr=0.1)  # the master as its own copy
+    for a, b, c, p, q in zip(W, w0, C, V, v0):
+        assert torch.equal(a, b) and torch.equal(c, a) and torch.equal(p, q)

@@ -157,3 +157,60 @@ def test_chunks_are_as_short_as_the_passes_own_tiles_allow(tmp_path):
         quarter, half, div, got = map(int, line.split())
         want = 4 if quarter <= 512 and div == 4 else 2 if half <= 700 and div >= 2 else 1  # parts of the standard length
         assert div // got == want and div % got == 0, line
+
+
+SPANS = r"""
+#include "spans.h"
+#include <cstdio>
+#include <random>
+#include <vector>
+using namespace sscn;
+static bool covers(const Span& s, int64_t x) {
+  for (int64_t r = 0; r < s.rows; ++r)
+    if (x >= (int64_t)s.at + r * s.step && x < (int64_t)s.at + r * s.step + s.len) return true;
+  return false;
+}
+int main() {
+  std::mt19937_64 rng(1);
+  long n = 0, hit = 0, same = 0;
+  for (int t = 0; t < 400000; ++t) {
+    const int64_t step = 1 + rng() % 12;
+    const auto make = [&](int64_t st) {
+      const int64_t rows = 1 + rng() % 5, len = 1 + rng() % (rows > 1 ? st : 30);
+      return span((const void*)(uintptr_t)(100 + rng() % 60), rows, len, st, rng() % 2, (int)(rng() % 3) - 1);
+    };
+    const Span a = make(step), b = make(rng() % 4 ? step : 1 + rng() % 12);
+    bool want = false;
+    for (int64_t x = 0; x < 300 && !want; ++x) want = covers(a, x) && covers(b, x);
+    if (a.rows > 1 && b.rows > 1 && a.step != b.step)  // ranges decide
+      want = a.at < span_end(b) && b.at < span_end(a);
+    if (spans_meet(a, b) != want || spans_meet(b, a) != want) { printf("meet %d\n", t); return 1; }
+    const bool place = a.in_place >= 0 && a.in_place == b.in_place && a.at == b.at && a.rows == b.rows &&
+                       a.len == b.len && a.step == b.step;
+    Span two[2] = {a, b};
+    if (outputs_overlap(two, 2) != (want && (a.out || b.out) && !place)) { printf("pair %d\n", t); return 1; }
+    hit += want, same += place, ++n;
+  }
+  for (int t = 0; t < 20000; ++t) {  // lists against all their pairs
+    const int k = rng() % 7;
+    std::vector<Span> s;
+    for (int i = 0; i < k; ++i) s.push_back(span((const void*)(uintptr_t)(rng() % 200), 1 + rng() % 3, 4, 9, rng() % 2));
+    bool want = false;
+    for (int i = 0; i < k; ++i)
+      for (int j = 0; j < i; ++j) want = want || ((s[i].out || s[j].out) && spans_meet(s[i], s[j]));
+    if (outputs_overlap(s.data(), k) != want) { printf("list %d\n", t); return 1; }
+  }
+  // far apart: rows 2^33 bytes long, bases past 63 bits
+  const Span far = span((const void*)(uintptr_t)0xF000000000000000ull, 1 << 20, 100, (int64_t)1 << 33, true);
+  const Span between = span((const void*)(uintptr_t)(0xF000000000000000ull + 100), 1 << 20, 100, (int64_t)1 << 33, true);
+  const Span into = span((const void*)(uintptr_t)(0xF000000000000000ull + ((uint64_t)5 << 33) + 99), 1, 1, 0, true);
+  if (spans_meet(far, between) || !spans_meet(far, into) || spans_meet(between, into)) { printf("far\n"); return 1; }
+  printf("%ld %d %d\n", n, (int)(hit > 10000), (int)(same > 20));
+  return 0;
+}
+"""
+
+
+def test_overlapping_arrays_are_found_row_by_row(tmp_path):
+    """Arrays of rows with gaps against all their bytes: the columns of one buffer side by side do not overlap."""
+    assert run_host(tmp_path, SPANS).split() == ["400000", "1", "1"]

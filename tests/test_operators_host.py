@@ -219,3 +219,36 @@ def test_arrays_past_the_address_space_are_refused():
         assert _bwd(rows=top, nb=0, **kw) == INVALID, kw  # (fewer bytes than any workspace: nothing is launched)
         assert _bwd(rows=1 << 28, nb=0, **kw) == WORKSPACE, kw  # 2^61 bytes
     assert _update(_param(top, top, 0)) == INVALID
+
+
+def _apart(n, rows=6, cols=4):
+    """n parameters whose masters, gradients and velocities are all apart (addresses that nothing reads)."""
+    at = iter(range(FAKE, FAKE + 4096 * 4 * n, 4096))
+    return [_param(rows, cols, i % 2, next(at), next(at), next(at)) for i in range(n)]
+
+
+@pytest.mark.parametrize("n", [2, 3, 40])
+def test_muon_update_refuses_arrays_that_overlap(n):
+    """One velocity or copy for two parameters, a gradient that is also a velocity, ...: two sets of workgroups would
+    write, or read and write, the same memory.  (Refused before anything is launched.)"""
+    ws = FAKE + (1 << 24)
+    size = 6 * 4 * 4
+    for i, j in ((0, 1), (0, n - 1), (n - 1, 0)):
+        for x in ("d_w", "d_v", "d_w_store"):
+            for y in ("d_w", "d_v", "d_g", "d_w_store"):
+                for off in (0, size - 4, 4 - size):  # the same array, its last and first element
+                    p = _apart(n)
+                    for q in p:
+                        q.d_w_store = q.d_w + 2048
+                    setattr(p[i], x, getattr(p[j], y) + off)
+                    assert _update(*p, ws=ws) == INVALID, (i, j, x, y, off)
+    for x, y in (("d_w", "d_v"), ("d_w", "d_g"), ("d_v", "d_g"), ("d_w_store", "d_v"), ("d_w_store", "d_g")):
+        p = _apart(n)
+        setattr(p[0], x, getattr(p[0], y))
+        assert _update(*p, ws=ws) == INVALID, (x, y)
+    p = _apart(n)
+    p[0].d_w_store = p[0].d_w + 4  # not the master itself, which means no copy
+    assert _update(*p, ws=ws) == INVALID
+    for name in ("d_w", "d_g", "d_v"):
+        p = _apart(n)
+        assert _update(*p, ws=(getattr(p[0], name) - 512) // 256 * 256) == INVALID  # in the workspace
