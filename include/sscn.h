@@ -297,7 +297,10 @@ SSCN_API sscn_status sscn_layer_norm_backward(int32_t dtype, const void* d_dy, i
                                               void* stream);
 
 /* One matrix for sscn_orthogonalize; in and out may be the same array (same
- * stride); an output may not overlap anything else that the call names. */
+ * stride).  An output that overlaps anything else that the call names, the
+ * workspace among it, is SSCN_ERR_INVALID_ARGUMENT: decided element by element
+ * where two arrays have one stride (columns of one buffer may lie side by side),
+ * by their ranges where the strides differ.  Inputs may overlap. */
 typedef struct {
   int64_t rows, cols;
   const void* d_in;

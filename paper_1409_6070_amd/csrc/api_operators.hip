@@ -248,6 +248,18 @@ sscn_status sscn_orthogonalize(int32_t dtype, int32_t n, const sscn_ortho_matrix
       return SSCN_ERR_INVALID_ARGUMENT;
   }
   if (bad_workspace(d_workspace, workspace_bytes, need)) return SSCN_ERR_WORKSPACE;
+  const sscn_status overlap = apart((int64_t)n * 2 + 1, [&](Span* list) {
+    const int64_t e = dtype == SSCN_BF16 ? 2 : 4;
+    int64_t k = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      const sscn_ortho_matrix& m = h_matrices[i];
+      list[k++] = span(m.d_in, m.rows, m.cols * e, m.in_stride * e, false, i);
+      list[k++] = span(m.d_out, m.rows, m.cols * e, m.out_stride * e, true, i);
+    }
+    if (need) list[k++] = span(d_workspace, 1, (int64_t)need, 0, true);
+    return k;
+  });
+  if (overlap != SSCN_OK) return overlap;
   NsGroup g{};
   return of_hip(run_groups(
       n, [&](int32_t i) { return std::make_pair(h_matrices[i].rows, h_matrices[i].cols); },

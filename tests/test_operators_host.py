@@ -252,3 +252,26 @@ def test_muon_update_refuses_arrays_that_overlap(n):
     for name in ("d_w", "d_g", "d_v"):
         p = _apart(n)
         assert _update(*p, ws=(getattr(p[0], name) - 512) // 256 * 256) == INVALID  # in the workspace
+
+
+def test_orthogonalize_refuses_outputs_that_overlap():
+    """Views of one buffer whose rows share elements."""
+    def call(*mats, ws=FAKE + (1 << 24), nb=1 << 40, dtype=0):
+        arr = (sscn.OrthoMatrix * len(mats))(*[sscn.OrthoMatrix(r, c, i, si, o, so) for r, c, i, si, o, so in mats])
+        return _ortho(arr, ws=ws, nb=nb, dtype=dtype)
+
+    A, B, C, D = (FAKE + 65536 * k for k in range(4))
+    for dtype, e in ((0, 4), (1, 2)):
+        one = lambda i, o, si=16, so=16: (8, 16, i, si, o, so)  # noqa: E731
+        for bad in ([one(A, C), one(B, C)],                       # an output twice
+                    [one(A, C), one(B, C + 7 * 16 * e + 15 * e)],  # its last element
+                    [one(A, B), one(B, A)], [one(A, C), one(C, D)],  # another's input
+                    [one(A, A), one(A, B)],                       # in place, and read by another
+                    [one(A, A + 4 * 16 * e)],                     # its own input, rows further on
+                    [one(A, A, 16, 20)], [one(A, A, 20, 16)],     # its own input in other strides
+                    [one(A, C, 40, 40), one(B, C + 15 * e, 40, 40)],  # columns that share one
+                    [one(A, C, 40, 40), one(B, C + 30 * e, 40, 40)],  # that wrap into the next row
+                    [one(A, C), (1, 5, B, 5, C + 100 * e, 5)]):
+            assert call(*bad, dtype=dtype) == INVALID, bad
+        ws = FAKE + (1 << 24)
+        assert call(one(A, ws), dtype=dtype) == INVALID and call(one(ws + 256, A), dtype=dtype) == INVALID
