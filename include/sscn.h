@@ -257,7 +257,11 @@ SSCN_API sscn_status sscn_sgd_step(sscn_net* net, float* const* h_W32, void* con
  * 256-byte aligned.  dtype is an sscn_dtype.  Row r of an array with stride s
  * starts s elements behind row r - 1 (s >= cols); elements between a row's end
  * and the next row are neither read nor written.  Arrays must be aligned to
- * their element type only. */
+ * their element type only.  An array that a call writes (a workspace too) may be
+ * another one of the call only where that is said, with the same stride; one that
+ * overlaps another is SSCN_ERR_INVALID_ARGUMENT.  That goes by elements where two
+ * arrays have one stride (columns of one buffer may lie side by side), by their
+ * ranges where the strides differ.  Arrays that are only read may overlap. */
 
 /* Limits: rows of an array (whose last element lies at most 2^60 elements behind
  * its first, with strides up to 2^31); columns of a layer norm; shorter and longer
@@ -274,7 +278,7 @@ SSCN_API sscn_status sscn_sgd_step(sscn_net* net, float* const* h_W32, void* con
  *   mean = sum x / cols,  r = 1 / sqrt(sum (x - mean)^2 / cols + eps),
  *   y = (x - mean) r gain + shift.
  * x and y have type dtype, the arithmetic is float32; d_gain and d_shift are
- * [cols] float32, each null for 1 and 0.  y may be x (same stride).  eps must be
+ * [cols] float32, each null for 1 and 0.  y may be x.  eps must be
  * finite and > 0.  rows = 0 does nothing.  A row with a NaN or an infinity comes
  * out as NaN and leaves the others alone. */
 SSCN_API sscn_status sscn_layer_norm_forward(int32_t dtype, const void* d_x, int64_t x_stride, int64_t rows,
@@ -286,7 +290,7 @@ SSCN_API sscn_status sscn_layer_norm_forward(int32_t dtype, const void* d_x, int
  *   dx = r (t - sum t / cols - h sum(t h) / cols)   (type dtype),
  *   dgain = sum over rows of dy h,  dshift = sum over rows of dy   ([cols] float32).
  * dgain and dshift are overwritten, each may be null; their sums are taken in an
- * order that the shape alone decides.  dx may be dy or x (same stride).  With
+ * order that the shape alone decides.  dx may be dy or x.  With
  * rows = 0 they are zero.  The workspace (needed when dgain or dshift is wanted
  * and rows > 0) has sscn_layer_norm_workspace_bytes, which grows with rows. */
 SSCN_API sscn_status sscn_layer_norm_workspace_bytes(int32_t dtype, int64_t rows, int32_t cols, size_t* bytes);
@@ -296,11 +300,7 @@ SSCN_API sscn_status sscn_layer_norm_backward(int32_t dtype, const void* d_dy, i
                                               float* d_dshift, void* d_workspace, size_t workspace_bytes,
                                               void* stream);
 
-/* One matrix for sscn_orthogonalize; in and out may be the same array (same
- * stride).  An output that overlaps anything else that the call names, the
- * workspace among it, is SSCN_ERR_INVALID_ARGUMENT: decided element by element
- * where two arrays have one stride (columns of one buffer may lie side by side),
- * by their ranges where the strides differ.  Inputs may overlap. */
+/* One matrix for sscn_orthogonalize; its in and out may be the same array. */
 typedef struct {
   int64_t rows, cols;
   const void* d_in;
@@ -348,9 +348,9 @@ typedef struct {
  *   w = w - lr (scale orthogonalise(u) + weight_decay w)
  * with sscn_orthogonalize's steps and coefficients; elsewhere (biases, gains)
  * sscn_sgd_step's rule: v = momentum v + (g + weight_decay w), w = w - lr v.
- * No array that is written (masters, velocities, copies, the workspace) may
- * overlap another one, else SSCN_ERR_INVALID_ARGUMENT; gradients may be shared.
- * lr, weight_decay and momentum must be finite and >= 0, scale finite.  Without an orthogonal array, steps and h_coef are ignored
+ * Masters, velocities and copies (other than a master as its own) may not overlap
+ * anything; gradients may be shared.  lr, weight_decay and momentum must be finite
+ * and >= 0, scale finite.  Without an orthogonal array, steps and h_coef are ignored
  * and no workspace is needed. */
 SSCN_API sscn_status sscn_muon_workspace_bytes(int32_t n, const sscn_muon_param* h_params, size_t* bytes);
 SSCN_API sscn_status sscn_muon_update(int32_t dtype, int32_t n, const sscn_muon_param* h_params, float momentum,
@@ -358,7 +358,8 @@ SSCN_API sscn_status sscn_muon_update(int32_t dtype, int32_t n, const sscn_muon_
                                       size_t workspace_bytes, void* stream);
 
 /* sscn_muon_update on a net's parameters, in the place of sscn_sgd_step: the same
- * arrays, from the gradients of the last sscn_backward, with the same errors.
+ * arrays, from the gradients of the last sscn_backward, with the same errors and
+ * sscn_muon_update's.
  * Convolutions (and with softmax != 0 the softmax layer's matrix) take the
  * orthogonal update with lr, weight_decay and scale = sqrt(max(1, cols / rows));
  * the other arrays the SGD rule with lr_rest (weight_decay on the softmax

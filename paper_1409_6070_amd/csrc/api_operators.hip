@@ -179,6 +179,16 @@ sscn_status sscn_layer_norm_forward(int32_t dtype, const void* d_x, int64_t x_st
     return SSCN_ERR_INVALID_ARGUMENT;
   if (rows == 0) return SSCN_OK;
   if (!d_x || !d_y) return SSCN_ERR_INVALID_ARGUMENT;
+  const int64_t e = dtype == SSCN_BF16 ? 2 : 4;
+  const sscn_status overlap = apart(4, [&](Span* list) {
+    int64_t k = 0;
+    list[k++] = span(d_x, rows, cols * e, x_stride * e, false, 0);
+    list[k++] = span(d_y, rows, cols * e, y_stride * e, true, 0);
+    if (d_gain) list[k++] = span(d_gain, 1, cols * 4, 0, false);
+    if (d_shift) list[k++] = span(d_shift, 1, cols * 4, 0, false);
+    return k;
+  });
+  if (overlap != SSCN_OK) return overlap;
   NormArgs a{};
   a.x = d_x;
   a.x_stride = x_stride;
@@ -211,6 +221,21 @@ sscn_status sscn_layer_norm_backward(int32_t dtype, const void* d_dy, int64_t dy
   size_t need = 0;
   if (params && rows > 0) sscn_layer_norm_workspace_bytes(dtype, rows, cols, &need);
   if (bad_workspace(d_workspace, workspace_bytes, need)) return SSCN_ERR_WORKSPACE;
+  const int64_t e = dtype == SSCN_BF16 ? 2 : 4;
+  const sscn_status overlap = apart(7, [&](Span* list) {
+    int64_t k = 0;
+    if (rows > 0) {
+      list[k++] = span(d_dy, rows, cols * e, dy_stride * e, false, 0);
+      list[k++] = span(d_x, rows, cols * e, x_stride * e, false, 0);
+      list[k++] = span(d_dx, rows, cols * e, dx_stride * e, true, 0);
+    }
+    if (d_gain) list[k++] = span(d_gain, 1, cols * 4, 0, false);
+    if (d_dgain) list[k++] = span(d_dgain, 1, cols * 4, 0, true);
+    if (d_dshift) list[k++] = span(d_dshift, 1, cols * 4, 0, true);
+    if (need) list[k++] = span(d_workspace, 1, (int64_t)need, 0, true);
+    return k;
+  });
+  if (overlap != SSCN_OK) return overlap;
   NormBwdArgs a{};
   a.dy = d_dy;
   a.dy_stride = dy_stride;

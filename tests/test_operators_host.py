@@ -275,3 +275,25 @@ def test_orthogonalize_refuses_outputs_that_overlap():
             assert call(*bad, dtype=dtype) == INVALID, bad
         ws = FAKE + (1 << 24)
         assert call(one(A, ws), dtype=dtype) == INVALID and call(one(ws + 256, A), dtype=dtype) == INVALID
+
+
+def test_norm_refuses_outputs_that_overlap():
+    """Other than x's (dy's) own array with the same stride; gain, shift, the parameters' gradients and the workspace."""
+    lib = sscn.load_library()
+    A, B, C, D, G, S = (FAKE + 65536 * k for k in range(6))
+    for dtype, e in ((0, 4), (1, 2)):
+        def fwd(x=A, xs=16, y=B, ys=16, gain=G, shift=S):
+            return lib.sscn_layer_norm_forward(dtype, x, xs, 8, 16, gain, shift, 1e-5, y, ys, None)
+        for bad in (dict(y=A, ys=20), dict(y=A, xs=20), dict(y=A + e), dict(y=A + 16 * e), dict(y=A - 7 * 16 * e),
+                    dict(y=A + 15 * e, xs=40, ys=40), dict(y=A + 30 * e, xs=40, ys=40), dict(y=G), dict(y=S), dict(y=G + 60),
+                    dict(y=S - 7 * 16 * e)):
+            assert fwd(**bad) == INVALID, bad
+        need = sscn.sscn_layer_norm_workspace_bytes(dtype, 8, 16)
+        W = FAKE + (1 << 20)
+
+        def bwd(dy=A, ds=16, x=B, xs=16, dx=C, os=16, gain=G, dg=D, dh=D + 64, ws=W):
+            return lib.sscn_layer_norm_backward(dtype, dy, ds, x, xs, 8, 16, gain, 1e-5, dx, os, dg, dh, ws, need, None)
+        for bad in (dict(dx=A, os=20), dict(dx=B, os=20), dict(dx=A, ds=20), dict(dx=A + e), dict(dx=B - e), dict(dx=G),
+                    dict(dx=D), dict(dx=W), dict(dh=D), dict(dh=D + 60), dict(dg=G), dict(dg=A), dict(dg=B), dict(dh=W + need - 4),
+                    dict(ws=A), dict(ws=C), dict(ws=G), dict(gain=W), dict(gain=C + 8)):
+            assert bwd(**bad) == INVALID, bad
