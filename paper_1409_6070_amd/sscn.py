@@ -656,7 +656,8 @@ class StrokeEncoder:
 
 class LayerNorm:
     """Layer norm of feature rows [rows, cols] over their columns, through sscn_layer_norm_*; holds the backward
-    pass's workspace for up to rows_max rows. One stream at a time, and kept until its calls have run."""
+    pass's workspace for up to rows_max rows, from the first backward pass on. One stream at a time, and kept until
+    its calls have run."""
 
     def __init__(self, cols: int, rows_max: int, dtype: str = "bf16", eps: float = 1e-5, device: str = "cuda"):
         if dtype not in _TYPES:
@@ -665,8 +666,7 @@ class LayerNorm:
         self.code, self.tdtype = _TYPES[dtype]
         self.ws_bytes = sscn_layer_norm_workspace_bytes(self.code, rows_max, cols)
         self.device = _gpu_device(device)
-        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
-        self.ws_ptr = self.ws.data_ptr()
+        self.ws = self.ws_ptr = None
 
     # (messages are made only where they are raised: the calls below are a few microseconds long)
     def _rows(self, t: torch.Tensor, what: str):
@@ -714,6 +714,9 @@ class LayerNorm:
             n, os = self._rows(dx, "dx")
             _need(n == rows, "dx: as many rows as x")
         g = self._param(gain, "gain")
+        if self.ws is None:
+            self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
+            self.ws_ptr = self.ws.data_ptr()
         dgain, dshift = torch.empty((2, self.cols), dtype=torch.float32, device=self.device).unbind(0)
         _launch(self.device, self._backward, dy.data_ptr(), ds, x.data_ptr(), xs, rows, g, dx.data_ptr(), os,
                 dgain.data_ptr(), dshift.data_ptr())

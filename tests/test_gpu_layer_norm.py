@@ -578,3 +578,56 @@ def test_outputs_side_by_side_and_overlapping(cols, dtype):
         both = ln.backward(x, x, gain)
         again = ln.backward(side[0], side[0], gain, dx=side[0])
         assert all(torch.equal(a, b) for a, b in zip(both, again))
+
+
+def test_a_forward_only_norm_holds_no_workspace():
+    """The backward pass's workspace (up to 256 MiB) comes with the first backward pass, and stays."""
+    from paper_1409_6070_amd.sscn import LayerNorm
+    cols, rows = 100000, 500
+    torch.cuda.synchronize()
+    base = torch.cuda.memory_allocated()
+    ln = LayerNorm(cols, rows, "bf16")
+    x = torch.randn(2, cols, device="cuda", dtype=torch.bfloat16)
+    own = torch.cuda.memory_allocated()
+    ln.forward(x, out=x)
+    assert own - base <= 2 * cols * 2 + 4096 and torch.cuda.memory_allocated() == own
+    dx, dg, ds = ln.backward(x, x)
+    ptr = ln.ws.data_ptr()
+    assert torch.cuda.memory_allocated() - own >= ln.ws_bytes > 1 << 26
+    again = ln.backward(x, x)
+    assert ln.ws.data_ptr() == ptr and all(torch.equal(a, b) for a, b in zip((dx, dg, ds), again))
+
+
+def test_a_first_backward_inside_a_capture():
+    """The workspace that a captured pass brings with it serves the eager passes and graphs behind it."""
+    from paper_1409_6070_amd.sscn import LayerNorm
+    x, dy, gain, _ = _make(500, 300, "bf16", 0, 21)
+    want = LayerNorm(300, 500, "bf16", EPS).backward(dy, x, gain)
+    ln = LayerNorm(300, 500, "bf16", EPS)
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        dx = torch.empty_like(x)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got = ln.backward(dy, x, gain, dx=dx)
+        graphs.append((g, got))
+    for i in range(3):
+        for g, got in graphs:
+            for t in got:
+                t.zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+            assert all(torch.equal(a, b) for a, b in zip(ln.backward(dy, x, gain), want)), i
+    graphs.pop(0)  # its memory pool goes, the workspace stays
+    torch.cuda.empty_cache()
+    torch.empty(1 << 24, device="cuda").fill_(float("nan"))
+    for i in range(3):
+        g, got = graphs[0]
+        for t in got:
+            t.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+        assert all(torch.equal(a, b) for a, b in zip(ln.backward(dy, x, gain), want)), i
