@@ -535,6 +535,10 @@ class SparseDeepCNet:
                   coef=MUON_COEF, steps: int = 5) -> None:
         """Muon's update from the last backward's gradients, in the place of sgd_step: orthogonalised updates of
         the convolutions (and with softmax=True of the softmax layer's matrix), momentum SGD with lr_rest elsewhere."""
+        for what, ts in (("W32", W32), ("W", W), ("bs", bs), ("vW", vW), ("vb", vb)):
+            sizes = [r * c if "W" in what else c for r, c in self.param_shapes]
+            _need(what == "W" and ts is None or [t.numel() for t in ts if t.device.type == self.device.type] == sizes,
+                  f"{what}: one array of each parameter's size on {self.device.type}")
         for t in list(W32) + list(bs) + list(vW) + list(vb):
             assert t.dtype == torch.float32 and t.is_contiguous()
         if W is not None:

@@ -297,3 +297,18 @@ def test_norm_refuses_outputs_that_overlap():
                     dict(dx=D), dict(dx=W), dict(dh=D), dict(dh=D + 60), dict(dg=G), dict(dg=A), dict(dg=B), dict(dh=W + need - 4),
                     dict(ws=A), dict(ws=C), dict(ws=G), dict(gain=W), dict(gain=C + 8)):
             assert bwd(**bad) == INVALID, bad
+
+
+def test_muon_step_wrapper_wants_every_array():
+    """A list that is too short, or an array that is too small or lies elsewhere, would be read where nothing is."""
+    import torch
+    net = sscn.SparseDeepCNet(2, 3, 9, 4, 4, 100, "bf16", device="cpu")  # (buffers only: nothing runs)
+    W32 = [torch.zeros(s) for s in net.param_shapes]
+    W = [w.bfloat16() for w in W32]
+    b = [torch.zeros(s[1]) for s in net.param_shapes]
+    good = [W32, W, b, [w.clone() for w in W32], [v.clone() for v in b]]
+    for i in range(5):
+        for bad in (good[i][:-1], good[i] + good[i][:1], good[i][:-1] + [good[i][-1][:-1]], good[i][::-1],
+                    good[i][:-1] + [good[i][-1].to("meta")]):  # (of another device)
+            with pytest.raises(ValueError):
+                net.muon_step(*good[:i], bad, *good[i + 1:], 0.1, 0.1)
