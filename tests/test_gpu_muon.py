@@ -711,3 +711,61 @@ def test_orthogonalize_outputs_side_by_side_and_overlapping(dtype):
     assert all(torch.equal(a, b) for a, b in zip(side, want))
     a, b, _ = plan.orthogonalize([mats[0], mats[0], mats[2]])
     assert torch.equal(a, want[0]) and torch.equal(b, want[0])
+
+
+def _direction(w0, w, g, v, lr, momentum, wd, nesterov, scale):
+    """(distance of the update that the weights show from the formula's, its bound), both relative to the formula's
+    norm.  The bound: that of the steps on the formula's u; u as float32 holds it, which is off by at most three
+    roundings of its terms' sizes, taken through the steps in random directions; and the weights' own roundings (of w,
+    lr, wd and scale: eight of the terms' sizes)."""
+    lr, momentum, wd = (float(np.float32(x)) for x in (lr, momentum, wd))
+    w0, w, g, v = (t.double().cpu() for t in (w0, w, g, v))
+    vn = momentum * v + g
+    u = g + momentum * vn if nesterov else vn
+    terms = g.abs() + momentum * (momentum * v.abs() + g.abs()) if nesterov else momentum * v.abs() + g.abs()
+    want = ns(u, torch.float64)
+    _, rel = _bound(u.float(), "f32")
+    gen = torch.Generator().manual_seed(0)
+    for _ in range(3):
+        sign = 2 * torch.randint(0, 2, u.shape, generator=gen) - 1
+        rel = max(rel, _bound(u.float(), "f32")[1] + 3 * (ns(u + 3 * U * sign * terms, torch.float64) - want).norm().item()
+                  / want.norm().item())
+    got = (w0 * (1 - lr * wd) - w) / (lr * scale)
+    rel += 8 * U * (1 + (w0.norm() / (lr * scale * want.norm())).item())
+    return (got - want).norm().item() / want.norm().item(), rel
+
+
+@pytest.mark.parametrize("nesterov", [True, False])
+@pytest.mark.parametrize("shape", [(9, 50), (60, 90), (120, 33), (200, 100), (100, 300), (700, 650)], ids=str)
+def test_direction_of_the_update_with_a_velocity(shape, nesterov):
+    """The orthogonalised direction from a velocity that is not zero, tightly enough that another momentum, the other
+    rule for u or another scale would show."""
+    from paper_1409_6070_amd.sscn import Muon
+    W, G, V = _rand(*shape, 1) * 0.02, _rand(*shape, 2), 2 * _rand(*shape, 3)
+    w0, v0 = W.clone(), V.clone()
+    scale = float(np.float32(max(1.0, shape[1] / shape[0]) ** 0.5))
+    Muon([shape], "f32").step([W], None, [G], [V], lr=0.02, momentum=0.95, weight_decay=0.1, nesterov=nesterov)
+    off, tol = _direction(w0, W, G, v0, 0.02, 0.95, 0.1, nesterov, scale)
+    log(f"[muon] direction {shape} nesterov {nesterov}: off {off:.3g}, allowed {tol:.3g}")
+    assert off <= tol
+    for wrong in (dict(momentum=0.94), dict(nesterov=not nesterov), dict(scale=scale * 1.002), dict(lr=0.02005)):
+        args = dict(dict(lr=0.02, momentum=0.95, wd=0.1, nesterov=nesterov, scale=scale), **wrong)
+        off, tol = _direction(w0, W, G, v0, **args)
+        assert off > 4 * tol, (wrong, off, tol)  # (a mistake planted in the formula)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("nesterov", [True, False])
+def test_direction_of_a_networks_second_step(dtype, nesterov):
+    net, feats, W32, W, b, labels = _net(dtype)
+    vW, vb = [torch.zeros_like(w) for w in W32], [torch.zeros_like(v) for v in b]
+    for k in range(2):
+        net.forward(feats, W, b, labels)
+        dW, _, _ = net.backward()
+        keep = [[t.clone() for t in ts] for ts in (W32, dW, vW)]
+        net.muon_step(W32, W, b, vW, vb, 0.03, 0.01, 0.95, 0.05, nesterov=nesterov, softmax=True)
+    for i, w in enumerate(W32):
+        scale = float(np.float32(math.sqrt(max(1.0, w.shape[1] / w.shape[0]))))
+        off, tol = _direction(keep[0][i], w, keep[1][i], keep[2][i], 0.03, 0.95, 0.05, nesterov, scale)
+        log(f"[muon] network's matrix {i} {tuple(w.shape)} nesterov {nesterov}: off {off:.3g}, allowed {tol:.3g}")
+        assert off <= tol
