@@ -11,7 +11,7 @@
 // split into two fp16 numbers each, hi + lo, and multiplied on the fp16 matrix cores
 // as hi hi + hi lo + lo hi with float32 sums: three times the matrix work of a plain
 // fp16 product, which the fp16 cores still do at five times the rate of float32 MFMA
-// (4096 x 4096: 387 TFLOP/s of the formula's operations; a library's float32 product
+// (4096 x 4096: 383 TFLOP/s of the formula's operations; a library's float32 product
 // reaches 154).  An operand is scaled by the power of two that brings the largest value
 // it may hold near fp16's end (NsStep).  An entry is then off by 2^-22 of itself or,
 // where its lo part falls below fp16's smallest step, by 2^-39 of that largest value.
@@ -123,16 +123,22 @@ __device__ inline int find_mat(const NsArgs& a, int t) {
 }
 
 // The kernels of a product, by its 128 x 128 tiles, their slabs of 32 k per compute unit
-// and its 64 x 64 tiles (plan_product).  Measured, us, 128 / 64 / 32 tiles:
+// and its 64 x 64 tiles, as plan_product counts them.  Measured, us, 128 / 64 / 32 tiles:
 //   X X^T  2100 x 3900 (73 slabs)  76 / 86 / -;  2048 x 2048 (34)  44 / 46 / -;  1800 x 1900 (28)
-//          41.7 / 31.5 / -;  DeepCNet(6,100) with softmax (23, 312 tiles of 64)  39.7 / 35.5 / 35.6;
-//          1500 x 1500 (14, 300)  31.7 / 21.0 / 33.4;  1300 x 1300 (231)  27.1 / 14.0 / 23.4;
-//          1100 x 1100 (171)  - / 12.0 / 14.2;  1000 x 600 three times (165)  24.8 / 14.0 / 12.5;
-//          DeepCNiN(5,50) with softmax (160)  27.3 / 23.0 / 14.7;  1000 x 300 (15)  17.0 / 10.0 / 6.3
+//          41.7 / 31.5 / -;  1500 x 1500 (14; 300 tiles of 64)  31.7 / 21.0 / 33.4;  1300 x 1300
+//          (231)  27.1 / 14.0 / 23.4;  1100 x 1100 (171)  - / 12.0 / 14.2;  1000 x 600 three times
+//          (165)  24.8 / 14.0 / 12.5;  1000 x 300 (15)  17.0 / 10.0 / 6.3
+//          lists with a softmax matrix (3755 columns, four times the others' sums):
+//          DeepCNet(6,100) (24; 277)  39.7 / 36.0 / 35.2;  DeepCNet(5,100) (200)  - / 26.4 / 27.5;
+//          DeepCNiN(6,55) (196)  - / 24.6 / 18.6;  DeepCNiN(5,65) (194)  - / 24.4 / 18.1;
+//          DeepCNet(5,90) (169)  - / 25.1 / 23.0;  DeepCNiN(5,50) (105)  27.3 / 23.2 / 14.8
 //   B X    1500 x 1500 (26 slabs)  36.5 / 42.5 / 63.9;  1300 x 1300 (19)  38.2 / 25.4 / 43.5;
 //          400 x 1600 four times (208 tiles of 128)  21.2 / 28.0 / 23.4;  700 x 3755 (180)  24.4 / 32.4 /
 //          38.9;  1000 x 600 three times (120; 480 of 64)  32.8 / 18.8 / 20.4;  2047 x 822 (112; 416)  34.4 /
-//          20.9 / 30.0;  1000 x 1000 (64; 256)  - / 14.0 / 19.4;  DeepCNet(5,50) (65; 216)  17.8 / 11.4 / 9.4
+//          20.9 / 30.0;  1000 x 1000 (64; 256)  - / 14.0 / 19.4;  DeepCNet(5,50) (59; 202)  17.8 / 11.4 / 9.4
+// NS_TILES_64 lies where matrices of like sums cross.  The rule does not see that some
+// sums are longer: lists like DeepCNiN(5,65)'s, whose 64 x 64 tiles wait for their longest
+// sums, are up to 6 us a product slower than in 32 x 32 tiles.
 constexpr int NS_CUS = 256, NS_SLABS = 30, NS_SLABS_APPLY = 20, NS_TILES_APPLY = 160, NS_TILES_64 = 170,
               NS_TILES_64_APPLY = 256, NS_FULL = 192;
 constexpr int NS_PARTS = 16;  // workgroups that share a tile, at most
@@ -294,7 +300,9 @@ struct NsWork {
   int pr, qr;         // row blocks of each inside the padded matrix (a last tile has fewer)
 
   // false: no tile for this workgroup.  Workgroup b runs on XCD b % 8: each XCD takes
-  // an eighth of every matrix's tiles, consecutive ones, whose operands its L2 shares.
+  // an eighth of every matrix's tiles, rounded up, consecutive ones, whose operands its
+  // L2 shares; the last XCDs take what is left (X X^T of eight 1024 x 1024: 40 tiles on
+  // seven of them, 8 on the last).
   __device__ inline bool find(const NsArgs& a) {
     const int xcd = blockIdx.x & 7, slot_of_xcd = blockIdx.x >> 3;
     const int j = find_mat(a, slot_of_xcd);
@@ -638,15 +646,15 @@ __device__ inline void stage_tile(float* Cs, const f32x4 (&acc)[FT][FT], int lan
 }
 
 // Large products: TM x TN tiles, a wave for each 64 x 64 of them, operands through a
-// ring of NST LDS slabs of 32 k.  Bound by the matrix cores: 4096 x 4096 takes 192 us
-// for X X^T, 199 for A A and 327 for B X, which is 1.14, 1.10 and 1.26 PFLOP/s of fp16
+// ring of NST LDS slabs of 32 k.  Bound by the matrix cores: 4096 x 4096 takes 191 us
+// for X X^T, 197 for A A and 329 for B X, which is 1.15, 1.11 and 1.25 PFLOP/s of fp16
 // products (a loop of nothing but such products on random numbers reaches 1.7 here,
 // its clock held down by power; a library's fp16 product of this size 1.1).  A slab of
 // a 256 x 128 tile takes 1800 cycles where its products take 1536, the rest of a
 // launch is the epilogue: every workgroup writes its results at the same time.
 // 128 x 128 tiles read 1.5 times as much from L2: for products whose last round of
 // larger ones would leave compute units idle, or that have few tiles (eight of
-// 1024 x 1024, X X^T: 288 tiles, two workgroups a compute unit, 47 us).
+// 1024 x 1024, X X^T: 288 tiles, two workgroups a compute unit, 48 us).
 template <int TM, int TN, int NST>
 struct NsTile {
   static constexpr int PB = TM / 16, QB = TN / 16, FT = 4;
@@ -768,8 +776,10 @@ __global__ void __launch_bounds__((NsTile<TM, TN, NST>::NW * 64), 2) k_ns_tiles(
 // epilogue reads beside them has arrived meanwhile.  No barrier before that: such a
 // product is bound by latencies, not by the matrix cores.  1000 x 300 takes 6.3 us for
 // X X^T, 4.7 for A A and 8.1 for B X, of which an empty launch is 2.4 and the operands'
-// way from another XCD's writes (through memory) 1.2.  With many tiles their operands'
-// way out of L2 bounds it: DeepCNet(6,100)'s matrices with softmax 35.5 us for X X^T.
+// way from another XCD's writes (through memory) 1.2.  The tiles with the longest sums
+// bound a list: DeepCNet(6,100)'s matrices with softmax take 36 us for X X^T, in which a
+// wave of the softmax matrix's tiles goes through 30 blocks of 64 x 64 with two in flight
+// (the matrix cores are busy 15% of the time, L2 gives about 14 bytes a cycle and compute unit).
 // The partial tiles that its waves stage in LDS: of 64 x 64, where something lies beside
 // them, the second half of the waves first, to which the first half then adds, so that two
 // workgroups fit a compute unit (B X of 1000 x 600 three times: 18.8 us, else 22.5).
@@ -1044,7 +1054,9 @@ __global__ void __launch_bounds__(512) k_ns_small(NsArgs a, NsTable t, NsCoef co
 enum NsPlan { NS_256, NS_128, NS_64, NS_32 };
 struct NsShape {
   int tm, tn;
-  int min_k;  // blocks of k that a part of a divided tile has at least; 0: tiles are not divided
+  // k is divided into runs of this many blocks or more, then evenly over their number, so
+  // that a part may have down to half as many; 0: tiles are not divided
+  int min_k;
 };
 constexpr NsShape NS_SHAPE[] = {{256, 128, 16}, {128, 128, 12}, {64, 64, 0}, {32, 32, 0}};
 
