@@ -631,3 +631,84 @@ def test_a_first_backward_inside_a_capture():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), i
         assert all(torch.equal(a, b) for a, b in zip(ln.backward(dy, x, gain), want)), i
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [5, 100, 3000, 40000])
+def test_parameter_gradients_that_are_not_wanted(cols, dtype):
+    """Each of dgain and dshift may be null; without both no workspace is needed. The others keep their bits."""
+    from paper_1409_6070_amd import sscn
+    rows = 70
+    x, dy, gain, _ = _make(rows, cols, dtype, 0, 15)
+    ln = sscn.LayerNorm(cols, rows, dtype, EPS)
+    want = ln.backward(dy, x, gain)
+    for wants in ((1, 0), (0, 1), (0, 0)):
+        dx = torch.zeros_like(x)
+        out = [torch.full((cols,), 7.5, device="cuda") for _ in range(2)]
+        sscn.sscn_layer_norm_backward(ln.code, dy.data_ptr(), cols, x.data_ptr(), cols, rows, cols, gain.data_ptr(), EPS,
+                                      dx.data_ptr(), cols, *[o.data_ptr() if w else None for o, w in zip(out, wants)],
+                                      ln.ws.data_ptr() if any(wants) else None, ln.ws_bytes if any(wants) else 0,
+                                      sscn._stream())
+        torch.cuda.synchronize()
+        assert torch.equal(dx, want[0])
+        for o, w, p in zip(out, wants, want[1:]):
+            assert torch.equal(o, p) if w else (o == 7.5).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("drop", [None, 0.4])
+def test_head_norm_of_a_network_in_network(dtype, drop):
+    """DeepCNiN: the leaky rectifier below the norm, several empty samples on one ground row. The norm's gradients and
+    the top layer's from the network's own top features, logits and weights."""
+    from paper_1409_6070_amd.sscn import SparseDeepCNet
+    from workloads import he_params, random_labels
+    rng = np.random.default_rng(5)
+    ell, k, c_in, classes, batch = 2, 11, 3, 12, 19
+    N, empty = 3 * 2 ** ell, (0, 4, 5, 18)
+    coords = np.concatenate([np.stack([np.full(6, b), *np.divmod(rng.choice(N * N, 6, replace=False), N)], 1)
+                             for b in range(batch) if b not in empty])
+    net = SparseDeepCNet(ell, k, c_in, classes, batch, len(coords), dtype, arch="deepcnin", dropout=drop is not None)
+    feats = torch.tensor(rng.normal(size=(len(coords), c_in))).to(net.tdtype).cuda()
+    Ws, bs = he_params(ell, k, c_in, classes, 1, arch="deepcnin")
+    Ws = [torch.tensor(w, dtype=torch.float32, device="cuda").to(net.tdtype) for w in Ws]
+    bs = [torch.tensor(v, dtype=torch.float32, device="cuda") + 0.05 for v in bs]
+    labels = torch.tensor(random_labels(batch, classes, 2), dtype=torch.int32, device="cuda")
+    if drop is not None:
+        net.set_dropout([0.0] * (ell + 1) + [drop], 91)
+    net.rulebook_build(torch.tensor(coords, dtype=torch.int32, device="cuda"), batch)
+    C = net.param_shapes[-1][0]
+    g = torch.Generator().manual_seed(3)
+    gain, shift = (1 + 0.3 * torch.randn(C, generator=g)).cuda(), (0.2 * torch.randn(C, generator=g)).cuda()
+    dgain, dshift = net.set_head_norm(gain, shift, EPS)
+    logits = _np(net.forward(feats, Ws, bs, labels)[0])
+    net.backward()
+    torch.cuda.synchronize()
+    view = net.layer_view(net.nlayers - 1)
+    rows = np.zeros(batch, dtype=int)
+    rows[_np(view["sites"]).astype(int)] = np.arange(1, view["n"] + 1)
+    assert set(np.flatnonzero(rows == 0)) == set(empty)
+    x, W = _np(view["features"])[rows, :C], _np(Ws[-1])
+    assert (x < 0).any() and (x > 0).any()
+    keep = np.ones((batch, C)) if drop is None else _keep(batch, C, ell + 1, drop, 91)
+    y, tol_y = _want_forward(x, _np(gain), _np(shift), dtype)
+    tol_y = tol_y * keep + (0 if drop is None else (HALF[dtype] + U) * np.abs(y * keep) * 1.01)
+    want = (y * keep) @ W + _np(bs[-1])
+    tol = tol_y @ np.abs(W) + (C + 4) * U * (np.abs(y * keep) @ np.abs(W) + np.abs(_np(bs[-1])))
+    assert (np.abs(logits - want) <= 1.01 * tol).all()
+    z = logits - logits.max(1, keepdims=True)
+    p = np.exp(z) / np.exp(z).sum(1, keepdims=True)
+    dl = p.copy()
+    dl[np.arange(batch), labels.cpu().numpy()] -= 1
+    dl /= batch
+    tol_dl = np.abs(dl) * HALF[dtype] + (40 + 2 * np.abs(z)) * U * p / batch + 4 * U / batch
+    dh, tol_dh = (dl @ W.T) * keep, (tol_dl @ np.abs(W.T) + (classes + 8) * U * (np.abs(dl) @ np.abs(W.T))) * keep
+    (dx, tol_dx), (dg, tol_dg), (ds, tol_ds) = _want_backward(dh, x, _np(gain), "f32", 1, 32)
+    _, r, h, _, _, _ = _stats(x)
+    t = tol_dh * np.abs(_np(gain))
+    tol_dx = tol_dx + r * (t + t.mean(1, keepdims=True) + np.abs(h) * (t * np.abs(h)).mean(1, keepdims=True))
+    _within(dgain, dg, 1.01 * (tol_dg + (tol_dh * np.abs(h)).sum(0)), "dgain")
+    _within(dshift, ds, 1.01 * (tol_ds + tol_dh.sum(0)), "dshift")
+    live = rows > 0
+    slope = np.where(x[live] >= 0, 1.0, 1.0 / 3.0)
+    got, want = _np(view["grad"])[rows[live], :C], dx[live] * slope
+    assert (np.abs(got - want) <= 1.01 * (tol_dx[live] * slope + (HALF[dtype] + 2 * U) * np.abs(want)) + 1e-38).all()

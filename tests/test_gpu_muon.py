@@ -769,3 +769,15 @@ def test_direction_of_a_networks_second_step(dtype, nesterov):
         off, tol = _direction(keep[0][i], w, keep[1][i], keep[2][i], 0.03, 0.95, 0.05, nesterov, scale)
         log(f"[muon] network's matrix {i} {tuple(w.shape)} nesterov {nesterov}: off {off:.3g}, allowed {tol:.3g}")
         assert off <= tol
+
+
+@pytest.mark.parametrize("shape", [(1, 1 << 20), (1 << 20, 1), (33, 1000003), (200000, 64)], ids=str)
+def test_longest_matrices(shape):
+    from paper_1409_6070_amd.sscn import Orthogonalizer
+    u = _rand(*shape, seed=9)
+    log(f"[orthogonalize] {shape}")
+    plan = Orthogonalizer([shape], "f32")
+    out = plan.orthogonalize([u])
+    _check(out, [u], "f32")
+    plan.ws.fill_(0xFF)
+    assert torch.equal(plan.orthogonalize([u])[0], out[0])
