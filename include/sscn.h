@@ -249,8 +249,9 @@ SSCN_API sscn_status sscn_sgd_step(sscn_net* net, float* const* h_W32, void* con
                                    float weight_decay, void* stream);
 
 /* ---------------------------------------------------------------------------
- * Operators on plain arrays, without a net: layer norm, orthogonalised
- * matrices, and the update that uses them.  The caller owns every buffer; the
+ * Operators on plain arrays, without a net: layer norm, group norm with an
+ * activation, rows held in 8 bits and their products, orthogonalised matrices,
+ * and the update that uses them.  The caller owns every buffer; the
  * calls are asynchronous on `stream`, keep nothing between calls and can be
  * captured into a graph.  A workspace is scratch during a call's kernels only:
  * it may serve any number of calls and graphs, one at a time.  It must be
@@ -299,6 +300,115 @@ SSCN_API sscn_status sscn_layer_norm_backward(int32_t dtype, const void* d_dy, i
                                               float eps, void* d_dx, int64_t dx_stride, float* d_dgain,
                                               float* d_dshift, void* d_workspace, size_t workspace_bytes,
                                               void* stream);
+
+/* Group norm with an activation over the rows of a sample and the channels of a
+ * group (rows are sites, channels last).  Group g holds channels g cols / groups ..
+ * (cols must be a multiple of groups), sample b rows d_begin[b] .. d_begin[b + 1] - 1:
+ * d_begin is a device array of batch + 1 int32, non-decreasing, within 0 .. rows, as
+ * sscn_rulebook_build_grouped takes it; null: `batch` samples of rows / batch rows each
+ * (rows must be a multiple of batch).  Rows before the first and behind the last
+ * sample are neither read nor written, and a sample may have no rows.  With n the
+ * values of a sample and group:
+ *   mean = sum x / n,  r = 1 / sqrt(sum (x - mean)^2 / n + eps),
+ *   h = (x - mean) r,  z = h gain + shift,  y = act(z).
+ * Offsets that decrease or lie outside 0 .. rows give undefined results within the
+ * call's arrays.  A NaN or an infinity makes its sample's group NaN and leaves the
+ * others alone. */
+typedef enum {
+  SSCN_ACT_NONE = 0,
+  SSCN_ACT_RELU = 1,  /* derivative 0 at 0                                 */
+  SSCN_ACT_LEAKY = 2, /* z / 3 below 0, derivative 1 at 0 (SSCN_DEEPCNIN's) */
+  SSCN_ACT_SILU = 3   /* z / (1 + exp(-z))                                 */
+} sscn_activation;
+#define SSCN_GROUP_NORM_MAX_COLS 4096
+typedef struct {
+  int32_t dtype;           /* of x, y, dy and dx; the arithmetic is float32            */
+  int32_t act;             /* sscn_activation                                          */
+  int64_t rows;
+  int32_t cols, groups, batch;
+  float eps;               /* finite, > 0; the forward pass's                          */
+  const int32_t* d_begin;
+  const float* d_gain;     /* [cols], null: 1                                          */
+  const float* d_shift;    /* [cols], null: 0                                          */
+  const void* d_x;         /* [rows][cols]; backward: null for 8-bit rows              */
+  int64_t x_stride;
+  const uint8_t* d_codes;  /* backward with d_x null: x held in 8 bits (sscn_rows8)    */
+  const uint8_t* d_scales;
+  float* d_stats;          /* [2][batch][groups]: means, then r.  Forward writes them
+                              (0 and 1 / sqrt(eps) for a sample without rows), backward
+                              reads them                                              */
+} sscn_group_norm;
+
+/* Forward and backward need workspaces of different size; both grow with rows and
+ * batch. */
+SSCN_API sscn_status sscn_group_norm_workspace_bytes(int32_t dtype, int64_t rows, int32_t cols, int32_t groups,
+                                                     int32_t batch, int32_t backward, size_t* bytes);
+
+/* Writes y (may be x) and d_stats. */
+SSCN_API sscn_status sscn_group_norm_forward(const sscn_group_norm* norm, void* d_y, int64_t y_stride,
+                                             void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* From dy, the forward's x (or what 8 bits hold of it) and its d_stats:
+ *   dz = dy act'(z),  t = dz gain,  dx = r (t - sum t / n - h sum(t h) / n),
+ *   dgain = sum over all samples' rows of dz h,  dshift = the same sum of dz  ([cols] float32,
+ * overwritten, each may be null).  z is computed as (x - mean) r, times gain, plus
+ * shift, each rounded to float32, so that forward and backward take the same branch of
+ * the activation where x is the same.  dx may be dy or x.  Sums are taken in an order that
+ * the arguments' sizes and d_begin alone decide. */
+SSCN_API sscn_status sscn_group_norm_backward(const sscn_group_norm* norm, const void* d_dy, int64_t dy_stride,
+                                              void* d_dx, int64_t dx_stride, float* d_dgain, float* d_dshift,
+                                              void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* Rows held in 8 bits: activations kept for the backward pass, and the operands of the
+ * products below.  For each row and block of 128 columns
+ *   e = the least integer >= -126 with max |x| <= 448 2^e over the block's finite values,
+ *   code = x 2^-e rounded to e4m3 (nearest, ties to even: relative 2^-4 at most, below
+ *   2^-6 2^e steps of 2^-9 2^e);  the value held is code 2^e.
+ * NaN and infinities are held as NaN.  (A value within 2^-4 of float32's largest may come
+ * back as an infinity.)  Codes lie in rows of sscn_rows8_strides' code_stride bytes
+ * (cols rounded up to 16), scale bytes e + 127 in rows of scale_stride (blocks rounded up
+ * to 4); what lies behind a row's columns and blocks is zero.  d_codes must be 16-byte
+ * and d_scales 4-byte aligned.  Runs of rows are 8-bit rows themselves. */
+#define SSCN_ROWS8_MAX_COLS 1048576
+typedef struct {
+  int64_t rows;
+  int32_t cols;
+  uint8_t* d_codes;
+  uint8_t* d_scales;
+} sscn_rows8;
+SSCN_API sscn_status sscn_rows8_strides(int32_t cols, int64_t* code_stride, int64_t* scale_stride);
+SSCN_API sscn_status sscn_rows8_store(int32_t dtype, const void* d_x, int64_t x_stride, const sscn_rows8* to,
+                                      void* stream);
+SSCN_API sscn_status sscn_rows8_load(int32_t dtype, const sscn_rows8* from, void* d_y, int64_t y_stride, void* stream);
+
+/* A matrix [k][n] (k, n <= SSCN_PRODUCT8_MAX) held in 8 bits in the same way, with one
+ * scale for each block of 128 x 128, in an array of sscn_weight8_bytes bytes (256-byte
+ * aligned) whose layout is the library's own.  d_w has type dtype. */
+#define SSCN_PRODUCT8_MAX 65536
+SSCN_API sscn_status sscn_weight8_bytes(int32_t k, int32_t n, size_t* bytes);
+SSCN_API sscn_status sscn_weight8_store(int32_t dtype, const void* d_w, int64_t w_stride, int32_t k, int32_t n,
+                                        void* d_weight8, size_t weight8_bytes, void* stream);
+
+/* Products of 8-bit rows with an 8-bit matrix (the 1x1 layers of Section 2.2 on rows
+ * held in 8 bits), xq, dyq and wq being the values that are held:
+ *   y = xq wq + bias        x: rows of k columns, y [rows][n], bias [n] float32 or null;
+ *   dx = dyq wq^T           dy: rows of n columns, dx [rows][k];
+ *   dw = xq^T dyq,  db = sum over rows of dyq        float32, overwritten, db may be null.
+ * y and dx have type dtype and are rounded once.  In float32 the products are exact and
+ * their sums float32; in bf16 the sums lose up to 1e-4 of the sum of the products'
+ * magnitudes besides (the matrix instructions' own precision).  dw and db do not depend on
+ * the device's scheduling.  With no rows dw and db are zero.  The weight gradient's
+ * workspace grows with rows. */
+SSCN_API sscn_status sscn_product8_forward(int32_t dtype, const sscn_rows8* x, const void* d_weight8,
+                                           size_t weight8_bytes, int32_t n, const float* d_bias, void* d_y,
+                                           int64_t y_stride, void* stream);
+SSCN_API sscn_status sscn_product8_input_grad(int32_t dtype, const sscn_rows8* dy, const void* d_weight8,
+                                              size_t weight8_bytes, int32_t k, void* d_dx, int64_t dx_stride,
+                                              void* stream);
+SSCN_API sscn_status sscn_product8_weight_grad_workspace_bytes(int64_t rows, int32_t k, int32_t n, size_t* bytes);
+SSCN_API sscn_status sscn_product8_weight_grad(const sscn_rows8* x, const sscn_rows8* dy, float* d_dw,
+                                               int64_t dw_stride, float* d_db, void* d_workspace,
+                                               size_t workspace_bytes, void* stream);
 
 /* One matrix for sscn_orthogonalize; its in and out may be the same array. */
 typedef struct {

@@ -17,6 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsscn.so")
 SOURCES = ["rulebook.hip", "gemm.hip", "gemm_direct.hip", "conv_narrow.hip", "pool.hip", "head.hip", "dropout.hip", "encode.hip", "sgd.hip", "layer_norm.hip", "newton_schulz.hip",
+           "rows8.hip", "group_norm.hip", "product8.hip", "api_rows8.hip",
            "api_operators.hip", "api.hip"]
 ARCH = "gfx950"
 

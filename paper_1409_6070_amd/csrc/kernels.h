@@ -2,11 +2,28 @@
 #pragma once
 
 #include <algorithm>
+#include <atomic>
 
 #include "common.h"
 #include "gemm_rules.h"
 
 namespace sscn {
+
+// Allows a kernel its LDS: once per kernel and device, since the call costs as much as
+// a launch.
+template <auto KERN>
+hipError_t allow_lds(int lds) {
+  static std::atomic<uint64_t> allowed{0};
+  if (lds <= 64 * 1024) return hipSuccess;
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (e == hipSuccess && !(allowed.load(std::memory_order_relaxed) & bit)) {
+    e = hipFuncSetAttribute((const void*)KERN, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e == hipSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
+  }
+  return e;
+}
 
 // Bitmap words of a layer per workgroup of the window-list kernel, for a build of
 // `words` bitmap words in all: 32 (eight threads a word) while that makes at
@@ -541,5 +558,91 @@ constexpr double NS_PLANE = 51200.0;  // fp16 ends at 65504: room for what round
 // Bytes of partial tiles that the group's products need (m, n, mp, np set).
 size_t ns_part_bytes(NsGroup& g);
 hipError_t launch_newton_schulz(NsGroup& g, bool bf16, bool muon, int steps, const NsStep* step, hipStream_t st);
+
+// rows8.hip: rows and matrices to 8 bits and back
+struct Rows8Args {
+  const void* x;        // store: rows to take
+  int64_t x_stride;
+  int64_t rows;
+  int32_t cols;
+  uint8_t* codes;
+  uint8_t* scales;
+  void* y;              // load: rows to write
+  int64_t y_stride;
+};
+hipError_t launch_rows8_store(bool bf16, const Rows8Args& a, hipStream_t st);
+hipError_t launch_rows8_load(bool bf16, const Rows8Args& a, hipStream_t st);
+struct Weight8Args {
+  const void* w;
+  int64_t w_stride;
+  int32_t k, n;
+  uint8_t* w8;          // weight8_parts
+};
+hipError_t launch_weight8_store(bool bf16, const Weight8Args& a, hipStream_t st);
+
+// product8.hip: products of 8-bit rows
+struct Product8Args {
+  const uint8_t* x;       // [rows][x_stride] codes along the sum
+  const uint8_t* xs;      // [rows][xs_stride] scales
+  int64_t x_stride, xs_stride;
+  int64_t rows;
+  const uint8_t* w;       // [n][w_stride] codes along the sum
+  const uint8_t* ws;      // [n blocks][ws_stride] scales
+  int64_t w_stride;
+  int32_t ws_stride;
+  int32_t n;              // result's columns
+  int32_t kb;             // blocks of the sum
+  const float* bias;      // [n], or null
+  void* y;
+  int64_t y_stride;
+};
+hipError_t launch_product8(bool bf16, const Product8Args& a, hipStream_t st);
+struct WeightGrad8Args {
+  const uint8_t* x;       // [rows][x_stride] codes of the layer's input
+  const uint8_t* xs;
+  int64_t x_stride, xs_stride;
+  const uint8_t* dy;      // [rows][dy_stride] codes of the output's gradient
+  const uint8_t* dys;
+  int64_t dy_stride, dys_stride;
+  int64_t rows;
+  int32_t k, n;
+  float* dw;              // [k][dw_stride]
+  int64_t dw_stride;
+  float* db;              // [n], or null
+  float* part;            // [splits][k][n], then [splits][n]; null where splits is 1
+};
+// Workgroups that share a tile's rows.
+int32_t weight_grad8_splits(int64_t rows, int32_t k, int32_t n);
+hipError_t launch_weight_grad8(const WeightGrad8Args& a, hipStream_t st);
+
+// group_norm.hip: normalisation over a sample's rows and a group's channels, with an activation
+struct GroupNormArgs {
+  const void* x;          // rows, or null: 8-bit rows
+  int64_t x_stride;
+  const uint8_t* codes;
+  const uint8_t* scales;
+  int64_t rows;
+  int32_t cols, groups, batch;
+  const int32_t* begin;   // [batch + 1], or null: samples of `span` rows
+  int64_t span;
+  const float* gain;      // [cols], null: 1
+  const float* shift;     // [cols], null: 0
+  float eps;
+  float slope;            // of the activation below zero
+  int32_t silu;
+  float* stats;           // [2][batch][groups]: mean, 1 / deviation
+  void* y;
+  int64_t y_stride;
+  const void* dy;
+  int64_t dy_stride;
+  void* dx;
+  int64_t dx_stride;
+  float* dgain;
+  float* dshift;
+  float* ws;
+};
+size_t group_norm_workspace(bool bf16, int64_t rows, int32_t cols, int32_t groups, int32_t batch, bool backward);
+hipError_t launch_group_norm(bool bf16, const GroupNormArgs& a, hipStream_t st);
+hipError_t launch_group_norm_bwd(bool bf16, const GroupNormArgs& a, hipStream_t st);
 
 }  // namespace sscn

@@ -1153,22 +1153,6 @@ constexpr int direct_lds(int T, int waves, int kind) {
   return direct_parts(T, waves, kind) * T * (T + 4) * 4 + (kind == NS_GRAM ? 0 : (T / 16) * (T / 32) * 2048);
 }
 
-// Allows a kernel its LDS: once per kernel and device, since the call costs as much as
-// a launch.
-template <auto KERN>
-hipError_t allow_lds(int lds) {
-  static std::atomic<uint64_t> allowed{0};
-  if (lds <= 64 * 1024) return hipSuccess;
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
-  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
-  if (e == hipSuccess && !(allowed.load(std::memory_order_relaxed) & bit)) {
-    e = hipFuncSetAttribute((const void*)KERN, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e == hipSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
-  }
-  return e;
-}
-
 template <auto KERN>
 hipError_t launch_tiles(int threads, int lds, const NsArgs& a, hipStream_t st) {
   const hipError_t e = allow_lds<KERN>(lds);

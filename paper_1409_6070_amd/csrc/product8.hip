@@ -1,0 +1,509 @@
+// Products of rows held in 8 bits (rows8.h).
+//
+//   forward         y = x w + bias     x [rows][k], w [k][n]: a scale for each row and 128 k,
+//   input gradient  dx = dy w^T        and for each 128 x 128 of w
+//   weight gradient dw = x^T dy, dbias = sum over rows of dy
+//
+// The first two are one product, of rows with a matrix that lies along the sum either
+// way.  A result in bf16 is computed by the scaled matrix instructions: 16 x 16 x 128 on
+// the codes themselves, each row's (and the matrix block's) power of two as an operand.
+// Their sums are float32, but within one instruction's 128 products what lies far below
+// the largest is dropped: results are off by 1.5e-5 to 4e-5 of their size on sums of
+// either sign (3e-6 where all are positive) whatever k is, a hundredth of the rounding to
+// bf16.  A result in float32 is computed by the bf16 instructions instead, in which a
+// code times its scale is exact and so is each product: 1e-7, at half the rate.
+//
+// The weight gradient sums over rows, whose scales differ from term to term: both operands
+// become bf16 (exactly) on their way to LDS and are read from there transposed.
+
+#include "common.h"
+#include "kernels.h"
+#include "rows8.h"
+
+#include <algorithm>
+
+namespace sscn {
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
+typedef int16_t i16x4 __attribute__((ext_vector_type(4)));
+
+constexpr uint32_t NO_SOURCE = 0x80000000u;  // past every buffer: reads zero
+
+__device__ inline u32x4 buffer_of(const void* base, uint32_t bytes) {
+  const uint64_t b = (uint64_t)base;
+  return u32x4{(uint32_t)b, (uint32_t)(b >> 32) & 0xffffu, bytes, 0x00020000u};
+}
+
+__device__ inline uint32_t lds_offset(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+
+// One 16-byte load per lane into LDS: lane l's bytes land at lds + 16 l (lds uniform over
+// the wave), zeros where off lies past the buffer.  The compiler does not see it;
+// wait_loads and the fences around the barriers order it.
+__device__ inline void load_lds(u32x4 rsrc, uint32_t lds, uint32_t off) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds),
+      "v"(off), "s"(rsrc)
+      : "m0");
+}
+// ... and this wave's own reads of LDS
+__device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+
+// Row r of the 64 that a wave's four blocks of the matrix operand cover: block j holds rows
+// 16 q + 4 j + e (q, e = 0 .. 3), so that a result lane's four blocks of four values are
+// sixteen neighbours of one row.
+__device__ inline int interleaved(int r16, int j) { return (r16 >> 2) * 16 + j * 4 + (r16 & 3); }
+
+// Where 16-byte chunk c of row r lies in a slab of 128-byte rows: the sixteen rows that an
+// operand's read touches (consecutive ones, or interleaved ones) cover all banks once.
+__device__ inline int slot_x(int r, int c) { return c ^ ((r >> 1) & 7); }
+__device__ inline int slot_w(int r, int c) { return c ^ (((r >> 3) & 6) | ((r >> 1) & 1)); }
+
+// Tile t of the result in an order in which the tiles that one XCD works on at a time (it
+// gets every eighth workgroup) lie together: eight rows of tiles by as many columns.
+struct TilePlace {
+  int64_t m;
+  int n;
+};
+__device__ inline TilePlace place_of(int64_t t, int64_t tiles, int64_t mt, int nt) {
+  const int64_t each = (tiles + 7) / 8;
+  t = (t & 7) * each + (t >> 3);
+  const int64_t group = t / (8 * nt), left = t - group * 8 * nt;
+  const int rows = (int)min((int64_t)8, mt - group * 8);
+  return TilePlace{group * 8 + left % rows, (int)(left / rows)};
+}
+
+// Sixteen neighbouring values of a result row, from column c on.
+template <typename T>
+__device__ inline void store_run16(T* row, int c, int n, const float (&v)[16]) {
+  T out[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) out[e] = Elem<T>::from_f32(v[e]);
+  if (c + 16 <= n) {
+    __builtin_memcpy(row + c, out, sizeof(out));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (c + e < n) row[c + e] = out[e];
+  }
+}
+
+__device__ inline void load_bias(const float* bias, int c, int n, float (&b)[16]) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) b[e] = bias && c + e < n ? bias[c + e] : 0.f;
+}
+
+// WX x WN waves, each TX blocks of 16 rows by 64 columns.
+template <int WX_, int WN_, int TX_>
+struct P8Tile {
+  static constexpr int WX = WX_, WN = WN_, TX = TX_;
+  static constexpr int NW = WX * WN, BM = WX * TX * 16, BN = WN * 64;
+  static constexpr int SLAB = (BM + BN) * 128;
+  static constexpr int XL = BM / 8 / NW, WL = BN / 8 / NW;  // loads of a wave and slab
+  static constexpr int LDS = 2 * SLAB;
+  static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "loads are dealt evenly");
+};
+
+// bf16 results: slabs of 128 codes through two LDS stages.
+template <class C>
+__global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int64_t tiles, int64_t mt, int nt) {
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wx = wave / C::WN, wn = wave % C::WN, r16 = lane & 15, g = lane >> 4;
+  const uint32_t lds0 = lds_offset(smem);
+  for (int64_t t = blockIdx.x; t < (tiles + 7) / 8 * 8; t += gridDim.x) {
+    if ((t & 7) * ((tiles + 7) / 8) + (t >> 3) >= tiles) continue;
+    const TilePlace at = place_of(t, tiles, mt, nt);
+    const int64_t m0 = at.m * C::BM;
+    const int n0 = at.n * C::BN;
+    const int rows = (int)min((int64_t)C::BM, a.rows - m0), cols = min(C::BN, a.n - n0);
+    const u32x4 rx = buffer_of(a.x + m0 * a.x_stride, (uint32_t)(rows * a.x_stride));
+    const u32x4 rw = buffer_of(a.w + n0 * a.w_stride, (uint32_t)(cols * a.w_stride));
+    const uint32_t xstride = (uint32_t)a.x_stride;
+    uint32_t xoff[C::XL], woff[C::WL], xk[C::XL];
+#pragma unroll
+    for (int i = 0; i < C::XL; ++i) {
+      const int r = (wave * C::XL + i) * 8 + (lane >> 3);
+      xk[i] = (uint32_t)slot_x(r, lane & 7) * 16u;
+      xoff[i] = r < rows ? (uint32_t)r * xstride : NO_SOURCE;
+    }
+#pragma unroll
+    for (int i = 0; i < C::WL; ++i) {
+      const int r = (wave * C::WL + i) * 8 + (lane >> 3);
+      woff[i] = r < cols ? (uint32_t)r * (uint32_t)a.w_stride + (uint32_t)slot_w(r, lane & 7) * 16u : NO_SOURCE;
+    }
+    auto issue = [&](int s, int st) {
+#pragma unroll
+      for (int i = 0; i < C::XL; ++i) {
+        const uint32_t k = xk[i] + (uint32_t)s * 128u;
+        load_lds(rx, lds0 + st * C::SLAB + (wave * C::XL + i) * 1024, k < xstride ? xoff[i] + k : NO_SOURCE);
+      }
+#pragma unroll
+      for (int i = 0; i < C::WL; ++i)
+        load_lds(rw, lds0 + st * C::SLAB + C::BM * 128 + (wave * C::WL + i) * 1024, woff[i] + (uint32_t)s * 128u);
+    };
+    const uint8_t* xs[C::TX];
+#pragma unroll
+    for (int i = 0; i < C::TX; ++i)
+      xs[i] = a.xs + min(m0 + (wx * C::TX + i) * 16 + r16, a.rows - 1) * a.xs_stride;
+    const uint8_t* ws = a.ws + (int64_t)(min(n0 + wn * 64, a.n - 1) >> 7) * a.ws_stride;
+    f32x4 acc[C::TX][4];
+#pragma unroll
+    for (int i = 0; i < C::TX; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    issue(0, 0);
+    uint32_t xw[C::TX], ww = 0;
+    for (int s = 0; s < a.kb; ++s) {
+      if ((s & 3) == 0) {
+#pragma unroll
+        for (int i = 0; i < C::TX; ++i) xw[i] = *(const uint32_t*)(xs[i] + s);
+        ww = *(const uint32_t*)(ws + s);
+      } else {
+#pragma unroll
+        for (int i = 0; i < C::TX; ++i) xw[i] >>= 8;
+        ww >>= 8;
+      }
+      wait_loads();
+      __builtin_amdgcn_s_barrier();  // slab s is whole, and every wave is done with slab s - 1
+      asm volatile("" ::: "memory");
+      if (s + 1 < a.kb) issue(s + 1, (s + 1) & 1);
+      const uint8_t* X = smem + (s & 1) * C::SLAB;
+      const uint8_t* W = X + C::BM * 128;
+      auto operand = [&](const uint8_t* base, int r, bool of_w) {
+        union {
+          i32x8 v;
+          u32x4 h[2];
+        } o;
+        const int c = g * 2;
+        o.h[0] = *(const u32x4*)(base + r * 128 + (of_w ? slot_w(r, c) : slot_x(r, c)) * 16);
+        o.h[1] = *(const u32x4*)(base + r * 128 + (of_w ? slot_w(r, c + 1) : slot_x(r, c + 1)) * 16);
+        return o.v;
+      };
+      i32x8 w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = operand(W, wn * 64 + interleaved(r16, j), true);
+#pragma unroll
+      for (int i = 0; i < C::TX; ++i) {
+        const i32x8 x = operand(X, (wx * C::TX + i) * 16 + r16, false);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[j], x, acc[i][j], 0, 0, 0, (int)ww, 0,
+                                                                       (int)xw[i]);
+      }
+    }
+    wait_loads();
+    __builtin_amdgcn_s_barrier();  // (the next tile's first slab overwrites what others may still read)
+    asm volatile("" ::: "memory");
+    const int c = n0 + wn * 64 + g * 16;
+    float b[16];
+    load_bias(a.bias, c, a.n, b);
+#pragma unroll
+    for (int i = 0; i < C::TX; ++i) {
+      const int64_t m = m0 + (wx * C::TX + i) * 16 + r16;
+      if (m >= a.rows || c >= a.n) continue;
+      float v[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = acc[i][e >> 2][e & 3] + b[e];
+      store_run16<__bf16>((__bf16*)a.y + m * a.y_stride, c, a.n, v);
+    }
+  }
+}
+
+// Sixteen codes times a power of two as sixteen bf16 values.
+struct Codes16 {
+  u32x4 lo, hi;
+};
+__device__ inline Codes16 to_bf16(u32x4 codes, float scale) {
+  Codes16 o;
+  uint32_t w[8];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    w[2 * q] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[q], scale, false));
+    w[2 * q + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[q], scale, true));
+  }
+  o.lo = u32x4{w[0], w[1], w[2], w[3]};
+  o.hi = u32x4{w[4], w[5], w[6], w[7]};
+  return o;
+}
+
+// float32 results: slabs of 64 codes, made bf16 on the way to LDS; 128 x 128 tiles of four
+// waves.
+__global__ void __launch_bounds__(256, 2) k_product8_exact(Product8Args a, int64_t tiles, int64_t mt, int nt) {
+  constexpr int STAGE = 2 * 128 * 128;  // bytes: two operands of 128 rows of 64 bf16
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wx = wave >> 1, wn = wave & 1, r16 = lane & 15, g = lane >> 4;
+  const int lr = threadIdx.x >> 1, lc = (threadIdx.x & 1) * 32;  // this thread's row of either operand, and its codes
+  for (int64_t t = blockIdx.x; t < (tiles + 7) / 8 * 8; t += gridDim.x) {
+    if ((t & 7) * ((tiles + 7) / 8) + (t >> 3) >= tiles) continue;
+    const TilePlace at = place_of(t, tiles, mt, nt);
+    const int64_t m0 = at.m * 128;
+    const int n0 = at.n * 128;
+    const bool xin = m0 + lr < a.rows, win = n0 + lr < a.n;
+    const uint8_t* x = a.x + (xin ? m0 + lr : m0) * a.x_stride + lc;
+    const uint8_t* xs = a.xs + (xin ? m0 + lr : m0) * a.xs_stride;
+    const uint8_t* w = a.w + (int64_t)(win ? n0 + lr : n0) * a.w_stride + lc;
+    const uint8_t* ws = a.ws + (int64_t)at.n * a.ws_stride;
+    u32x4 xv[2], wv[2];
+    uint32_t sx = 127, sw = 127;
+    auto fetch = [&](int s) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        xv[h] = wv[h] = u32x4{0, 0, 0, 0};
+        if (xin && s * 64 + lc + h * 16 < a.x_stride) xv[h] = *(const u32x4*)(x + s * 64 + h * 16);
+        if (win) wv[h] = *(const u32x4*)(w + s * 64 + h * 16);
+      }
+      sx = xs[s >> 1];
+      sw = ws[s >> 1];
+    };
+    auto put = [&](int st) {
+      uint8_t* X = smem + st * STAGE + lr * 128;
+      uint8_t* W = X + STAGE / 2;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int c = lc / 8 + h * 2;
+        const Codes16 vx = to_bf16(xv[h], row8_pow2(sx)), vw = to_bf16(wv[h], row8_pow2(sw));
+        *(u32x4*)(X + slot_x(lr, c) * 16) = vx.lo;
+        *(u32x4*)(X + slot_x(lr, c + 1) * 16) = vx.hi;
+        *(u32x4*)(W + slot_w(lr, c) * 16) = vw.lo;
+        *(u32x4*)(W + slot_w(lr, c + 1) * 16) = vw.hi;
+      }
+    };
+    f32x4 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int slabs = (int)((a.x_stride + 63) / 64);
+    fetch(0);
+    __syncthreads();  // (every wave done with the tile before)
+    put(0);
+    for (int s = 0; s < slabs; ++s) {
+      if (s + 1 < slabs) fetch(s + 1);
+      __syncthreads();
+      const uint8_t* X = smem + (s & 1) * STAGE;
+      const uint8_t* W = X + STAGE / 2;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        bf16x8 xo[4], wo[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = wx * 64 + i * 16 + r16, q = wn * 64 + interleaved(r16, i);
+          xo[i] = *(const bf16x8*)(X + r * 128 + slot_x(r, kb * 4 + g) * 16);
+          wo[i] = *(const bf16x8*)(W + q * 128 + slot_w(q, kb * 4 + g) * 16);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wo[j], xo[i], acc[i][j], 0, 0, 0);
+      }
+      if (s + 1 < slabs) put((s + 1) & 1);
+    }
+    const int c = n0 + wn * 64 + g * 16;
+    float b[16];
+    load_bias(a.bias, c, a.n, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t m = m0 + wx * 64 + i * 16 + r16;
+      if (m >= a.rows || c >= a.n) continue;
+      float v[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = acc[i][e >> 2][e & 3] + b[e];
+      store_run16<float>((float*)a.y + m * a.y_stride, c, a.n, v);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// weight gradient
+
+constexpr int WG_ROWS = 64;  // rows of a slab
+
+// Eight rows' values of one column of a staged slab [64 rows][128 bf16], for each lane: the
+// lanes of a 16-lane group read rows 8 g .. + 3 (then + 4 .. 7) in pieces of four columns,
+// 16 apart, and get them transposed: lane 4 q + e column c0 + 16 q + 4 j + e.  A piece of
+// 8 bytes lies where the 32 lanes that read together cover all banks once.
+__device__ inline int piece_at(int row, int unit, int sub) {
+  return row * 256 + (unit ^ ((row >> 1) & 4)) * 32 + (sub ^ (row & 3)) * 8;
+}
+__device__ inline bf16x8 column_operand(uint32_t lds, int row, int unit, int sub) {
+  typedef __attribute__((address_space(3))) i16x4* P;
+  union {
+    i16x4 h[2];
+    bf16x8 v;
+  } o;
+  o.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(lds + piece_at(row, unit, sub)));
+  o.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(lds + piece_at(row + 4, unit, sub)));
+  return o.v;
+}
+
+// A 128 x 128 tile of dw over a run of rows.
+__global__ void __launch_bounds__(256, 2) k_weight_grad8(WeightGrad8Args a, int kt, int nt, int splits) {
+  constexpr int STAGE = 2 * WG_ROWS * 256;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wk = wave >> 1, wn = wave & 1, r16 = lane & 15, g = lane >> 4;
+  const int split = blockIdx.x / (kt * nt), tile = blockIdx.x - split * (kt * nt);
+  const int tk = tile / nt, tn = tile - tk * nt;
+  const int64_t slabs = (a.rows + WG_ROWS - 1) / WG_ROWS;
+  const int64_t s0 = slabs * split / splits, s1 = slabs * (split + 1) / splits;
+  const int lr = threadIdx.x >> 2, lc = (threadIdx.x & 3) * 32;
+  const int xc = tk * 128 + lc, yc = tn * 128 + lc;
+  u32x4 xv[2], yv[2];
+  uint32_t sx = 127, sy = 127;
+  auto fetch = [&](int64_t s) {
+    const int64_t m = s * WG_ROWS + lr;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) xv[h] = yv[h] = u32x4{0, 0, 0, 0};
+    if (m < a.rows) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (xc + h * 16 < a.x_stride) xv[h] = *(const u32x4*)(a.x + m * a.x_stride + xc + h * 16);
+        if (yc + h * 16 < a.dy_stride) yv[h] = *(const u32x4*)(a.dy + m * a.dy_stride + yc + h * 16);
+      }
+      sx = a.xs[m * a.xs_stride + tk];
+      sy = a.dys[m * a.dys_stride + tn];
+    }
+  };
+  auto put = [&](int st) {
+    uint8_t* X = smem + st * STAGE;
+    uint8_t* Y = X + STAGE / 2;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int unit = lc / 16 + h;
+      Codes16 vx = to_bf16(xv[h], row8_pow2(sx)), vy = to_bf16(yv[h], row8_pow2(sy));
+      const u32x4* px = &vx.lo;
+      const u32x4* py = &vy.lo;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        *(uint2*)(X + piece_at(lr, unit, q)) = uint2{px[q >> 1][(q & 1) * 2], px[q >> 1][(q & 1) * 2 + 1]};
+        *(uint2*)(Y + piece_at(lr, unit, q)) = uint2{py[q >> 1][(q & 1) * 2], py[q >> 1][(q & 1) * 2 + 1]};
+      }
+    }
+  };
+  f32x4 acc[4][4], bacc[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    bacc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const bool bias = a.db && tk == 0 && wk == 0;
+  bf16x8 one;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) one[e] = (__bf16)1.f;
+  if (s0 < s1) {
+    fetch(s0);
+    put(0);
+  }
+  for (int64_t s = s0; s < s1; ++s) {
+    const int st = (int)(s - s0) & 1;
+    if (s + 1 < s1) fetch(s + 1);
+    __syncthreads();
+    const uint32_t X = lds_offset(smem) + st * STAGE, Y = X + STAGE / 2;
+#pragma unroll
+    for (int mb = 0; mb < 2; ++mb) {
+      bf16x8 xo[4], yo[4];
+      const int row = mb * 32 + g * 8 + (r16 >> 2);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        xo[i] = column_operand(X, row, wk * 4 + (r16 & 3), i);
+        yo[i] = column_operand(Y, row, wn * 4 + (r16 & 3), i);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(yo[j], xo[i], acc[i][j], 0, 0, 0);
+      if (bias)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) bacc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(yo[j], one, bacc[j], 0, 0, 0);
+    }
+    if (s + 1 < s1) put(st ^ 1);
+  }
+  // lane: rows k = 16 (r16 / 4) + 4 i + r16 % 4 of the wave's 64, columns n = 16 g .. + 15
+  float* out = a.part ? a.part + (int64_t)split * a.k * a.n : a.dw;
+  const int64_t stride = a.part ? a.n : a.dw_stride;
+  const int c = tn * 128 + wn * 64 + g * 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int k = tk * 128 + wk * 64 + interleaved(r16, i);
+    if (k >= a.k || c >= a.n) continue;
+    float v[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = acc[i][e >> 2][e & 3];
+    store_run16<float>(out + (int64_t)k * stride, c, a.n, v);
+  }
+  if (bias && r16 == 0 && c < a.n) {
+    float v[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = bacc[e >> 2][e & 3];
+    store_run16<float>(a.part ? a.part + (int64_t)splits * a.k * a.n + (int64_t)split * a.n : a.db, c, a.n, v);
+  }
+}
+
+// The partial tiles added in order; row k of the grid is the bias gradient.
+__global__ void __launch_bounds__(256) k_weight_grad8_sum(WeightGrad8Args a, int splits) {
+  const int64_t size = (int64_t)a.k * a.n;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size + (a.db ? a.n : 0); i += (int64_t)gridDim.x * 256) {
+    const bool bias = i >= size;
+    const float* p = bias ? a.part + splits * size + (i - size) : a.part + i;
+    const int64_t step = bias ? a.n : size;
+    float v = 0.f;
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) v += p[s * step];
+    if (bias)
+      a.db[i - size] = v;
+    else
+      a.dw[i / a.n * a.dw_stride + i % a.n] = v;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_product8(bool bf16, const Product8Args& a, hipStream_t st) {
+  if (a.rows <= 0) return hipSuccess;
+  const int64_t mt = (a.rows + 127) / 128;
+  const int nt = (a.n + 127) / 128;
+  const int64_t tiles = mt * nt;
+  const dim3 grid((unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, 1 << 20));
+  if (bf16) {
+    using C = P8Tile<2, 2, 4>;
+    const hipError_t e = allow_lds<k_product8<C>>(C::LDS);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k_product8<C>, grid, dim3(C::NW * 64), C::LDS, st, a, tiles, mt, nt);
+  } else {
+    const hipError_t e = allow_lds<k_product8_exact>(65536);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k_product8_exact, grid, dim3(256), 65536, st, a, tiles, mt, nt);
+  }
+  return hipGetLastError();
+}
+
+int32_t weight_grad8_splits(int64_t rows, int32_t k, int32_t n) {
+  const int64_t tiles = row8_blocks(k) * row8_blocks(n), slabs = (rows + WG_ROWS - 1) / WG_ROWS;
+  // two workgroups a compute unit, each with four slabs at least
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(slabs / 4, 512 / tiles));
+}
+
+hipError_t launch_weight_grad8(const WeightGrad8Args& a, hipStream_t st) {
+  const int kt = (int)row8_blocks(a.k), nt = (int)row8_blocks(a.n);
+  const int splits = weight_grad8_splits(a.rows, a.k, a.n);
+  hipError_t e = allow_lds<k_weight_grad8>(65536);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_weight_grad8, dim3((unsigned)(kt * nt * splits)), dim3(256), 65536, st, a, kt, nt, splits);
+  e = hipGetLastError();
+  if (e != hipSuccess || splits == 1) return e;
+  const int64_t size = (int64_t)a.k * a.n + (a.db ? a.n : 0);
+  hipLaunchKernelGGL(k_weight_grad8_sum, dim3((unsigned)std::min<int64_t>((size + 255) / 256, 4096)), dim3(256), 0, st, a,
+                     splits);
+  return hipGetLastError();
+}
+
+}  // namespace sscn

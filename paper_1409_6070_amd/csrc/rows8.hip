@@ -1,0 +1,241 @@
+// Rows and matrices to 8 bits and back (the format: rows8.h).
+
+#include "common.h"
+#include "kernels.h"
+#include "rows8.h"
+
+#include <algorithm>
+
+namespace sscn {
+
+namespace {
+
+// Eight consecutive elements from an address aligned to one, of which the first n exist.
+template <typename T>
+struct Run8 {
+  T e[8];
+};
+template <typename T>
+__device__ inline Run8<T> load_run(const T* p, int n) {
+  Run8<T> r;
+  if (n >= 8) {
+    __builtin_memcpy(&r, p, sizeof(r));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.e[e] = e < n ? p[e] : Elem<T>::from_f32(0.f);
+  }
+  return r;
+}
+
+template <typename T>
+__device__ inline float largest(const Run8<T>& r) {
+  float m = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float f = fabsf(Elem<T>::to_f32(r.e[e]));
+    m = fmaxf(m, is_finite(f) ? f : 0.f);
+  }
+  return m;
+}
+
+template <typename T>
+__device__ inline uint2 codes_of(const Run8<T>& r, float inv) {
+  float f[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float x = Elem<T>::to_f32(r.e[e]);
+    f[e] = is_finite(x) ? x * inv : __uint_as_float(0x7fc00000u);
+  }
+  return uint2{row8_codes4(f[0], f[1], f[2], f[3]), row8_codes4(f[4], f[5], f[6], f[7])};
+}
+
+template <int CTRL>
+__device__ inline float max_dpp(float v) {
+  return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true)));
+}
+// Largest over aligned groups of 16 lanes, in all of them.
+__device__ inline float max16(float v) {
+  v = max_dpp<0xB1>(v);   // quad_perm 1,0,3,2
+  v = max_dpp<0x4E>(v);   // quad_perm 2,3,0,1
+  v = max_dpp<0x141>(v);  // row_half_mirror
+  return max_dpp<0x140>(v);  // row_mirror
+}
+
+// A workgroup takes R rows at a time, 16 lanes a block of 128 columns, eight columns a lane;
+// PER blocks a lane group are in flight together.
+constexpr int PER = 4, GROUPS = 16, ITEMS = PER * GROUPS;
+constexpr int NO_ITEM = -(1 << 30);
+
+__device__ inline int div_by(int i, int nb, float rcp) {
+  int q = (int)((float)i * rcp);
+  q += (q + 1) * nb <= i ? 1 : 0;
+  q -= q * nb > i ? 1 : 0;
+  return q;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) k_rows8_store(Rows8Args a, int R, int64_t tiles) {
+  const int nb = (int)row8_blocks(a.cols), lane = threadIdx.x & 15, group = threadIdx.x >> 4;
+  const int64_t cs = row8_code_stride(a.cols), ss = row8_scale_stride(a.cols);
+  const float rcp = 1.f / (float)nb;
+  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const int64_t row0 = tile * R;
+    const int n = (int)min((int64_t)R, a.rows - row0) * nb;
+    for (int i0 = 0; i0 < n; i0 += ITEMS) {
+      Run8<T> x[PER];
+      int row[PER], blk[PER], live[PER];
+#pragma unroll
+      for (int p = 0; p < PER; ++p) {
+        const int i = i0 + p * GROUPS + group;
+        row[p] = nb > ITEMS ? 0 : div_by(i, nb, rcp);  // (more blocks than a tile's items: a row at a time)
+        blk[p] = i - row[p] * nb;
+        const int c = blk[p] * ROW8_BLOCK + lane * 8;
+        live[p] = i < n ? a.cols - c : NO_ITEM;  // this lane's elements: more than eight, some, or none
+        x[p] = load_run<T>((const T*)a.x + (row0 + row[p]) * a.x_stride + c, live[p]);
+      }
+#pragma unroll
+      for (int p = 0; p < PER; ++p) {
+        const uint32_t s = row8_scale(max16(largest(x[p])));
+        if (live[p] == NO_ITEM) continue;
+        const uint2 w = codes_of(x[p], row8_inverse(s));
+        const int c = blk[p] * ROW8_BLOCK + lane * 8;
+        if (c < cs) *(uint2*)(a.codes + (row0 + row[p]) * cs + c) = w;
+        uint8_t* sc = a.scales + (row0 + row[p]) * ss + blk[p];
+        if (lane == 0) *sc = (uint8_t)s;
+        if (blk[p] == nb - 1 && lane > 0 && lane < ss - blk[p]) sc[lane] = 0;
+      }
+    }
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) k_rows8_load(Rows8Args a, int R, int64_t tiles) {
+  const int nb = (int)row8_blocks(a.cols), lane = threadIdx.x & 15, group = threadIdx.x >> 4;
+  const int64_t cs = row8_code_stride(a.cols), ss = row8_scale_stride(a.cols);
+  const float rcp = 1.f / (float)nb;
+  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const int64_t row0 = tile * R;
+    const int n = (int)min((int64_t)R, a.rows - row0) * nb;
+    for (int i0 = 0; i0 < n; i0 += ITEMS) {
+      uint2 w[PER];
+      uint32_t s[PER];
+      int row[PER], col[PER], live[PER];
+#pragma unroll
+      for (int p = 0; p < PER; ++p) {
+        const int i = i0 + p * GROUPS + group;
+        row[p] = nb > ITEMS ? 0 : div_by(i, nb, rcp);
+        const int blk = i - row[p] * nb;
+        col[p] = blk * ROW8_BLOCK + lane * 8;
+        live[p] = i < n ? a.cols - col[p] : 0;
+        if (live[p] > 0) {
+          w[p] = *(const uint2*)(a.codes + (row0 + row[p]) * cs + col[p]);
+          s[p] = a.scales[(row0 + row[p]) * ss + blk];
+        }
+      }
+#pragma unroll
+      for (int p = 0; p < PER; ++p) {
+        if (live[p] <= 0) continue;
+        float f[8];
+        row8_values4(w[p].x, row8_pow2(s[p]), f);
+        row8_values4(w[p].y, row8_pow2(s[p]), f + 4);
+        T* y = (T*)a.y + (row0 + row[p]) * a.y_stride + col[p];
+        Run8<T> r;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.e[e] = Elem<T>::from_f32(f[e]);
+        if (live[p] >= 8) {
+          __builtin_memcpy(y, &r, sizeof(r));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (e < live[p]) y[e] = r.e[e];
+        }
+      }
+    }
+  }
+}
+
+// A matrix [k][n] in blocks of 128 x 128, a workgroup each: codes as they lie and, through
+// LDS, transposed (both products of a matrix read it along their sum).
+template <typename T>
+__global__ void __launch_bounds__(256) k_weight8_store(Weight8Args a) {
+  constexpr int LS = ROW8_BLOCK + 16;  // a row of the staged block, bytes
+  __shared__ __attribute__((aligned(16))) uint8_t tile[ROW8_BLOCK * LS];
+  __shared__ float red[4];
+  const int lane = threadIdx.x & 15, group = threadIdx.x >> 4;
+  const int kb = blockIdx.y, nb = blockIdx.x;
+  const Weight8 w = weight8_parts(a.w8, a.k, a.n);
+  Run8<T> x[8];
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = kb * ROW8_BLOCK + i * 16 + group, c = nb * ROW8_BLOCK + lane * 8;
+    x[i] = load_run<T>((const T*)a.w + (int64_t)min(r, a.k - 1) * a.w_stride + c, r < a.k ? a.n - c : 0);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, largest(x[i]));
+  m = max16(m);
+  for (int d = 16; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+  __syncthreads();
+  const uint32_t s = row8_scale(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = i * 16 + group, c = lane * 8;
+    const uint2 v = codes_of(x[i], row8_inverse(s));
+    *(uint2*)(tile + r * LS + c) = v;
+    if (kb * ROW8_BLOCK + r < a.k)
+      *(uint2*)(w.codes + (int64_t)(kb * ROW8_BLOCK + r) * w.stride + nb * ROW8_BLOCK + c) = v;
+  }
+  __syncthreads();
+  // row n of the transposed matrix: 128 codes by eight threads
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int n = i * 32 + (threadIdx.x >> 3), k = (threadIdx.x & 7) * 16;
+    uint32_t v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      v[q] = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[q] |= (uint32_t)tile[(k + q * 4 + e) * LS + n] << (8 * e);
+    }
+    if (nb * ROW8_BLOCK + n < a.n)
+      *(uint4*)(w.codes_t + (int64_t)(nb * ROW8_BLOCK + n) * w.stride_t + kb * ROW8_BLOCK + k) =
+          uint4{v[0], v[1], v[2], v[3]};
+  }
+  if (threadIdx.x == 0) {
+    w.scales[kb * w.scale_stride + nb] = (uint8_t)s;
+    w.scales_t[nb * w.scale_stride_t + kb] = (uint8_t)s;
+  }
+}
+
+int rows_of_tile(int64_t cols) { return (int)std::max<int64_t>(1, ITEMS / row8_blocks(cols)); }
+
+template <typename K>
+hipError_t by_tiles(K kernel, const Rows8Args& a, hipStream_t st) {
+  if (a.rows <= 0) return hipSuccess;
+  const int R = rows_of_tile(a.cols);
+  const int64_t tiles = (a.rows + R - 1) / R;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(tiles, 1 << 20)), dim3(256), 0, st, a, R, tiles);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rows8_store(bool bf16, const Rows8Args& a, hipStream_t st) {
+  return bf16 ? by_tiles(k_rows8_store<__bf16>, a, st) : by_tiles(k_rows8_store<float>, a, st);
+}
+
+hipError_t launch_rows8_load(bool bf16, const Rows8Args& a, hipStream_t st) {
+  return bf16 ? by_tiles(k_rows8_load<__bf16>, a, st) : by_tiles(k_rows8_load<float>, a, st);
+}
+
+hipError_t launch_weight8_store(bool bf16, const Weight8Args& a, hipStream_t st) {
+  const dim3 grid((unsigned)row8_blocks(a.n), (unsigned)row8_blocks(a.k));
+  if (bf16)
+    hipLaunchKernelGGL(k_weight8_store<__bf16>, grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL(k_weight8_store<float>, grid, dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace sscn

@@ -39,6 +39,9 @@ EXPORTED = [
     "sscn_layer_norm_forward", "sscn_layer_norm_workspace_bytes", "sscn_layer_norm_backward",
     "sscn_orthogonalize_workspace_bytes", "sscn_orthogonalize", "sscn_muon_workspace_bytes", "sscn_muon_update",
     "sscn_net_muon_workspace_bytes", "sscn_muon_step", "sscn_head_norm_workspace_bytes", "sscn_set_head_norm",
+    "sscn_group_norm_workspace_bytes", "sscn_group_norm_forward", "sscn_group_norm_backward", "sscn_rows8_strides",
+    "sscn_rows8_store", "sscn_rows8_load", "sscn_weight8_bytes", "sscn_weight8_store", "sscn_product8_forward",
+    "sscn_product8_input_grad", "sscn_product8_weight_grad_workspace_bytes", "sscn_product8_weight_grad",
 ]
 KERNEL_CLASSES = ["rulebook", "gather_gemm", "wgrad", "wgrad_reduce", "pool_fwd", "pool_bwd", "head", "ground",
                   "dropout", "sgd", "conv_narrow"]
@@ -84,6 +87,21 @@ class MuonOptions(ctypes.Structure):
                 ("steps", ctypes.c_int32), ("h_coef", ctypes.c_void_p)]
 
 
+class GroupNormCall(ctypes.Structure):
+    """sscn_group_norm"""
+    _fields_ = [("dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("rows", ctypes.c_int64), ("cols", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("batch", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("d_begin", ctypes.c_void_p), ("d_gain", ctypes.c_void_p), ("d_shift", ctypes.c_void_p),
+                ("d_x", ctypes.c_void_p), ("x_stride", ctypes.c_int64), ("d_codes", ctypes.c_void_p),
+                ("d_scales", ctypes.c_void_p), ("d_stats", ctypes.c_void_p)]
+
+
+class Rows8Call(ctypes.Structure):
+    """sscn_rows8"""
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("d_codes", ctypes.c_void_p),
+                ("d_scales", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -127,6 +145,18 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "sscn_layer_norm_backward": (I32, [I32, VP, I64, VP, I64, I64, I32, VP, F32, VP, I64, VP, VP, VP, SZ, VP]),
         "sscn_orthogonalize_workspace_bytes": (I32, [I32, P(OrthoMatrix), P(SZ)]),
         "sscn_orthogonalize": (I32, [I32, I32, P(OrthoMatrix), I32, P(F32), VP, SZ, VP]),
+        "sscn_group_norm_workspace_bytes": (I32, [I32, I64, I32, I32, I32, I32, P(SZ)]),
+        "sscn_group_norm_forward": (I32, [P(GroupNormCall), VP, I64, VP, SZ, VP]),
+        "sscn_group_norm_backward": (I32, [P(GroupNormCall), VP, I64, VP, I64, VP, VP, VP, SZ, VP]),
+        "sscn_rows8_strides": (I32, [I32, P(I64), P(I64)]),
+        "sscn_rows8_store": (I32, [I32, VP, I64, P(Rows8Call), VP]),
+        "sscn_rows8_load": (I32, [I32, P(Rows8Call), VP, I64, VP]),
+        "sscn_weight8_bytes": (I32, [I32, I32, P(SZ)]),
+        "sscn_weight8_store": (I32, [I32, VP, I64, I32, I32, VP, SZ, VP]),
+        "sscn_product8_forward": (I32, [I32, P(Rows8Call), VP, SZ, I32, VP, VP, I64, VP]),
+        "sscn_product8_input_grad": (I32, [I32, P(Rows8Call), VP, SZ, I32, VP, I64, VP]),
+        "sscn_product8_weight_grad_workspace_bytes": (I32, [I64, I32, I32, P(SZ)]),
+        "sscn_product8_weight_grad": (I32, [P(Rows8Call), P(Rows8Call), VP, I64, VP, VP, SZ, VP]),
         "sscn_muon_workspace_bytes": (I32, [I32, P(MuonParam), P(SZ)]),
         "sscn_muon_update": (I32, [I32, I32, P(MuonParam), F32, I32, I32, P(F32), VP, SZ, VP]),
         "sscn_net_muon_workspace_bytes": (I32, [VP, P(MuonOptions), P(SZ)]),
@@ -375,6 +405,71 @@ def sscn_set_head_norm(net, d_gain, d_shift, d_dgain, d_dshift, eps, d_ws, ws_by
            "sscn_set_head_norm")
 
 
+def sscn_group_norm_workspace_bytes(dtype, rows, cols, groups, batch, backward) -> int:
+    b = ctypes.c_size_t()
+    _check(load_library().sscn_group_norm_workspace_bytes(dtype, rows, cols, groups, batch, backward, ctypes.byref(b)),
+           "sscn_group_norm_workspace_bytes")
+    return b.value
+
+
+def sscn_group_norm_forward(norm: GroupNormCall, d_y, y_stride, d_ws, ws_bytes, stream) -> None:
+    _check(load_library().sscn_group_norm_forward(norm, d_y, y_stride, d_ws, ws_bytes, stream), "sscn_group_norm_forward")
+
+
+def sscn_group_norm_backward(norm: GroupNormCall, d_dy, dy_stride, d_dx, dx_stride, d_dgain, d_dshift, d_ws, ws_bytes,
+                             stream) -> None:
+    _check(load_library().sscn_group_norm_backward(norm, d_dy, dy_stride, d_dx, dx_stride, d_dgain, d_dshift, d_ws,
+                                                   ws_bytes, stream), "sscn_group_norm_backward")
+
+
+def sscn_rows8_strides(cols):
+    """(bytes between rows of codes, of scales)"""
+    c, s = ctypes.c_int64(), ctypes.c_int64()
+    _check(load_library().sscn_rows8_strides(cols, ctypes.byref(c), ctypes.byref(s)), "sscn_rows8_strides")
+    return c.value, s.value
+
+
+def sscn_rows8_store(dtype, d_x, x_stride, to: Rows8Call, stream) -> None:
+    _check(load_library().sscn_rows8_store(dtype, d_x, x_stride, to, stream), "sscn_rows8_store")
+
+
+def sscn_rows8_load(dtype, rows8: Rows8Call, d_y, y_stride, stream) -> None:
+    _check(load_library().sscn_rows8_load(dtype, rows8, d_y, y_stride, stream), "sscn_rows8_load")
+
+
+def sscn_weight8_bytes(k, n) -> int:
+    b = ctypes.c_size_t()
+    _check(load_library().sscn_weight8_bytes(k, n, ctypes.byref(b)), "sscn_weight8_bytes")
+    return b.value
+
+
+def sscn_weight8_store(dtype, d_w, w_stride, k, n, d_weight8, weight8_bytes, stream) -> None:
+    _check(load_library().sscn_weight8_store(dtype, d_w, w_stride, k, n, d_weight8, weight8_bytes, stream),
+           "sscn_weight8_store")
+
+
+def sscn_product8_forward(dtype, x: Rows8Call, d_weight8, weight8_bytes, n, d_bias, d_y, y_stride, stream) -> None:
+    _check(load_library().sscn_product8_forward(dtype, x, d_weight8, weight8_bytes, n, d_bias, d_y, y_stride, stream),
+           "sscn_product8_forward")
+
+
+def sscn_product8_input_grad(dtype, dy: Rows8Call, d_weight8, weight8_bytes, k, d_dx, dx_stride, stream) -> None:
+    _check(load_library().sscn_product8_input_grad(dtype, dy, d_weight8, weight8_bytes, k, d_dx, dx_stride, stream),
+           "sscn_product8_input_grad")
+
+
+def sscn_product8_weight_grad_workspace_bytes(rows, k, n) -> int:
+    b = ctypes.c_size_t()
+    _check(load_library().sscn_product8_weight_grad_workspace_bytes(rows, k, n, ctypes.byref(b)),
+           "sscn_product8_weight_grad_workspace_bytes")
+    return b.value
+
+
+def sscn_product8_weight_grad(x: Rows8Call, dy: Rows8Call, d_dw, dw_stride, d_db, d_ws, ws_bytes, stream) -> None:
+    _check(load_library().sscn_product8_weight_grad(x, dy, d_dw, dw_stride, d_db, d_ws, ws_bytes, stream),
+           "sscn_product8_weight_grad")
+
+
 # ---------------------------------------------------------------------------
 # convenience wrapper
 
@@ -382,6 +477,9 @@ NORM_MAX_COLS = 1 << 20  # SSCN_NORM_MAX_COLS
 # coefficients (a, b, c) of the quintic commonly used with Muon
 MUON_COEF = (3.4445, -4.7750, 2.0315)
 _TYPES = {"f32": (SSCN_F32, torch.float32), "bf16": (SSCN_BF16, torch.bfloat16)}
+_CODES = {t: code for code, t in _TYPES.values()}
+ACTIVATIONS = ("none", "relu", "leaky", "silu")  # sscn_activation values 0 .. 3
+ROWS8_MAX_COLS, GROUP_NORM_MAX_COLS, PRODUCT8_MAX = 1 << 20, 4096, 65536
 
 
 def _gpu_device(device) -> torch.device:
@@ -729,6 +827,251 @@ class LayerNorm:
     def _backward(self, stream, dy, ds, x, xs, rows, g, dx, os, dgain, dshift):
         sscn_layer_norm_backward(self.code, dy, ds, x, xs, rows, self.cols, g, self.eps, dx, os, dgain, dshift,
                                  self.ws_ptr, self.ws_bytes, stream)
+
+
+class Rows8:
+    """Rows [rows, cols] held in 8 bits (e4m3 codes, a power of two for each row and 128 columns), through
+    sscn_rows8_*: activations kept for the backward pass, and the operands of Product8. Allocates its two arrays, or
+    takes given ones: codes [rows, cols rounded up to 16] and scales [rows, blocks rounded up to 4], uint8, contiguous."""
+
+    def __init__(self, rows: int, cols: int, device: str = "cuda", codes: Optional[torch.Tensor] = None,
+                 scales: Optional[torch.Tensor] = None):
+        _need(0 <= rows < 2 ** 31, "rows: 0 .. 2^31 - 1")
+        self.rows, self.cols = rows, cols
+        cs, ss = sscn_rows8_strides(cols)
+        self.device = _gpu_device(device) if codes is None else codes.device
+        if codes is None:
+            codes = torch.empty((rows, cs), dtype=torch.uint8, device=self.device)
+        if scales is None:
+            scales = torch.empty((rows, ss), dtype=torch.uint8, device=self.device)
+        for t, shape, what in ((codes, (rows, cs), "codes"), (scales, (rows, ss), "scales")):
+            if tuple(t.shape) != shape or t.dtype != torch.uint8 or t.device != self.device or not t.is_contiguous():
+                raise ValueError(f"{what}: {shape} uint8 on {self.device}, contiguous")
+        self.codes, self.scales = codes, scales
+        self.call = Rows8Call(rows, cols, codes.data_ptr() if rows else None, scales.data_ptr() if rows else None)
+
+    def rows_from(self, begin: int, end: int) -> "Rows8":
+        """Rows begin .. end - 1 as 8-bit rows over the same memory."""
+        _need(0 <= begin <= end <= self.rows, f"rows: within 0 .. {self.rows}")
+        return Rows8(end - begin, self.cols, codes=self.codes[begin:end], scales=self.scales[begin:end])
+
+    def _matrix(self, t: torch.Tensor, what: str):
+        """(sscn_dtype, elements between rows) of a matrix of these rows' shape."""
+        code = _CODES.get(t.dtype)
+        if code is None or t.dim() != 2 or t.shape[0] != self.rows or t.shape[1] != self.cols or t.device != self.device:
+            raise ValueError(f"{what}: [{self.rows}, {self.cols}] float32 or bfloat16 on {self.device}")
+        return code, self.cols if t.is_contiguous() else _row_stride(t, what)
+
+    def store(self, x: torch.Tensor) -> "Rows8":
+        """Takes the values of x [rows, cols] (float32 or bfloat16); returns itself."""
+        code, stride = self._matrix(x, "x")
+        _launch(self.device, self._store, code, x.data_ptr(), stride)
+        return self
+
+    def _store(self, stream, code, x, stride):
+        sscn_rows8_store(code, x, stride, self.call, stream)
+
+    def load(self, dtype: str = "bf16", out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The values held, in out (float32 or bfloat16) or a new tensor of the type named."""
+        if out is None:
+            if dtype not in _TYPES:
+                raise ValueError(dtype)
+            out = torch.empty((self.rows, self.cols), dtype=_TYPES[dtype][1], device=self.device)
+        code, stride = self._matrix(out, "out")
+        _launch(self.device, self._load, code, out.data_ptr(), stride)
+        return out
+
+    def _load(self, stream, code, y, stride):
+        sscn_rows8_load(code, self.call, y, stride, stream)
+
+
+class GroupNorm:
+    """Group norm with an activation ("none", "relu", "leaky": x/3 below 0, or "silu") over the rows of a sample and
+    the channels of a group, through sscn_group_norm_*; holds the workspaces for up to rows_max rows and batch_max
+    samples, each from its first use on. begin: int32 [batch + 1] row offsets of the samples on the device, or the
+    number of samples of equal length. One stream at a time, and kept until its calls have run."""
+
+    def __init__(self, cols: int, groups: int, rows_max: int, batch_max: int, dtype: str = "bf16", act: str = "none",
+                 eps: float = 1e-5, device: str = "cuda"):
+        if dtype not in _TYPES:
+            raise ValueError(dtype)
+        if act not in ACTIVATIONS:
+            raise ValueError(act)
+        self.cols, self.groups, self.rows_max, self.batch_max = cols, groups, rows_max, batch_max
+        self.dtype, self.act, self.eps = dtype, act, eps
+        self.code, self.tdtype = _TYPES[dtype]
+        self.ws_bytes = [sscn_group_norm_workspace_bytes(self.code, rows_max, cols, groups, batch_max, b) for b in (0, 1)]
+        self.device = _gpu_device(device)
+        self.ws = [None, None]
+        self.call = GroupNormCall(dtype=self.code, act=ACTIVATIONS.index(act), cols=cols, groups=groups, eps=eps)
+
+    def _rows(self, t: torch.Tensor, what: str):
+        if t.dtype != self.tdtype or t.device != self.device or t.dim() != 2 or t.shape[1] != self.cols:
+            raise ValueError(f"{what}: [rows, {self.cols}] {self.dtype} on {self.device}")
+        if t.is_contiguous():
+            return t.shape[0], self.cols
+        return t.shape[0], _row_stride(t, what)
+
+    def _param(self, t: Optional[torch.Tensor], what: str):
+        if t is None:
+            return None
+        if t.dtype != torch.float32 or t.device != self.device or t.numel() != self.cols or not t.is_contiguous():
+            raise ValueError(f"{what}: [{self.cols}] float32 on {self.device}")
+        return t.data_ptr()
+
+    def _prepare(self, rows, begin, gain, shift, backward):
+        """Fills in what both directions share; returns (batch, workspace)."""
+        c = self.call
+        if isinstance(begin, int):
+            batch, c.d_begin = begin, None
+        else:
+            if begin.dtype != torch.int32 or begin.device != self.device or begin.dim() != 1 or not begin.is_contiguous():
+                raise ValueError(f"begin: [batch + 1] int32 on {self.device}")
+            batch, c.d_begin = begin.shape[0] - 1, begin.data_ptr()
+        if rows > self.rows_max or not 0 <= batch <= self.batch_max:
+            raise ValueError(f"at most {self.rows_max} rows and {self.batch_max} samples")
+        c.rows, c.batch = rows, batch
+        c.d_gain, c.d_shift = self._param(gain, "gain"), self._param(shift, "shift")
+        if self.ws[backward] is None:
+            self.ws[backward] = torch.empty(self.ws_bytes[backward], dtype=torch.uint8, device=self.device)
+        return batch, self.ws[backward]
+
+    def forward(self, x: torch.Tensor, begin, gain: Optional[torch.Tensor] = None, shift: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None):
+        """(y, stats [2, batch, groups]: means and 1 / deviations); out may be x. Rows outside all samples are left
+        as they were (undefined in a new tensor)."""
+        rows, xs = self._rows(x, "x")
+        batch, ws = self._prepare(rows, begin, gain, shift, 0)
+        if out is None:
+            out, ys = torch.empty((rows, self.cols), dtype=self.tdtype, device=self.device), self.cols
+        else:
+            n, ys = self._rows(out, "out")
+            _need(n == rows, "out: as many rows as x")
+        stats = torch.empty((2, batch, self.groups), dtype=torch.float32, device=self.device)
+        c = self.call
+        c.d_x, c.x_stride, c.d_codes, c.d_scales, c.d_stats = x.data_ptr(), xs, None, None, stats.data_ptr()
+        _launch(self.device, self._forward, out.data_ptr(), ys, ws.data_ptr(), ws.numel())
+        return out, stats
+
+    def _forward(self, stream, y, ys, ws, ws_bytes):
+        sscn_group_norm_forward(self.call, y, ys, ws, ws_bytes, stream)
+
+    def backward(self, dy: torch.Tensor, x, stats: torch.Tensor, begin, gain: Optional[torch.Tensor] = None,
+                 shift: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None):
+        """(dx, dgain, dshift) from the output's gradient, the forward's statistics, gain and shift, and its input x: a
+        tensor, or Rows8 that hold it. dx may be given (dy and x too)."""
+        rows, ds = self._rows(dy, "dy")
+        batch, ws = self._prepare(rows, begin, gain, shift, 1)
+        c = self.call
+        if isinstance(x, Rows8):
+            if x.rows != rows or x.cols != self.cols or x.device != self.device:
+                raise ValueError(f"x: [{rows}, {self.cols}] on {self.device}")
+            c.d_x, c.x_stride, c.d_codes, c.d_scales = None, 0, x.call.d_codes, x.call.d_scales
+        else:
+            n, xs = self._rows(x, "x")
+            _need(n == rows, "x: as many rows as dy")
+            c.d_x, c.x_stride, c.d_codes, c.d_scales = x.data_ptr(), xs, None, None
+        if (stats.dtype != torch.float32 or stats.device != self.device or stats.numel() != 2 * batch * self.groups
+                or not stats.is_contiguous()):
+            raise ValueError(f"stats: [2, {batch}, {self.groups}] float32 on {self.device}")
+        c.d_stats = stats.data_ptr()
+        if dx is None:
+            dx, os = torch.empty((rows, self.cols), dtype=self.tdtype, device=self.device), self.cols
+        else:
+            n, os = self._rows(dx, "dx")
+            _need(n == rows, "dx: as many rows as dy")
+        dgain, dshift = torch.empty((2, self.cols), dtype=torch.float32, device=self.device).unbind(0)
+        _launch(self.device, self._backward, dy.data_ptr(), ds, dx.data_ptr(), os, dgain.data_ptr(), dshift.data_ptr(),
+                ws.data_ptr(), ws.numel())
+        return dx, dgain, dshift
+
+    def _backward(self, stream, dy, ds, dx, os, dgain, dshift, ws, ws_bytes):
+        sscn_group_norm_backward(self.call, dy, ds, dx, os, dgain, dshift, ws, ws_bytes, stream)
+
+
+class Product8:
+    """Products of 8-bit rows with a matrix [k, n] in 8 bits (a scale for each 128 x 128), through sscn_product8_*: a
+    1x1 layer on rows of sites. Holds the 8-bit matrix and, from the first weight gradient on, the workspace for up to
+    rows_max rows. Results have the type named (gradients of the weights float32). One stream at a time, and kept until
+    its calls have run."""
+
+    def __init__(self, k: int, n: int, rows_max: int, dtype: str = "bf16", device: str = "cuda"):
+        if dtype not in _TYPES:
+            raise ValueError(dtype)
+        self.k, self.n, self.rows_max, self.dtype = k, n, rows_max, dtype
+        self.code, self.tdtype = _TYPES[dtype]
+        self.w8_bytes = sscn_weight8_bytes(k, n)
+        self.ws_bytes = sscn_product8_weight_grad_workspace_bytes(rows_max, k, n)
+        self.device = _gpu_device(device)
+        self.w8 = torch.empty(self.w8_bytes, dtype=torch.uint8, device=self.device)
+        self.w8_ptr, self.ws, self._set = self.w8.data_ptr(), None, False
+
+    def set_weights(self, w: torch.Tensor) -> "Product8":
+        """Takes w [k, n] (float32 or bfloat16) into 8 bits, for the calls that follow; returns itself."""
+        code = _CODES.get(w.dtype)
+        if code is None or tuple(w.shape) != (self.k, self.n) or w.device != self.device:
+            raise ValueError(f"w: [{self.k}, {self.n}] float32 or bfloat16 on {self.device}")
+        stride = self.n if w.is_contiguous() else _row_stride(w, "w")
+        _launch(self.device, self._store, code, w.data_ptr(), stride)
+        self._set = True
+        return self
+
+    def _store(self, stream, code, w, stride):
+        sscn_weight8_store(code, w, stride, self.k, self.n, self.w8_ptr, self.w8_bytes, stream)
+
+    def _rows(self, r: "Rows8", cols: int, what: str):
+        if not isinstance(r, Rows8) or r.cols != cols or r.device != self.device:
+            raise ValueError(f"{what}: Rows8 of {cols} columns on {self.device}")
+        return r.rows
+
+    def _result(self, out, rows, cols, dtype, what):
+        """A result's tensor and the elements between its rows."""
+        if out is None:
+            return torch.empty((rows, cols), dtype=dtype, device=self.device), cols
+        if tuple(out.shape) != (rows, cols) or out.dtype != dtype or out.device != self.device:
+            raise ValueError(f"{what}: [{rows}, {cols}] {dtype} on {self.device}")
+        return out, cols if out.is_contiguous() else _row_stride(out, what)
+
+    def forward(self, x: "Rows8", bias: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """x w + bias (bias [n] float32)."""
+        _need(self._set, "no weights: call set_weights first")
+        rows = self._rows(x, self.k, "x")
+        if bias is not None and (bias.dtype != torch.float32 or bias.device != self.device or bias.numel() != self.n
+                                 or not bias.is_contiguous()):
+            raise ValueError(f"bias: [{self.n}] float32 on {self.device}")
+        out, stride = self._result(out, rows, self.n, self.tdtype, "out")
+        _launch(self.device, self._forward, x.call, None if bias is None else bias.data_ptr(), out.data_ptr(), stride)
+        return out
+
+    def _forward(self, stream, x, bias, y, stride):
+        sscn_product8_forward(self.code, x, self.w8_ptr, self.w8_bytes, self.n, bias, y, stride, stream)
+
+    def input_grad(self, dy: "Rows8", out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """dy w^T"""
+        _need(self._set, "no weights: call set_weights first")
+        rows = self._rows(dy, self.n, "dy")
+        out, stride = self._result(out, rows, self.k, self.tdtype, "out")
+        _launch(self.device, self._input_grad, dy.call, out.data_ptr(), stride)
+        return out
+
+    def _input_grad(self, stream, dy, dx, stride):
+        sscn_product8_input_grad(self.code, dy, self.w8_ptr, self.w8_bytes, self.k, dx, stride, stream)
+
+    def weight_grad(self, x: "Rows8", dy: "Rows8", out: Optional[torch.Tensor] = None):
+        """(x^T dy, sum over rows of dy), float32; out: the first one's tensor."""
+        rows = self._rows(x, self.k, "x")
+        _need(self._rows(dy, self.n, "dy") == rows, "dy: as many rows as x")
+        if rows > self.rows_max:
+            raise ValueError(f"rows: at most {self.rows_max}")
+        if self.ws is None:
+            self.ws = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=self.device)
+        out, stride = self._result(out, self.k, self.n, torch.float32, "out")
+        db = torch.empty(self.n, dtype=torch.float32, device=self.device)
+        _launch(self.device, self._weight_grad, x.call, dy.call, out.data_ptr(), stride, db.data_ptr())
+        return out, db
+
+    def _weight_grad(self, stream, x, dy, dw, stride, db):
+        sscn_product8_weight_grad(x, dy, dw, stride, db, self.ws.data_ptr(), self.ws_bytes, stream)
 
 
 class Orthogonalizer:
