@@ -6,19 +6,25 @@
 //   backward  dz = dy act'(z), t = dz gain, dx = r (t - sum t / n - h sum(t h) / n),
 //             dgain = sum over rows of dz h, dshift = sum over rows of dz
 //
-// Memory-bound.  Samples are runs of rows of any lengths, known on the device only, so
-// work is dealt by equal chunks of rows: a workgroup walks through the samples that its
-// chunk meets.  The part of sample s in chunk c is piece c + s, which numbers all pieces
-// without a scan.  Three launches: sums of each piece, sums of each sample, the result.
-// The last one goes through the chunks backwards, so that it finds in the last-level cache
-// what the first one read last.
+// Memory-bound.  Samples are runs of rows of any lengths, known on the device only.
+//
+// Samples that are small on average: one launch, a workgroup for a sample and a slice of
+// whole groups, its rows in registers (k_group_norm_small, k_group_norm_bwd_small).  A
+// sample that is larger than that is read again for each step.
+//
+// Larger ones: work is dealt by equal chunks of rows, and a workgroup walks through the
+// samples that its chunk meets.  The part of sample s in chunk c is piece c + s, which
+// numbers all pieces without a scan.  Three launches: sums of each piece, sums of each
+// sample, the result.  The last one goes through the chunks backwards, so that it finds in
+// the last-level cache what the first one read last.
 //
 // A thread owns one vector of V columns and every rpb-th row.  The last vector starts V
-// columns before the row's end, where its first `skip` columns repeat those of the vector
-// before (left out of every sum and not stored).  Variances: a thread
-// sums deviations from its own first value of a column, which cannot cancel by more than
-// the number of its rows, and threads, pieces and columns are joined by their means.
-// Every sum is taken in an order that sizes alone decide.  All arithmetic is float32.
+// columns before the end, where its first `skip` columns repeat those of the vector
+// before (left out of every sum and not stored).  Variances: in registers from the
+// deviations themselves; in streams a thread sums deviations from its own first value of a
+// column, which cannot cancel by more than the number of its rows, and threads, pieces and
+// columns are joined by their means.  Every sum is taken in an order that sizes alone
+// decide.  All arithmetic is float32.
 
 #include "common.h"
 #include "kernels.h"
@@ -70,33 +76,35 @@ struct Held {
 };
 template <typename T, int V>
 struct Held<T, V, true> {
-  uint8_t c[V], s0, s1;
+  uint32_t c[(V + 3) / 4];
+  uint32_t s;  // the scales of its two blocks
   // split: elements before the next scale's block
   __device__ inline void load(const GroupNormArgs& a, int64_t r, int col, int split) {
+    c[0] = 0;
     __builtin_memcpy(c, a.codes + r * row8_code_stride(a.cols) + col, V);
-    const uint8_t* s = a.scales + r * row8_scale_stride(a.cols) + (col >> 7);
-    s0 = s[0];
-    s1 = split < V ? s[1] : s0;
+    const uint8_t* p = a.scales + r * row8_scale_stride(a.cols) + (col >> 7);
+    s = p[0];
+    if (split < V) s |= (uint32_t)p[1] << 8;
   }
   __device__ inline void values(float (&f)[V], int split) const {
-    if constexpr (V >= 4) {
-#pragma unroll
-      for (int q = 0; q < V; q += 4) {
-        uint32_t w;
-        __builtin_memcpy(&w, c + q, 4);
-        row8_values4(w, 1.f, f + q);
-      }
-    } else {
+    const float s0 = row8_pow2(s & 255u), s1 = row8_pow2(s >> 8);
+    if constexpr (V == 1) {
       float t[4];
-      row8_values4(c[0], 1.f, t);
+      row8_values4(c[0], s0, t);
       f[0] = t[0];
-    }
+    } else if (split >= V) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) f[e] *= row8_pow2(e < split ? s0 : s1);
+      for (int q = 0; q < V; q += 4) row8_values4(c[q / 4], s0, f + q);
+    } else {
+#pragma unroll
+      for (int q = 0; q < V; q += 4) row8_values4(c[q / 4], 1.f, f + q);
+#pragma unroll
+      for (int e = 0; e < V; ++e) f[e] *= e < split ? s0 : s1;
+    }
   }
 };
 
-// z, every operation rounded by itself: forward and backward take the same branch of the
+// Every operation is rounded by itself: forward and backward take the same branch of the
 // activation, and so does any program that follows the formula in float32.
 __device__ inline float normal(float x, float mean, float r) {
 #pragma clang fp contract(off)
@@ -108,168 +116,319 @@ __device__ inline float affine(float h, float gain, float shift) {
   return p + shift;
 }
 __device__ inline float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
-__device__ inline float activated(float z, float slope, bool silu) {
-  if (silu) return z * sigmoid(z);
-  return z < 0.f ? (slope == 0.f ? 0.f : slope * z) : z;
+template <bool SILU>
+__device__ inline float activated(float z, float slope) {
+  if constexpr (SILU) return z * sigmoid(z);
+  const float below = slope == 0.f ? 0.f : slope * z;
+  return z < 0.f ? below : z;
 }
-// The framework's rule at zero: a rectifier's derivative is 0 there, the leaky one's 1.
-__device__ inline float slope_at(float z, float slope, bool silu) {
-  if (silu) {
+// dy act'(z).  The framework's rule at zero: a rectifier's derivative is 0 there, the leaky
+// one's 1.
+template <bool SILU>
+__device__ inline float gradient(float dy, float h, float gain, float shift, float slope) {
+  const float z = affine(h, gain, shift);
+  if constexpr (SILU) {
     const float s = sigmoid(z);
-    return s * (1.f + z * (1.f - s));
+    return dy * (s * (1.f + z * (1.f - s)));
   }
-  return (slope == 0.f ? z > 0.f : z >= 0.f) ? 1.f : slope;
+  return (slope == 0.f ? z > 0.f : z >= 0.f) ? dy : dy * slope;
 }
 
-// The last sample that starts at row r or before it (-1: none; batch: r lies behind the
-// last one), by a whole wave, 64 probes at a time.  Bounds hold for any offsets.
-__device__ inline int sample_of(const GroupNormArgs& a, int64_t r) {
-  if (!a.begin) return (int)(r / a.span);
-  int lo = -1, hi = a.batch + 1;
-  while (hi - lo > 1) {
-    const int step = (hi - lo - 1 + 63) / 64;
-    const int64_t at = (int64_t)lo + 1 + (int64_t)(threadIdx.x & 63) * step;
-    const int m = __popcll(__ballot(at < hi && a.begin[at < hi ? at : 0] <= r));
-    const int64_t top = (int64_t)lo + 1 + (int64_t)m * step;
-    if (m > 0) lo = lo + 1 + (m - 1) * step;
-    if (top < hi) hi = (int)top;
-  }
-  return __builtin_amdgcn_readfirstlane(lo);
+// Sums over lanes of aligned groups of L = 1, 8, 64.
+__device__ inline float lanes_sum(float s, int L) {
+  for (int d = 1; d < L; d *= 2) s += __shfl_xor(s, d);
+  return s;
 }
+
 __device__ inline int64_t sample_begin(const GroupNormArgs& a, int s) { return a.begin ? a.begin[s] : s * a.span; }
 
-// Calls run(sample, first row, end) for the samples' parts of rows r0 .. r1 - 1, in order
-// (uniform over the workgroup).
+// The last sample that starts at row r or before it (-1: none; batch: r lies behind the
+// last one), and its rows, by a whole wave: 256 probes a round, all in flight.  Bounds hold
+// for any offsets.
+struct Span {
+  int s;
+  int64_t begin, end;
+};
+__device__ inline Span span_of(const GroupNormArgs& a, int64_t r) {
+  if (!a.begin) {
+    const int s = (int)(r / a.span);
+    return Span{s, s * a.span, (s + 1) * a.span};
+  }
+  const int lane = threadIdx.x & 63;
+  int lo = -1, hi = a.batch + 1;
+  int32_t begin = 0, end = 0;
+  while (hi - lo > 1) {
+    const int step = (hi - lo - 1 + 255) / 256;
+    int32_t v[4];
+    int m = 0;  // probes at r or before it
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t at = (int64_t)lo + 1 + (int64_t)(i * 64 + lane) * step;
+      v[i] = a.begin[min(at, (int64_t)a.batch)];
+      m += at < hi && v[i] <= r ? 1 : 0;
+    }
+    m = (int)lanes_sum((float)m, 64);
+    auto probe = [&](int k) { return __shfl(k < 64 ? v[0] : k < 128 ? v[1] : k < 192 ? v[2] : v[3], k & 63); };
+    const int64_t top = (int64_t)lo + 1 + (int64_t)m * step;
+    if (m > 0) {
+      lo = lo + 1 + (m - 1) * step;
+      begin = probe(m - 1);
+    }
+    if (m < 256 && top < hi) {
+      hi = (int)top;
+      end = probe(m);
+    }
+  }
+  return Span{__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(begin),
+              __builtin_amdgcn_readfirstlane(end)};
+}
+
+// Calls run(sample's span, first row, end) for the samples' parts of rows r0 .. r1 - 1, in
+// order (uniform over the workgroup).
 template <class Run>
 __device__ inline void pieces_of(const GroupNormArgs& a, int64_t r0, int64_t r1, Run&& run) {
   int64_t r = r0;
   while (r < r1) {
-    const int s = sample_of(a, r);
-    if (s >= a.batch) return;
-    const int64_t next = sample_begin(a, s + 1);
-    const int64_t end = min(r1, max(next, r + 1));  // (offsets that decrease still end)
-    if (s >= 0) run(s, r, end);
+    const Span s = span_of(a, r);
+    if (s.s >= a.batch) return;
+    const int64_t end = min(r1, max(s.end, r + 1));  // (offsets that decrease still end)
+    if (s.s >= 0) run(s, r, end);
     r = end;
   }
 }
 
-// A thread's place: vector t of the row, row lane rl of rpb.
+// A thread's place among columns first .. first + width - 1 of whole groups: vector t of a
+// row, row lane rl of rpb.
 template <int V>
 struct Place {
-  int t, rl, rpb, col, skip, split, group[V];
+  int rl, rpb, col, skip, split, group[V];
   bool on;
-  __device__ inline Place(int cols, int groups, int nt) {
-    const int nvec = (cols + V - 1) / V;
+  __device__ inline Place(int first, int width, int per, int nt) {
+    const int nvec = (width + V - 1) / V, t = threadIdx.x % nvec;
     rpb = nt / nvec;
-    t = threadIdx.x % nvec;
     rl = threadIdx.x / nvec;
     on = rl < rpb;
-    const int at = t * V;
-    col = min(at, cols - V);
-    skip = at - col;
+    const int at = min(t * V, width - V);
+    col = first + at;
+    skip = t * V - at;
     split = min(V, ROW8_BLOCK - (col & (ROW8_BLOCK - 1)));
-    const int per = cols / groups;
 #pragma unroll
     for (int e = 0; e < V; ++e) group[e] = (col + e) / per;
   }
 };
 
-// Sums over the row lanes of every column: red is [rpb][cols], the totals are in its first row.
+// gain and shift of a thread's columns
 template <int V>
-__device__ inline void column_totals(const Place<V>& p, float* red, int cols, const float (&v)[V]) {
-  __syncthreads();  // (the last totals have been read)
-  if (p.on)
+struct Params {
+  float gain[V], shift[V];
+  __device__ inline Params(const GroupNormArgs& a, int col) {
 #pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (e >= p.skip) red[p.rl * cols + p.col + e] = v[e];
-  __syncthreads();
-  for (int c = threadIdx.x; c < cols; c += blockDim.x) {
-    float s = 0.f;
-    for (int k = 0; k < p.rpb; ++k) s += red[k * cols + c];
-    red[c] = s;
+    for (int e = 0; e < V; ++e) {
+      gain[e] = a.gain ? a.gain[col + e] : 1.f;
+      shift[e] = a.shift ? a.shift[col + e] : 0.f;
+    }
   }
-  __syncthreads();
+};
+
+constexpr int FEW = 16;  // row lanes that one thread adds
+
+// Sums over the row lanes of every column of the slice.  put() brings the threads' values
+// together (uniform over the workgroup), col(c) is then the total of column c of the slice;
+// `red` holds [rpb][width] floats and, for more than FEW row lanes, [FEW][width] behind them.
+struct Totals {
+  float* red;
+  int width, rpb, nt;
+  const float* from;
+  int n;
+  template <int V>
+  __device__ inline void put(const Place<V>& p, int first, const float (&v)[V]) {
+    __syncthreads();  // (the last totals have been read)
+    if (p.on)
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (e >= p.skip) red[p.rl * width + p.col - first + e] = v[e];
+    __syncthreads();
+    from = red;
+    n = rpb;
+    if (rpb > FEW) {  // (then there are more threads than columns)
+      const int parts = min(nt / width, FEW), q = threadIdx.x / width, c = threadIdx.x - q * width;
+      float* to = red + rpb * width;
+      if (q < parts) {
+        float s = 0.f;
+#pragma unroll 4
+        for (int k = q; k < rpb; k += parts) s += red[k * width + c];
+        to[q * width + c] = s;
+      }
+      __syncthreads();
+      from = to;
+      n = parts;
+    }
+  }
+  __device__ inline float col(int c) const {
+    float s = from[c];
+#pragma unroll 4
+    for (int k = 1; k < n; ++k) s += from[k * width + c];
+    return s;
+  }
+};
+// floats of `red`
+__host__ __device__ inline int totals_floats(int rpb, int width) {
+  return (rpb > 0 ? rpb : 1) * width + (rpb > FEW ? FEW * width : 0);
 }
 
 // lanes that share a group's sum
 __device__ inline int lanes_of(int per) { return per <= 4 ? 1 : per <= 64 ? 8 : 64; }
 
-// done(group, sum over its channels c of value(c)), by the first lane of each group's lanes.
+// done(group, sum of value(c) over its columns c, counted from the slice's first) for the
+// `groups` groups of a slice, by the first of each group's lanes.
 template <class Value, class Done>
-__device__ inline void group_totals(int first, int end, int per, Value&& value, Done&& done) {
+__device__ inline void group_totals(int groups, int per, Value&& value, Done&& done) {
   const int L = lanes_of(per), sub = threadIdx.x % L;
-  for (int g = first + threadIdx.x / L; g < end; g += blockDim.x / L) {
+  for (int g = threadIdx.x / L; g < groups; g += blockDim.x / L) {
     float s = 0.f;
     for (int c = sub; c < per; c += L) s += value(g * per + c);
-    for (int d = 1; d < L; d *= 2) s += __shfl_xor(s, d);
+    s = lanes_sum(s, L);
     if (sub == 0) done(g, s);
   }
 }
 
-// Forward, first launch: mean and summed squares of deviations of every piece and group.
-template <typename T, int V>
-__global__ void __launch_bounds__(1024) k_group_norm_sums(GroupNormArgs a, int64_t chunk) {
-  extern __shared__ float smem[];
-  const Place<V> p(a.cols, a.groups, blockDim.x);
-  float* red = smem;                          // [rpb][cols]
-  float* mean = smem + max(p.rpb, 1) * a.cols;  // [groups]
+// Sum of value(k) for k = first, first + step, .. below end, U at a time in flight (none of
+// them alone behind the last whole group: a trip through memory for each would be most of
+// a short sum's time).
+template <int U, class Value>
+__device__ inline float strided_sum(int64_t first, int64_t end, int64_t step, Value&& value) {
+  float s = 0.f;
+  for (int64_t k = first; k < end; k += U * step) {
+    float v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = value(min(k + u * step, end - 1));
+#pragma unroll
+    for (int u = 0; u < U; ++u) s += k + u * step < end ? v[u] : 0.f;
+  }
+  return s;
+}
+
+// A thread's rows first + rl, + rpb, .. of a run, U of them in flight.  load(q, row) brings
+// one, mask(q) empties what lies behind the run, add(q) takes it.  The first U rows of a
+// chunk are loaded (within `end`) before its samples are known.
+template <class Q, int U>
+struct Stream {
+  Q q[U];
+  template <class Load>
+  __device__ inline void start(int64_t first, int64_t end, int rl, int rpb, Load&& load) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) load(q[u], min(first + rl + (int64_t)u * rpb, end - 1));
+  }
+  // started: q holds the run's first rows
+  template <class Load, class Mask, class Add>
+  __device__ inline void run(bool started, int64_t lo, int64_t hi, int rl, int rpb, Load&& load, Mask&& mask, Add&& add) {
+    int64_t row = lo + rl;
+    if (!started) start(lo, hi, rl, rpb, load);
+    for (; row + (int64_t)(U - 1) * rpb < hi;) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) add(q[u]);
+      row += (int64_t)U * rpb;
+      if (row < hi)
+#pragma unroll
+        for (int u = 0; u < U; ++u) load(q[u], min(row + (int64_t)u * rpb, hi - 1));
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (row + (int64_t)u * rpb >= hi) mask(q[u]);
+    if (row < hi)
+#pragma unroll
+      for (int u = 0; u < U; ++u) add(q[u]);
+  }
+};
+
+// ---------------------------------------------------------------------------
+// forward
+
+__device__ inline void empty_stats(const GroupNormArgs& a, int64_t b) {
+  for (int g = 0; g < a.groups; ++g) {
+    a.stats[b * a.groups + g] = 0.f;
+    a.stats[((int64_t)a.batch + b) * a.groups + g] = 1.f / sqrtf(a.eps);
+  }
+}
+
+// Mean and 1 / deviation of group g of a sample out of its pieces, by L lanes of which this
+// is number `lane`.
+struct Stats {
+  float mean, r;
+};
+template <int L>
+__device__ inline Stats join_pieces(const GroupNormArgs& a, int64_t chunk, const Span& s, int g, int lane) {
+  const int64_t lo = max(s.begin, (int64_t)0), hi = min(s.end, a.rows);
+  if (lo >= hi) return Stats{0.f, 1.f / sqrtf(a.eps)};
   const int per = a.cols / a.groups;
+  const int64_t c0 = lo / chunk, c1 = (hi - 1) / chunk;
+  const float n = (float)(hi - lo) * (float)per;
+  const float* part = a.ws + (int64_t)s.s * 2 * a.groups + 2 * g;
+  auto rows = [&](int64_t c) { return (float)(min(hi, (c + 1) * chunk) - max(lo, c * chunk)) * (float)per; };
+  const float mean =
+      lanes_sum(strided_sum<4>(c0 + lane, c1 + 1, L, [&](int64_t c) { return rows(c) * part[c * 2 * a.groups]; }), L) / n;
+  const float m2 = lanes_sum(strided_sum<4>(c0 + lane, c1 + 1, L,
+                                            [&](int64_t c) {
+                                              const float d = part[c * 2 * a.groups] - mean;
+                                              return part[c * 2 * a.groups + 1] + rows(c) * d * d;
+                                            }),
+                             L);
+  return Stats{mean, 1.f / sqrtf(m2 / n + a.eps)};
+}
+
+// First launch: mean and summed squares of deviations of every piece and group.
+template <typename T, int V, int NT>
+__global__ void __launch_bounds__(NT) k_group_norm_sums(GroupNormArgs a, int64_t chunk) {
+  extern __shared__ float smem[];
+  const int per = a.cols / a.groups;
+  const Place<V> p(0, a.cols, per, NT);
+  Totals tot{smem, a.cols, p.rpb, NT};
+  float* mean = smem + totals_floats(p.rpb, a.cols);  // [groups]
   const int64_t c = blockIdx.x, r0 = c * chunk, r1 = min(a.rows, r0 + chunk);
-  pieces_of(a, r0, r1, [&](int s, int64_t lo, int64_t hi) {
+  typedef Held<T, V, false> Q;
+  auto load = [&](Q& q, int64_t row) { q.load(a, row, p.col, p.split); };
+  Stream<Q, 8> rows;
+  rows.start(r0, r1, p.rl, p.rpb, load);
+  if (a.begin)  // samples without rows have no piece
+    for (int64_t b = c * NT + threadIdx.x; b < a.batch; b += (int64_t)gridDim.x * NT)
+      if (a.begin[b] >= a.begin[b + 1]) empty_stats(a, b);
+  pieces_of(a, r0, r1, [&](const Span& s, int64_t lo, int64_t hi) {
     float pivot[V], s1[V], s2[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) pivot[e] = s1[e] = s2[e] = 0.f;
-    int n = 0;
+    float n = 0.f;
     if (p.on && lo + p.rl < hi) {
-      Held<T, V, false> x;
-      x.load(a, lo + p.rl, p.col, p.split);
-      x.values(pivot, p.split);
-      n = (int)((hi - lo - p.rl + p.rpb - 1) / p.rpb);
-      constexpr int U = 4;
-      int i = 1;
-      for (; i + U <= n; i += U) {
-        Held<T, V, false> q[U];
+      n = (float)((hi - lo - p.rl + p.rpb - 1) / p.rpb);
+      if (lo > r0) rows.start(lo, hi, p.rl, p.rpb, load);
+      const Q first = rows.q[0];
+      first.values(pivot, p.split);
+      rows.run(true, lo, hi, p.rl, p.rpb, load, [&](Q& q) { q = first; },
+               [&](const Q& q) {
+                 float f[V];
+                 q.values(f, p.split);
 #pragma unroll
-        for (int u = 0; u < U; ++u) q[u].load(a, lo + p.rl + (int64_t)(i + u) * p.rpb, p.col, p.split);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          float f[V];
-          q[u].values(f, p.split);
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const float d = f[e] - pivot[e];
-            s1[e] += d;
-            s2[e] += d * d;
-          }
-        }
-      }
-      for (; i < n; ++i) {
-        float f[V];
-        x.load(a, lo + p.rl + (int64_t)i * p.rpb, p.col, p.split);
-        x.values(f, p.split);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float d = f[e] - pivot[e];
-          s1[e] += d;
-          s2[e] += d * d;
-        }
-      }
+                 for (int e = 0; e < V; ++e) {
+                   const float d = f[e] - pivot[e];
+                   s1[e] += d;
+                   s2[e] += d * d;
+                 }
+               });
     }
-    const float rn = n ? 1.f / (float)n : 0.f, count = (float)(hi - lo) * (float)per;
+    const float rn = n > 0.f ? 1.f / n : 0.f, count = (float)(hi - lo) * (float)per;
     float v[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = s1[e] + (float)n * pivot[e];
-    column_totals<V>(p, red, a.cols, v);
-    group_totals(0, a.groups, per, [&](int col) { return red[col]; }, [&](int g, float sum) { mean[g] = sum / count; });
+    for (int e = 0; e < V; ++e) v[e] = s1[e] + n * pivot[e];
+    tot.put(p, 0, v);
+    group_totals(a.groups, per, [&](int col) { return tot.col(col); }, [&](int g, float sum) { mean[g] = sum / count; });
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       const float d = pivot[e] + s1[e] * rn - mean[p.group[e]];
-      v[e] = n ? (s2[e] - s1[e] * s1[e] * rn) + (float)n * d * d : 0.f;
+      v[e] = n > 0.f ? (s2[e] - s1[e] * s1[e] * rn) + n * d * d : 0.f;
     }
-    column_totals<V>(p, red, a.cols, v);
-    float* out = a.ws + (c + s) * 2 * a.groups;
-    group_totals(0, a.groups, per, [&](int col) { return red[col]; },
+    tot.put(p, 0, v);
+    float* out = a.ws + (c + s.s) * 2 * a.groups;
+    group_totals(a.groups, per, [&](int col) { return tot.col(col); },
                  [&](int g, float sum) {
                    out[2 * g] = mean[g];
                    out[2 * g + 1] = sum;
@@ -277,360 +436,718 @@ __global__ void __launch_bounds__(1024) k_group_norm_sums(GroupNormArgs a, int64
   });
 }
 
-// Second launch: mean and 1 / deviation of every sample and group out of its pieces.
+// Where samples have many pieces, a launch of its own: mean and 1 / deviation of every sample
+// and group.
 __global__ void __launch_bounds__(256) k_group_norm_stats(GroupNormArgs a, int64_t chunk) {
-  const int per = a.cols / a.groups, lane = threadIdx.x & 63;
   const int64_t items = (int64_t)a.batch * a.groups;
   for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < items; i += (int64_t)gridDim.x * 4) {
-    const int s = (int)(i / a.groups), g = (int)(i - (int64_t)s * a.groups);
-    const int64_t lo = min(max(sample_begin(a, s), (int64_t)0), a.rows), hi = min(sample_begin(a, s + 1), a.rows);
-    float mean = 0.f, m2 = 0.f;
-    const float n = (float)max(hi - lo, (int64_t)0) * (float)per;
-    if (lo < hi) {
-      const int64_t c0 = lo / chunk, c1 = (hi - 1) / chunk;
-      const float* part = a.ws + (int64_t)s * 2 * a.groups + 2 * g;
-      auto rows = [&](int64_t c) { return (float)(min(hi, (c + 1) * chunk) - max(lo, c * chunk)) * (float)per; };
-      float sum = 0.f;
-      for (int64_t c = c0 + lane; c <= c1; c += 64) sum += rows(c) * part[c * 2 * a.groups];
-      for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-      mean = sum / n;
-      for (int64_t c = c0 + lane; c <= c1; c += 64) {
-        const float d = part[c * 2 * a.groups] - mean;
-        m2 += part[c * 2 * a.groups + 1] + rows(c) * d * d;
-      }
-      for (int d = 1; d < 64; d *= 2) m2 += __shfl_xor(m2, d);
-      m2 /= n;
-    }
-    if (lane == 0) {
-      a.stats[i] = mean;
-      a.stats[items + i] = 1.f / sqrtf(m2 + a.eps);
+    const int s = (int)(i / a.groups);
+    const Stats v = join_pieces<64>(a, chunk, Span{s, sample_begin(a, s), sample_begin(a, s + 1)}, (int)(i - (int64_t)s * a.groups),
+                                    threadIdx.x & 63);
+    if ((threadIdx.x & 63) == 0) {
+      a.stats[i] = v.mean;
+      a.stats[items + i] = v.r;
     }
   }
 }
 
-// Third launch: the rows.
-template <typename T, int V>
-__global__ void __launch_bounds__(1024) k_group_norm_rows(GroupNormArgs a, int64_t chunk) {
-  const Place<V> p(a.cols, a.groups, blockDim.x);
+// Last launch: the rows.  JOIN: the statistics come from the pieces, and the workgroup with
+// a sample's first row stores them.
+template <typename T, int V, int NT, bool SILU, bool JOIN>
+__global__ void __launch_bounds__(NT) k_group_norm_rows(GroupNormArgs a, int64_t chunk) {
+  extern __shared__ float smem[];  // JOIN: [2][groups]
+  const Place<V> p(0, a.cols, a.cols / a.groups, NT);
   const int64_t c = (int64_t)gridDim.x - 1 - blockIdx.x, r0 = c * chunk, r1 = min(a.rows, r0 + chunk);
-  float gain[V], shift[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    gain[e] = a.gain ? a.gain[p.col + e] : 1.f;
-    shift[e] = a.shift ? a.shift[p.col + e] : 0.f;
-  }
-  pieces_of(a, r0, r1, [&](int s, int64_t lo, int64_t hi) {
+  struct Q {
+    Held<T, V, false> x;
+    int64_t row;
+  };
+  auto load = [&](Q& q, int64_t row) {
+    q.x.load(a, row, p.col, p.split);
+    q.row = row;
+  };
+  Stream<Q, 4> rows;
+  rows.start(r0, r1, p.rl, p.rpb, load);
+  const Params<V> w(a, p.col);
+  pieces_of(a, r0, r1, [&](const Span& s, int64_t lo, int64_t hi) {
+    const int64_t all = (int64_t)a.batch * a.groups, at = (int64_t)s.s * a.groups;
     float mean[V], r[V];
+    if constexpr (JOIN) {
+      __syncthreads();  // (the last piece's have been read)
+      for (int g = threadIdx.x >> 3; g < a.groups; g += NT / 8) {
+        const Stats v = join_pieces<8>(a, chunk, s, g, threadIdx.x & 7);
+        if ((threadIdx.x & 7) == 0) {
+          smem[g] = v.mean;
+          smem[a.groups + g] = v.r;
+          if (lo == s.begin) {
+            a.stats[at + g] = v.mean;
+            a.stats[all + at + g] = v.r;
+          }
+        }
+      }
+      __syncthreads();
+    }
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      const int64_t at = (int64_t)s * a.groups + p.group[e];
-      mean[e] = a.stats[at];
-      r[e] = a.stats[(int64_t)a.batch * a.groups + at];
+      mean[e] = JOIN ? smem[p.group[e]] : a.stats[at + p.group[e]];
+      r[e] = JOIN ? smem[a.groups + p.group[e]] : a.stats[all + at + p.group[e]];
     }
     if (!p.on) return;
-    auto put = [&](const Held<T, V, false>& x, int64_t row) {
-      float f[V];
-      x.values(f, p.split);
+    rows.run(lo == r0, lo, hi, p.rl, p.rpb, load, [&](Q& q) { q.row = -1; },
+             [&](const Q& q) {
+               float f[V];
+               q.x.values(f, p.split);
 #pragma unroll
-      for (int e = 0; e < V; ++e)
-        f[e] = activated(affine(normal(f[e], mean[e], r[e]), gain[e], shift[e]), a.slope, a.silu);
-      store_pack<T, V>((T*)a.y + row * a.y_stride + p.col, f, p.skip);
-    };
-    constexpr int U = 4;
-    int64_t row = lo + p.rl;
-    for (; row + (U - 1) * p.rpb < hi; row += U * p.rpb) {
-      Held<T, V, false> q[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) q[u].load(a, row + u * p.rpb, p.col, p.split);
-#pragma unroll
-      for (int u = 0; u < U; ++u) put(q[u], row + u * p.rpb);
-    }
-    for (; row < hi; row += p.rpb) {
-      Held<T, V, false> q;
-      q.load(a, row, p.col, p.split);
-      put(q, row);
-    }
+               for (int e = 0; e < V; ++e)
+                 f[e] = activated<SILU>(affine(normal(f[e], mean[e], r[e]), w.gain[e], w.shift[e]), a.slope);
+               if (q.row >= 0) store_pack<T, V>((T*)a.y + q.row * a.y_stride + p.col, f, p.skip);
+             });
   });
 }
 
-// dz and h of a thread's vector.
+// Workgroups of the small kernels: samples s0, s0 + step, .. of a slice of `slice` groups.
+struct Slice {
+  int first, width, g0, groups, s0, step;
+  __device__ inline Slice(const GroupNormArgs& a, int slice, int slices) {
+    const int k = blockIdx.x % slices, per = a.cols / a.groups;
+    s0 = blockIdx.x / slices;
+    step = gridDim.x / slices;
+    g0 = k * slice;
+    groups = min(slice, a.groups - g0);
+    first = g0 * per;
+    width = groups * per;
+  }
+};
+
+// Small samples: a thread's NV rows in registers.
+template <typename T, int V, int NT, int NV, bool SILU>
+__global__ void __launch_bounds__(NT) k_group_norm_small(GroupNormArgs a, int slice, int slices) {
+  extern __shared__ float smem[];
+  const Slice b(a, slice, slices);
+  const int per = a.cols / a.groups;
+  const Place<V> p(b.first, b.width, per, NT);
+  Totals tot{smem, b.width, p.rpb, NT};
+  float* mean = smem + totals_floats(p.rpb, b.width);  // [groups], then 1 / deviation
+  float* dev = mean + b.groups;
+  const Params<V> w(a, p.col);
+  typedef Held<T, V, false> Q;
+  for (int s = b.s0; s < a.batch; s += b.step) {
+    const int64_t lo = min(max(sample_begin(a, s), (int64_t)0), a.rows);
+    const int64_t hi = max(lo, min(sample_begin(a, s + 1), a.rows));
+    const bool held = hi - lo <= (int64_t)p.rpb * NV;
+    Q q[NV];
+    if (held && p.on)
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (lo + p.rl + i * p.rpb < hi) q[i].load(a, lo + p.rl + i * p.rpb, p.col, p.split);
+    // run(values, row) for this thread's rows
+    auto rows = [&](auto&& run) {
+      if (!p.on) return;
+      float f[V];
+      if (held) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          if (lo + p.rl + i * p.rpb < hi) {
+            q[i].values(f, p.split);
+            run(f, lo + p.rl + i * p.rpb);
+          }
+      } else {
+        for (int64_t row = lo + p.rl; row < hi; row += (int64_t)p.rpb * 8) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) q[i].load(a, min(row + (int64_t)i * p.rpb, hi - 1), p.col, p.split);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (row + (int64_t)i * p.rpb < hi) {
+              q[i].values(f, p.split);
+              run(f, row + (int64_t)i * p.rpb);
+            }
+        }
+      }
+    };
+    const float count = (float)(hi - lo) * (float)per;
+    float v[V], m[V], r[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = 0.f;
+    rows([&](const float(&f)[V], int64_t) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[e] += f[e];
+    });
+    tot.put(p, b.first, v);
+    group_totals(b.groups, per, [&](int c) { return tot.col(c); },
+                 [&](int g, float sum) { mean[g] = hi > lo ? sum / count : 0.f; });
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      m[e] = mean[p.group[e] - b.g0];
+      v[e] = 0.f;
+    }
+    rows([&](const float(&f)[V], int64_t) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float d = f[e] - m[e];
+        v[e] += d * d;
+      }
+    });
+    tot.put(p, b.first, v);
+    group_totals(b.groups, per, [&](int c) { return tot.col(c); },
+                 [&](int g, float sum) {
+                   const float d = 1.f / sqrtf((hi > lo ? sum / count : 0.f) + a.eps);
+                   dev[g] = d;
+                   const int64_t at = (int64_t)s * a.groups + b.g0 + g;
+                   a.stats[at] = mean[g];
+                   a.stats[(int64_t)a.batch * a.groups + at] = d;
+                 });
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < V; ++e) r[e] = dev[p.group[e] - b.g0];
+    rows([&](const float(&f)[V], int64_t row) {
+      float o[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) o[e] = activated<SILU>(affine(normal(f[e], m[e], r[e]), w.gain[e], w.shift[e]), a.slope);
+      store_pack<T, V>((T*)a.y + row * a.y_stride + p.col, o, p.skip);
+    });
+  }
+}
+
+// ---------------------------------------------------------------------------
+// backward
+
 template <typename T, int V, bool X8>
-struct Gradient {
+struct Pair {
   Held<T, V, X8> x;
   Pack<T, V> d;
-  __device__ inline void load(const GroupNormArgs& a, int64_t row, const Place<V>& p) {
-    x.load(a, row, p.col, p.split);
-    d = load_pack<T, V>((const T*)a.dy + row * a.dy_stride + p.col);
+  int64_t row;
+  __device__ inline void load(const GroupNormArgs& a, int64_t r, const Place<V>& p) {
+    x.load(a, r, p.col, p.split);
+    d = load_pack<T, V>((const T*)a.dy + r * a.dy_stride + p.col);
+    row = r;
   }
-  __device__ inline void values(const GroupNormArgs& a, const Place<V>& p, const float (&mean)[V], const float (&r)[V],
-                                const float (&gain)[V], const float (&shift)[V], float (&dz)[V], float (&h)[V]) const {
+  __device__ inline void empty() {
+#pragma unroll
+    for (int e = 0; e < V; ++e) d.e[e] = Elem<T>::from_f32(0.f);
+    row = -1;
+  }
+  template <bool SILU>
+  __device__ inline void values(const GroupNormArgs& a, const Place<V>& p, const Params<V>& w, const float (&mean)[V],
+                                const float (&r)[V], float (&dz)[V], float (&h)[V]) const {
     x.values(h, p.split);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       h[e] = normal(h[e], mean[e], r[e]);
-      dz[e] = Elem<T>::to_f32(d.e[e]) * slope_at(affine(h[e], gain[e], shift[e]), a.slope, a.silu);
+      dz[e] = gradient<SILU>(Elem<T>::to_f32(d.e[e]), h[e], w.gain[e], w.shift[e], a.slope);
     }
   }
+};
+
+// r (dz gain - m1 - h m2) = dz (r gain) - r m1 - h (r m2), the products made once a thread
+template <int V>
+struct Slopes {
+  float g[V], c1[V], c2[V];
 };
 
 // What the backward pass keeps in its workspace.
 struct BwdParts {
-  float* piece;  // [chunks + batch][2][cols]: sums of dz and of dz h over a piece's rows
-  float* chunk;  // the same over a chunk's rows: [2][chunks][cols], dz h first
+  float* chunk;  // sums of dz h and of dz over a chunk's (a workgroup's) rows: [2][parts][cols]
+  float* piece;  // [chunks + batch][2][cols]: of dz and of dz h over a piece's rows
   float* means;  // [2][batch][groups]: sum t / n, sum t h / n
 };
-__device__ inline BwdParts bwd_parts(const GroupNormArgs& a, int64_t chunks) {
+__device__ inline BwdParts bwd_parts(const GroupNormArgs& a, int64_t parts) {
   BwdParts b;
-  b.piece = a.ws;
-  b.chunk = b.piece + (chunks + a.batch) * 2 * a.cols;
-  b.means = b.chunk + chunks * 2 * a.cols;
+  b.chunk = a.ws;
+  b.piece = b.chunk + parts * 2 * a.cols;
+  b.means = b.piece + (parts + a.batch) * 2 * a.cols;
   return b;
 }
 
-// Backward, first launch: a piece's sums of dz and dz h for every column, and a chunk's.
-template <typename T, int V, bool X8>
-__global__ void __launch_bounds__(1024) k_group_norm_bwd_sums(GroupNormArgs a, int64_t chunk) {
+// First launch: a piece's sums of dz and dz h for every column, and a chunk's.
+template <typename T, int V, int NT, bool X8, bool SILU>
+__global__ void __launch_bounds__(NT) k_group_norm_bwd_sums(GroupNormArgs a, int64_t chunk) {
   extern __shared__ float smem[];
-  const Place<V> p(a.cols, a.groups, blockDim.x);
-  float* red = smem;                           // [rpb][cols]
-  float* total = smem + max(p.rpb, 1) * a.cols;  // [2][cols]
+  const Place<V> p(0, a.cols, a.cols / a.groups, NT);
+  Totals tot{smem, a.cols, p.rpb, NT};
+  float* total = smem + totals_floats(p.rpb, a.cols);  // [2][cols]
   const int64_t c = blockIdx.x, r0 = c * chunk, r1 = min(a.rows, r0 + chunk);
   const BwdParts parts = bwd_parts(a, gridDim.x);
-  float gain[V], shift[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    gain[e] = a.gain ? a.gain[p.col + e] : 1.f;
-    shift[e] = a.shift ? a.shift[p.col + e] : 0.f;
-  }
-  for (int i = threadIdx.x; i < 2 * a.cols; i += blockDim.x) total[i] = 0.f;
-  pieces_of(a, r0, r1, [&](int s, int64_t lo, int64_t hi) {
+  const Params<V> w(a, p.col);
+  typedef Pair<T, V, X8> Q;
+  auto load = [&](Q& q, int64_t row) { q.load(a, row, p); };
+  Stream<Q, 4> rows;
+  rows.start(r0, r1, p.rl, p.rpb, load);
+  for (int i = threadIdx.x; i < 2 * a.cols; i += NT) total[i] = 0.f;
+  pieces_of(a, r0, r1, [&](const Span& s, int64_t lo, int64_t hi) {
     float mean[V], r[V], sum[2][V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      const int64_t at = (int64_t)s * a.groups + p.group[e];
+      const int64_t at = (int64_t)s.s * a.groups + p.group[e];
       mean[e] = a.stats[at];
       r[e] = a.stats[(int64_t)a.batch * a.groups + at];
       sum[0][e] = sum[1][e] = 0.f;
     }
-    if (p.on) {
-      auto add = [&](const Gradient<T, V, X8>& q) {
-        float dz[V], h[V];
-        q.values(a, p, mean, r, gain, shift, dz, h);
+    if (p.on)
+      rows.run(lo == r0, lo, hi, p.rl, p.rpb, load, [&](Q& q) { q.empty(); },
+               [&](const Q& q) {
+                 float dz[V], h[V];
+                 q.template values<SILU>(a, p, w, mean, r, dz, h);
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          sum[0][e] += dz[e];
-          sum[1][e] += dz[e] * h[e];
-        }
-      };
-      constexpr int U = 4;
-      int64_t row = lo + p.rl;
-      for (; row + (U - 1) * p.rpb < hi; row += U * p.rpb) {
-        Gradient<T, V, X8> q[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) q[u].load(a, row + u * p.rpb, p);
-#pragma unroll
-        for (int u = 0; u < U; ++u) add(q[u]);
-      }
-      for (; row < hi; row += p.rpb) {
-        Gradient<T, V, X8> q;
-        q.load(a, row, p);
-        add(q);
-      }
-    }
-    float* out = parts.piece + (c + s) * 2 * a.cols;
+                 for (int e = 0; e < V; ++e) {
+                   sum[0][e] += dz[e];
+                   sum[1][e] += dz[e] * h[e];
+                 }
+               });
+    float* out = parts.piece + (c + s.s) * 2 * a.cols;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      column_totals<V>(p, red, a.cols, sum[k]);
-      for (int i = threadIdx.x; i < a.cols; i += blockDim.x) {
-        out[k * a.cols + i] = red[i];
-        total[k * a.cols + i] += red[i];  // (each column is one thread's)
+      tot.put(p, 0, sum[k]);
+      for (int i = threadIdx.x; i < a.cols; i += NT) {  // (each column is one thread's)
+        const float v = tot.col(i);
+        out[k * a.cols + i] = v;
+        total[k * a.cols + i] += v;
       }
     }
   });
-  for (int i = threadIdx.x; i < a.cols; i += blockDim.x) {
+  for (int i = threadIdx.x; i < a.cols; i += NT) {
     parts.chunk[c * a.cols + i] = total[a.cols + i];
     parts.chunk[((int64_t)gridDim.x + c) * a.cols + i] = total[i];
   }
 }
 
-constexpr int BWD_COLS = 64;  // columns of a workgroup of the second launch
+// dgain (which = 0) and dshift: some columns' sums over the chunks, in NT / cols_of lanes a
+// column, interleaved.
+template <int NT>
+__device__ inline void param_sums(const GroupNormArgs& a, const float* chunk, int parts, int block, float* smem) {
+  constexpr int COLS = NT / 16;
+  const int cb = (a.cols + COLS - 1) / COLS, which = block / cb;
+  const int at = threadIdx.x % COLS, c = (block - which * cb) * COLS + at, sl = threadIdx.x / COLS;
+  const float* p = chunk + (int64_t)which * parts * a.cols;
+  float* out = which ? a.dshift : a.dgain;
+  float v = c < a.cols ? strided_sum<16>(sl, parts, 16, [&](int64_t k) { return p[k * a.cols + c]; }) : 0.f;
+  smem[sl * COLS + at] = v;
+  __syncthreads();
+  if (sl == 0 && c < a.cols && out) {
+    for (int k = 1; k < 16; ++k) v += smem[k * COLS + at];
+    out[c] = v;
+  }
+}
+template <int NT>
+int param_blocks(int cols) {
+  return 2 * ((cols + NT / 16 - 1) / (NT / 16));
+}
 
-// Second launch.  Its first `sample_blocks` workgroups: the means of t and t h over the
-// samples and some of their groups; the others: the gain's and shift's gradients, 64
-// columns each, in 16 interleaved slices of the chunks.
+__global__ void __launch_bounds__(1024) k_group_norm_params(GroupNormArgs a, int parts) {
+  __shared__ float smem[1024];
+  param_sums<1024>(a, a.ws, parts, blockIdx.x, smem);
+}
+
+// sum t / n and sum t h / n of a slice of a sample's groups, out of its pieces: done(k, group of
+// the slice, value) with k = 0 for the first.  smem: [2][max(1, NT / width)][width].
+template <int NT, class Done>
+__device__ inline void join_means(const GroupNormArgs& a, const float* piece, int64_t chunk, const Span& s, int first,
+                                  int groups, int per, float* smem, Done&& done) {
+  const int64_t lo = max(s.begin, (int64_t)0), hi = min(s.end, a.rows);
+  const int64_t c0 = lo / chunk, c1 = (hi - 1) / chunk;
+  const float rn = 1.f / ((float)(hi - lo) * (float)per);
+  const int width = groups * per, lanes = (int)min((int64_t)max(1, NT / width), c1 - c0 + 1);
+  __syncthreads();  // (what smem held has been read)
+  for (int i = threadIdx.x; i < lanes * width; i += NT) {
+    const int l = i / width, col = first + i - l * width;
+    const float* q = piece + (int64_t)s.s * 2 * a.cols + col;
+    const float g = a.gain ? a.gain[col] : 1.f;
+    float u = 0.f, v = 0.f;
+    constexpr int U = 8;
+    for (int64_t c = c0 + l; c <= c1; c += U * lanes) {
+      float x[U], y[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int64_t at = min(c + k * lanes, c1) * 2 * a.cols;
+        x[k] = q[at];
+        y[k] = q[at + a.cols];
+      }
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        u += c + k * lanes <= c1 ? x[k] : 0.f;
+        v += c + k * lanes <= c1 ? y[k] : 0.f;
+      }
+    }
+    smem[i] = u * g;
+    smem[lanes * width + i] = v * g;
+  }
+  __syncthreads();
+  for (int k = 0; k < 2; ++k)
+    group_totals(groups, per,
+                 [&](int c) {
+                   float v = 0.f;
+#pragma unroll 4
+                   for (int l = 0; l < lanes; ++l) v += smem[(k * lanes + l) * width + c];
+                   return v;
+                 },
+                 [&](int g, float sum) { done(k, g, sum * rn); });
+}
+int join_floats(int nt, int width) { return 2 * std::max(1, nt / width) * width; }
+
+constexpr int BWD_COLS = 64;  // columns of a sample that a workgroup of the second launch sums
+
+// Where samples have many pieces, a launch of its own.  Its first `sample_blocks` workgroups: the means of
+// t and t h over the samples and some of their groups; the others: the gain's and shift's
+// gradients.
 __global__ void __launch_bounds__(1024) k_group_norm_bwd_means(GroupNormArgs a, int64_t chunk, int chunks,
                                                                int sample_blocks, int slice) {
   extern __shared__ float smem[];
   const BwdParts parts = bwd_parts(a, chunks);
-  const int per = a.cols / a.groups;
   if ((int)blockIdx.x >= sample_blocks) {
-    const int b = (int)blockIdx.x - sample_blocks, cb = (a.cols + 63) / 64, which = b / cb;
-    const int c = (b - which * cb) * 64 + (threadIdx.x & 63), sl = threadIdx.x >> 6;
-    const float* p = parts.chunk + (int64_t)which * chunks * a.cols;
-    float* out = which ? a.dshift : a.dgain;
-    float v = 0.f;
-    if (c < a.cols)
-#pragma unroll 16
-      for (int k = sl; k < chunks; k += 16) v += p[(int64_t)k * a.cols + c];
-    smem[sl * 64 + (threadIdx.x & 63)] = v;
-    __syncthreads();
-    if (sl == 0 && c < a.cols && out) {
-      for (int k = 1; k < 16; ++k) v += smem[k * 64 + threadIdx.x];
-      out[c] = v;
-    }
+    param_sums<1024>(a, parts.chunk, chunks, (int)blockIdx.x - sample_blocks, smem);
     return;
   }
-  const int slices = (a.groups + slice - 1) / slice;
+  const int per = a.cols / a.groups, slices = (a.groups + slice - 1) / slice;
   const int64_t items = (int64_t)a.batch * slices;
   for (int64_t item = blockIdx.x; item < items; item += sample_blocks) {
     const int s = (int)(item / slices), g0 = (int)(item - (int64_t)s * slices) * slice;
-    const int g1 = min(g0 + slice, a.groups), first = g0 * per, width = (g1 - g0) * per;
-    const int64_t lo = min(max(sample_begin(a, s), (int64_t)0), a.rows), hi = min(sample_begin(a, s + 1), a.rows);
-    if (lo >= hi) continue;
-    const int64_t c0 = lo / chunk, c1 = (hi - 1) / chunk;
-    const float rn = 1.f / ((float)(hi - lo) * (float)per);
-    const int lanes = max(1, (int)blockDim.x / width);  // smem: [lanes][width], the totals first
-    for (int k = 0; k < 2; ++k) {
-      __syncthreads();
-      for (int i = threadIdx.x; i < lanes * width; i += blockDim.x) {
-        const int l = i / width, col = first + i - l * width;
-        float v = 0.f;
-        const float* q = parts.piece + (int64_t)s * 2 * a.cols + k * a.cols + col;
-#pragma unroll 8
-        for (int64_t c = c0 + l; c <= c1; c += lanes) v += q[c * 2 * a.cols];
-        smem[i] = v * (a.gain ? a.gain[col] : 1.f);
-      }
-      __syncthreads();
-      for (int i = threadIdx.x; i < width; i += blockDim.x) {
-        float v = smem[i];
-        for (int l = 1; l < lanes; ++l) v += smem[l * width + i];
-        smem[i] = v;
-      }
-      __syncthreads();
-      group_totals(g0, g1, per, [&](int col) { return smem[col - first]; },
-                   [&](int g, float sum) { parts.means[((int64_t)k * a.batch + s) * a.groups + g] = sum * rn; });
-    }
+    const Span sp{s, sample_begin(a, s), sample_begin(a, s + 1)};
+    if (max(sp.begin, (int64_t)0) >= min(sp.end, a.rows)) continue;
+    join_means<1024>(a, parts.piece, chunk, sp, g0 * per, min(slice, a.groups - g0), per, smem,
+                     [&](int k, int g, float v) { parts.means[((int64_t)k * a.batch + s) * a.groups + g0 + g] = v; });
   }
 }
 
-// Third launch: dx.
-template <typename T, int V, bool X8>
-__global__ void __launch_bounds__(1024) k_group_norm_bwd_rows(GroupNormArgs a, int64_t chunk) {
-  const Place<V> p(a.cols, a.groups, blockDim.x);
-  const int64_t c = (int64_t)gridDim.x - 1 - blockIdx.x, r0 = c * chunk, r1 = min(a.rows, r0 + chunk);
-  const BwdParts parts = bwd_parts(a, gridDim.x);
-  float gain[V], shift[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    gain[e] = a.gain ? a.gain[p.col + e] : 1.f;
-    shift[e] = a.shift ? a.shift[p.col + e] : 0.f;
+// Last launch: dx.  JOIN: the means come from the pieces, and the workgroups behind those of the
+// chunks sum the gain's and shift's gradients.
+template <typename T, int V, int NT, bool X8, bool SILU, bool JOIN>
+__global__ void __launch_bounds__(NT) k_group_norm_bwd_rows(GroupNormArgs a, int64_t chunk, int chunks) {
+  extern __shared__ float smem[];  // JOIN: join_floats, then [2][groups]
+  const BwdParts parts = bwd_parts(a, chunks);
+  const int per = a.cols / a.groups;
+  float* joined = smem + 2 * max(1, NT / a.cols) * a.cols;
+  if (JOIN && (int)blockIdx.x >= chunks) {
+    param_sums<NT>(a, parts.chunk, chunks, (int)blockIdx.x - chunks, smem);
+    return;
   }
-  pieces_of(a, r0, r1, [&](int s, int64_t lo, int64_t hi) {
-    float mean[V], r[V], m1[V], m2[V];
+  const Place<V> p(0, a.cols, per, NT);
+  const int64_t c = (int64_t)chunks - 1 - blockIdx.x, r0 = c * chunk, r1 = min(a.rows, r0 + chunk);
+  typedef Pair<T, V, X8> Q;
+  auto load = [&](Q& q, int64_t row) { q.load(a, row, p); };
+  Stream<Q, 4> rows;
+  rows.start(r0, r1, p.rl, p.rpb, load);
+  const Params<V> w(a, p.col);
+  pieces_of(a, r0, r1, [&](const Span& s, int64_t lo, int64_t hi) {
+    if constexpr (JOIN) {
+      join_means<NT>(a, parts.piece, chunk, s, 0, a.groups, per, smem,
+                     [&](int k, int g, float v) { joined[k * a.groups + g] = v; });
+      __syncthreads();
+    }
+    float mean[V], r[V];
+    Slopes<V> k;
+    const int64_t all = (int64_t)a.batch * a.groups, at = (int64_t)s.s * a.groups;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      const int64_t at = (int64_t)s * a.groups + p.group[e], all = (int64_t)a.batch * a.groups;
-      mean[e] = a.stats[at];
-      r[e] = a.stats[all + at];
-      m1[e] = parts.means[at];
-      m2[e] = parts.means[all + at];
+      mean[e] = a.stats[at + p.group[e]];
+      r[e] = a.stats[all + at + p.group[e]];
+      k.g[e] = r[e] * w.gain[e];
+      k.c1[e] = -r[e] * (JOIN ? joined[p.group[e]] : parts.means[at + p.group[e]]);
+      k.c2[e] = -r[e] * (JOIN ? joined[a.groups + p.group[e]] : parts.means[all + at + p.group[e]]);
     }
     if (!p.on) return;
-    auto put = [&](const Gradient<T, V, X8>& q, int64_t row) {
-      float dz[V], h[V];
-      q.values(a, p, mean, r, gain, shift, dz, h);
+    rows.run(lo == r0, lo, hi, p.rl, p.rpb, load, [&](Q& q) { q.empty(); },
+             [&](const Q& q) {
+               float dz[V], h[V];
+               q.template values<SILU>(a, p, w, mean, r, dz, h);
 #pragma unroll
-      for (int e = 0; e < V; ++e) dz[e] = r[e] * (dz[e] * gain[e] - m1[e] - h[e] * m2[e]);
-      store_pack<T, V>((T*)a.dx + row * a.dx_stride + p.col, dz, p.skip);
-    };
-    constexpr int U = 2;
-    int64_t row = lo + p.rl;
-    for (; row + (U - 1) * p.rpb < hi; row += U * p.rpb) {
-      Gradient<T, V, X8> q[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) q[u].load(a, row + u * p.rpb, p);
-#pragma unroll
-      for (int u = 0; u < U; ++u) put(q[u], row + u * p.rpb);
-    }
-    for (; row < hi; row += p.rpb) {
-      Gradient<T, V, X8> q;
-      q.load(a, row, p);
-      put(q, row);
-    }
+               for (int e = 0; e < V; ++e) dz[e] = fmaf(dz[e], k.g[e], fmaf(h[e], k.c2[e], k.c1[e]));
+               if (q.row >= 0) store_pack<T, V>((T*)a.dx + q.row * a.dx_stride + p.col, dz, p.skip);
+             });
   });
+}
+
+// Small samples: both rows in registers; a workgroup's sums of dz h and dz over its samples
+// go to its row of the partial sums.
+template <typename T, int V, int NT, int NV, bool X8, bool SILU>
+__global__ void __launch_bounds__(NT) k_group_norm_bwd_small(GroupNormArgs a, int slice, int slices) {
+  extern __shared__ float smem[];
+  const Slice b(a, slice, slices);
+  const int per = a.cols / a.groups;
+  const Place<V> p(b.first, b.width, per, NT);
+  Totals tot{smem, b.width, p.rpb, NT};
+  float* total = smem + totals_floats(p.rpb, b.width);  // [2][width]
+  float* mean = total + 2 * b.width;                     // [2][groups]
+  const Params<V> w(a, p.col);
+  typedef Pair<T, V, X8> Q;
+  for (int i = threadIdx.x; i < 2 * b.width; i += NT) total[i] = 0.f;
+  for (int s = b.s0; s < a.batch; s += b.step) {
+    const int64_t lo = min(max(sample_begin(a, s), (int64_t)0), a.rows);
+    const int64_t hi = max(lo, min(sample_begin(a, s + 1), a.rows));
+    if (lo >= hi) continue;
+    const bool held = hi - lo <= (int64_t)p.rpb * NV;
+    Q q[NV];
+    if (held && p.on)
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (lo + p.rl + i * p.rpb < hi) q[i].load(a, lo + p.rl + i * p.rpb, p);
+    float m[V], r[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const int64_t at = (int64_t)s * a.groups + p.group[e];
+      m[e] = a.stats[at];
+      r[e] = a.stats[(int64_t)a.batch * a.groups + at];
+    }
+    auto rows = [&](auto&& run) {
+      if (!p.on) return;
+      float dz[V], h[V];
+      if (held) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          if (lo + p.rl + i * p.rpb < hi) {
+            q[i].template values<SILU>(a, p, w, m, r, dz, h);
+            run(dz, h, lo + p.rl + i * p.rpb);
+          }
+      } else {
+        for (int64_t row = lo + p.rl; row < hi; row += (int64_t)p.rpb * 4) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) q[i].load(a, min(row + (int64_t)i * p.rpb, hi - 1), p);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (row + (int64_t)i * p.rpb < hi) {
+              q[i].template values<SILU>(a, p, w, m, r, dz, h);
+              run(dz, h, row + (int64_t)i * p.rpb);
+            }
+        }
+      }
+    };
+    float sum[2][V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum[0][e] = sum[1][e] = 0.f;
+    rows([&](const float(&dz)[V], const float(&h)[V], int64_t) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        sum[0][e] += dz[e];
+        sum[1][e] += dz[e] * h[e];
+      }
+    });
+    const float rn = 1.f / ((float)(hi - lo) * (float)per);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      tot.put(p, b.first, sum[k]);
+      for (int i = threadIdx.x; i < b.width; i += NT) total[k * b.width + i] += tot.col(i);
+      group_totals(b.groups, per, [&](int c) { return tot.col(c) * (a.gain ? a.gain[b.first + c] : 1.f); },
+                   [&](int g, float v) { mean[k * b.groups + g] = v * rn; });
+    }
+    __syncthreads();
+    Slopes<V> k;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      k.g[e] = r[e] * w.gain[e];
+      k.c1[e] = -r[e] * mean[p.group[e] - b.g0];
+      k.c2[e] = -r[e] * mean[b.groups + p.group[e] - b.g0];
+    }
+    rows([&](const float(&dz)[V], const float(&h)[V], int64_t row) {
+      float o[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) o[e] = fmaf(dz[e], k.g[e], fmaf(h[e], k.c2[e], k.c1[e]));
+      store_pack<T, V>((T*)a.dx + row * a.dx_stride + p.col, o, p.skip);
+    });
+  }
+  for (int i = threadIdx.x; i < b.width; i += NT) {  // (each column is one thread's)
+    a.ws[(int64_t)b.s0 * a.cols + b.first + i] = total[b.width + i];
+    a.ws[((int64_t)b.step + b.s0) * a.cols + b.first + i] = total[i];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// how work is dealt
+
+// Elements of a thread's vector: 16 bytes of x; in the backward pass 8 bytes of bf16, whose
+// values and parameters take twice the registers (200001 rows of 100 in bf16: 19.1 + 25.1 us,
+// with eight elements 27.0 + 31.7; forward 589824 rows of 256: 141 us, with four 201).
+int vec_of(bool bf16, int cols, bool backward) {
+  const int ve = bf16 && !backward ? 8 : 4;
+  return cols < ve ? 1 : ve;
 }
 
 struct Deal {
   int threads, rpb;
   int64_t chunk;
   int chunks, most;  // and a bound on them that grows with the rows
+  bool join;         // few pieces a sample: they are joined by the last launch
 };
 
-Deal deal(bool bf16, int64_t rows, int32_t cols) {
-  const int ve = bf16 ? 8 : 4, v = cols < ve ? 1 : ve, nvec = (cols + v - 1) / v;
+Deal deal(bool bf16, int64_t rows, int32_t cols, int32_t batch, bool backward) {
+  const int v = vec_of(bf16, cols, backward), nvec = (cols + v - 1) / v;
   Deal d;
-  d.threads = nvec <= 256 ? 256 : nvec <= 512 ? 512 : 1024;
+  d.threads = nvec <= 256 ? 256 : v == 8 ? 512 : 1024;
   d.rpb = d.threads / nvec;
-  const int64_t most = 1024 * 256 / d.threads;  // workgroups that the compute units hold at once, or twice as many
+  const int64_t most = 1024 * 256 / d.threads;  // workgroups that the compute units hold at once
   const int64_t least = 8 * d.rpb;              // rows that pay for a workgroup's sums
   d.chunk = std::max(least, (rows + most - 1) / most);
   d.chunks = (int)((rows + d.chunk - 1) / d.chunk);
   d.most = (int)std::min(most, (rows + least - 1) / least);
+  d.join = d.chunks <= 16 * (int64_t)batch;
   return d;
 }
 
-int sum_lds(const Deal& d, int32_t cols, int extra) { return (std::max(d.rpb, 1) * cols + extra) * 4; }
+// Small samples.
+constexpr int SMALL_PARTS = 1024;  // workgroups of a slice
+// rows of a thread in registers: 128 bytes of x, or 64 of x and 64 of dy, with 256 threads
+constexpr int small_rows(int threads, bool bf16, bool backward) {
+  return (threads == 256 ? 1 : 2) * (backward ? (bf16 ? 8 : 4) : 8);
+}
+constexpr int SLICE_BYTES = 64;
+struct Small {
+  bool on;
+  int threads, slice, slices, parts, width;
+};
+Small small_of(bool bf16, int64_t rows, int32_t cols, int32_t groups, int32_t batch, bool backward) {
+  Small s{};
+  if (batch <= 0 || rows <= 0) return s;
+  const int per = cols / groups, size = bf16 ? 2 : 4;
+  // as many slices as make two workgroups a compute unit, of SLICE_BYTES at least, and the
+  // last one, which may be narrower, of a vector
+  const int most = std::max(1, std::min(groups, per * size * groups / SLICE_BYTES));
+  for (int want = std::min(most, std::max(1, (512 + batch - 1) / batch));; --want) {
+    s.slice = (groups + want - 1) / want;
+    s.slices = (groups + s.slice - 1) / s.slice;
+    if (s.slices == 1 || (groups - (s.slices - 1) * s.slice) * per >= vec_of(bf16, cols, backward)) break;
+  }
+  s.width = s.slice * per;
+  const int v = vec_of(bf16, s.width, backward), nvec = (s.width + v - 1) / v;
+  const double mean = (double)rows / batch;  // rows of a sample; the largest have several times as many
+  if (nvec > 512) return s;
+  s.threads = nvec <= 256 && 3.0 * mean <= 256 / nvec * small_rows(256, bf16, backward) ? 256 : 512;
+  s.parts = std::min(batch, SMALL_PARTS);
+  s.on = (batch == 1 ? 1.0 : 3.0) * mean <= s.threads / nvec * small_rows(s.threads, bf16, backward);
+  return s;
+}
 
-template <typename T, int V>
-hipError_t forward(const GroupNormArgs& a, hipStream_t st) {
-  if (a.batch <= 0) return hipSuccess;
-  const Deal d = deal(sizeof(T) == 2, a.rows, a.cols);
+int sum_lds(int rpb, int width, int extra) { return (totals_floats(rpb, width) + extra) * 4; }
+
+// LDS of a small kernel, `columns` and `each` floats beside the totals for every column and
+// group.  The last slice may be narrower than the others, and its rows be dealt to more lanes.
+template <int V>
+int small_lds(const Small& s, const GroupNormArgs& a, int columns, int each) {
+  const int last = a.groups - (s.slices - 1) * s.slice, per = a.cols / a.groups;
+  int most = 0;
+  for (const int groups : {s.slice, last}) {
+    const int width = groups * per;
+    most = std::max(most, sum_lds(s.threads / ((width + V - 1) / V), width, columns * width + each * groups));
+  }
+  return most;
+}
+
+template <typename T, int V, int NT, bool SILU>
+hipError_t forward_large(const GroupNormArgs& a, const Deal& d, hipStream_t st) {
   hipError_t e = hipSuccess;
   if (a.rows > 0) {
-    hipLaunchKernelGGL((k_group_norm_sums<T, V>), dim3(d.chunks), dim3(d.threads), sum_lds(d, a.cols, a.groups), st, a,
+    hipLaunchKernelGGL((k_group_norm_sums<T, V, NT>), dim3(d.chunks), dim3(NT), sum_lds(d.rpb, a.cols, a.groups), st, a,
                        d.chunk);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
+    if (d.join) {
+      hipLaunchKernelGGL((k_group_norm_rows<T, V, NT, SILU, true>), dim3(d.chunks), dim3(NT), 2 * a.groups * 4, st, a,
+                         d.chunk);
+      return hipGetLastError();
+    }
   }
   const int64_t items = ((int64_t)a.batch * a.groups + 3) / 4;
   hipLaunchKernelGGL(k_group_norm_stats, dim3((unsigned)std::min<int64_t>(items, 4096)), dim3(256), 0, st, a, d.chunk);
   e = hipGetLastError();
   if (e != hipSuccess || a.rows <= 0) return e;
-  hipLaunchKernelGGL((k_group_norm_rows<T, V>), dim3(d.chunks), dim3(d.threads), 0, st, a, d.chunk);
+  hipLaunchKernelGGL((k_group_norm_rows<T, V, NT, SILU, false>), dim3(d.chunks), dim3(NT), 0, st, a, d.chunk);
   return hipGetLastError();
 }
 
-template <typename T, int V, bool X8>
-hipError_t backward(const GroupNormArgs& a, hipStream_t st) {
-  const Deal d = deal(sizeof(T) == 2, a.rows, a.cols);
-  hipLaunchKernelGGL((k_group_norm_bwd_sums<T, V, X8>), dim3(d.chunks), dim3(d.threads), sum_lds(d, a.cols, 2 * a.cols),
-                     st, a, d.chunk);
+template <typename T, int V, int NT, bool SILU>
+hipError_t forward_small(const GroupNormArgs& a, const Small& s, hipStream_t st) {
+  constexpr auto kernel = k_group_norm_small<T, V, NT, small_rows(NT, sizeof(T) == 2, false), SILU>;
+  const int lds = small_lds<V>(s, a, 0, 2);
+  const hipError_t e = allow_lds<kernel>(lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3(s.parts * s.slices), dim3(NT), lds, st, a, s.slice, s.slices);
+  return hipGetLastError();
+}
+
+template <typename T, bool SILU>
+hipError_t forward(const GroupNormArgs& a, hipStream_t st) {
+  constexpr bool bf16 = sizeof(T) == 2;
+  constexpr int VE = bf16 ? 8 : 4, WIDE = bf16 ? 512 : 1024;
+  if (a.batch <= 0) return hipSuccess;
+  const Small s = small_of(bf16, a.rows, a.cols, a.groups, a.batch, false);
+  if (s.on) {
+    const bool scalar = s.width < VE;
+    if (s.threads == 256) return scalar ? forward_small<T, 1, 256, SILU>(a, s, st) : forward_small<T, VE, 256, SILU>(a, s, st);
+    return scalar ? forward_small<T, 1, 512, SILU>(a, s, st) : forward_small<T, VE, 512, SILU>(a, s, st);
+  }
+  const Deal d = deal(bf16, a.rows, a.cols, a.batch, false);
+  if (a.cols < VE) return forward_large<T, 1, 256, SILU>(a, d, st);
+  return d.threads == 256 ? forward_large<T, VE, 256, SILU>(a, d, st) : forward_large<T, VE, WIDE, SILU>(a, d, st);
+}
+
+template <typename T, int V, int NT, bool X8, bool SILU>
+hipError_t backward_large(const GroupNormArgs& a, const Deal& d, hipStream_t st) {
+  hipLaunchKernelGGL((k_group_norm_bwd_sums<T, V, NT, X8, SILU>), dim3(d.chunks), dim3(NT),
+                     sum_lds(d.rpb, a.cols, 2 * a.cols), st, a, d.chunk);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int per = a.cols / a.groups, slice = std::max(1, BWD_COLS / per);
+  if (d.join) {
+    constexpr auto kernel = k_group_norm_bwd_rows<T, V, NT, X8, SILU, true>;
+    const int lds = std::max(NT, join_floats(NT, a.cols) + 2 * a.groups) * 4;
+    e = allow_lds<kernel>(lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3(d.chunks + param_blocks<NT>(a.cols)), dim3(NT), lds, st, a, d.chunk, d.chunks);
+    return hipGetLastError();
+  }
+  const int per = a.cols / a.groups;
+  const int slice = (int)std::max<int64_t>(
+      1, std::min<int64_t>(BWD_COLS / per, (int64_t)a.batch * a.groups / 512));  // (enough workgroups first)
   const int blocks = (int)std::min<int64_t>((int64_t)a.batch * ((a.groups + slice - 1) / slice), 1 << 16);
-  const int width = std::min(slice, a.groups) * per, lds = std::max(1024, std::max(1, 1024 / width) * width) * 4;
-  hipLaunchKernelGGL(k_group_norm_bwd_means, dim3((unsigned)(blocks + 2 * ((a.cols + 63) / 64))), dim3(1024), lds, st, a,
-                     d.chunk, d.chunks, blocks, slice);
+  hipLaunchKernelGGL(k_group_norm_bwd_means, dim3((unsigned)(blocks + param_blocks<1024>(a.cols))), dim3(1024),
+                     std::max(1024, join_floats(1024, std::min(slice, a.groups) * per)) * 4, st, a, d.chunk, d.chunks,
+                     blocks, slice);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_group_norm_bwd_rows<T, V, X8>), dim3(d.chunks), dim3(d.threads), 0, st, a, d.chunk);
+  hipLaunchKernelGGL((k_group_norm_bwd_rows<T, V, NT, X8, SILU, false>), dim3(d.chunks), dim3(NT), 0, st, a, d.chunk,
+                     d.chunks);
   return hipGetLastError();
+}
+
+template <typename T, int V, int NT, bool X8, bool SILU>
+hipError_t backward_small(const GroupNormArgs& a, const Small& s, hipStream_t st) {
+  constexpr auto kernel = k_group_norm_bwd_small<T, V, NT, small_rows(NT, sizeof(T) == 2, true), X8, SILU>;
+  const int lds = small_lds<V>(s, a, 2, 2);
+  hipError_t e = allow_lds<kernel>(lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3(s.parts * s.slices), dim3(NT), lds, st, a, s.slice, s.slices);
+  e = hipGetLastError();
+  if (e != hipSuccess || (!a.dgain && !a.dshift)) return e;
+  hipLaunchKernelGGL(k_group_norm_params, dim3(param_blocks<1024>(a.cols)), dim3(1024), 0, st, a, s.parts);
+  return hipGetLastError();
+}
+
+template <typename T, bool X8, bool SILU>
+hipError_t backward(const GroupNormArgs& a, hipStream_t st) {
+  constexpr bool bf16 = sizeof(T) == 2;
+  const Small s = small_of(bf16, a.rows, a.cols, a.groups, a.batch, true);
+  if (s.on) {
+    const bool scalar = s.width < 4;
+    if (s.threads == 256)
+      return scalar ? backward_small<T, 1, 256, X8, SILU>(a, s, st) : backward_small<T, 4, 256, X8, SILU>(a, s, st);
+    return scalar ? backward_small<T, 1, 512, X8, SILU>(a, s, st) : backward_small<T, 4, 512, X8, SILU>(a, s, st);
+  }
+  const Deal d = deal(bf16, a.rows, a.cols, a.batch, true);
+  if (a.cols < 4) return backward_large<T, 1, 256, X8, SILU>(a, d, st);
+  return d.threads == 256 ? backward_large<T, 4, 256, X8, SILU>(a, d, st) : backward_large<T, 4, 1024, X8, SILU>(a, d, st);
 }
 
 }  // namespace
 
+// Either way of dealing: which one a call takes may differ with its rows.
 size_t group_norm_workspace(bool bf16, int64_t rows, int32_t cols, int32_t groups, int32_t batch, bool backward) {
   if (rows <= 0) return 0;
-  const Deal d = deal(bf16, rows, cols);
+  const Deal d = deal(bf16, rows, cols, batch, backward);
   const size_t pieces = (size_t)d.most + (size_t)batch;
   if (!backward) return pieces * 2 * (size_t)groups * 4;
-  return ((pieces + (size_t)d.most) * 2 * (size_t)cols + 2 * (size_t)batch * (size_t)groups) * 4;
+  const size_t large = ((pieces + (size_t)d.most) * 2 * (size_t)cols + 2 * (size_t)batch * (size_t)groups) * 4;
+  return std::max(large, (size_t)std::min(batch, SMALL_PARTS) * 2 * (size_t)cols * 4);
 }
 
 hipError_t launch_group_norm(bool bf16, const GroupNormArgs& a, hipStream_t st) {
-  if (bf16) return a.cols < 8 ? forward<__bf16, 1>(a, st) : forward<__bf16, 8>(a, st);
-  return a.cols < 4 ? forward<float, 1>(a, st) : forward<float, 4>(a, st);
+  if (bf16) return a.silu ? forward<__bf16, true>(a, st) : forward<__bf16, false>(a, st);
+  return a.silu ? forward<float, true>(a, st) : forward<float, false>(a, st);
 }
 
 hipError_t launch_group_norm_bwd(bool bf16, const GroupNormArgs& a, hipStream_t st) {
@@ -638,13 +1155,12 @@ hipError_t launch_group_norm_bwd(bool bf16, const GroupNormArgs& a, hipStream_t 
     const hipError_t e = a.dgain ? launch_fill_zero(a.dgain, (int64_t)a.cols * 4, st) : hipSuccess;
     return e == hipSuccess && a.dshift ? launch_fill_zero(a.dshift, (int64_t)a.cols * 4, st) : e;
   }
-  const bool x8 = a.codes;
-  if (bf16) {
-    if (a.cols < 8) return x8 ? backward<__bf16, 1, true>(a, st) : backward<__bf16, 1, false>(a, st);
-    return x8 ? backward<__bf16, 8, true>(a, st) : backward<__bf16, 8, false>(a, st);
+  if (a.codes) {
+    if (bf16) return a.silu ? backward<__bf16, true, true>(a, st) : backward<__bf16, true, false>(a, st);
+    return a.silu ? backward<float, true, true>(a, st) : backward<float, true, false>(a, st);
   }
-  if (a.cols < 4) return x8 ? backward<float, 1, true>(a, st) : backward<float, 1, false>(a, st);
-  return x8 ? backward<float, 4, true>(a, st) : backward<float, 4, false>(a, st);
+  if (bf16) return a.silu ? backward<__bf16, false, true>(a, st) : backward<__bf16, false, false>(a, st);
+  return a.silu ? backward<float, false, true>(a, st) : backward<float, false, false>(a, st);
 }
 
 }  // namespace sscn
