@@ -72,6 +72,7 @@ GroupNormArgs args_of(const sscn_group_norm& n, void* ws) {
   a.cols = n.cols;
   a.groups = n.groups;
   a.batch = n.batch;
+  a.per = n.cols / n.groups;
   a.begin = n.d_begin;
   a.span = n.batch > 0 ? n.rows / n.batch : 0;
   a.gain = n.d_gain;

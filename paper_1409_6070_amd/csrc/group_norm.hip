@@ -28,7 +28,10 @@
 
 #include "common.h"
 #include "kernels.h"
+#include "lanes.h"
 #include "rows8.h"
+
+#include <type_traits>
 
 namespace sscn {
 
@@ -66,9 +69,6 @@ __device__ inline void store_pack(T* p, const float (&f)[V], int skip) {
 template <typename T, int V, bool X8>
 struct Held {
   Pack<T, V> v;
-  __device__ inline void load(const GroupNormArgs& a, int64_t r, int col, int) {
-    v = load_pack<T, V>((const T*)a.x + r * a.x_stride + col);
-  }
   __device__ inline void values(float (&f)[V], int) const {
 #pragma unroll
     for (int e = 0; e < V; ++e) f[e] = Elem<T>::to_f32(v.e[e]);
@@ -77,17 +77,10 @@ struct Held {
 template <typename T, int V>
 struct Held<T, V, true> {
   uint32_t c[(V + 3) / 4];
-  uint32_t s;  // the scales of its two blocks
+  uint8_t s[2];  // the scales of its two blocks
   // split: elements before the next scale's block
-  __device__ inline void load(const GroupNormArgs& a, int64_t r, int col, int split) {
-    c[0] = 0;
-    __builtin_memcpy(c, a.codes + r * row8_code_stride(a.cols) + col, V);
-    const uint8_t* p = a.scales + r * row8_scale_stride(a.cols) + (col >> 7);
-    s = p[0];
-    if (split < V) s |= (uint32_t)p[1] << 8;
-  }
   __device__ inline void values(float (&f)[V], int split) const {
-    const float s0 = row8_pow2(s & 255u), s1 = row8_pow2(s >> 8);
+    const float s0 = row8_pow2(s[0]), s1 = row8_pow2(s[1]);
     if constexpr (V == 1) {
       float t[4];
       row8_values4(c[0], s0, t);
@@ -101,6 +94,46 @@ struct Held<T, V, true> {
 #pragma unroll
       for (int e = 0; e < V; ++e) f[e] *= e < split ? s0 : s1;
     }
+  }
+};
+
+// Where a thread's rows lie: `at` its first one's vector, `step` bytes from one of its rows to
+// the next.
+template <typename T, int V>
+struct From {
+  const char* at;
+  int64_t step;
+  __device__ inline From(const void* base, int64_t stride, int64_t row, int col, int rpb)
+      : at((const char*)base + (row * stride + col) * (int64_t)sizeof(T)), step(stride * (int64_t)sizeof(T) * rpb) {}
+  __device__ inline void load(Pack<T, V>& v, int k) const { v = load_pack<T, V>((const T*)(at + k * step)); }
+  __device__ inline T* put(int k) const { return (T*)(const_cast<char*>(at) + k * step); }
+};
+template <typename T, int V, bool X8>
+struct FromX {
+  From<T, V> f;
+  __device__ inline FromX(const GroupNormArgs& a, int64_t row, int col, int, int rpb)
+      : f(a.x, a.x_stride, row, col, rpb) {}
+  __device__ inline void load(Held<T, V, X8>& h, int k) const { f.load(h.v, k); }
+};
+template <typename T, int V>
+struct FromX<T, V, true> {
+  const uint8_t* codes;
+  const uint8_t* scales;
+  int64_t step, sstep;
+  int split;
+  __device__ inline FromX(const GroupNormArgs& a, int64_t row, int col, int split, int rpb) : split(split) {
+    const int64_t cs = row8_code_stride(a.cols), ss = row8_scale_stride(a.cols);
+    codes = a.codes + row * cs + col;
+    scales = a.scales + row * ss + (col >> 7);
+    step = cs * rpb;
+    sstep = ss * rpb;
+  }
+  __device__ inline void load(Held<T, V, true>& h, int k) const {
+    h.c[0] = 0;
+    __builtin_memcpy(h.c, codes + k * step, V);
+    const uint8_t* p = scales + k * sstep;
+    h.s[0] = p[0];
+    h.s[1] = p[split < V ? 1 : 0];
   }
 };
 
@@ -134,12 +167,6 @@ __device__ inline float gradient(float dy, float h, float gain, float shift, flo
   return (slope == 0.f ? z > 0.f : z >= 0.f) ? dy : dy * slope;
 }
 
-// Sums over lanes of aligned groups of L = 1, 8, 64.
-__device__ inline float lanes_sum(float s, int L) {
-  for (int d = 1; d < L; d *= 2) s += __shfl_xor(s, d);
-  return s;
-}
-
 __device__ inline int64_t sample_begin(const GroupNormArgs& a, int s) { return a.begin ? a.begin[s] : s * a.span; }
 
 // The last sample that starts at row r or before it (-1: none; batch: r lies behind the
@@ -160,15 +187,18 @@ __device__ inline Span span_of(const GroupNormArgs& a, int64_t r) {
   while (hi - lo > 1) {
     const int step = (hi - lo - 1 + 255) / 256;
     int32_t v[4];
+    uint32_t at[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // (below 2^31 + 256 steps: no overflow)
+      at[i] = (uint32_t)(lo + 1) + (uint32_t)(i * 64 + lane) * (uint32_t)step;
+      v[i] = a.begin[min(at[i], (uint32_t)a.batch)];
+    }
     int m = 0;  // probes at r or before it
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t at = (int64_t)lo + 1 + (int64_t)(i * 64 + lane) * step;
-      v[i] = a.begin[min(at, (int64_t)a.batch)];
-      m += at < hi && v[i] <= r ? 1 : 0;
-    }
-    m = (int)lanes_sum((float)m, 64);
-    auto probe = [&](int k) { return __shfl(k < 64 ? v[0] : k < 128 ? v[1] : k < 192 ? v[2] : v[3], k & 63); };
+    for (int i = 0; i < 4; ++i) m += __popcll(__ballot(at[i] < (uint32_t)hi && v[i] <= r));
+    auto probe = [&](int k) {
+      return __builtin_amdgcn_readlane(k < 64 ? v[0] : k < 128 ? v[1] : k < 192 ? v[2] : v[3], k & 63);
+    };
     const int64_t top = (int64_t)lo + 1 + (int64_t)m * step;
     if (m > 0) {
       lo = lo + 1 + (m - 1) * step;
@@ -179,8 +209,7 @@ __device__ inline Span span_of(const GroupNormArgs& a, int64_t r) {
       end = probe(m);
     }
   }
-  return Span{__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(begin),
-              __builtin_amdgcn_readfirstlane(end)};
+  return Span{lo, begin, end};
 }
 
 // Calls run(sample's span, first row, end) for the samples' parts of rows r0 .. r1 - 1, in
@@ -204,16 +233,23 @@ struct Place {
   int rl, rpb, col, skip, split, group[V];
   bool on;
   __device__ inline Place(int first, int width, int per, int nt) {
-    const int nvec = (width + V - 1) / V, t = threadIdx.x % nvec;
+    const int nvec = (width + V - 1) / V;
     rpb = nt / nvec;
     rl = threadIdx.x / nvec;
+    const int t = threadIdx.x - rl * nvec;
     on = rl < rpb;
     const int at = min(t * V, width - V);
     col = first + at;
     skip = t * V - at;
     split = min(V, ROW8_BLOCK - (col & (ROW8_BLOCK - 1)));
+    group[0] = col / per;
+    int left = per - (col - group[0] * per);  // columns of the group from here on
 #pragma unroll
-    for (int e = 0; e < V; ++e) group[e] = (col + e) / per;
+    for (int e = 1; e < V; ++e) {
+      --left;
+      group[e] = group[e - 1] + (left == 0 ? 1 : 0);
+      left = left == 0 ? per : left;
+    }
   }
 };
 
@@ -276,29 +312,32 @@ __host__ __device__ inline int totals_floats(int rpb, int width) {
   return (rpb > 0 ? rpb : 1) * width + (rpb > FEW ? FEW * width : 0);
 }
 
-// lanes that share a group's sum
-__device__ inline int lanes_of(int per) { return per <= 4 ? 1 : per <= 64 ? 8 : 64; }
-
 // done(group, sum of value(c) over its columns c, counted from the slice's first) for the
 // `groups` groups of a slice, by the first of each group's lanes.
-template <class Value, class Done>
-__device__ inline void group_totals(int groups, int per, Value&& value, Done&& done) {
-  const int L = lanes_of(per), sub = threadIdx.x % L;
+template <int L, class Value, class Done>
+__device__ inline void group_totals_by(int groups, int per, Value&& value, Done&& done) {
+  const int sub = threadIdx.x % L;
   for (int g = threadIdx.x / L; g < groups; g += blockDim.x / L) {
     float s = 0.f;
     for (int c = sub; c < per; c += L) s += value(g * per + c);
-    s = lanes_sum(s, L);
+    if constexpr (L > 1) s = group_sum<L>(s);
     if (sub == 0) done(g, s);
   }
+}
+template <class Value, class Done>
+__device__ inline void group_totals(int groups, int per, Value&& value, Done&& done) {
+  if (per <= 4) group_totals_by<1>(groups, per, value, done);
+  else if (per <= 64) group_totals_by<8>(groups, per, value, done);
+  else group_totals_by<64>(groups, per, value, done);
 }
 
 // Sum of value(k) for k = first, first + step, .. below end, U at a time in flight (none of
 // them alone behind the last whole group: a trip through memory for each would be most of
 // a short sum's time).
 template <int U, class Value>
-__device__ inline float strided_sum(int64_t first, int64_t end, int64_t step, Value&& value) {
+__device__ inline float strided_sum(int first, int end, int step, Value&& value) {
   float s = 0.f;
-  for (int64_t k = first; k < end; k += U * step) {
+  for (int k = first; k < end; k += U * step) {
     float v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) v[u] = value(min(k + u * step, end - 1));
@@ -308,36 +347,45 @@ __device__ inline float strided_sum(int64_t first, int64_t end, int64_t step, Va
   return s;
 }
 
-// A thread's rows first + rl, + rpb, .. of a run, U of them in flight.  load(q, row) brings
-// one, mask(q) empties what lies behind the run, add(q) takes it.  The first U rows of a
-// chunk are loaded (within `end`) before its samples are known.
+// The rows of a run of `count` that a thread takes: n of them, `all` that every thread has and
+// `most` that any has.  Threads without any stay at the run's last row.
+struct Share {
+  int rl, n, all, most;
+  __device__ inline Share(int count, int rl_, int rpb, bool on) {
+    rl = min(rl_, count - 1);
+    all = count / rpb;
+    most = all + (all * rpb < count ? 1 : 0);
+    n = on ? all + (rl_ < count - all * rpb ? 1 : 0) : 0;
+  }
+};
+
+// U of a thread's rows in flight.  take(q, k, valid) gets row k; `valid` is the constant true
+// where every thread has that many.
 template <class Q, int U>
 struct Stream {
   Q q[U];
-  template <class Load>
-  __device__ inline void start(int64_t first, int64_t end, int rl, int rpb, Load&& load) {
+  template <class F>
+  __device__ inline void fetch(const F& from, int i, int last) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) load(q[u], min(first + rl + (int64_t)u * rpb, end - 1));
+    for (int u = 0; u < U; ++u) from.load(q[u], min(i + u, last));
   }
-  // started: q holds the run's first rows
-  template <class Load, class Mask, class Add>
-  __device__ inline void run(bool started, int64_t lo, int64_t hi, int rl, int rpb, Load&& load, Mask&& mask, Add&& add) {
-    int64_t row = lo + rl;
-    if (!started) start(lo, hi, rl, rpb, load);
-    for (; row + (int64_t)(U - 1) * rpb < hi;) {
+  // the first rows have been fetched
+  template <class F, class Take>
+  __device__ inline void run(const F& from, const Share& s, Take&& take) {
+    int i = 0;
+    for (; i + U <= s.all; i += U) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) add(q[u]);
-      row += (int64_t)U * rpb;
-      if (row < hi)
+      for (int u = 0; u < U; ++u) take(q[u], i + u, std::true_type{});
+      if (i + 2 * U <= s.all) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) load(q[u], min(row + (int64_t)u * rpb, hi - 1));
+        for (int u = 0; u < U; ++u) from.load(q[u], i + U + u);
+      } else if (i + U < s.most) {
+        fetch(from, i + U, max(s.n - 1, 0));
+      }
     }
+    if (i < s.most)
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (row + (int64_t)u * rpb >= hi) mask(q[u]);
-    if (row < hi)
-#pragma unroll
-      for (int u = 0; u < U; ++u) add(q[u]);
+      for (int u = 0; u < U; ++u) take(q[u], i + u, i + u < s.n);
   }
 };
 
@@ -360,19 +408,20 @@ template <int L>
 __device__ inline Stats join_pieces(const GroupNormArgs& a, int64_t chunk, const Span& s, int g, int lane) {
   const int64_t lo = max(s.begin, (int64_t)0), hi = min(s.end, a.rows);
   if (lo >= hi) return Stats{0.f, 1.f / sqrtf(a.eps)};
-  const int per = a.cols / a.groups;
-  const int64_t c0 = lo / chunk, c1 = (hi - 1) / chunk;
-  const float n = (float)(hi - lo) * (float)per;
-  const float* part = a.ws + (int64_t)s.s * 2 * a.groups + 2 * g;
-  auto rows = [&](int64_t c) { return (float)(min(hi, (c + 1) * chunk) - max(lo, c * chunk)) * (float)per; };
+  const int c0 = (int)(lo / chunk), pieces = (int)((hi - 1) / chunk) - c0 + 1;
+  const float n = (float)(int)(hi - lo) * (float)a.per;
+  const float* part = a.ws + ((int64_t)c0 + s.s) * 2 * a.groups + 2 * g;
+  const int step = 2 * a.groups;
+  auto rows = [&](int k) {
+    const int64_t c = (c0 + k) * chunk;
+    return (float)(int)(min(hi, c + chunk) - max(lo, c)) * (float)a.per;
+  };
   const float mean =
-      lanes_sum(strided_sum<4>(c0 + lane, c1 + 1, L, [&](int64_t c) { return rows(c) * part[c * 2 * a.groups]; }), L) / n;
-  const float m2 = lanes_sum(strided_sum<4>(c0 + lane, c1 + 1, L,
-                                            [&](int64_t c) {
-                                              const float d = part[c * 2 * a.groups] - mean;
-                                              return part[c * 2 * a.groups + 1] + rows(c) * d * d;
-                                            }),
-                             L);
+      group_sum<L>(strided_sum<4>(lane, pieces, L, [&](int k) { return rows(k) * part[k * step]; })) / n;
+  const float m2 = group_sum<L>(strided_sum<4>(lane, pieces, L, [&](int k) {
+    const float d = part[k * step] - mean;
+    return part[k * step + 1] + rows(k) * d * d;
+  }));
   return Stats{mean, 1.f / sqrtf(m2 / n + a.eps)};
 }
 
@@ -380,55 +429,52 @@ __device__ inline Stats join_pieces(const GroupNormArgs& a, int64_t chunk, const
 template <typename T, int V, int NT>
 __global__ void __launch_bounds__(NT) k_group_norm_sums(GroupNormArgs a, int64_t chunk) {
   extern __shared__ float smem[];
-  const int per = a.cols / a.groups;
-  const Place<V> p(0, a.cols, per, NT);
-  Totals tot{smem, a.cols, p.rpb, NT};
-  float* mean = smem + totals_floats(p.rpb, a.cols);  // [groups]
+  const Place<V> p(0, a.cols, a.per, NT);
   const int64_t c = blockIdx.x, r0 = c * chunk, r1 = min(a.rows, r0 + chunk);
   typedef Held<T, V, false> Q;
-  auto load = [&](Q& q, int64_t row) { q.load(a, row, p.col, p.split); };
+  typedef FromX<T, V, false> X;
+  const Share whole((int)(r1 - r0), p.rl, p.rpb, p.on);
+  const X first(a, r0 + whole.rl, p.col, p.split, p.rpb);
   Stream<Q, 8> rows;
-  rows.start(r0, r1, p.rl, p.rpb, load);
+  rows.fetch(first, 0, max(whole.n - 1, 0));
+  Totals tot{smem, a.cols, p.rpb, NT};
+  float* mean = smem + totals_floats(p.rpb, a.cols);  // [groups]
   if (a.begin)  // samples without rows have no piece
     for (int64_t b = c * NT + threadIdx.x; b < a.batch; b += (int64_t)gridDim.x * NT)
       if (a.begin[b] >= a.begin[b + 1]) empty_stats(a, b);
   pieces_of(a, r0, r1, [&](const Span& s, int64_t lo, int64_t hi) {
+    const Share h((int)(hi - lo), p.rl, p.rpb, p.on);
+    const X x(a, lo + h.rl, p.col, p.split, p.rpb);
+    if (lo > r0) rows.fetch(x, 0, max(h.n - 1, 0));
     float pivot[V], s1[V], s2[V];
+    rows.q[0].values(pivot, p.split);
 #pragma unroll
-    for (int e = 0; e < V; ++e) pivot[e] = s1[e] = s2[e] = 0.f;
-    float n = 0.f;
-    if (p.on && lo + p.rl < hi) {
-      n = (float)((hi - lo - p.rl + p.rpb - 1) / p.rpb);
-      if (lo > r0) rows.start(lo, hi, p.rl, p.rpb, load);
-      const Q first = rows.q[0];
-      first.values(pivot, p.split);
-      rows.run(true, lo, hi, p.rl, p.rpb, load, [&](Q& q) { q = first; },
-               [&](const Q& q) {
-                 float f[V];
-                 q.values(f, p.split);
+    for (int e = 0; e < V; ++e) s1[e] = s2[e] = 0.f;
+    rows.run(x, h, [&](const Q& q, int, auto valid) {
+      float f[V];
+      q.values(f, p.split);
 #pragma unroll
-                 for (int e = 0; e < V; ++e) {
-                   const float d = f[e] - pivot[e];
-                   s1[e] += d;
-                   s2[e] += d * d;
-                 }
-               });
-    }
-    const float rn = n > 0.f ? 1.f / n : 0.f, count = (float)(hi - lo) * (float)per;
+      for (int e = 0; e < V; ++e) {
+        const float d = valid ? f[e] - pivot[e] : 0.f;
+        s1[e] += d;
+        s2[e] += d * d;
+      }
+    });
+    const float n = (float)h.n, rn = h.n ? 1.f / n : 0.f, count = (float)(int)(hi - lo) * (float)a.per;
     float v[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = s1[e] + n * pivot[e];
+    for (int e = 0; e < V; ++e) v[e] = h.n ? s1[e] + n * pivot[e] : 0.f;
     tot.put(p, 0, v);
-    group_totals(a.groups, per, [&](int col) { return tot.col(col); }, [&](int g, float sum) { mean[g] = sum / count; });
+    group_totals(a.groups, a.per, [&](int col) { return tot.col(col); }, [&](int g, float sum) { mean[g] = sum / count; });
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       const float d = pivot[e] + s1[e] * rn - mean[p.group[e]];
-      v[e] = n > 0.f ? (s2[e] - s1[e] * s1[e] * rn) + n * d * d : 0.f;
+      v[e] = h.n ? (s2[e] - s1[e] * s1[e] * rn) + n * d * d : 0.f;
     }
     tot.put(p, 0, v);
     float* out = a.ws + (c + s.s) * 2 * a.groups;
-    group_totals(a.groups, per, [&](int col) { return tot.col(col); },
+    group_totals(a.groups, a.per, [&](int col) { return tot.col(col); },
                  [&](int g, float sum) {
                    out[2 * g] = mean[g];
                    out[2 * g + 1] = sum;
@@ -456,20 +502,19 @@ __global__ void __launch_bounds__(256) k_group_norm_stats(GroupNormArgs a, int64
 template <typename T, int V, int NT, bool SILU, bool JOIN>
 __global__ void __launch_bounds__(NT) k_group_norm_rows(GroupNormArgs a, int64_t chunk) {
   extern __shared__ float smem[];  // JOIN: [2][groups]
-  const Place<V> p(0, a.cols, a.cols / a.groups, NT);
+  const Place<V> p(0, a.cols, a.per, NT);
   const int64_t c = (int64_t)gridDim.x - 1 - blockIdx.x, r0 = c * chunk, r1 = min(a.rows, r0 + chunk);
-  struct Q {
-    Held<T, V, false> x;
-    int64_t row;
-  };
-  auto load = [&](Q& q, int64_t row) {
-    q.x.load(a, row, p.col, p.split);
-    q.row = row;
-  };
+  typedef Held<T, V, false> Q;
+  typedef FromX<T, V, false> X;
+  const Share whole((int)(r1 - r0), p.rl, p.rpb, p.on);
+  const X first(a, r0 + whole.rl, p.col, p.split, p.rpb);
   Stream<Q, 4> rows;
-  rows.start(r0, r1, p.rl, p.rpb, load);
+  rows.fetch(first, 0, max(whole.n - 1, 0));
   const Params<V> w(a, p.col);
   pieces_of(a, r0, r1, [&](const Span& s, int64_t lo, int64_t hi) {
+    const Share h((int)(hi - lo), p.rl, p.rpb, p.on);
+    const X x(a, lo + h.rl, p.col, p.split, p.rpb);
+    if (lo > r0) rows.fetch(x, 0, max(h.n - 1, 0));
     const int64_t all = (int64_t)a.batch * a.groups, at = (int64_t)s.s * a.groups;
     float mean[V], r[V];
     if constexpr (JOIN) {
@@ -492,16 +537,15 @@ __global__ void __launch_bounds__(NT) k_group_norm_rows(GroupNormArgs a, int64_t
       mean[e] = JOIN ? smem[p.group[e]] : a.stats[at + p.group[e]];
       r[e] = JOIN ? smem[a.groups + p.group[e]] : a.stats[all + at + p.group[e]];
     }
-    if (!p.on) return;
-    rows.run(lo == r0, lo, hi, p.rl, p.rpb, load, [&](Q& q) { q.row = -1; },
-             [&](const Q& q) {
-               float f[V];
-               q.x.values(f, p.split);
+    const From<T, V> y(a.y, a.y_stride, lo + h.rl, p.col, p.rpb);
+    rows.run(x, h, [&](const Q& q, int k, auto valid) {
+      float f[V];
+      q.values(f, p.split);
 #pragma unroll
-               for (int e = 0; e < V; ++e)
-                 f[e] = activated<SILU>(affine(normal(f[e], mean[e], r[e]), w.gain[e], w.shift[e]), a.slope);
-               if (q.row >= 0) store_pack<T, V>((T*)a.y + q.row * a.y_stride + p.col, f, p.skip);
-             });
+      for (int e = 0; e < V; ++e)
+        f[e] = activated<SILU>(affine(normal(f[e], mean[e], r[e]), w.gain[e], w.shift[e]), a.slope);
+      if (valid && p.on) store_pack<T, V>(y.put(k), f, p.skip);
+    });
   });
 }
 
@@ -509,8 +553,9 @@ __global__ void __launch_bounds__(NT) k_group_norm_rows(GroupNormArgs a, int64_t
 struct Slice {
   int first, width, g0, groups, s0, step;
   __device__ inline Slice(const GroupNormArgs& a, int slice, int slices) {
-    const int k = blockIdx.x % slices, per = a.cols / a.groups;
+    const int per = a.per;
     s0 = blockIdx.x / slices;
+    const int k = blockIdx.x - s0 * slices;
     step = gridDim.x / slices;
     g0 = k * slice;
     groups = min(slice, a.groups - g0);
@@ -524,7 +569,7 @@ template <typename T, int V, int NT, int NV, bool SILU>
 __global__ void __launch_bounds__(NT) k_group_norm_small(GroupNormArgs a, int slice, int slices) {
   extern __shared__ float smem[];
   const Slice b(a, slice, slices);
-  const int per = a.cols / a.groups;
+  const int per = a.per;
   const Place<V> p(b.first, b.width, per, NT);
   Totals tot{smem, b.width, p.rpb, NT};
   float* mean = smem + totals_floats(p.rpb, b.width);  // [groups], then 1 / deviation
@@ -534,41 +579,42 @@ __global__ void __launch_bounds__(NT) k_group_norm_small(GroupNormArgs a, int sl
   for (int s = b.s0; s < a.batch; s += b.step) {
     const int64_t lo = min(max(sample_begin(a, s), (int64_t)0), a.rows);
     const int64_t hi = max(lo, min(sample_begin(a, s + 1), a.rows));
-    const bool held = hi - lo <= (int64_t)p.rpb * NV;
+    const Share h((int)(hi - lo), p.rl, p.rpb, p.on);
+    const bool held = h.most <= NV;
+    const FromX<T, V, false> x(a, lo + max(h.rl, 0), p.col, p.split, p.rpb);
     Q q[NV];
-    if (held && p.on)
+    if (held)
 #pragma unroll
       for (int i = 0; i < NV; ++i)
-        if (lo + p.rl + i * p.rpb < hi) q[i].load(a, lo + p.rl + i * p.rpb, p.col, p.split);
-    // run(values, row) for this thread's rows
+        if (i < h.n) x.load(q[i], i);
+    // run(values, k) for this thread's rows
     auto rows = [&](auto&& run) {
-      if (!p.on) return;
       float f[V];
       if (held) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-          if (lo + p.rl + i * p.rpb < hi) {
+          if (i < h.n) {
             q[i].values(f, p.split);
-            run(f, lo + p.rl + i * p.rpb);
+            run(f, i);
           }
       } else {
-        for (int64_t row = lo + p.rl; row < hi; row += (int64_t)p.rpb * 8) {
+        for (int k = 0; k < h.n; k += 8) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) q[i].load(a, min(row + (int64_t)i * p.rpb, hi - 1), p.col, p.split);
+          for (int i = 0; i < 8; ++i) x.load(q[i], min(k + i, h.n - 1));
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            if (row + (int64_t)i * p.rpb < hi) {
+            if (k + i < h.n) {
               q[i].values(f, p.split);
-              run(f, row + (int64_t)i * p.rpb);
+              run(f, k + i);
             }
         }
       }
     };
-    const float count = (float)(hi - lo) * (float)per;
+    const float count = (float)(int)(hi - lo) * (float)per;
     float v[V], m[V], r[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] = 0.f;
-    rows([&](const float(&f)[V], int64_t) {
+    rows([&](const float(&f)[V], int) {
 #pragma unroll
       for (int e = 0; e < V; ++e) v[e] += f[e];
     });
@@ -581,7 +627,7 @@ __global__ void __launch_bounds__(NT) k_group_norm_small(GroupNormArgs a, int sl
       m[e] = mean[p.group[e] - b.g0];
       v[e] = 0.f;
     }
-    rows([&](const float(&f)[V], int64_t) {
+    rows([&](const float(&f)[V], int) {
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const float d = f[e] - m[e];
@@ -600,11 +646,12 @@ __global__ void __launch_bounds__(NT) k_group_norm_small(GroupNormArgs a, int sl
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < V; ++e) r[e] = dev[p.group[e] - b.g0];
-    rows([&](const float(&f)[V], int64_t row) {
+    const From<T, V> y(a.y, a.y_stride, lo + max(h.rl, 0), p.col, p.rpb);
+    rows([&](const float(&f)[V], int k) {
       float o[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) o[e] = activated<SILU>(affine(normal(f[e], m[e], r[e]), w.gain[e], w.shift[e]), a.slope);
-      store_pack<T, V>((T*)a.y + row * a.y_stride + p.col, o, p.skip);
+      store_pack<T, V>(y.put(k), o, p.skip);
     });
   }
 }
@@ -616,17 +663,6 @@ template <typename T, int V, bool X8>
 struct Pair {
   Held<T, V, X8> x;
   Pack<T, V> d;
-  int64_t row;
-  __device__ inline void load(const GroupNormArgs& a, int64_t r, const Place<V>& p) {
-    x.load(a, r, p.col, p.split);
-    d = load_pack<T, V>((const T*)a.dy + r * a.dy_stride + p.col);
-    row = r;
-  }
-  __device__ inline void empty() {
-#pragma unroll
-    for (int e = 0; e < V; ++e) d.e[e] = Elem<T>::from_f32(0.f);
-    row = -1;
-  }
   template <bool SILU>
   __device__ inline void values(const GroupNormArgs& a, const Place<V>& p, const Params<V>& w, const float (&mean)[V],
                                 const float (&r)[V], float (&dz)[V], float (&h)[V]) const {
@@ -636,6 +672,18 @@ struct Pair {
       h[e] = normal(h[e], mean[e], r[e]);
       dz[e] = gradient<SILU>(Elem<T>::to_f32(d.e[e]), h[e], w.gain[e], w.shift[e], a.slope);
     }
+  }
+};
+
+template <typename T, int V, bool X8>
+struct FromBoth {
+  FromX<T, V, X8> x;
+  From<T, V> d;
+  __device__ inline FromBoth(const GroupNormArgs& a, int64_t row, const Place<V>& p)
+      : x(a, row, p.col, p.split, p.rpb), d(a.dy, a.dy_stride, row, p.col, p.rpb) {}
+  __device__ inline void load(Pair<T, V, X8>& q, int k) const {
+    x.load(q.x, k);
+    d.load(q.d, k);
   }
 };
 
@@ -663,18 +711,23 @@ __device__ inline BwdParts bwd_parts(const GroupNormArgs& a, int64_t parts) {
 template <typename T, int V, int NT, bool X8, bool SILU>
 __global__ void __launch_bounds__(NT) k_group_norm_bwd_sums(GroupNormArgs a, int64_t chunk) {
   extern __shared__ float smem[];
-  const Place<V> p(0, a.cols, a.cols / a.groups, NT);
+  const Place<V> p(0, a.cols, a.per, NT);
+  const int64_t c = blockIdx.x, r0 = c * chunk, r1 = min(a.rows, r0 + chunk);
+  typedef Pair<T, V, X8> Q;
+  typedef FromBoth<T, V, X8> X;
+  const Share whole((int)(r1 - r0), p.rl, p.rpb, p.on);
+  const X first(a, r0 + whole.rl, p);
+  Stream<Q, 4> rows;
+  rows.fetch(first, 0, max(whole.n - 1, 0));
   Totals tot{smem, a.cols, p.rpb, NT};
   float* total = smem + totals_floats(p.rpb, a.cols);  // [2][cols]
-  const int64_t c = blockIdx.x, r0 = c * chunk, r1 = min(a.rows, r0 + chunk);
   const BwdParts parts = bwd_parts(a, gridDim.x);
   const Params<V> w(a, p.col);
-  typedef Pair<T, V, X8> Q;
-  auto load = [&](Q& q, int64_t row) { q.load(a, row, p); };
-  Stream<Q, 4> rows;
-  rows.start(r0, r1, p.rl, p.rpb, load);
   for (int i = threadIdx.x; i < 2 * a.cols; i += NT) total[i] = 0.f;
   pieces_of(a, r0, r1, [&](const Span& s, int64_t lo, int64_t hi) {
+    const Share h((int)(hi - lo), p.rl, p.rpb, p.on);
+    const X x(a, lo + h.rl, p);
+    if (lo > r0) rows.fetch(x, 0, max(h.n - 1, 0));
     float mean[V], r[V], sum[2][V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
@@ -683,17 +736,15 @@ __global__ void __launch_bounds__(NT) k_group_norm_bwd_sums(GroupNormArgs a, int
       r[e] = a.stats[(int64_t)a.batch * a.groups + at];
       sum[0][e] = sum[1][e] = 0.f;
     }
-    if (p.on)
-      rows.run(lo == r0, lo, hi, p.rl, p.rpb, load, [&](Q& q) { q.empty(); },
-               [&](const Q& q) {
-                 float dz[V], h[V];
-                 q.template values<SILU>(a, p, w, mean, r, dz, h);
+    rows.run(x, h, [&](const Q& q, int, auto valid) {
+      float dz[V], h[V];
+      q.template values<SILU>(a, p, w, mean, r, dz, h);
 #pragma unroll
-                 for (int e = 0; e < V; ++e) {
-                   sum[0][e] += dz[e];
-                   sum[1][e] += dz[e] * h[e];
-                 }
-               });
+      for (int e = 0; e < V; ++e) {
+        sum[0][e] += valid ? dz[e] : 0.f;
+        sum[1][e] += valid ? dz[e] * h[e] : 0.f;
+      }
+    });
     float* out = parts.piece + (c + s.s) * 2 * a.cols;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -720,7 +771,7 @@ __device__ inline void param_sums(const GroupNormArgs& a, const float* chunk, in
   const int at = threadIdx.x % COLS, c = (block - which * cb) * COLS + at, sl = threadIdx.x / COLS;
   const float* p = chunk + (int64_t)which * parts * a.cols;
   float* out = which ? a.dshift : a.dgain;
-  float v = c < a.cols ? strided_sum<16>(sl, parts, 16, [&](int64_t k) { return p[k * a.cols + c]; }) : 0.f;
+  float v = c < a.cols ? strided_sum<16>(sl, parts, 16, [&](int k) { return p[(int64_t)k * a.cols + c]; }) : 0.f;
   smem[sl * COLS + at] = v;
   __syncthreads();
   if (sl == 0 && c < a.cols && out) {
@@ -744,28 +795,29 @@ template <int NT, class Done>
 __device__ inline void join_means(const GroupNormArgs& a, const float* piece, int64_t chunk, const Span& s, int first,
                                   int groups, int per, float* smem, Done&& done) {
   const int64_t lo = max(s.begin, (int64_t)0), hi = min(s.end, a.rows);
-  const int64_t c0 = lo / chunk, c1 = (hi - 1) / chunk;
-  const float rn = 1.f / ((float)(hi - lo) * (float)per);
-  const int width = groups * per, lanes = (int)min((int64_t)max(1, NT / width), c1 - c0 + 1);
+  const int64_t c0 = lo / chunk;
+  const int pieces = (int)((hi - 1) / chunk - c0) + 1, step = 2 * a.cols;
+  const float rn = 1.f / ((float)(int)(hi - lo) * (float)per);
+  const int width = groups * per, lanes = min(max(1, NT / width), pieces);
   __syncthreads();  // (what smem held has been read)
   for (int i = threadIdx.x; i < lanes * width; i += NT) {
     const int l = i / width, col = first + i - l * width;
-    const float* q = piece + (int64_t)s.s * 2 * a.cols + col;
+    const float* q = piece + (c0 + s.s) * step + col;
     const float g = a.gain ? a.gain[col] : 1.f;
     float u = 0.f, v = 0.f;
     constexpr int U = 8;
-    for (int64_t c = c0 + l; c <= c1; c += U * lanes) {
+    for (int c = l; c < pieces; c += U * lanes) {
       float x[U], y[U];
 #pragma unroll
       for (int k = 0; k < U; ++k) {
-        const int64_t at = min(c + k * lanes, c1) * 2 * a.cols;
+        const int64_t at = (int64_t)min(c + k * lanes, pieces - 1) * step;
         x[k] = q[at];
         y[k] = q[at + a.cols];
       }
 #pragma unroll
       for (int k = 0; k < U; ++k) {
-        u += c + k * lanes <= c1 ? x[k] : 0.f;
-        v += c + k * lanes <= c1 ? y[k] : 0.f;
+        u += c + k * lanes < pieces ? x[k] : 0.f;
+        v += c + k * lanes < pieces ? y[k] : 0.f;
       }
     }
     smem[i] = u * g;
@@ -797,7 +849,7 @@ __global__ void __launch_bounds__(1024) k_group_norm_bwd_means(GroupNormArgs a, 
     param_sums<1024>(a, parts.chunk, chunks, (int)blockIdx.x - sample_blocks, smem);
     return;
   }
-  const int per = a.cols / a.groups, slices = (a.groups + slice - 1) / slice;
+  const int per = a.per, slices = (a.groups + slice - 1) / slice;
   const int64_t items = (int64_t)a.batch * slices;
   for (int64_t item = blockIdx.x; item < items; item += sample_blocks) {
     const int s = (int)(item / slices), g0 = (int)(item - (int64_t)s * slices) * slice;
@@ -814,7 +866,7 @@ template <typename T, int V, int NT, bool X8, bool SILU, bool JOIN>
 __global__ void __launch_bounds__(NT) k_group_norm_bwd_rows(GroupNormArgs a, int64_t chunk, int chunks) {
   extern __shared__ float smem[];  // JOIN: join_floats, then [2][groups]
   const BwdParts parts = bwd_parts(a, chunks);
-  const int per = a.cols / a.groups;
+  const int per = a.per;
   float* joined = smem + 2 * max(1, NT / a.cols) * a.cols;
   if (JOIN && (int)blockIdx.x >= chunks) {
     param_sums<NT>(a, parts.chunk, chunks, (int)blockIdx.x - chunks, smem);
@@ -823,11 +875,16 @@ __global__ void __launch_bounds__(NT) k_group_norm_bwd_rows(GroupNormArgs a, int
   const Place<V> p(0, a.cols, per, NT);
   const int64_t c = (int64_t)chunks - 1 - blockIdx.x, r0 = c * chunk, r1 = min(a.rows, r0 + chunk);
   typedef Pair<T, V, X8> Q;
-  auto load = [&](Q& q, int64_t row) { q.load(a, row, p); };
+  typedef FromBoth<T, V, X8> X;
+  const Share whole((int)(r1 - r0), p.rl, p.rpb, p.on);
+  const X ahead(a, r0 + whole.rl, p);
   Stream<Q, 4> rows;
-  rows.start(r0, r1, p.rl, p.rpb, load);
+  rows.fetch(ahead, 0, max(whole.n - 1, 0));
   const Params<V> w(a, p.col);
   pieces_of(a, r0, r1, [&](const Span& s, int64_t lo, int64_t hi) {
+    const Share h((int)(hi - lo), p.rl, p.rpb, p.on);
+    const X x(a, lo + h.rl, p);
+    if (lo > r0) rows.fetch(x, 0, max(h.n - 1, 0));
     if constexpr (JOIN) {
       join_means<NT>(a, parts.piece, chunk, s, 0, a.groups, per, smem,
                      [&](int k, int g, float v) { joined[k * a.groups + g] = v; });
@@ -844,15 +901,14 @@ __global__ void __launch_bounds__(NT) k_group_norm_bwd_rows(GroupNormArgs a, int
       k.c1[e] = -r[e] * (JOIN ? joined[p.group[e]] : parts.means[at + p.group[e]]);
       k.c2[e] = -r[e] * (JOIN ? joined[a.groups + p.group[e]] : parts.means[all + at + p.group[e]]);
     }
-    if (!p.on) return;
-    rows.run(lo == r0, lo, hi, p.rl, p.rpb, load, [&](Q& q) { q.empty(); },
-             [&](const Q& q) {
-               float dz[V], h[V];
-               q.template values<SILU>(a, p, w, mean, r, dz, h);
+    const From<T, V> dx(a.dx, a.dx_stride, lo + h.rl, p.col, p.rpb);
+    rows.run(x, h, [&](const Q& q, int i, auto valid) {
+      float dz[V], h[V];
+      q.template values<SILU>(a, p, w, mean, r, dz, h);
 #pragma unroll
-               for (int e = 0; e < V; ++e) dz[e] = fmaf(dz[e], k.g[e], fmaf(h[e], k.c2[e], k.c1[e]));
-               if (q.row >= 0) store_pack<T, V>((T*)a.dx + q.row * a.dx_stride + p.col, dz, p.skip);
-             });
+      for (int e = 0; e < V; ++e) dz[e] = fmaf(dz[e], k.g[e], fmaf(h[e], k.c2[e], k.c1[e]));
+      if (valid && p.on) store_pack<T, V>(dx.put(i), dz, p.skip);
+    });
   });
 }
 
@@ -862,7 +918,7 @@ template <typename T, int V, int NT, int NV, bool X8, bool SILU>
 __global__ void __launch_bounds__(NT) k_group_norm_bwd_small(GroupNormArgs a, int slice, int slices) {
   extern __shared__ float smem[];
   const Slice b(a, slice, slices);
-  const int per = a.cols / a.groups;
+  const int per = a.per;
   const Place<V> p(b.first, b.width, per, NT);
   Totals tot{smem, b.width, p.rpb, NT};
   float* total = smem + totals_floats(p.rpb, b.width);  // [2][width]
@@ -874,12 +930,14 @@ __global__ void __launch_bounds__(NT) k_group_norm_bwd_small(GroupNormArgs a, in
     const int64_t lo = min(max(sample_begin(a, s), (int64_t)0), a.rows);
     const int64_t hi = max(lo, min(sample_begin(a, s + 1), a.rows));
     if (lo >= hi) continue;
-    const bool held = hi - lo <= (int64_t)p.rpb * NV;
+    const Share h((int)(hi - lo), p.rl, p.rpb, p.on);
+    const bool held = h.most <= NV;
+    const FromBoth<T, V, X8> x(a, lo + h.rl, p);
     Q q[NV];
-    if (held && p.on)
+    if (held)
 #pragma unroll
       for (int i = 0; i < NV; ++i)
-        if (lo + p.rl + i * p.rpb < hi) q[i].load(a, lo + p.rl + i * p.rpb, p);
+        if (i < h.n) x.load(q[i], i);
     float m[V], r[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
@@ -887,25 +945,25 @@ __global__ void __launch_bounds__(NT) k_group_norm_bwd_small(GroupNormArgs a, in
       m[e] = a.stats[at];
       r[e] = a.stats[(int64_t)a.batch * a.groups + at];
     }
+    // run(dz, h, k) for this thread's rows
     auto rows = [&](auto&& run) {
-      if (!p.on) return;
-      float dz[V], h[V];
+      float dz[V], hh[V];
       if (held) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-          if (lo + p.rl + i * p.rpb < hi) {
-            q[i].template values<SILU>(a, p, w, m, r, dz, h);
-            run(dz, h, lo + p.rl + i * p.rpb);
+          if (i < h.n) {
+            q[i].template values<SILU>(a, p, w, m, r, dz, hh);
+            run(dz, hh, i);
           }
       } else {
-        for (int64_t row = lo + p.rl; row < hi; row += (int64_t)p.rpb * 4) {
+        for (int k = 0; k < h.n; k += 4) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) q[i].load(a, min(row + (int64_t)i * p.rpb, hi - 1), p);
+          for (int i = 0; i < 4; ++i) x.load(q[i], min(k + i, h.n - 1));
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (row + (int64_t)i * p.rpb < hi) {
-              q[i].template values<SILU>(a, p, w, m, r, dz, h);
-              run(dz, h, row + (int64_t)i * p.rpb);
+            if (k + i < h.n) {
+              q[i].template values<SILU>(a, p, w, m, r, dz, hh);
+              run(dz, hh, k + i);
             }
         }
       }
@@ -913,14 +971,14 @@ __global__ void __launch_bounds__(NT) k_group_norm_bwd_small(GroupNormArgs a, in
     float sum[2][V];
 #pragma unroll
     for (int e = 0; e < V; ++e) sum[0][e] = sum[1][e] = 0.f;
-    rows([&](const float(&dz)[V], const float(&h)[V], int64_t) {
+    rows([&](const float(&dz)[V], const float(&h)[V], int) {
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         sum[0][e] += dz[e];
         sum[1][e] += dz[e] * h[e];
       }
     });
-    const float rn = 1.f / ((float)(hi - lo) * (float)per);
+    const float rn = 1.f / ((float)(int)(hi - lo) * (float)per);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       tot.put(p, b.first, sum[k]);
@@ -936,11 +994,12 @@ __global__ void __launch_bounds__(NT) k_group_norm_bwd_small(GroupNormArgs a, in
       k.c1[e] = -r[e] * mean[p.group[e] - b.g0];
       k.c2[e] = -r[e] * mean[b.groups + p.group[e] - b.g0];
     }
-    rows([&](const float(&dz)[V], const float(&h)[V], int64_t row) {
+    const From<T, V> dx(a.dx, a.dx_stride, lo + h.rl, p.col, p.rpb);
+    rows([&](const float(&dz)[V], const float(&h)[V], int i) {
       float o[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) o[e] = fmaf(dz[e], k.g[e], fmaf(h[e], k.c2[e], k.c1[e]));
-      store_pack<T, V>((T*)a.dx + row * a.dx_stride + p.col, o, p.skip);
+      store_pack<T, V>(dx.put(i), o, p.skip);
     });
   }
   for (int i = threadIdx.x; i < b.width; i += NT) {  // (each column is one thread's)
@@ -1020,7 +1079,7 @@ int sum_lds(int rpb, int width, int extra) { return (totals_floats(rpb, width) +
 // group.  The last slice may be narrower than the others, and its rows be dealt to more lanes.
 template <int V>
 int small_lds(const Small& s, const GroupNormArgs& a, int columns, int each) {
-  const int last = a.groups - (s.slices - 1) * s.slice, per = a.cols / a.groups;
+  const int last = a.groups - (s.slices - 1) * s.slice, per = a.per;
   int most = 0;
   for (const int groups : {s.slice, last}) {
     const int width = groups * per;
@@ -1091,7 +1150,7 @@ hipError_t backward_large(const GroupNormArgs& a, const Deal& d, hipStream_t st)
     hipLaunchKernelGGL(kernel, dim3(d.chunks + param_blocks<NT>(a.cols)), dim3(NT), lds, st, a, d.chunk, d.chunks);
     return hipGetLastError();
   }
-  const int per = a.cols / a.groups;
+  const int per = a.per;
   const int slice = (int)std::max<int64_t>(
       1, std::min<int64_t>(BWD_COLS / per, (int64_t)a.batch * a.groups / 512));  // (enough workgroups first)
   const int blocks = (int)std::min<int64_t>((int64_t)a.batch * ((a.groups + slice - 1) / slice), 1 << 16);

@@ -623,6 +623,7 @@ struct GroupNormArgs {
   const uint8_t* scales;
   int64_t rows;
   int32_t cols, groups, batch;
+  int32_t per;            // cols / groups
   const int32_t* begin;   // [batch + 1], or null: samples of `span` rows
   int64_t span;
   const float* gain;      // [cols], null: 1
