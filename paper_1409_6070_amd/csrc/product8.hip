@@ -29,6 +29,7 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
 typedef int16_t i16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr uint32_t NO_SOURCE = 0x80000000u;  // past every buffer: reads zero
 
@@ -52,7 +53,16 @@ __device__ inline void load_lds(u32x4 rsrc, uint32_t lds, uint32_t off) {
       "v"(off), "s"(rsrc)
       : "m0");
 }
-// ... and this wave's own reads of LDS
+// The same for 4 bytes: lane l's land at lds + 4 l.
+__device__ inline void load_lds_word(u32x4 rsrc, uint32_t lds, uint32_t off) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
+      "v"(off), "s"(rsrc)
+      : "m0");
+}
+// Waits for them, and for this wave's own reads of LDS.
 __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
 // Row r of the 64 that a wave's four blocks of the matrix operand cover: block j holds rows
@@ -99,120 +109,193 @@ __device__ inline void load_bias(const float* bias, int c, int n, float (&b)[16]
   for (int e = 0; e < 16; ++e) b[e] = bias && c + e < n ? bias[c + e] : 0.f;
 }
 
-// WX x WN waves, each TX blocks of 16 rows by 64 columns.
+// The matrix operand's rows (result columns) that lane r of 32 reads for block j of a wave's
+// 64: its result registers, rows 8 (i / 4) + 4 (lane / 32) + i % 4 of the block, are then
+// sixteen neighbouring columns of one result row.
+__device__ inline int interleaved32(int r, int j) { return j * 32 + ((r >> 2) & 1) * 16 + (r >> 3) * 4 + (r & 3); }
+// ... and where its chunks lie (as slot_x, for those rows)
+__device__ inline int slot_w32(int r, int c) { return c ^ (((r >> 1) & 3) | ((r >> 2) & 4)); }
+
+// WX x WN waves, each TX blocks of 32 rows by 64 columns.
 template <int WX_, int WN_, int TX_>
 struct P8Tile {
   static constexpr int WX = WX_, WN = WN_, TX = TX_;
-  static constexpr int NW = WX * WN, BM = WX * TX * 16, BN = WN * 64;
+  static constexpr int NW = WX * WN, BM = WX * TX * 32, BN = WN * 64;
   static constexpr int SLAB = (BM + BN) * 128;
   static constexpr int XL = BM / 8 / NW, WL = BN / 8 / NW;  // loads of a wave and slab
-  static constexpr int LDS = 2 * SLAB;
-  static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "loads are dealt evenly");
+  static constexpr int LDS = 2 * SLAB + 2 * BM * 4;         // two slabs, scales of twice four slabs
+  static_assert(BM % (16 * NW) == 0 && BN % (8 * NW) == 0 && BM / 64 <= NW, "loads are dealt evenly");
 };
 
-// bf16 results: slabs of 128 codes through two LDS stages.
+// bf16 results: slabs of 128 codes through two LDS stages, multiplied in halves of 64.  A
+// half's operands are read while the half before it is multiplied; a slab is loaded while
+// the one before it is, and one barrier a slab says that it has arrived and that the stage
+// of the one before is free.  Workgroups go on to further tiles, whose first slab is
+// loaded while the results of the last one are stored.
 template <class C>
 __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int64_t tiles, int64_t mt, int nt) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int wx = wave / C::WN, wn = wave % C::WN, r16 = lane & 15, g = lane >> 4;
+  const int wx = wave / C::WN, wn = wave % C::WN, r32 = lane & 31, h = lane >> 5;
   const uint32_t lds0 = lds_offset(smem);
-  for (int64_t t = blockIdx.x; t < (tiles + 7) / 8 * 8; t += gridDim.x) {
-    if ((t & 7) * ((tiles + 7) / 8) + (t >> 3) >= tiles) continue;
+  const uint32_t xstride = (uint32_t)a.x_stride, wstride = (uint32_t)a.w_stride, sstride = (uint32_t)a.xs_stride;
+  const int64_t places = (tiles + 7) / 8 * 8;
+  // this workgroup's next tile from place t on (places without a tile are passed over)
+  auto next_tile = [&](int64_t t) {
+    while (t < places && (t & 7) * (places >> 3) + (t >> 3) >= tiles) t += gridDim.x;
+    return t;
+  };
+  int64_t m0;
+  int n0;
+  u32x4 rx, rw, rs;
+  uint32_t xoff[C::XL], woff[C::WL];  // a lane's row in each of its loads, NO_SOURCE: none
+  const uint32_t xk0 = (uint32_t)slot_x((wave * C::XL) * 8 + (lane >> 3), lane & 7) * 16u;
+  const uint8_t* ws;
+  auto set_tile = [&](int64_t t) {
     const TilePlace at = place_of(t, tiles, mt, nt);
-    const int64_t m0 = at.m * C::BM;
-    const int n0 = at.n * C::BN;
+    m0 = at.m * C::BM;
+    n0 = at.n * C::BN;
     const int rows = (int)min((int64_t)C::BM, a.rows - m0), cols = min(C::BN, a.n - n0);
-    const u32x4 rx = buffer_of(a.x + m0 * a.x_stride, (uint32_t)(rows * a.x_stride));
-    const u32x4 rw = buffer_of(a.w + n0 * a.w_stride, (uint32_t)(cols * a.w_stride));
-    const uint32_t xstride = (uint32_t)a.x_stride;
-    uint32_t xoff[C::XL], woff[C::WL], xk[C::XL];
+    rx = buffer_of(a.x + m0 * a.x_stride, (uint32_t)rows * xstride);
+    rw = buffer_of(a.w + n0 * a.w_stride, (uint32_t)cols * wstride);
+    rs = buffer_of(a.xs + m0 * a.xs_stride, (uint32_t)rows * sstride);
 #pragma unroll
     for (int i = 0; i < C::XL; ++i) {
       const int r = (wave * C::XL + i) * 8 + (lane >> 3);
-      xk[i] = (uint32_t)slot_x(r, lane & 7) * 16u;
       xoff[i] = r < rows ? (uint32_t)r * xstride : NO_SOURCE;
     }
 #pragma unroll
     for (int i = 0; i < C::WL; ++i) {
       const int r = (wave * C::WL + i) * 8 + (lane >> 3);
-      woff[i] = r < cols ? (uint32_t)r * (uint32_t)a.w_stride + (uint32_t)slot_w(r, lane & 7) * 16u : NO_SOURCE;
+      woff[i] = r < cols ? (uint32_t)r * wstride + (uint32_t)slot_w32(r, lane & 7) * 16u : NO_SOURCE;
     }
-    auto issue = [&](int s, int st) {
+    ws = a.ws + (int64_t)(min(n0 + wn * 64, a.n - 1) >> 7) * a.ws_stride;
+  };
+  auto issue = [&](int s) {
+    const uint32_t st = lds0 + (s & 1) * C::SLAB;
 #pragma unroll
-      for (int i = 0; i < C::XL; ++i) {
-        const uint32_t k = xk[i] + (uint32_t)s * 128u;
-        load_lds(rx, lds0 + st * C::SLAB + (wave * C::XL + i) * 1024, k < xstride ? xoff[i] + k : NO_SOURCE);
-      }
-#pragma unroll
-      for (int i = 0; i < C::WL; ++i)
-        load_lds(rw, lds0 + st * C::SLAB + C::BM * 128 + (wave * C::WL + i) * 1024, woff[i] + (uint32_t)s * 128u);
-    };
-    const uint8_t* xs[C::TX];
-#pragma unroll
-    for (int i = 0; i < C::TX; ++i)
-      xs[i] = a.xs + min(m0 + (wx * C::TX + i) * 16 + r16, a.rows - 1) * a.xs_stride;
-    const uint8_t* ws = a.ws + (int64_t)(min(n0 + wn * 64, a.n - 1) >> 7) * a.ws_stride;
-    f32x4 acc[C::TX][4];
-#pragma unroll
-    for (int i = 0; i < C::TX; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    issue(0, 0);
-    uint32_t xw[C::TX], ww = 0;
-    for (int s = 0; s < a.kb; ++s) {
-      if ((s & 3) == 0) {
-#pragma unroll
-        for (int i = 0; i < C::TX; ++i) xw[i] = *(const uint32_t*)(xs[i] + s);
-        ww = *(const uint32_t*)(ws + s);
-      } else {
-#pragma unroll
-        for (int i = 0; i < C::TX; ++i) xw[i] >>= 8;
-        ww >>= 8;
-      }
-      wait_loads();
-      __builtin_amdgcn_s_barrier();  // slab s is whole, and every wave is done with slab s - 1
-      asm volatile("" ::: "memory");
-      if (s + 1 < a.kb) issue(s + 1, (s + 1) & 1);
-      const uint8_t* X = smem + (s & 1) * C::SLAB;
-      const uint8_t* W = X + C::BM * 128;
-      auto operand = [&](const uint8_t* base, int r, bool of_w) {
-        union {
-          i32x8 v;
-          u32x4 h[2];
-        } o;
-        const int c = g * 2;
-        o.h[0] = *(const u32x4*)(base + r * 128 + (of_w ? slot_w(r, c) : slot_x(r, c)) * 16);
-        o.h[1] = *(const u32x4*)(base + r * 128 + (of_w ? slot_w(r, c + 1) : slot_x(r, c + 1)) * 16);
-        return o.v;
-      };
-      i32x8 w[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = operand(W, wn * 64 + interleaved(r16, j), true);
-#pragma unroll
-      for (int i = 0; i < C::TX; ++i) {
-        const i32x8 x = operand(X, (wx * C::TX + i) * 16 + r16, false);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[j], x, acc[i][j], 0, 0, 0, (int)ww, 0,
-                                                                       (int)xw[i]);
-      }
+    for (int i = 0; i < C::XL; ++i) {
+      // (the chunk's swizzle alternates from one eight rows to the next)
+      const uint32_t k = (xk0 ^ ((i & 1) * 64u)) + (uint32_t)s * 128u;
+      load_lds(rx, st + (wave * C::XL + i) * 1024, k < xstride ? xoff[i] + k : NO_SOURCE);
     }
+#pragma unroll
+    for (int i = 0; i < C::WL; ++i)
+      load_lds(rw, st + C::BM * 128 + (wave * C::WL + i) * 1024, woff[i] + (uint32_t)s * 128u);
+    if ((s & 3) == 0 && wave < C::BM / 64)
+      load_lds_word(rs, lds0 + 2 * C::SLAB + ((s >> 2) & 1) * (C::BM * 4) + wave * 256,
+                    (uint32_t)(wave * 64 + lane) * sstride + (uint32_t)s);  // (rows behind the last: past the buffer)
+  };
+  auto operand = [&](const uint8_t* row, int slot0, int slot1) {
+    union {
+      i32x8 v;
+      u32x4 q[2];
+    } o;
+    o.q[0] = *(const u32x4*)(row + slot0 * 16);
+    o.q[1] = *(const u32x4*)(row + slot1 * 16);
+    return o.v;
+  };
+  i32x8 x[C::TX], w[2][2];  // (w: of the half being multiplied, and of the next)
+  uint32_t xs[C::TX];
+  auto read_x = [&](int s, int half, int i) {
+    const int r = (wx * C::TX + i) * 32 + r32, c = half * 4 + h * 2;
+    x[i] = operand(smem + (s & 1) * C::SLAB + r * 128, slot_x(r, c), slot_x(r, c + 1));
+  };
+  auto read_w = [&](int s, int half, int j) {
+    const int r = wn * 64 + interleaved32(r32, j), c = half * 4 + h * 2;
+    w[half][j] = operand(smem + (s & 1) * C::SLAB + (C::BM + r) * 128, slot_w32(r, c), slot_w32(r, c + 1));
+  };
+  auto read_scale = [&](int s, int i) {
+    xs[i] = smem[2 * C::SLAB + ((s >> 2) & 1) * (C::BM * 4) + ((wx * C::TX + i) * 32 + r32) * 4 + (s & 3)];
+  };
+  auto arrive = [&]() {
     wait_loads();
-    __builtin_amdgcn_s_barrier();  // (the next tile's first slab overwrites what others may still read)
+    __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    const int c = n0 + wn * 64 + g * 16;
-    float b[16];
-    load_bias(a.bias, c, a.n, b);
+  };
+  int64_t t = next_tile(blockIdx.x);
+  if (t >= places) return;
+  set_tile(t);
+  issue(0);
+  for (;;) {
+    f32x16 acc[C::TX][2];
+#pragma unroll
+    for (int i = 0; i < C::TX; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    arrive();
+    if (a.kb > 1) issue(1);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) read_w(0, 0, j);
 #pragma unroll
     for (int i = 0; i < C::TX; ++i) {
-      const int64_t m = m0 + (wx * C::TX + i) * 16 + r16;
-      if (m >= a.rows || c >= a.n) continue;
-      float v[16];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) v[e] = acc[i][e >> 2][e & 3] + b[e];
-      store_run16<__bf16>((__bf16*)a.y + m * a.y_stride, c, a.n, v);
+      read_scale(0, i);
+      read_x(0, 0, i);
     }
+    uint32_t wword = *(const uint32_t*)ws;
+    auto multiply = [&](int half, int i, uint32_t wsc) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[half][j], x[i], acc[i][j], 0, 0, 0, (int)wsc, 0,
+                                                                    (int)xs[i]);
+    };
+    for (int s = 0; s < a.kb; ++s) {
+      const uint32_t wsc = wword >> (8 * (s & 3));
+      // a block of x is read again as soon as it has been multiplied
+#pragma unroll
+      for (int i = 0; i < C::TX; ++i) {
+        if (i < 2) read_w(s, 1, i);
+        multiply(0, i, wsc);
+        read_x(s, 1, i);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (s + 1 < a.kb) {
+        if (((s + 1) & 3) == 0) wword = *(const uint32_t*)(ws + s + 1);
+#pragma unroll
+        for (int i = 0; i < C::TX; ++i) {
+          multiply(1, i, wsc);
+          if (i == 0) {
+            arrive();
+            if (s + 2 < a.kb) issue(s + 2);
+          }
+          if (i < 2) read_w(s + 1, 0, i);
+          read_scale(s + 1, i);
+          read_x(s + 1, 0, i);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < C::TX; ++i) multiply(1, i, wsc);
+      }
+    }
+    const int64_t m1 = m0;
+    const int n1 = n0;
+    t = next_tile(t + gridDim.x);
+    if (t < places) {
+      wait_loads();
+      __builtin_amdgcn_s_barrier();  // every wave has read the last slab
+      asm volatile("" ::: "memory");
+      set_tile(t);
+      issue(0);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int c = n1 + wn * 64 + j * 32 + h * 16;
+      float b[16];
+      load_bias(a.bias, c, a.n, b);
+#pragma unroll
+      for (int i = 0; i < C::TX; ++i) {
+        const int64_t m = m1 + (wx * C::TX + i) * 32 + r32;
+        if (m >= a.rows || c >= a.n) continue;
+        float v[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = acc[i][j][e] + b[e];
+        store_run16<__bf16>((__bf16*)a.y + m * a.y_stride, c, a.n, v);
+      }
+    }
+    if (t >= places) return;
   }
 }
 
@@ -465,20 +548,31 @@ __global__ void __launch_bounds__(256) k_weight_grad8_sum(WeightGrad8Args a, int
   }
 }
 
+template <class C>
+hipError_t launch_tiles(const Product8Args& a, int workgroups, hipStream_t st) {
+  const int64_t mt = (a.rows + C::BM - 1) / C::BM;
+  const int nt = (a.n + C::BN - 1) / C::BN;
+  const int64_t tiles = mt * nt;
+  const hipError_t e = allow_lds<k_product8<C>>(C::LDS);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_product8<C>, dim3((unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, workgroups)), dim3(C::NW * 64),
+                     C::LDS, st, a, tiles, mt, nt);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_product8(bool bf16, const Product8Args& a, hipStream_t st) {
   if (a.rows <= 0) return hipSuccess;
+  if (bf16) {
+    if (a.rows >= 4096 && a.n >= 1024) return launch_tiles<P8Tile<2, 4, 4>>(a, 256, st);
+    return launch_tiles<P8Tile<2, 2, 2>>(a, 512, st);
+  }
   const int64_t mt = (a.rows + 127) / 128;
   const int nt = (a.n + 127) / 128;
   const int64_t tiles = mt * nt;
   const dim3 grid((unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, 1 << 20));
-  if (bf16) {
-    using C = P8Tile<2, 2, 4>;
-    const hipError_t e = allow_lds<k_product8<C>>(C::LDS);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_product8<C>, grid, dim3(C::NW * 64), C::LDS, st, a, tiles, mt, nt);
-  } else {
+  {
     const hipError_t e = allow_lds<k_product8_exact>(65536);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(k_product8_exact, grid, dim3(256), 65536, st, a, tiles, mt, nt);
