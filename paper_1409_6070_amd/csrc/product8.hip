@@ -42,25 +42,49 @@ __device__ inline uint32_t lds_offset(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
 
-// One 16-byte load per lane into LDS: lane l's bytes land at lds + 16 l (lds uniform over
-// the wave), zeros where off lies past the buffer.  The compiler does not see it;
-// wait_loads and the fences around the barriers order it.
-__device__ inline void load_lds(u32x4 rsrc, uint32_t lds, uint32_t off) {
+// A wave's loads of a slab straight into LDS, none where s >= end: four of x and four of w,
+// eight rows of 128 bytes each (lane l's 16 bytes land 16 l behind the load's place, the
+// loads' places lie 1 KiB apart), and one word a lane of scales.  Zeros land where an offset
+// lies past its buffer.  The compiler does not see the loads; wait_loads and the fences around
+// the barriers order them.  One block, since a branch here would let it move the products
+// of the loop's first half behind it.
+__device__ inline void load_slab(int s, int end, uint32_t to_x, uint32_t to_w, uint32_t to_s, u32x4 rx, u32x4 rw,
+                                 u32x4 rs, const uint32_t (&x)[4], const uint32_t (&w)[4], uint32_t sc) {
   asm volatile(
-      "s_mov_b32 m0, %0\n\t"
+      "s_cmp_lt_i32 %[s], %[end]\n\t"
+      "s_cbranch_scc0 .Lslab_none%=\n\t"
+      "s_mov_b32 m0, %[tx]\n\t"
       "s_nop 0\n\t"
-      "buffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds),
-      "v"(off), "s"(rsrc)
-      : "m0");
-}
-// The same for 4 bytes: lane l's land at lds + 4 l.
-__device__ inline void load_lds_word(u32x4 rsrc, uint32_t lds, uint32_t off) {
-  asm volatile(
-      "s_mov_b32 m0, %0\n\t"
+      "buffer_load_dwordx4 %[x0], %[rx], 0 offen lds\n\t"
+      "s_add_u32 m0, m0, 0x400\n\t"
       "s_nop 0\n\t"
-      "buffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
-      "v"(off), "s"(rsrc)
-      : "m0");
+      "buffer_load_dwordx4 %[x1], %[rx], 0 offen lds\n\t"
+      "s_add_u32 m0, m0, 0x400\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %[x2], %[rx], 0 offen lds\n\t"
+      "s_add_u32 m0, m0, 0x400\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %[x3], %[rx], 0 offen lds\n\t"
+      "s_mov_b32 m0, %[tw]\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %[w0], %[rw], 0 offen lds\n\t"
+      "s_add_u32 m0, m0, 0x400\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %[w1], %[rw], 0 offen lds\n\t"
+      "s_add_u32 m0, m0, 0x400\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %[w2], %[rw], 0 offen lds\n\t"
+      "s_add_u32 m0, m0, 0x400\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %[w3], %[rw], 0 offen lds\n\t"
+      "s_mov_b32 m0, %[ts]\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dword %[sc], %[rs], 0 offen lds\n\t"
+      ".Lslab_none%=:" ::[s] "s"(s),
+      [end] "s"(end), [tx] "s"(to_x), [tw] "s"(to_w), [ts] "s"(to_s), [rx] "s"(rx), [rw] "s"(rw), [rs] "s"(rs),
+      [x0] "v"(x[0]), [x1] "v"(x[1]), [x2] "v"(x[2]), [x3] "v"(x[3]), [w0] "v"(w[0]), [w1] "v"(w[1]), [w2] "v"(w[2]),
+      [w3] "v"(w[3]), [sc] "v"(sc)
+      : "m0", "scc");
 }
 // Waits for them, and for this wave's own reads of LDS.
 __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
@@ -104,9 +128,24 @@ __device__ inline void store_run16(T* row, int c, int n, const float (&v)[16]) {
   }
 }
 
-__device__ inline void load_bias(const float* bias, int c, int n, float (&b)[16]) {
+// Eight neighbouring bf16 values of a result row, from column c on.
+__device__ inline void store_run8(__bf16* row, int c, int n, u32x4 v) {
+  if (c + 8 <= n) {
+    __builtin_memcpy(row + c, &v, sizeof(v));
+  } else {
 #pragma unroll
-  for (int e = 0; e < 16; ++e) b[e] = bias && c + e < n ? bias[c + e] : 0.f;
+    for (int e = 0; e < 8; ++e)
+      if (c + e < n) ((uint16_t*)row)[c + e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+  }
+}
+
+__device__ inline void load_bias(const float* bias, int c, int n, float (&b)[16]) {
+  if (bias && c + 16 <= n) {
+    __builtin_memcpy(b, bias + c, sizeof(b));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) b[e] = bias && c + e < n ? bias[c + e] : 0.f;
+  }
 }
 
 // The matrix operand's rows (result columns) that lane r of 32 reads for block j of a wave's
@@ -123,8 +162,10 @@ struct P8Tile {
   static constexpr int NW = WX * WN, BM = WX * TX * 32, BN = WN * 64;
   static constexpr int SLAB = (BM + BN) * 128;
   static constexpr int XL = BM / 8 / NW, WL = BN / 8 / NW;  // loads of a wave and slab
-  static constexpr int LDS = 2 * SLAB + 2 * BM * 4;         // two slabs, scales of twice four slabs
-  static_assert(BM % (16 * NW) == 0 && BN % (8 * NW) == 0 && BM / 64 <= NW, "loads are dealt evenly");
+  static constexpr int SCALES = NW * 256;                    // of four slabs: the rows', then the column blocks'
+  static constexpr int LDS = 2 * SLAB + 2 * SCALES;
+  static_assert(XL == 4 && WL == 4 && BM / 64 < NW, "load_slab");
+  static_assert(TX % 2 == 0 && NW * 8192 <= SLAB, "results pass through the second stage, 64 x 64 of a wave at a time");
 };
 
 // bf16 results: slabs of 128 codes through two LDS stages, multiplied in halves of 64.  A
@@ -148,9 +189,16 @@ __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int6
   int64_t m0;
   int n0;
   u32x4 rx, rw, rs;
-  uint32_t xoff[C::XL], woff[C::WL];  // a lane's row in each of its loads, NO_SOURCE: none
-  const uint32_t xk0 = (uint32_t)slot_x((wave * C::XL) * 8 + (lane >> 3), lane & 7) * 16u;
-  const uint8_t* ws;
+  // A lane's row and chunk in its wave's first loads of x and w; the others are eight rows
+  // further each, where the chunks' swizzle flips with the row's eights (x) and sixteens (w).
+  // (Rows behind the last one lie past the buffer.)
+  const int r0 = wave * C::XL * 8 + (lane >> 3), q0 = wave * C::WL * 8 + (lane >> 3);
+  const uint32_t xrow = (uint32_t)r0 * xstride, wrow = (uint32_t)q0 * wstride;
+  const uint32_t scale_row = wave < C::BM / 64    ? (uint32_t)(wave * 64 + lane) * sstride
+                             : wave == C::BM / 64 ? (uint32_t)lane * (uint32_t)a.ws_stride
+                                                  : NO_SOURCE;
+  const uint32_t xk = (uint32_t)slot_x(r0, lane & 7) * 16u, wk = (uint32_t)slot_w32(q0, lane & 7) * 16u;
+  u32x4 rws;
   auto set_tile = [&](int64_t t) {
     const TilePlace at = place_of(t, tiles, mt, nt);
     m0 = at.m * C::BM;
@@ -159,32 +207,23 @@ __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int6
     rx = buffer_of(a.x + m0 * a.x_stride, (uint32_t)rows * xstride);
     rw = buffer_of(a.w + n0 * a.w_stride, (uint32_t)cols * wstride);
     rs = buffer_of(a.xs + m0 * a.xs_stride, (uint32_t)rows * sstride);
-#pragma unroll
-    for (int i = 0; i < C::XL; ++i) {
-      const int r = (wave * C::XL + i) * 8 + (lane >> 3);
-      xoff[i] = r < rows ? (uint32_t)r * xstride : NO_SOURCE;
-    }
-#pragma unroll
-    for (int i = 0; i < C::WL; ++i) {
-      const int r = (wave * C::WL + i) * 8 + (lane >> 3);
-      woff[i] = r < cols ? (uint32_t)r * wstride + (uint32_t)slot_w32(r, lane & 7) * 16u : NO_SOURCE;
-    }
-    ws = a.ws + (int64_t)(min(n0 + wn * 64, a.n - 1) >> 7) * a.ws_stride;
+    rws = buffer_of(a.ws + (int64_t)(n0 >> 7) * a.ws_stride, (uint32_t)((cols + 127) >> 7) * (uint32_t)a.ws_stride);
   };
   auto issue = [&](int s) {
-    const uint32_t st = lds0 + (s & 1) * C::SLAB;
+    const uint32_t st = lds0 + (s & 1) * C::SLAB + wave * 4096;
+    uint32_t x[4], w[4];
 #pragma unroll
-    for (int i = 0; i < C::XL; ++i) {
-      // (the chunk's swizzle alternates from one eight rows to the next)
-      const uint32_t k = (xk0 ^ ((i & 1) * 64u)) + (uint32_t)s * 128u;
-      load_lds(rx, st + (wave * C::XL + i) * 1024, k < xstride ? xoff[i] + k : NO_SOURCE);
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t k = (xk ^ ((i & 1) * 64u)) + (uint32_t)s * 128u;
+      x[i] = k < xstride ? xrow + (uint32_t)i * 8u * xstride + k : NO_SOURCE;
+      w[i] = wrow + (uint32_t)i * 8u * wstride + (wk ^ ((i & 2) * 32u)) + (uint32_t)s * 128u;
     }
-#pragma unroll
-    for (int i = 0; i < C::WL; ++i)
-      load_lds(rw, st + C::BM * 128 + (wave * C::WL + i) * 1024, woff[i] + (uint32_t)s * 128u);
-    if ((s & 3) == 0 && wave < C::BM / 64)
-      load_lds_word(rs, lds0 + 2 * C::SLAB + ((s >> 2) & 1) * (C::BM * 4) + wave * 256,
-                    (uint32_t)(wave * 64 + lane) * sstride + (uint32_t)s);  // (rows behind the last: past the buffer)
+    // the words with this slab's scales, again with each of their four slabs (rows and blocks
+    // behind the last, and waves without any: past the buffer)
+    load_slab(__builtin_amdgcn_readfirstlane(s), a.kb, __builtin_amdgcn_readfirstlane(st),
+              __builtin_amdgcn_readfirstlane(st + C::BM * 128),
+              __builtin_amdgcn_readfirstlane(lds0 + 2 * C::SLAB + ((s >> 2) & 1) * C::SCALES + wave * 256), rx, rw,
+              wave < C::BM / 64 ? rs : rws, x, w, scale_row + (uint32_t)(s & ~3));
   };
   auto operand = [&](const uint8_t* row, int slot0, int slot1) {
     union {
@@ -196,7 +235,7 @@ __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int6
     return o.v;
   };
   i32x8 x[C::TX], w[2][2];  // (w: of the half being multiplied, and of the next)
-  uint32_t xs[C::TX];
+  uint32_t xs[C::TX], wsc;
   auto read_x = [&](int s, int half, int i) {
     const int r = (wx * C::TX + i) * 32 + r32, c = half * 4 + h * 2;
     x[i] = operand(smem + (s & 1) * C::SLAB + r * 128, slot_x(r, c), slot_x(r, c + 1));
@@ -206,7 +245,10 @@ __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int6
     w[half][j] = operand(smem + (s & 1) * C::SLAB + (C::BM + r) * 128, slot_w32(r, c), slot_w32(r, c + 1));
   };
   auto read_scale = [&](int s, int i) {
-    xs[i] = smem[2 * C::SLAB + ((s >> 2) & 1) * (C::BM * 4) + ((wx * C::TX + i) * 32 + r32) * 4 + (s & 3)];
+    xs[i] = smem[2 * C::SLAB + ((s >> 2) & 1) * C::SCALES + ((wx * C::TX + i) * 32 + r32) * 4 + (s & 3)];
+  };
+  auto read_wscale = [&](int s) {
+    return (uint32_t)smem[2 * C::SLAB + ((s >> 2) & 1) * C::SCALES + C::BM * 4 + (wn >> 1) * 4 + (s & 3)];
   };
   auto arrive = [&]() {
     wait_loads();
@@ -222,11 +264,19 @@ __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int6
 #pragma unroll
     for (int i = 0; i < C::TX; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int j = 0; j < 2; ++j) acc[i][j] = f32x16{};
+    if (a.bias)  // (the sums start from it)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+      for (int j = 0; j < 2; ++j) {
+        float b[16];
+        load_bias(a.bias, n0 + wn * 64 + j * 32 + h * 16, a.n, b);
+#pragma unroll
+        for (int i = 0; i < C::TX; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[i][j][e] = b[e];
+      }
     arrive();
-    if (a.kb > 1) issue(1);
+    issue(1);
 #pragma unroll
     for (int j = 0; j < 2; ++j) read_w(0, 0, j);
 #pragma unroll
@@ -234,65 +284,79 @@ __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int6
       read_scale(0, i);
       read_x(0, 0, i);
     }
-    uint32_t wword = *(const uint32_t*)ws;
-    auto multiply = [&](int half, int i, uint32_t wsc) {
+    wsc = read_wscale(0);
+    auto multiply = [&](int half, int i) {
 #pragma unroll
       for (int j = 0; j < 2; ++j)
         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[half][j], x[i], acc[i][j], 0, 0, 0, (int)wsc, 0,
                                                                     (int)xs[i]);
     };
     for (int s = 0; s < a.kb; ++s) {
-      const uint32_t wsc = wword >> (8 * (s & 3));
       // a block of x is read again as soon as it has been multiplied
 #pragma unroll
       for (int i = 0; i < C::TX; ++i) {
         if (i < 2) read_w(s, 1, i);
-        multiply(0, i, wsc);
+        multiply(0, i);
+        __builtin_amdgcn_sched_barrier(0);  // (or the block would be read elsewhere, early)
         read_x(s, 1, i);
+      }
+      uint32_t next = 0;
+#pragma unroll
+      for (int i = 0; i < C::TX; ++i) {
+        multiply(1, i);
         __builtin_amdgcn_sched_barrier(0);
-      }
-      if (s + 1 < a.kb) {
-        if (((s + 1) & 3) == 0) wword = *(const uint32_t*)(ws + s + 1);
-#pragma unroll
-        for (int i = 0; i < C::TX; ++i) {
-          multiply(1, i, wsc);
-          if (i == 0) {
-            arrive();
-            if (s + 2 < a.kb) issue(s + 2);
-          }
-          if (i < 2) read_w(s + 1, 0, i);
-          read_scale(s + 1, i);
-          read_x(s + 1, 0, i);
+        if (i == 0) {
+          arrive();
+          issue(s + 2);
           __builtin_amdgcn_sched_barrier(0);
+          next = read_wscale(s + 1);
         }
-      } else {
-#pragma unroll
-        for (int i = 0; i < C::TX; ++i) multiply(1, i, wsc);
+        // (behind the last slab: what lies in LDS, not used)
+        if (i < 2) read_w(s + 1, 0, i);
+        read_scale(s + 1, i);
+        read_x(s + 1, 0, i);
       }
+      wsc = next;
     }
     const int64_t m1 = m0;
     const int n1 = n0;
     t = next_tile(t + gridDim.x);
-    if (t < places) {
-      wait_loads();
-      __builtin_amdgcn_s_barrier();  // every wave has read the last slab
-      asm volatile("" ::: "memory");
+    if (t < places) {  // (every wave has read the last slab: the last barrier said so)
       set_tile(t);
       issue(0);
     }
+    // 64 x 64 results of a wave at a time through its part of the second stage, from where whole
+    // lines are stored: eight rows of 128 bytes by an instruction (from the registers 64
+    // pieces of 16 bytes: 15 us instead of .. for a round of 256 x 256 tiles)
+    uint8_t* stage = smem + C::SLAB + wave * 8192;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int c = n1 + wn * 64 + j * 32 + h * 16;
-      float b[16];
-      load_bias(a.bias, c, a.n, b);
+    for (int p = 0; p < C::TX; p += 2) {
 #pragma unroll
-      for (int i = 0; i < C::TX; ++i) {
-        const int64_t m = m1 + (wx * C::TX + i) * 32 + r32;
-        if (m >= a.rows || c >= a.n) continue;
-        float v[16];
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = acc[i][j][e] + b[e];
-        store_run16<__bf16>((__bf16*)a.y + m * a.y_stride, c, a.n, v);
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            uint32_t v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const __bf16 lo = (__bf16)acc[p + i][j][q * 8 + e * 2], hi = (__bf16)acc[p + i][j][q * 8 + e * 2 + 1];
+              v[e] = (uint32_t)__builtin_bit_cast(uint16_t, lo) | (uint32_t)__builtin_bit_cast(uint16_t, hi) << 16;
+            }
+            const int r = i * 32 + r32;
+            *(u32x4*)(stage + r * 128 + slot_x(r, j * 4 + h * 2 + q) * 16) = u32x4{v[0], v[1], v[2], v[3]};
+          }
+      u32x4 line[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int r = k * 8 + (lane >> 3);
+        line[k] = *(const u32x4*)(stage + r * 128 + slot_x(r, lane & 7) * 16);
+      }
+      const int c = n1 + wn * 64 + (lane & 7) * 8;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int64_t m = m1 + (wx * C::TX + p) * 32 + k * 8 + (lane >> 3);
+        if (m < a.rows && c < a.n) store_run8((__bf16*)a.y + m * a.y_stride, c, a.n, line[k]);
       }
     }
     if (t >= places) return;
