@@ -42,49 +42,32 @@ __device__ inline uint32_t lds_offset(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
 
-// A wave's loads of a slab straight into LDS, none where s >= end: four of x and four of w,
-// eight rows of 128 bytes each (lane l's 16 bytes land 16 l behind the load's place, the
-// loads' places lie 1 KiB apart), and one word a lane of scales.  Zeros land where an offset
-// lies past its buffer.  The compiler does not see the loads; wait_loads and the fences around
-// the barriers order them.  One block, since a branch here would let it move the products
-// of the loop's first half behind it.
-__device__ inline void load_slab(int s, int end, uint32_t to_x, uint32_t to_w, uint32_t to_s, u32x4 rx, u32x4 rw,
-                                 u32x4 rs, const uint32_t (&x)[4], const uint32_t (&w)[4], uint32_t sc) {
-  asm volatile(
-      "s_cmp_lt_i32 %[s], %[end]\n\t"
-      "s_cbranch_scc0 .Lslab_none%=\n\t"
-      "s_mov_b32 m0, %[tx]\n\t"
-      "s_nop 0\n\t"
-      "buffer_load_dwordx4 %[x0], %[rx], 0 offen lds\n\t"
-      "s_add_u32 m0, m0, 0x400\n\t"
-      "s_nop 0\n\t"
-      "buffer_load_dwordx4 %[x1], %[rx], 0 offen lds\n\t"
-      "s_add_u32 m0, m0, 0x400\n\t"
-      "s_nop 0\n\t"
-      "buffer_load_dwordx4 %[x2], %[rx], 0 offen lds\n\t"
-      "s_add_u32 m0, m0, 0x400\n\t"
-      "s_nop 0\n\t"
-      "buffer_load_dwordx4 %[x3], %[rx], 0 offen lds\n\t"
-      "s_mov_b32 m0, %[tw]\n\t"
-      "s_nop 0\n\t"
-      "buffer_load_dwordx4 %[w0], %[rw], 0 offen lds\n\t"
-      "s_add_u32 m0, m0, 0x400\n\t"
-      "s_nop 0\n\t"
-      "buffer_load_dwordx4 %[w1], %[rw], 0 offen lds\n\t"
-      "s_add_u32 m0, m0, 0x400\n\t"
-      "s_nop 0\n\t"
-      "buffer_load_dwordx4 %[w2], %[rw], 0 offen lds\n\t"
-      "s_add_u32 m0, m0, 0x400\n\t"
-      "s_nop 0\n\t"
-      "buffer_load_dwordx4 %[w3], %[rw], 0 offen lds\n\t"
-      "s_mov_b32 m0, %[ts]\n\t"
-      "s_nop 0\n\t"
-      "buffer_load_dword %[sc], %[rs], 0 offen lds\n\t"
-      ".Lslab_none%=:" ::[s] "s"(s),
-      [end] "s"(end), [tx] "s"(to_x), [tw] "s"(to_w), [ts] "s"(to_s), [rx] "s"(rx), [rw] "s"(rw), [rs] "s"(rs),
-      [x0] "v"(x[0]), [x1] "v"(x[1]), [x2] "v"(x[2]), [x3] "v"(x[3]), [w0] "v"(w[0]), [w1] "v"(w[1]), [w2] "v"(w[2]),
-      [w3] "v"(w[3]), [sc] "v"(sc)
-      : "m0", "scc");
+// One load per lane straight into LDS, none where s >= end: lane l's 16 bytes (4) land at
+// to + 16 l (4 l), zeros where the offset lies past its buffer.  The compiler does not see the
+// loads; wait_loads and the fences around the barriers order them.  The condition is in the
+// block, since a branch of the compiler's would let it move the products of a loop's first
+// half behind it.
+template <int BYTES>
+__device__ inline void load_lds(int s, int end, uint32_t to, u32x4 rsrc, uint32_t off) {
+  static_assert(BYTES == 16 || BYTES == 4, "a vector or a word");
+  if constexpr (BYTES == 16)
+    asm volatile(
+        "s_cmp_lt_i32 %0, %1\n\t"
+        "s_cbranch_scc0 .Lnone%=\n\t"
+        "s_mov_b32 m0, %2\n\t"
+        "s_nop 0\n\t"
+        "buffer_load_dwordx4 %3, %4, 0 offen lds\n\t"
+        ".Lnone%=:" ::"s"(s), "s"(end), "s"(to), "v"(off), "s"(rsrc)
+        : "m0", "scc");
+  else
+    asm volatile(
+        "s_cmp_lt_i32 %0, %1\n\t"
+        "s_cbranch_scc0 .Lnone%=\n\t"
+        "s_mov_b32 m0, %2\n\t"
+        "s_nop 0\n\t"
+        "buffer_load_dword %3, %4, 0 offen lds\n\t"
+        ".Lnone%=:" ::"s"(s), "s"(end), "s"(to), "v"(off), "s"(rsrc)
+        : "m0", "scc");
 }
 // Waits for them, and for this wave's own reads of LDS.
 __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
@@ -164,7 +147,9 @@ struct P8Tile {
   static constexpr int XL = BM / 8 / NW, WL = BN / 8 / NW;  // loads of a wave and slab
   static constexpr int SCALES = NW * 256;                    // of four slabs: the rows', then the column blocks'
   static constexpr int LDS = 2 * SLAB + 2 * SCALES;
-  static_assert(XL == 4 && WL == 4 && BM / 64 < NW, "load_slab");
+  // the first of a wave's nine loads that slot k of a slab's 2 TX issues
+  static constexpr int at(int k) { return TX == 4 ? (k < 5 ? 2 * k : 9) : k == 0 ? 0 : k == 1 ? 3 : k == 2 ? 5 : k == 3 ? 7 : 9; }
+  static_assert(XL == 4 && WL == 4 && BM / 64 < NW, "nine loads a wave and slab");
   static_assert(TX % 2 == 0 && NW * 8192 <= SLAB, "results pass through the second stage, 64 x 64 of a wave at a time");
 };
 
@@ -209,21 +194,28 @@ __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int6
     rs = buffer_of(a.xs + m0 * a.xs_stride, (uint32_t)rows * sstride);
     rws = buffer_of(a.ws + (int64_t)(n0 >> 7) * a.ws_stride, (uint32_t)((cols + 127) >> 7) * (uint32_t)a.ws_stride);
   };
-  auto issue = [&](int s) {
-    const uint32_t st = lds0 + (s & 1) * C::SLAB + wave * 4096;
-    uint32_t x[4], w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t k = (xk ^ ((i & 1) * 64u)) + (uint32_t)s * 128u;
-      x[i] = k < xstride ? xrow + (uint32_t)i * 8u * xstride + k : NO_SOURCE;
-      w[i] = wrow + (uint32_t)i * 8u * wstride + (wk ^ ((i & 2) * 32u)) + (uint32_t)s * 128u;
+  // Load i of a wave for slab s: four of x, four of w, and the words with the slab's scales,
+  // again with each of their four slabs (rows and blocks behind the last, and waves without
+  // any: past the buffer).
+  auto issue_one = [&](int s, int i) {
+    const int su = __builtin_amdgcn_readfirstlane(s);
+    const uint32_t st = lds0 + (su & 1) * C::SLAB + wave * 4096;
+    if (i < 4) {
+      const uint32_t k = (xk ^ ((i & 1) * 64u)) + (uint32_t)su * 128u;
+      load_lds<16>(su, a.kb, __builtin_amdgcn_readfirstlane(st + i * 1024), rx,
+                   k < xstride ? xrow + (uint32_t)i * 8u * xstride + k : NO_SOURCE);
+    } else if (i < 8) {
+      load_lds<16>(su, a.kb, __builtin_amdgcn_readfirstlane(st + C::BM * 128 + (i - 4) * 1024), rw,
+                   wrow + (uint32_t)(i - 4) * 8u * wstride + (wk ^ ((i & 2) * 32u)) + (uint32_t)su * 128u);
+    } else {
+      load_lds<4>(su, a.kb,
+                  __builtin_amdgcn_readfirstlane(lds0 + 2 * C::SLAB + ((su >> 2) & 1) * C::SCALES + wave * 256),
+                  wave < C::BM / 64 ? rs : rws, scale_row + (uint32_t)(su & ~3));
     }
-    // the words with this slab's scales, again with each of their four slabs (rows and blocks
-    // behind the last, and waves without any: past the buffer)
-    load_slab(__builtin_amdgcn_readfirstlane(s), a.kb, __builtin_amdgcn_readfirstlane(st),
-              __builtin_amdgcn_readfirstlane(st + C::BM * 128),
-              __builtin_amdgcn_readfirstlane(lds0 + 2 * C::SLAB + ((s >> 2) & 1) * C::SCALES + wave * 256), rx, rw,
-              wave < C::BM / 64 ? rs : rws, x, w, scale_row + (uint32_t)(s & ~3));
+  };
+  auto issue = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < 9; ++i) issue_one(s, i);
   };
   auto operand = [&](const uint8_t* row, int slot0, int slot1) {
     union {
@@ -276,7 +268,8 @@ __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int6
           for (int e = 0; e < 16; ++e) acc[i][j][e] = b[e];
       }
     arrive();
-    issue(1);
+#pragma unroll
+    for (int l = 0; l < C::at(C::TX); ++l) issue_one(1, l);
 #pragma unroll
     for (int j = 0; j < 2; ++j) read_w(0, 0, j);
 #pragma unroll
@@ -291,6 +284,12 @@ __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int6
         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[half][j], x[i], acc[i][j], 0, 0, 0, (int)wsc, 0,
                                                                     (int)xs[i]);
     };
+    // Loads are dealt between the products: a wave that issues nine in a row waits for them, and
+    // feeds no product meanwhile (32768 x 4096 x 4096: 552 us; four slots of three and two 514).
+    auto deal = [&](int slot, int s) {  // slots 0 .. TX - 1: second halves, TX ..: the first halves behind them
+#pragma unroll
+      for (int l = C::at(slot); l < C::at(slot + 1); ++l) issue_one(s, l);
+    };
     for (int s = 0; s < a.kb; ++s) {
       // a block of x is read again as soon as it has been multiplied
 #pragma unroll
@@ -299,6 +298,8 @@ __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int6
         multiply(0, i);
         __builtin_amdgcn_sched_barrier(0);  // (or the block would be read elsewhere, early)
         read_x(s, 1, i);
+        __builtin_amdgcn_sched_barrier(0);
+        deal(C::TX + i, s + 1);
       }
       uint32_t next = 0;
 #pragma unroll
@@ -307,14 +308,14 @@ __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int6
         __builtin_amdgcn_sched_barrier(0);
         if (i == 0) {
           arrive();
-          issue(s + 2);
-          __builtin_amdgcn_sched_barrier(0);
           next = read_wscale(s + 1);
         }
         // (behind the last slab: what lies in LDS, not used)
         if (i < 2) read_w(s + 1, 0, i);
         read_scale(s + 1, i);
         read_x(s + 1, 0, i);
+        __builtin_amdgcn_sched_barrier(0);
+        deal(i, s + 2);
       }
       wsc = next;
     }
