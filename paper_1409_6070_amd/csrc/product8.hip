@@ -470,6 +470,126 @@ __global__ void __launch_bounds__(256, 2) k_product8_exact(Product8Args a, int64
 }
 
 // ---------------------------------------------------------------------------
+// Few rows: a workgroup's waves share the sum of MB x 16 rows by NB x 16 columns, every wave
+// a run of its blocks of 128, operands straight into registers (16 rows of 128 bytes by two
+// loads), and meet in LDS.  Bound by latency and by reading the matrix once: one row, 300 ->
+// 3755 ..
+constexpr int FEW_WAVES = 8;
+
+template <typename T, int MB, int NB>
+__global__ void __launch_bounds__(FEW_WAVES * 64) k_product8_few(Product8Args a, int nt) {
+  constexpr int CS = NB * 16 + 4;  // floats of a staged row
+  __shared__ __attribute__((aligned(16))) float sums[FEW_WAVES][MB * 16][CS];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int r16 = lane & 15, g = lane >> 4;
+  const int tn = blockIdx.x % nt;
+  const int64_t m0 = (int64_t)(blockIdx.x / nt) * (MB * 16);
+  const int n0 = tn * (NB * 16);
+  const int b0 = a.kb * wave / FEW_WAVES, b1 = a.kb * (wave + 1) / FEW_WAVES;
+  const uint8_t* x[MB];
+  const uint8_t* xs[MB];
+  const uint8_t* w[NB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {  // (rows and columns behind the last: the last one, not stored)
+    const int64_t m = min(m0 + i * 16 + r16, a.rows - 1);
+    x[i] = a.x + m * a.x_stride + g * 32;
+    xs[i] = a.xs + m * a.xs_stride;
+  }
+#pragma unroll
+  for (int j = 0; j < NB; ++j) w[j] = a.w + (int64_t)min(n0 + j * 16 + r16, a.n - 1) * a.w_stride + g * 32;
+  const uint8_t* ws = a.ws + (int64_t)(n0 >> 7) * a.ws_stride;
+  struct Block {
+    u32x4 x[MB][2], w[NB][2];
+    uint32_t xs[MB], ws;
+  };
+  auto load = [&](Block& o, int b) {
+    const int k = b * 128 + g * 32;
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) o.w[j][h] = *(const u32x4*)(w[j] + b * 128 + h * 16);
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        o.x[i][h] = k + h * 16 < a.x_stride ? *(const u32x4*)(x[i] + b * 128 + h * 16) : u32x4{0, 0, 0, 0};
+      o.xs[i] = xs[i][b];
+    }
+    o.ws = ws[b];
+  };
+  f32x4 acc[MB][NB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto multiply = [&](const Block& o) {
+    if constexpr (sizeof(T) == 2) {
+      union {
+        u32x4 h[2];
+        i32x8 v;
+      } p, q;
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        p.h[0] = o.w[j][0];
+        p.h[1] = o.w[j][1];
+#pragma unroll
+        for (int i = 0; i < MB; ++i) {
+          q.h[0] = o.x[i][0];
+          q.h[1] = o.x[i][1];
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p.v, q.v, acc[i][j], 0, 0, 0, (int)o.ws, 0,
+                                                                       (int)o.xs[i]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        Codes16 cw[NB], cx[MB];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) cw[j] = to_bf16(o.w[j][h], row8_pow2(o.ws));
+#pragma unroll
+        for (int i = 0; i < MB; ++i) cx[i] = to_bf16(o.x[i][h], row8_pow2(o.xs[i]));
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int i = 0; i < MB; ++i) {
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, cw[j].lo),
+                                                                __builtin_bit_cast(bf16x8, cx[i].lo), acc[i][j], 0, 0, 0);
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, cw[j].hi),
+                                                                __builtin_bit_cast(bf16x8, cx[i].hi), acc[i][j], 0, 0, 0);
+          }
+      }
+    }
+  };
+  constexpr int DEPTH = MB + NB <= 2 ? 4 : 2;  // blocks in flight
+  int b = b0;
+  for (; b + DEPTH <= b1; b += DEPTH) {
+    Block o[DEPTH];
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) load(o[d], b + d);
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) multiply(o[d]);
+  }
+  for (; b < b1; ++b) {
+    Block o;
+    load(o, b);
+    multiply(o);
+  }
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) *(f32x4*)&sums[wave][i * 16 + r16][j * 16 + g * 4] = acc[i][j];
+  __syncthreads();
+  for (int v = threadIdx.x; v < MB * 16 * NB * 16; v += FEW_WAVES * 64) {
+    const int r = v / (NB * 16), c = v % (NB * 16);
+    if (m0 + r >= a.rows || n0 + c >= a.n) continue;
+    float s = a.bias ? a.bias[n0 + c] : 0.f;
+#pragma unroll
+    for (int k = 0; k < FEW_WAVES; ++k) s += sums[k][r][c];
+    ((T*)a.y)[(m0 + r) * a.y_stride + n0 + c] = Elem<T>::from_f32(s);
+  }
+}
+
+// ---------------------------------------------------------------------------
 // weight gradient
 
 constexpr int WG_ROWS = 64;  // rows of a slab
@@ -627,22 +747,46 @@ hipError_t launch_tiles(const Product8Args& a, int workgroups, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_product8(bool bf16, const Product8Args& a, hipStream_t st) {
-  if (a.rows <= 0) return hipSuccess;
-  if (bf16) {
-    if (a.rows >= 4096 && a.n >= 1024) return launch_tiles<P8Tile<2, 4, 4>>(a, 256, st);
-    return launch_tiles<P8Tile<2, 2, 2>>(a, 512, st);
-  }
+template <typename T>
+hipError_t launch_few(const Product8Args& a, hipStream_t st) {
+  auto go = [&](auto kernel, int mb, int nb) {
+    const int nt = (a.n + nb * 16 - 1) / (nb * 16);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((a.rows + mb * 16 - 1) / (mb * 16) * nt)), dim3(FEW_WAVES * 64), 0, st, a, nt);
+    return hipGetLastError();
+  };
+  if (a.rows <= 16) return go(k_product8_few<T, 1, 1>, 1, 1);
+  if (a.rows <= 32) return go(k_product8_few<T, 2, 1>, 2, 1);
+  if (a.rows <= 64) return go(k_product8_few<T, 2, 2>, 2, 2);  // (64 x 4096 x 4096: 12.0 us, 64 x 32 17.7)
+  return go(k_product8_few<T, 4, 2>, 4, 2);
+}
+
+hipError_t launch_exact(const Product8Args& a, hipStream_t st) {
   const int64_t mt = (a.rows + 127) / 128;
   const int nt = (a.n + 127) / 128;
   const int64_t tiles = mt * nt;
-  const dim3 grid((unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, 1 << 20));
-  {
-    const hipError_t e = allow_lds<k_product8_exact>(65536);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_product8_exact, grid, dim3(256), 65536, st, a, tiles, mt, nt);
-  }
+  const hipError_t e = allow_lds<k_product8_exact>(65536);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_product8_exact, dim3((unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, 1 << 20)), dim3(256), 65536,
+                     st, a, tiles, mt, nt);
   return hipGetLastError();
+}
+
+hipError_t launch_product8(bool bf16, const Product8Args& a, hipStream_t st) {
+  if (a.rows <= 0) return hipSuccess;
+  // Few rows, or results of few tiles (by 64 x 32), go to the kernel whose waves share a sum:
+  // 1 x 4096 x 4096 5.4 us, in 128 x 128 tiles 19.7; 128 x 4096 x 4096 (256 tiles) 17.7 and 22,
+  // in float32 18.7 and 54; 256 x 4096 x 4096 (512) 33.6 and 22, in float32 35 and 55.
+  const int64_t few = (a.rows + 63) / 64 * ((a.n + 31) / 32);
+  if (a.rows <= 32 || few <= (bf16 ? 256 : 512)) return bf16 ? launch_few<__bf16>(a, st) : launch_few<float>(a, st);
+  if (!bf16) return launch_exact(a, st);
+  // Rounds of workgroups times what one takes, measured: 11 + 1.68 us a slab for 256 x 256,
+  // 2.1 + 1.25 for two workgroups of 128 x 128 on a compute unit (32768 x 4096 x 4096: 522
+  // and 675 us; 32768 x 512 x 4096: 143 and 114; 2000 x 2000 x 2000: 26.5 and 15.5).
+  const int64_t big = ((a.rows + 255) / 256 * ((a.n + 255) / 256) + 255) / 256;
+  const int64_t small = ((a.rows + 127) / 128 * ((a.n + 127) / 128) + 511) / 512;
+  if ((double)big * (11.0 + 1.68 * a.kb) < (double)small * (2.1 + 1.25 * a.kb))
+    return launch_tiles<P8Tile<2, 4, 4>>(a, 256, st);
+  return launch_tiles<P8Tile<2, 2, 2>>(a, 512, st);
 }
 
 int32_t weight_grad8_splits(int64_t rows, int32_t k, int32_t n) {
