@@ -50,12 +50,15 @@ __device__ inline Pack<T, V> load_pack(const T* p) {
 // All but the first `skip` elements: those are another thread's, which may still have to
 // read what lies there (a result may take its input's place).
 template <typename T, int V>
-__device__ inline void store_pack(T* p, const float (&f)[V], int skip) {
+__device__ inline void store_pack(T* p, const float (&f)[V], int skip, bool stream) {
   Pack<T, V> v;
 #pragma unroll
   for (int e = 0; e < V; ++e) v.e[e] = Elem<T>::from_f32(f[e]);
   if (skip == 0) {
-    __builtin_memcpy(p, &v, sizeof(v));
+    if constexpr (sizeof(v) >= 4)
+      store_vector(p, v, stream);
+    else
+      *p = v.e[0];
     return;
   }
   if constexpr (V >= 8)
@@ -544,7 +547,7 @@ __global__ void __launch_bounds__(NT) k_group_norm_rows(GroupNormArgs a, int64_t
 #pragma unroll
       for (int e = 0; e < V; ++e)
         f[e] = activated<SILU>(affine(normal(f[e], mean[e], r[e]), w.gain[e], w.shift[e]), a.slope);
-      if (valid && p.on) store_pack<T, V>(y.put(k), f, p.skip);
+      if (valid && p.on) store_pack<T, V>(y.put(k), f, p.skip, a.stream);
     });
   });
 }
@@ -651,7 +654,7 @@ __global__ void __launch_bounds__(NT) k_group_norm_small(GroupNormArgs a, int sl
       float o[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) o[e] = activated<SILU>(affine(normal(f[e], m[e], r[e]), w.gain[e], w.shift[e]), a.slope);
-      store_pack<T, V>(y.put(k), o, p.skip);
+      store_pack<T, V>(y.put(k), o, p.skip, a.stream);
     });
   }
 }
@@ -762,26 +765,26 @@ __global__ void __launch_bounds__(NT) k_group_norm_bwd_sums(GroupNormArgs a, int
   }
 }
 
-// dgain (which = 0) and dshift: some columns' sums over the chunks, in NT / cols_of lanes a
-// column, interleaved.
+// dgain (which = 0) and dshift: some columns' sums over the chunks, 64 lanes a column.
 template <int NT>
 __device__ inline void param_sums(const GroupNormArgs& a, const float* chunk, int parts, int block, float* smem) {
-  constexpr int COLS = NT / 16;
+  constexpr int LANES = 64, COLS = NT / LANES;
   const int cb = (a.cols + COLS - 1) / COLS, which = block / cb;
   const int at = threadIdx.x % COLS, c = (block - which * cb) * COLS + at, sl = threadIdx.x / COLS;
   const float* p = chunk + (int64_t)which * parts * a.cols;
   float* out = which ? a.dshift : a.dgain;
-  float v = c < a.cols ? strided_sum<16>(sl, parts, 16, [&](int k) { return p[(int64_t)k * a.cols + c]; }) : 0.f;
+  float v = c < a.cols ? strided_sum<16>(sl, parts, LANES, [&](int k) { return p[(int64_t)k * a.cols + c]; }) : 0.f;
   smem[sl * COLS + at] = v;
   __syncthreads();
   if (sl == 0 && c < a.cols && out) {
-    for (int k = 1; k < 16; ++k) v += smem[k * COLS + at];
+#pragma unroll 8
+    for (int k = 1; k < LANES; ++k) v += smem[k * COLS + at];
     out[c] = v;
   }
 }
 template <int NT>
 int param_blocks(int cols) {
-  return 2 * ((cols + NT / 16 - 1) / (NT / 16));
+  return 2 * ((cols + NT / 64 - 1) / (NT / 64));
 }
 
 __global__ void __launch_bounds__(1024) k_group_norm_params(GroupNormArgs a, int parts) {
@@ -805,7 +808,7 @@ __device__ inline void join_means(const GroupNormArgs& a, const float* piece, in
     const float* q = piece + (c0 + s.s) * step + col;
     const float g = a.gain ? a.gain[col] : 1.f;
     float u = 0.f, v = 0.f;
-    constexpr int U = 8;
+    constexpr int U = NT == 1024 ? 16 : 8;
     for (int c = l; c < pieces; c += U * lanes) {
       float x[U], y[U];
 #pragma unroll
@@ -907,7 +910,7 @@ __global__ void __launch_bounds__(NT) k_group_norm_bwd_rows(GroupNormArgs a, int
       q.template values<SILU>(a, p, w, mean, r, dz, h);
 #pragma unroll
       for (int e = 0; e < V; ++e) dz[e] = fmaf(dz[e], k.g[e], fmaf(h[e], k.c2[e], k.c1[e]));
-      if (valid && p.on) store_pack<T, V>(dx.put(i), dz, p.skip);
+      if (valid && p.on) store_pack<T, V>(dx.put(i), dz, p.skip, a.stream);
     });
   });
 }
@@ -999,7 +1002,7 @@ __global__ void __launch_bounds__(NT) k_group_norm_bwd_small(GroupNormArgs a, in
       float o[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) o[e] = fmaf(dz[e], k.g[e], fmaf(h[e], k.c2[e], k.c1[e]));
-      store_pack<T, V>(dx.put(i), o, p.skip);
+      store_pack<T, V>(dx.put(i), o, p.skip, a.stream);
     });
   }
   for (int i = threadIdx.x; i < b.width; i += NT) {  // (each column is one thread's)

@@ -569,6 +569,7 @@ struct Rows8Args {
   uint8_t* scales;
   void* y;              // load: rows to write
   int64_t y_stride;
+  bool stream;          // past the caches
 };
 hipError_t launch_rows8_store(bool bf16, const Rows8Args& a, hipStream_t st);
 hipError_t launch_rows8_load(bool bf16, const Rows8Args& a, hipStream_t st);
@@ -595,6 +596,7 @@ struct Product8Args {
   const float* bias;      // [n], or null
   void* y;
   int64_t y_stride;
+  bool stream;            // past the caches
 };
 hipError_t launch_product8(bool bf16, const Product8Args& a, hipStream_t st);
 struct WeightGrad8Args {
@@ -641,6 +643,7 @@ struct GroupNormArgs {
   float* dgain;
   float* dshift;
   float* ws;
+  bool stream;            // y or dx: past the caches
 };
 size_t group_norm_workspace(bool bf16, int64_t rows, int32_t cols, int32_t groups, int32_t batch, bool backward);
 hipError_t launch_group_norm(bool bf16, const GroupNormArgs& a, hipStream_t st);

@@ -21,6 +21,7 @@
 #include "rows8.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace sscn {
 
@@ -112,9 +113,9 @@ __device__ inline void store_run16(T* row, int c, int n, const float (&v)[16]) {
 }
 
 // Eight neighbouring bf16 values of a result row, from column c on.
-__device__ inline void store_run8(__bf16* row, int c, int n, u32x4 v) {
+__device__ inline void store_run8(__bf16* row, int c, int n, u32x4 v, bool stream) {
   if (c + 8 <= n) {
-    __builtin_memcpy(row + c, &v, sizeof(v));
+    store_vector(row + c, v, stream);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
@@ -357,7 +358,7 @@ __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int6
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const int64_t m = m1 + (wx * C::TX + p) * 32 + k * 8 + (lane >> 3);
-        if (m < a.rows && c < a.n) store_run8((__bf16*)a.y + m * a.y_stride, c, a.n, line[k]);
+        if (m < a.rows && c < a.n) store_run8((__bf16*)a.y + m * a.y_stride, c, a.n, line[k], a.stream);
       }
     }
     if (t >= places) return;
@@ -592,116 +593,172 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) k_product8_few(Product8Args a,
 // ---------------------------------------------------------------------------
 // weight gradient
 
-constexpr int WG_ROWS = 64;  // rows of a slab
+constexpr int WG_ROWS = 64;        // rows of a slab
+constexpr int PANEL = WG_ROWS * 256;  // bytes of its 128 columns in bf16
 
-// Eight rows' values of one column of a staged slab [64 rows][128 bf16], for each lane: the
+// Eight rows' values of one column of a staged panel [64 rows][128 bf16], for each lane: the
 // lanes of a 16-lane group read rows 8 g .. + 3 (then + 4 .. 7) in pieces of four columns,
-// 16 apart, and get them transposed: lane 4 q + e column c0 + 16 q + 4 j + e.  A piece of
-// 8 bytes lies where the 32 lanes that read together cover all banks once.
+// 16 apart, and get them transposed: lane 4 q + e column 16 (unit + q) + 4 j + e.  A piece of
+// 8 bytes lies where the 32 lanes that read together, and the 16 that write 16 bytes each,
+// cover all banks once.
 __device__ inline int piece_at(int row, int unit, int sub) {
-  return row * 256 + (unit ^ ((row >> 1) & 4)) * 32 + (sub ^ (row & 3)) * 8;
+  return row * 256 + (unit ^ ((row >> 1) & 4) ^ (row & 1)) * 32 + (sub ^ (row & 3)) * 8;
 }
-__device__ inline bf16x8 column_operand(uint32_t lds, int row, int unit, int sub) {
+// at: piece_at of the lane's row and column piece; four rows on, the swizzle is the same.
+__device__ inline bf16x8 column_operand(uint32_t at) {
   typedef __attribute__((address_space(3))) i16x4* P;
   union {
     i16x4 h[2];
     bf16x8 v;
   } o;
-  o.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(lds + piece_at(row, unit, sub)));
-  o.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(lds + piece_at(row + 4, unit, sub)));
+  o.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)at);
+  o.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(at + 4 * 256));
   return o.v;
 }
+// WK x WN waves, each 16 TK rows of dw by 64 columns.
+template <int WK_, int WN_, int TK_>
+struct Wg8Tile {
+  static constexpr int WK = WK_, WN = WN_, TK = TK_;
+  static constexpr int NT = WK * WN * 64, BK = WK * TK * 16, BN = WN * 64;
+  static constexpr int STAGE = (BK + BN) / 128 * PANEL, LDS = 2 * STAGE;
+  static_assert(BK == BN && BK * 2 == NT, "a thread stages 32 codes of either operand");
+};
 
-// A 128 x 128 tile of dw over a run of rows.
-__global__ void __launch_bounds__(256, 2) k_weight_grad8(WeightGrad8Args a, int kt, int nt, int splits) {
-  constexpr int STAGE = 2 * WG_ROWS * 256;
+// A tile of dw over a run of rows.
+template <class C>
+__global__ void __launch_bounds__(C::NT, 2) k_weight_grad8(WeightGrad8Args a, int kt, int nt, int splits) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int wk = wave >> 1, wn = wave & 1, r16 = lane & 15, g = lane >> 4;
+  const int wk = wave / C::WN, wn = wave % C::WN, r16 = lane & 15, g = lane >> 4;
   const int split = blockIdx.x / (kt * nt), tile = blockIdx.x - split * (kt * nt);
   const int tk = tile / nt, tn = tile - tk * nt;
   const int64_t slabs = (a.rows + WG_ROWS - 1) / WG_ROWS;
   const int64_t s0 = slabs * split / splits, s1 = slabs * (split + 1) / splits;
-  const int lr = threadIdx.x >> 2, lc = (threadIdx.x & 3) * 32;
-  const int xc = tk * 128 + lc, yc = tn * 128 + lc;
-  u32x4 xv[2], yv[2];
-  uint32_t sx = 127, sy = 127;
-  auto fetch = [&](int64_t s) {
-    const int64_t m = s * WG_ROWS + lr;
+  // Staging: this thread's 32 codes of a row of either operand (zeros behind the last row and
+  // column: past the buffer, whose end is the last row's within a slab).
+  const int panel = threadIdx.x >> 8, lr = (threadIdx.x & 255) >> 2, lc = (threadIdx.x & 3) * 32;
+  const int xc = tk * C::BK + panel * 128 + lc, yc = tn * C::BN + panel * 128 + lc;
+  uint32_t xo[2], yo[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) xv[h] = yv[h] = u32x4{0, 0, 0, 0};
-    if (m < a.rows) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (xc + h * 16 < a.x_stride) xv[h] = *(const u32x4*)(a.x + m * a.x_stride + xc + h * 16);
-        if (yc + h * 16 < a.dy_stride) yv[h] = *(const u32x4*)(a.dy + m * a.dy_stride + yc + h * 16);
-      }
-      sx = a.xs[m * a.xs_stride + tk];
-      sy = a.dys[m * a.dys_stride + tn];
-    }
+  for (int h = 0; h < 2; ++h) {
+    xo[h] = xc + h * 16 < a.x_stride ? (uint32_t)(lr * a.x_stride + xc + h * 16) : NO_SOURCE;
+    yo[h] = yc + h * 16 < a.dy_stride ? (uint32_t)(lr * a.dy_stride + yc + h * 16) : NO_SOURCE;
+  }
+  // (scales of blocks behind the last: the last one's, for codes that are zero)
+  const uint32_t xso = (uint32_t)(lr * a.xs_stride + (min(xc, a.k - 1) >> 7));
+  const uint32_t yso = (uint32_t)(lr * a.dys_stride + (min(yc, a.n - 1) >> 7));
+  struct Staged {
+    u32x4 x[2], y[2];
+    uint32_t sx, sy;
   };
-  auto put = [&](int st) {
-    uint8_t* X = smem + st * STAGE;
-    uint8_t* Y = X + STAGE / 2;
+  auto fetch = [&](Staged& o, int64_t s) {
+    const int rows = (int)(s < s1 ? min((int64_t)WG_ROWS, a.rows - s * WG_ROWS) : 0);
+    const int64_t m = (s < s1 ? s : s0) * WG_ROWS;
+    auto of = [&](const uint8_t* base, int64_t stride) {
+      return __builtin_amdgcn_make_buffer_rsrc((void*)(base + m * stride), 0, (int)((uint32_t)rows * (uint32_t)stride),
+                                               0x00020000);
+    };
+    const auto rx = of(a.x, a.x_stride), ry = of(a.dy, a.dy_stride), rsx = of(a.xs, a.xs_stride), rsy = of(a.dys, a.dys_stride);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int unit = lc / 16 + h;
-      Codes16 vx = to_bf16(xv[h], row8_pow2(sx)), vy = to_bf16(yv[h], row8_pow2(sy));
-      const u32x4* px = &vx.lo;
-      const u32x4* py = &vy.lo;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        *(uint2*)(X + piece_at(lr, unit, q)) = uint2{px[q >> 1][(q & 1) * 2], px[q >> 1][(q & 1) * 2 + 1]};
-        *(uint2*)(Y + piece_at(lr, unit, q)) = uint2{py[q >> 1][(q & 1) * 2], py[q >> 1][(q & 1) * 2 + 1]};
-      }
+      o.x[h] = __builtin_amdgcn_raw_buffer_load_b128(rx, (int)xo[h], 0, 0);
+      o.y[h] = __builtin_amdgcn_raw_buffer_load_b128(ry, (int)yo[h], 0, 0);
     }
+    o.sx = __builtin_amdgcn_raw_buffer_load_b8(rsx, (int)xso, 0, 0);
+    o.sy = __builtin_amdgcn_raw_buffer_load_b8(rsy, (int)yso, 0, 0);
   };
-  f32x4 acc[4][4], bacc[4];
+  // Sixteen codes at a time (a unit), two pieces to a store: an odd row's swizzle exchanges
+  // the pieces of each pair, an exchange of words while they are codes.
+  const uint32_t lds0 = lds_offset(smem), at0 = (uint32_t)(panel * PANEL + piece_at(lr, lc / 16, 0) - (lr & 1) * 8);
+  auto put = [&](const Staged& o, int st) {
+    uint8_t* to = smem + st * C::STAGE;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    bacc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int of_y = 0; of_y < 2; ++of_y) {
+        const u32x4 c = of_y ? o.y[h] : o.x[h];
+        const u32x4 d = lr & 1 ? u32x4{c[1], c[0], c[3], c[2]} : c;
+        const Codes16 v = to_bf16(d, row8_pow2(of_y ? o.sy : o.sx));
+        // (unit and pair of pieces: bits 5 and 4 of the place)
+        *(u32x4*)(to + of_y * (C::BK / 128 * PANEL) + (at0 ^ (h * 32))) = v.lo;
+        *(u32x4*)(to + of_y * (C::BK / 128 * PANEL) + (at0 ^ (h * 32 + 16))) = v.hi;
+      }
+  };
+  f32x4 acc[C::TK][4], bacc[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    bacc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < C::TK; ++i) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const bool bias = a.db && tk == 0 && wk == 0;
   bf16x8 one;
 #pragma unroll
   for (int e = 0; e < 8; ++e) one[e] = (__bf16)1.f;
+  // Where this lane's pieces of its wave's columns lie, 64 of them at a time (half a panel;
+  // the other half is 128 bytes off), in each of the four interleaved blocks.
+  const int row0 = g * 8 + (r16 >> 2), xh = C::TK == 8 ? 0 : wk & 1;
+  uint32_t xa[4], ya[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    xa[j] = lds0 + (wk * C::TK / 8) * PANEL + piece_at(row0, xh * 4 + (r16 & 3), j);
+    ya[j] = lds0 + C::BK / 128 * PANEL + (wn >> 1) * PANEL + piece_at(row0, (wn & 1) * 4 + (r16 & 3), j);
+  }
+  // Slab s is multiplied while the next one is staged, between its halves, and the one
+  // behind that is on its way: a trip through memory has a whole slab's time.
+  Staged ahead;
   if (s0 < s1) {
-    fetch(s0);
-    put(0);
+    fetch(ahead, s0);
+    put(ahead, 0);
+    fetch(ahead, s0 + 1);
   }
-  for (int64_t s = s0; s < s1; ++s) {
-    const int st = (int)(s - s0) & 1;
-    if (s + 1 < s1) fetch(s + 1);
-    __syncthreads();
-    const uint32_t X = lds_offset(smem) + st * STAGE, Y = X + STAGE / 2;
+  // with_bias: the waves that also sum dy (a loop of their own: a branch in it would let the
+  // products move behind it)
+  auto loop = [&](auto with_bias) {
+    for (int64_t s = s0; s < s1; ++s) {
+      const int st = (int)(s - s0) & 1;
+      __syncthreads();
+      bf16x8 x[2], y[2][4];
+      auto x_read = [&](int n) {  // block n % TK of 32 rows n / TK
+        const int i = n % C::TK;
+        x[n & 1] = column_operand((xa[i & 3] ^ ((i >> 2) * 128)) + st * C::STAGE + n / C::TK * 32 * 256);
+      };
+      auto y_read = [&](int mb, int j) { y[mb][j] = column_operand(ya[j] + st * C::STAGE + mb * 32 * 256); };
 #pragma unroll
-    for (int mb = 0; mb < 2; ++mb) {
-      bf16x8 xo[4], yo[4];
-      const int row = mb * 32 + g * 8 + (r16 >> 2);
+      for (int j = 0; j < 4; ++j) y_read(0, j);
+      x_read(0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        xo[i] = column_operand(X, row, wk * 4 + (r16 & 3), i);
-        yo[i] = column_operand(Y, row, wn * 4 + (r16 & 3), i);
+      for (int n = 0; n < 2 * C::TK; ++n) {
+        const int mb = n / C::TK, i = n % C::TK;
+        // an operand is read while the one before it is multiplied
+        if (n + 1 < 2 * C::TK) x_read(n + 1);
+        if (mb == 0 && i >= C::TK - 4) y_read(1, i - (C::TK - 4));
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[mb][j], x[n & 1], acc[i][j], 0, 0, 0);
+        if (decltype(with_bias)::value && i == C::TK - 1)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) bacc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[mb][j], one, bacc[j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (n == C::TK - 1) {
+          put(ahead, st ^ 1);  // (behind the last slab: zeros, not read)
+          fetch(ahead, s + 2);
+        }
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(yo[j], xo[i], acc[i][j], 0, 0, 0);
-      if (bias)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) bacc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(yo[j], one, bacc[j], 0, 0, 0);
     }
-    if (s + 1 < s1) put(st ^ 1);
-  }
-  // lane: rows k = 16 (r16 / 4) + 4 i + r16 % 4 of the wave's 64, columns n = 16 g .. + 15
+  };
+  if (bias)
+    loop(std::true_type{});
+  else
+    loop(std::false_type{});
+  // lane: rows k of the wave's as the pieces interleave them, columns n = 16 g .. + 15
   float* out = a.part ? a.part + (int64_t)split * a.k * a.n : a.dw;
   const int64_t stride = a.part ? a.n : a.dw_stride;
-  const int c = tn * 128 + wn * 64 + g * 16;
+  const int c = tn * C::BN + wn * 64 + g * 16;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int k = tk * 128 + wk * 64 + interleaved(r16, i);
+  for (int i = 0; i < C::TK; ++i) {
+    const int k = tk * C::BK + wk * (C::TK * 16) + (i >> 2) * 64 + interleaved(r16, i & 3);
     if (k >= a.k || c >= a.n) continue;
     float v[16];
 #pragma unroll
@@ -789,19 +846,40 @@ hipError_t launch_product8(bool bf16, const Product8Args& a, hipStream_t st) {
   return launch_tiles<P8Tile<2, 2, 2>>(a, 512, st);
 }
 
+namespace {
+
+typedef Wg8Tile<2, 4, 8> WgBig;
+typedef Wg8Tile<2, 2, 4> WgSmall;
+
+// 256 x 256 tiles where they pad the result little enough.
+bool weight_grad8_big(int32_t k, int32_t n) {
+  const int64_t big = (int64_t)((k + 255) / 256) * ((n + 255) / 256) * 4;
+  return (double)big < 1.5 * (double)(row8_blocks(k) * row8_blocks(n));
+}
+
+template <class C>
+hipError_t weight_grad8(const WeightGrad8Args& a, int splits, hipStream_t st) {
+  const int kt = (a.k + C::BK - 1) / C::BK, nt = (a.n + C::BN - 1) / C::BN;
+  const hipError_t e = allow_lds<k_weight_grad8<C>>(C::LDS);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_weight_grad8<C>, dim3((unsigned)(kt * nt * splits)), dim3(C::NT), C::LDS, st, a, kt, nt, splits);
+  return hipGetLastError();
+}
+
+}  // namespace
+
 int32_t weight_grad8_splits(int64_t rows, int32_t k, int32_t n) {
-  const int64_t tiles = row8_blocks(k) * row8_blocks(n), slabs = (rows + WG_ROWS - 1) / WG_ROWS;
-  // two workgroups a compute unit, each with four slabs at least
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(slabs / 4, 512 / tiles));
+  const bool big = weight_grad8_big(k, n);
+  const int64_t tiles = big ? (int64_t)((k + 255) / 256) * ((n + 255) / 256) : row8_blocks(k) * row8_blocks(n);
+  const int64_t slabs = (rows + WG_ROWS - 1) / WG_ROWS;
+  // as many workgroups as the compute units hold at once, each with four slabs at least
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(slabs / 4, (big ? 256 : 512) / tiles));
 }
 
 hipError_t launch_weight_grad8(const WeightGrad8Args& a, hipStream_t st) {
-  const int kt = (int)row8_blocks(a.k), nt = (int)row8_blocks(a.n);
   const int splits = weight_grad8_splits(a.rows, a.k, a.n);
-  hipError_t e = allow_lds<k_weight_grad8>(65536);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_weight_grad8, dim3((unsigned)(kt * nt * splits)), dim3(256), 65536, st, a, kt, nt, splits);
-  e = hipGetLastError();
+  const hipError_t e =
+      weight_grad8_big(a.k, a.n) ? weight_grad8<WgBig>(a, splits, st) : weight_grad8<WgSmall>(a, splits, st);
   if (e != hipSuccess || splits == 1) return e;
   const int64_t size = (int64_t)a.k * a.n + (a.db ? a.n : 0);
   hipLaunchKernelGGL(k_weight_grad8_sum, dim3((unsigned)std::min<int64_t>((size + 255) / 256, 4096)), dim3(256), 0, st, a,

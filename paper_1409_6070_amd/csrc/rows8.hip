@@ -110,6 +110,7 @@ __global__ void __launch_bounds__(256) k_rows8_store(Rows8Args a, int R, int64_t
 
 template <typename T>
 __global__ void __launch_bounds__(256) k_rows8_load(Rows8Args a, int R, int64_t tiles) {
+  constexpr int V = Elem<T>::VE, N = 8 / V;  // a lane's columns: N runs of 16 bytes, 16 V columns apart
   const int nb = (int)row8_blocks(a.cols), lane = threadIdx.x & 15, group = threadIdx.x >> 4;
   const int64_t cs = row8_code_stride(a.cols), ss = row8_scale_stride(a.cols);
   const float rcp = 1.f / (float)nb;
@@ -117,37 +118,46 @@ __global__ void __launch_bounds__(256) k_rows8_load(Rows8Args a, int R, int64_t 
     const int64_t row0 = tile * R;
     const int n = (int)min((int64_t)R, a.rows - row0) * nb;
     for (int i0 = 0; i0 < n; i0 += ITEMS) {
-      uint2 w[PER];
-      uint32_t s[PER];
+      uint32_t w[PER][N][V / 4], s[PER];
       int row[PER], col[PER], live[PER];
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
         const int i = i0 + p * GROUPS + group;
         row[p] = nb > ITEMS ? 0 : div_by(i, nb, rcp);
         const int blk = i - row[p] * nb;
-        col[p] = blk * ROW8_BLOCK + lane * 8;
+        col[p] = blk * ROW8_BLOCK + lane * V;
         live[p] = i < n ? a.cols - col[p] : 0;
         if (live[p] > 0) {
-          w[p] = *(const uint2*)(a.codes + (row0 + row[p]) * cs + col[p]);
           s[p] = a.scales[(row0 + row[p]) * ss + blk];
+#pragma unroll
+          for (int k = 0; k < N; ++k)
+            if (live[p] > k * 16 * V)
+              __builtin_memcpy(w[p][k], a.codes + (row0 + row[p]) * cs + col[p] + k * 16 * V, V);
         }
       }
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
         if (live[p] <= 0) continue;
-        float f[8];
-        row8_values4(w[p].x, row8_pow2(s[p]), f);
-        row8_values4(w[p].y, row8_pow2(s[p]), f + 4);
         T* y = (T*)a.y + (row0 + row[p]) * a.y_stride + col[p];
-        Run8<T> r;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r.e[e] = Elem<T>::from_f32(f[e]);
-        if (live[p] >= 8) {
-          __builtin_memcpy(y, &r, sizeof(r));
-        } else {
+        for (int k = 0; k < N; ++k) {
+          const int left = live[p] - k * 16 * V;
+          if (left <= 0) continue;
+          float f[V];
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (e < live[p]) y[e] = r.e[e];
+          for (int e = 0; e < V; e += 4) row8_values4(w[p][k][e / 4], row8_pow2(s[p]), f + e);
+          struct {
+            T e[V];
+          } r;
+#pragma unroll
+          for (int e = 0; e < V; ++e) r.e[e] = Elem<T>::from_f32(f[e]);
+          if (left >= V) {
+            store_vector(y + k * 16 * V, r, a.stream);
+          } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+              if (e < left) y[k * 16 * V + e] = r.e[e];
+          }
         }
       }
     }
