@@ -827,12 +827,25 @@ __device__ inline void join_means(const GroupNormArgs& a, const float* piece, in
     smem[lanes * width + i] = v * g;
   }
   __syncthreads();
+  // many lanes: eight of them first
+  const int few = min(lanes, 8);
+  if (lanes > few) {
+    for (int i = threadIdx.x; i < 2 * few * width; i += NT) {
+      const int l = i / width, c = i - l * width, k = l / few;
+      float* p = smem + (k * lanes + l - k * few) * width + c;
+      float v = p[0];
+#pragma unroll 4
+      for (int q = few; q < lanes - (l - k * few); q += few) v += p[q * width];
+      p[0] = v;  // (this thread's alone)
+    }
+    __syncthreads();
+  }
   for (int k = 0; k < 2; ++k)
     group_totals(groups, per,
                  [&](int c) {
                    float v = 0.f;
-#pragma unroll 4
-                   for (int l = 0; l < lanes; ++l) v += smem[(k * lanes + l) * width + c];
+#pragma unroll 8
+                   for (int l = 0; l < few; ++l) v += smem[(k * lanes + l) * width + c];
                    return v;
                  },
                  [&](int g, float sum) { done(k, g, sum * rn); });

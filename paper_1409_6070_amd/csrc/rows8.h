@@ -22,22 +22,15 @@ __host__ __device__ inline int64_t row8_blocks(int64_t cols) { return (cols + RO
 __host__ __device__ inline int64_t row8_code_stride(int64_t cols) { return round_up(cols, 16); }
 __host__ __device__ inline int64_t row8_scale_stride(int64_t cols) { return round_up(row8_blocks(cols), 4); }
 
-// The scale byte of a block whose largest finite magnitude is `most`: 448 = 1.75 * 2^8, so
+// The scale byte of a block whose largest finite magnitude has bits `most`: 448 = 1.75 * 2^8, so
 // the exponent is the magnitude's less 8, one more where its fraction passes 1.75.
-__device__ inline uint32_t row8_scale(float most) {
-  const int s = (int)((__float_as_uint(most) + 0x1FFFFFu) >> 23) - 8;
+__device__ inline uint32_t row8_scale(uint32_t most) {
+  const int s = (int)((most + 0x1FFFFFu) >> 23) - 8;
   return (uint32_t)(s < 1 ? 1 : s);
 }
-__device__ inline float row8_pow2(uint32_t s) { return __uint_as_float(s << 23); }           // 2^(s - 127), s >= 1
-__device__ inline float row8_inverse(uint32_t s) { return __uint_as_float((254u - s) << 23); }  // 2^(127 - s)
+__device__ inline float row8_pow2(uint32_t s) { return __uint_as_float(s << 23); }  // 2^(s - 127), s >= 1
 
 __device__ inline bool is_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
-
-// Four values, already scaled, as four codes; values that are not finite become NaN.
-__device__ inline uint32_t row8_codes4(float a, float b, float c, float d) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
-}
 
 typedef float row8_f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 row8_bf16x2 __attribute__((ext_vector_type(2)));

@@ -27,34 +27,77 @@ __device__ inline Run8<T> load_run(const T* p, int n) {
   return r;
 }
 
+// The bits of a run's largest magnitude; any that is not finite passes 0x7f800000 or counts
+// for nothing (a float32 NaN).
+__device__ inline uint32_t largest(const Run8<float>& r) {
+  float m = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(r.e[e]));
+  return __float_as_uint(m);
+}
+__device__ inline uint32_t largest(const Run8<__bf16>& r) {
+  typedef uint16_t U16x2 __attribute__((ext_vector_type(2)));
+  uint32_t w[4];
+  __builtin_memcpy(w, &r, sizeof(r));
+  U16x2 m = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(U16x2, w[i] & 0x7fff7fffu));
+  return (uint32_t)max(m[0], m[1]) << 16;
+}
+// ... of its finite values.
 template <typename T>
-__device__ inline float largest(const Run8<T>& r) {
+__device__ inline uint32_t largest_finite(const Run8<T>& r) {
   float m = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float f = fabsf(Elem<T>::to_f32(r.e[e]));
     m = fmaxf(m, is_finite(f) ? f : 0.f);
   }
-  return m;
+  return __float_as_uint(m);
 }
 
-template <typename T>
-__device__ inline uint2 codes_of(const Run8<T>& r, float inv) {
-  float f[8];
+typedef int16_t I16x2 __attribute__((ext_vector_type(2)));
+
+// Codes under scale byte s: values that are NaN become NaN.
+__device__ inline uint2 codes_of(const Run8<float>& r, uint32_t s) {
+  const float scale = row8_pow2(s);
+  I16x2 w[2] = {{0, 0}, {0, 0}};
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float x = Elem<T>::to_f32(r.e[e]);
-    f[e] = is_finite(x) ? x * inv : __uint_as_float(0x7fc00000u);
+  for (int i = 0; i < 2; ++i) {
+    w[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w[i], r.e[4 * i], r.e[4 * i + 1], scale, false);
+    w[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w[i], r.e[4 * i + 2], r.e[4 * i + 3], scale, true);
   }
-  return uint2{row8_codes4(f[0], f[1], f[2], f[3]), row8_codes4(f[4], f[5], f[6], f[7])};
+  return uint2{__builtin_bit_cast(uint32_t, w[0]), __builtin_bit_cast(uint32_t, w[1])};
 }
+__device__ inline uint2 codes_of(const Run8<__bf16>& r, uint32_t s) {
+  const float scale = row8_pow2(s);
+  row8_bf16x2 x[4];
+  __builtin_memcpy(x, &r, sizeof(r));
+  I16x2 w[2] = {{0, 0}, {0, 0}};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    w[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w[i], x[2 * i], scale, false);
+    w[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w[i], x[2 * i + 1], scale, true);
+  }
+  return uint2{__builtin_bit_cast(uint32_t, w[0]), __builtin_bit_cast(uint32_t, w[1])};
+}
+// ... and infinities too.
+template <typename T>
+__device__ inline Run8<T> without_infinities(Run8<T> r) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (!is_finite(Elem<T>::to_f32(r.e[e]))) r.e[e] = Elem<T>::from_f32(__uint_as_float(0x7fc00000u));
+  return r;
+}
+constexpr uint32_t NOT_FINITE = 0x7f800000u;
 
 template <int CTRL>
-__device__ inline float max_dpp(float v) {
-  return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true)));
+__device__ inline uint32_t max_dpp(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true));
 }
 // Largest over aligned groups of 16 lanes, in all of them.
-__device__ inline float max16(float v) {
+__device__ inline uint32_t max16(uint32_t v) {
   v = max_dpp<0xB1>(v);   // quad_perm 1,0,3,2
   v = max_dpp<0x4E>(v);   // quad_perm 2,3,0,1
   v = max_dpp<0x141>(v);  // row_half_mirror
@@ -95,9 +138,14 @@ __global__ void __launch_bounds__(256) k_rows8_store(Rows8Args a, int R, int64_t
       }
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
-        const uint32_t s = row8_scale(max16(largest(x[p])));
+        uint32_t most = max16(largest(x[p]));
+        if (most >= NOT_FINITE) {  // (the block's sixteen lanes together)
+          most = max16(largest_finite(x[p]));
+          x[p] = without_infinities(x[p]);
+        }
+        const uint32_t s = row8_scale(most);
         if (live[p] == NO_ITEM) continue;
-        const uint2 w = codes_of(x[p], row8_inverse(s));
+        const uint2 w = codes_of(x[p], s);
         const int c = blk[p] * ROW8_BLOCK + lane * 8;
         if (c < cs) *(uint2*)(a.codes + (row0 + row[p]) * cs + c) = w;
         uint8_t* sc = a.scales + (row0 + row[p]) * ss + blk[p];
@@ -170,28 +218,43 @@ template <typename T>
 __global__ void __launch_bounds__(256) k_weight8_store(Weight8Args a) {
   constexpr int LS = ROW8_BLOCK + 16;  // a row of the staged block, bytes
   __shared__ __attribute__((aligned(16))) uint8_t tile[ROW8_BLOCK * LS];
-  __shared__ float red[4];
+  __shared__ uint32_t red[4];
   const int lane = threadIdx.x & 15, group = threadIdx.x >> 4;
   const int kb = blockIdx.y, nb = blockIdx.x;
   const Weight8 w = weight8_parts(a.w8, a.k, a.n);
   Run8<T> x[8];
-  float m = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int r = kb * ROW8_BLOCK + i * 16 + group, c = nb * ROW8_BLOCK + lane * 8;
     x[i] = load_run<T>((const T*)a.w + (int64_t)min(r, a.k - 1) * a.w_stride + c, r < a.k ? a.n - c : 0);
   }
+  // the largest magnitude's bits over the workgroup
+  auto over_all = [&](uint32_t m) {
+    m = max16(m);
+    for (int d = 16; d < 64; d *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, d));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+    __syncthreads();
+    return max(max(red[0], red[1]), max(red[2], red[3]));
+  };
+  uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = fmaxf(m, largest(x[i]));
-  m = max16(m);
-  for (int d = 16; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-  __syncthreads();
-  const uint32_t s = row8_scale(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+  for (int i = 0; i < 8; ++i) m = max(m, largest(x[i]));
+  m = over_all(m);
+  if (m >= NOT_FINITE) {
+    m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      m = max(m, largest_finite(x[i]));
+      x[i] = without_infinities(x[i]);
+    }
+    m = over_all(m);
+  }
+  const uint32_t s = row8_scale(m);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int r = i * 16 + group, c = lane * 8;
-    const uint2 v = codes_of(x[i], row8_inverse(s));
+    const uint2 v = codes_of(x[i], s);
     *(uint2*)(tile + r * LS + c) = v;
     if (kb * ROW8_BLOCK + r < a.k)
       *(uint2*)(w.codes + (int64_t)(kb * ROW8_BLOCK + r) * w.stride + nb * ROW8_BLOCK + c) = v;
