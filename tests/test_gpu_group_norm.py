@@ -3,9 +3,10 @@ of one channel and of all, odd lengths, strides and alignments, rows outside the
 pass, infinities and NaN; and a stage of 8-bit product, group norm and network as they are used together.
 
 Bounds.  u = 2^-24.  A term passes at most D additions in a sum: a thread's rows of a chunk (8, or its share of
-1024 chunks), the row lanes of a workgroup (1024 at most where rows are short, and as many in the channels of a group),
-the pieces of a sample by 64 lanes: D = 32 + rows / 1024 + lanes + channels + pieces / 64, lanes <= 1024 / vectors of a
-row.  e = D u mean|x| for the mean.  The variance sums deviations from one of a thread's own n values, whose squares sum
+1024 chunks) or of a small sample (16 in registers), the row lanes of a workgroup (1024 at most where rows are short, and
+as many in the channels of a group), the pieces of a sample by 64 lanes: D = 32 + rows / 1024 + lanes + channels +
+pieces / 64, lanes <= 1024 / vectors of a row.  A sample of more than three times the mean length may be read in a loop
+by one workgroup of 256 threads or more: its rows times the vectors of a row, over 256, besides.  e = D u mean|x| for the mean.  The variance sums deviations from one of a thread's own n values, whose squares sum
 to at most 2 (1 + n) times those from the mean: D u (3 + 2 n) relative, and (e r)^2 for the mean's error; r half of that
 plus 3 u.  The rest counts one u per operation; the result's rounding is half a step of its type.  The exponential's
 argument is rounded once more and its result by 2 u: a sigmoid is off by (6 + |z|) u relative, SiLU's derivative by
@@ -40,10 +41,13 @@ def _np(t):
     return t.double().cpu().numpy()
 
 
-def _depth(rows, cols, per, dtype):
+def _depth(rows, cols, per, dtype, mean=None):
+    """D, rows of a thread (mean: rows of a sample on average, where there are several)"""
     v = 8 if dtype == "bf16" else 4
-    lanes = max(1, 1024 // max(1, -(-cols // v)))
-    return 32 + rows / 1024 + lanes + per + (rows / 8 + 2) / 64, 8 + rows / 1024  # D, rows of a thread
+    vecs = -(-cols // v)
+    lanes = max(1, 1024 // vecs)
+    loop = rows * 2 * vecs / 256 if mean is not None and rows > 3 * mean else 0
+    return 32 + rows / 1024 + lanes + per + (rows / 8 + 2) / 64 + loop, 16 + rows / 1024
 
 
 def _act(z, act):
@@ -71,7 +75,7 @@ def _want_forward(x, begin, gain, shift, groups, act, dtype):
         if lo == hi:
             continue
         p = x[lo:hi].reshape(hi - lo, groups, per)
-        D, n = _depth(hi - lo, cols, per, dtype)
+        D, n = _depth(hi - lo, cols, per, dtype, rows / batch)
         m = p.mean((0, 2))
         d = p - m[:, None]
         r = 1.0 / np.sqrt((d * d).mean((0, 2)) + EPS)
@@ -118,7 +122,7 @@ def _want_backward(dy, x, stats, begin, gain, shift, groups, act, dtype):
         dz = d * slope
         edz = np.abs(d) * eslope + U * np.abs(dz)
         t, et = dz * gain, np.abs(gain) * edz + U * np.abs(dz * gain)
-        D, _ = _depth(hi - lo, cols, per, dtype)
+        D, _ = _depth(hi - lo, cols, per, dtype, rows / (len(begin) - 1))
 
         def mean(v):
             return np.repeat(v.sum(0).reshape(groups, per).sum(1) / ((hi - lo) * per), per)
@@ -232,6 +236,17 @@ def test_samples(dtype):
                                                           (9000, 1024, 32, 9, "bf16")])
 def test_many_rows(rows, cols, groups, batch, dtype):
     _check(rows, cols, groups, _begins(rows, batch, 5), dtype, "leaky", x8=batch % 2 == 1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_small_samples(dtype):
+    """One launch: slices of groups of unequal number, samples that fill the registers and ones that outgrow them."""
+    for cols, groups, lengths, act in ((100, 10, [600] * 3 + [0, 3, 2500], "silu"), (60, 12, [30] * 40, "leaky"), (100, 100, [1, 5, 2], "none"),
+                                       (24, 3, [200] * 9 + [4000], "relu"), (7, 7, [100, 3], "silu"), (300, 20, [64, 1, 190], "leaky"),
+                                       (2048, 16, [9, 7], "silu"), (34, 17, [20] * 1100, "leaky"), (4096, 4, [3, 1, 2], "none")):
+        begin = [0] + np.cumsum(lengths).tolist()
+        for x8 in (False, True):
+            _check(begin[-1], cols, groups, begin, dtype, act, 1, seed=cols, x8=x8)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

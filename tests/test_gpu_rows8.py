@@ -5,8 +5,8 @@ on small whole numbers (every product and partial sum fits the instructions' nar
 against 64 bits.
 
 Bounds.  u = 2^-24.  Results in float32: products of codes are exact, a sum in which a term passes at most D additions
-is off by at most D u sum|terms|; one instruction adds 32 products, one follows the other: D = 32 + terms / 32 + 4, and
-the parts of a weight gradient's rows add their number.  Results in bf16: of eight products what lies under 2^-13 of
+is off by at most D u sum|terms|; one instruction adds 32 products, one follows the other: D = 32 + terms / 32 + 4, where
+waves share a sum eight more, and the parts of a weight gradient's rows add their number.  Results in bf16: of eight products what lies under 2^-13 of
 the largest may be dropped: at most 7 * 2^-13 sum|terms| beside the rounding of 2^-8; as a whole (2-norm) the roundings
 alone make at most 2^-8 and 2^-9 in the root mean square over mantissas spread over an octave (half a step is between
 2^-9 and 2^-8 of a value: 2^-8 / sqrt 3 times the mean of that over the octave, under 0.0018), to which errors of
@@ -228,7 +228,7 @@ def _inside(got, want, tol, what):
 def _product_bound(a, b, dtype):
     """[m, k] @ [k, n] in 64 bits, with the bound of each entry."""
     want, mag = a @ b, np.abs(a) @ np.abs(b)
-    D = 32 + a.shape[1] / 32 + 4
+    D = 32 + a.shape[1] / 32 + 4 + 8
     if dtype == "f32":
         return want, D * U * mag + 1e-300
     return want, (7 * 2.0 ** -13 + D * U) * mag + 2.0 ** -8 * np.abs(want) + 1e-300
@@ -270,6 +270,35 @@ def test_products(rows, k, n, dtype):
     D = 32 + rows / 32 + 4 + 512
     _inside(dw, xq.T @ dyq, D * U * (np.abs(xq).T @ np.abs(dyq)) + 1e-300, "dw")
     _inside(db, dyq.sum(0), D * U * np.abs(dyq).sum(0) + 1e-300, "db")
+
+
+@pytest.mark.parametrize("rows,k,n", [(8187, 2050, 2040), (16400, 4100, 2048), (40000, 129, 300), (3000, 520, 515), (260, 4099, 4101)])
+def test_large_products_of_whole_numbers(rows, k, n):
+    """The large tiles, several of them to a workgroup, results that go past the caches; sums checked in 64 bits on the
+    GPU.  Entries are -1 .. 1: every sum is exact, rounded once to bf16."""
+    from paper_1409_6070_amd.sscn import Product8, Rows8
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x, w, dy = (torch.randint(-1, 2, s, generator=g, device="cuda").float() for s in ((rows, k), (k, n), (rows, n)))
+    x8, dy8 = Rows8(rows, k).store(x), Rows8(rows, n).store(dy)
+    xd, wd, dyd = x.double(), w.double(), dy.double()
+    y, dx = torch.mm(xd, wd), torch.mm(dyd, wd.t().contiguous())
+    for dtype in ("bf16", "f32"):
+        p = Product8(k, n, rows, dtype).set_weights(w)
+        assert torch.equal(p.forward(x8), y.to(TORCH[dtype])), "forward"
+        assert torch.equal(p.input_grad(dy8), dx.to(TORCH[dtype])), "input gradient"
+    dw, db = p.weight_grad(x8, dy8)
+    assert torch.equal(dw.double(), torch.mm(xd.t().contiguous(), dyd)) and torch.equal(db.double(), dyd.sum(0))
+
+
+@pytest.mark.parametrize("rows,cols", [(20000, 1024), (40001, 1000)])
+def test_large_loads(rows, cols):
+    """Results that go past the caches, of whole lines and not."""
+    from paper_1409_6070_amd.sscn import Rows8
+    r = Rows8(rows, cols).store(torch.randn(rows, cols, device="cuda"))
+    a, b = r.load("f32"), r.load("bf16")
+    assert torch.equal(a, b.float())
+    part = r.rows_from(rows - 50, rows)
+    assert torch.equal(part.load("f32"), a[-50:])
 
 
 @pytest.mark.parametrize("k,n", [(1, 1), (130, 257), (300, 129), (128, 128)])
