@@ -5,13 +5,14 @@
 //   weight gradient dw = x^T dy, dbias = sum over rows of dy
 //
 // The first two are one product, of rows with a matrix that lies along the sum either
-// way.  A result in bf16 is computed by the scaled matrix instructions: 16 x 16 x 128 on
+// way.  A result in bf16 is computed by the scaled matrix instructions, 32 x 32 x 64 on
 // the codes themselves, each row's (and the matrix block's) power of two as an operand.
-// Their sums are float32, but within one instruction's 128 products what lies far below
-// the largest is dropped: results are off by 1.5e-5 to 4e-5 of their size on sums of
-// either sign (3e-6 where all are positive) whatever k is, a hundredth of the rounding to
-// bf16.  A result in float32 is computed by the bf16 instructions instead, in which a
-// code times its scale is exact and so is each product: 1e-7, at half the rate.
+// Their sums are float32, but of every eight products they drop what lies below 2^-13 of
+// the largest (7 2^-13 of the sum of the magnitudes at most): results are off by 1.5e-5 to
+// 4e-5 of their size on sums of either sign, 3e-6 where all are positive, whatever k is: a
+// hundredth of the rounding to bf16.  A result in float32 is computed by the bf16
+// instructions instead, in which a code times its scale is exact and so is each product:
+// 1e-7, at half the rate.
 //
 // The weight gradient sums over rows, whose scales differ from term to term: both operands
 // become bf16 (exactly) on their way to LDS and are read from there transposed.
@@ -382,90 +383,143 @@ __device__ inline Codes16 to_bf16(u32x4 codes, float scale) {
   return o;
 }
 
-// float32 results: slabs of 64 codes, made bf16 on the way to LDS; 128 x 128 tiles of four
-// waves.
-__global__ void __launch_bounds__(256, 2) k_product8_exact(Product8Args a, int64_t tiles, int64_t mt, int nt) {
-  constexpr int STAGE = 2 * 128 * 128;  // bytes: two operands of 128 rows of 64 bf16
+// WX x WN waves, each 16 TX rows by 64 columns, of results in float32.
+template <int WX_, int WN_, int TX_>
+struct P8Exact {
+  static constexpr int WX = WX_, WN = WN_, TX = TX_;
+  static constexpr int NT = WX * WN * 64, BM = WX * TX * 16, BN = WN * 64;
+  static constexpr int STAGE = (BM + BN) * 128, LDS = 2 * STAGE;  // 64 bf16 of every row of either operand
+  static_assert(BM == BN && BM * 2 == NT, "a thread stages 32 codes of either operand");
+};
+
+// float32 results: slabs of 64 codes, made bf16 on the way to LDS.  A slab is multiplied while
+// the next one is staged, between its halves, and the one behind that is on its way; an
+// operand is read while the one before it is multiplied.
+template <class C>
+__global__ void __launch_bounds__(C::NT, 2) k_product8_exact(Product8Args a, int64_t tiles, int64_t mt, int nt) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int wx = wave >> 1, wn = wave & 1, r16 = lane & 15, g = lane >> 4;
+  const int wx = wave / C::WN, wn = wave % C::WN, r16 = lane & 15, g = lane >> 4;
   const int lr = threadIdx.x >> 1, lc = (threadIdx.x & 1) * 32;  // this thread's row of either operand, and its codes
+  // Where this lane's chunks of its first blocks lie: x's others are 16 rows on, w's four (of
+  // interleaved ones), and the second half's chunks 64 bytes off.
+  const uint32_t xa = (uint32_t)((wx * C::TX * 16 + r16) * 128 + slot_x(r16, g) * 16);
+  const int wr = interleaved(r16, 0);
+  const uint32_t wa = (uint32_t)((C::BM + wn * 64 + wr) * 128 + slot_w(wr, g) * 16);
+  const int slabs = (int)((a.x_stride + 63) / 64);
   for (int64_t t = blockIdx.x; t < (tiles + 7) / 8 * 8; t += gridDim.x) {
     if ((t & 7) * ((tiles + 7) / 8) + (t >> 3) >= tiles) continue;
     const TilePlace at = place_of(t, tiles, mt, nt);
-    const int64_t m0 = at.m * 128;
-    const int n0 = at.n * 128;
-    const bool xin = m0 + lr < a.rows, win = n0 + lr < a.n;
-    const uint8_t* x = a.x + (xin ? m0 + lr : m0) * a.x_stride + lc;
-    const uint8_t* xs = a.xs + (xin ? m0 + lr : m0) * a.xs_stride;
-    const uint8_t* w = a.w + (int64_t)(win ? n0 + lr : n0) * a.w_stride + lc;
-    const uint8_t* ws = a.ws + (int64_t)at.n * a.ws_stride;
-    u32x4 xv[2], wv[2];
-    uint32_t sx = 127, sw = 127;
-    auto fetch = [&](int s) {
+    const int64_t m0 = at.m * C::BM;
+    const int n0 = at.n * C::BN;
+    const int rows = (int)min((int64_t)C::BM, a.rows - m0), cols = min(C::BN, a.n - n0);
+    auto of = [&](const uint8_t* base, int64_t stride, int n) {
+      return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)((uint32_t)n * (uint32_t)stride), 0x00020000);
+    };
+    // (rows behind the last: past the buffer)
+    const auto rx = of(a.x + m0 * a.x_stride, a.x_stride, rows), rsx = of(a.xs + m0 * a.xs_stride, a.xs_stride, rows);
+    const auto rw = of(a.w + n0 * a.w_stride, a.w_stride, cols);
+    const auto rsw = of(a.ws + (int64_t)(n0 >> 7) * a.ws_stride, a.ws_stride, (cols + 127) >> 7);
+    const uint32_t xo = (uint32_t)(lr * a.x_stride) + lc, wo = (uint32_t)(lr * a.w_stride) + lc;
+    const uint32_t xso = (uint32_t)(lr * a.xs_stride), wso = (uint32_t)(lr >> 7) * (uint32_t)a.ws_stride;
+    struct Staged {
+      u32x4 x[2], w[2];
+      uint32_t sx, sw;
+    };
+    auto fetch = [&](Staged& o, int s) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        xv[h] = wv[h] = u32x4{0, 0, 0, 0};
-        if (xin && s * 64 + lc + h * 16 < a.x_stride) xv[h] = *(const u32x4*)(x + s * 64 + h * 16);
-        if (win) wv[h] = *(const u32x4*)(w + s * 64 + h * 16);
+        const uint32_t k = (uint32_t)s * 64u + h * 16u;
+        const bool in = k + lc < (uint32_t)a.x_stride;
+        o.x[h] = __builtin_amdgcn_raw_buffer_load_b128(rx, (int)(in ? xo + k : NO_SOURCE), 0, 0);
+        o.w[h] = __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(in ? wo + k : NO_SOURCE), 0, 0);
       }
-      sx = xs[s >> 1];
-      sw = ws[s >> 1];
+      const uint32_t b = (uint32_t)min(s, slabs - 1) >> 1;
+      o.sx = __builtin_amdgcn_raw_buffer_load_b8(rsx, (int)(xso + b), 0, 0);
+      o.sw = __builtin_amdgcn_raw_buffer_load_b8(rsw, (int)(wso + b), 0, 0);
     };
-    auto put = [&](int st) {
-      uint8_t* X = smem + st * STAGE + lr * 128;
-      uint8_t* W = X + STAGE / 2;
+    auto put = [&](const Staged& o, int st) {
+      uint8_t* X = smem + st * C::STAGE + lr * 128;
+      uint8_t* W = X + C::BM * 128;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int c = lc / 8 + h * 2;
-        const Codes16 vx = to_bf16(xv[h], row8_pow2(sx)), vw = to_bf16(wv[h], row8_pow2(sw));
+        const Codes16 vx = to_bf16(o.x[h], row8_pow2(o.sx)), vw = to_bf16(o.w[h], row8_pow2(o.sw));
         *(u32x4*)(X + slot_x(lr, c) * 16) = vx.lo;
         *(u32x4*)(X + slot_x(lr, c + 1) * 16) = vx.hi;
         *(u32x4*)(W + slot_w(lr, c) * 16) = vw.lo;
         *(u32x4*)(W + slot_w(lr, c + 1) * 16) = vw.hi;
       }
     };
-    f32x4 acc[4][4];
+    f32x4 acc[C::TX][4];
+    {  // the sums start from the bias
+      float b[16];
+      load_bias(a.bias, n0 + wn * 64 + g * 16, a.n, b);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < C::TX; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int slabs = (int)((a.x_stride + 63) / 64);
-    fetch(0);
-    __syncthreads();  // (every wave done with the tile before)
-    put(0);
-    for (int s = 0; s < slabs; ++s) {
-      if (s + 1 < slabs) fetch(s + 1);
-      __syncthreads();
-      const uint8_t* X = smem + (s & 1) * STAGE;
-      const uint8_t* W = X + STAGE / 2;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        bf16x8 xo[4], wo[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = wx * 64 + i * 16 + r16, q = wn * 64 + interleaved(r16, i);
-          xo[i] = *(const bf16x8*)(X + r * 128 + slot_x(r, kb * 4 + g) * 16);
-          wo[i] = *(const bf16x8*)(W + q * 128 + slot_w(q, kb * 4 + g) * 16);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wo[j], xo[i], acc[i][j], 0, 0, 0);
-      }
-      if (s + 1 < slabs) put((s + 1) & 1);
+        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{b[4 * j], b[4 * j + 1], b[4 * j + 2], b[4 * j + 3]};
     }
-    const int c = n0 + wn * 64 + g * 16;
-    float b[16];
-    load_bias(a.bias, c, a.n, b);
+    Staged ahead;
+    fetch(ahead, 0);
+    __syncthreads();  // (every wave is done with the tile before)
+    put(ahead, 0);
+    fetch(ahead, 1);
+    for (int s = 0; s < slabs; ++s) {
+      const int st = s & 1;
+      __syncthreads();
+      bf16x8 x[2], w[2][4];
+      const uint8_t* base = smem + st * C::STAGE;
+      auto x_read = [&](int n) {
+        x[n & 1] = *(const bf16x8*)(base + (xa ^ (n / C::TX * 64u)) + n % C::TX * 2048);
+      };
+      auto w_read = [&](int half, int j) { w[half][j] = *(const bf16x8*)(base + (wa ^ (half * 64u)) + j * 512); };
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t m = m0 + wx * 64 + i * 16 + r16;
-      if (m >= a.rows || c >= a.n) continue;
-      float v[16];
+      for (int j = 0; j < 4; ++j) w_read(0, j);
+      x_read(0);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) v[e] = acc[i][e >> 2][e & 3] + b[e];
-      store_run16<float>((float*)a.y + m * a.y_stride, c, a.n, v);
+      for (int n = 0; n < 2 * C::TX; ++n) {
+        const int half = n / C::TX, i = n % C::TX;
+        if (n + 1 < 2 * C::TX) x_read(n + 1);
+        if (half == 0 && i >= C::TX - 4) w_read(1, i - (C::TX - 4));
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[half][j], x[n & 1], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (n == C::TX - 1) {
+          put(ahead, st ^ 1);  // (behind the last slab: zeros, not read)
+          fetch(ahead, s + 2);
+        }
+      }
+    }
+    // 16 x 64 results of a wave at a time through LDS, from where whole lines are stored
+    __syncthreads();
+    uint8_t* stage = smem + wave * 4096;
+    const int c = n0 + wn * 64 + (lane & 15) * 4;
+#pragma unroll
+    for (int i = 0; i < C::TX; ++i) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) *(f32x4*)(stage + r16 * 256 + ((g * 4 + j) ^ r16) * 16) = acc[i][j];
+      f32x4 line[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int r = k * 4 + g;
+        line[k] = *(const f32x4*)(stage + r * 256 + (r16 ^ r) * 16);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int64_t m = m0 + (wx * C::TX + i) * 16 + k * 4 + g;
+        if (m >= a.rows || c >= a.n) continue;
+        float* y = (float*)a.y + m * a.y_stride + c;
+        if (c + 4 <= a.n) {
+          store_vector(y, line[k], a.stream);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (c + e < a.n) y[e] = line[k][e];
+        }
+      }
     }
   }
 }
@@ -817,14 +871,15 @@ hipError_t launch_few(const Product8Args& a, hipStream_t st) {
   return go(k_product8_few<T, 4, 2>, 4, 2);
 }
 
+template <class C>
 hipError_t launch_exact(const Product8Args& a, hipStream_t st) {
-  const int64_t mt = (a.rows + 127) / 128;
-  const int nt = (a.n + 127) / 128;
+  const int64_t mt = (a.rows + C::BM - 1) / C::BM;
+  const int nt = (a.n + C::BN - 1) / C::BN;
   const int64_t tiles = mt * nt;
-  const hipError_t e = allow_lds<k_product8_exact>(65536);
+  const hipError_t e = allow_lds<k_product8_exact<C>>(C::LDS);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_product8_exact, dim3((unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, 1 << 20)), dim3(256), 65536,
-                     st, a, tiles, mt, nt);
+  hipLaunchKernelGGL(k_product8_exact<C>, dim3((unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, 1 << 20)), dim3(C::NT),
+                     C::LDS, st, a, tiles, mt, nt);
   return hipGetLastError();
 }
 
@@ -835,15 +890,19 @@ hipError_t launch_product8(bool bf16, const Product8Args& a, hipStream_t st) {
   // in float32 18.7 and 54; 256 x 4096 x 4096 (512) 33.6 and 22, in float32 35 and 55.
   const int64_t few = (a.rows + 63) / 64 * ((a.n + 31) / 32);
   if (a.rows <= 32 || few <= (bf16 ? 256 : 512)) return bf16 ? launch_few<__bf16>(a, st) : launch_few<float>(a, st);
-  if (!bf16) return launch_exact(a, st);
-  // Rounds of workgroups times what one takes, measured: 11 + 1.68 us a slab for 256 x 256,
-  // 2.1 + 1.25 for two workgroups of 128 x 128 on a compute unit (32768 x 4096 x 4096: 522
-  // and 675 us; 32768 x 512 x 4096: 143 and 114; 2000 x 2000 x 2000: 26.5 and 15.5).
-  const int64_t big = ((a.rows + 255) / 256 * ((a.n + 255) / 256) + 255) / 256;
-  const int64_t small = ((a.rows + 127) / 128 * ((a.n + 127) / 128) + 511) / 512;
-  if ((double)big * (11.0 + 1.68 * a.kb) < (double)small * (2.1 + 1.25 * a.kb))
-    return launch_tiles<P8Tile<2, 4, 4>>(a, 256, st);
-  return launch_tiles<P8Tile<2, 2, 2>>(a, 512, st);
+  // Rounds of workgroups times what one takes, in us for `slabs` slabs, as measured: 256 x 256
+  // tiles, one a compute unit, and 128 x 128, two.  32768 x 4096 x 4096 bf16 502 and 675 us,
+  // float32 950 and 1152; 32768 x 512 x 4096 bf16 143 and 114; 200001 x 300 x 300 bf16 82 and
+  // 52, float32 129 and 120; 2000 x 2000 x 2000 bf16 26 and 16, float32 59 and 30.
+  const double big = (double)(((a.rows + 255) / 256 * ((a.n + 255) / 256) + 255) / 256);
+  const double small = (double)(((a.rows + 127) / 128 * ((a.n + 127) / 128) + 511) / 512);
+  if (bf16) {
+    if (big * (11.0 + 1.68 * a.kb) < small * (2.1 + 1.25 * a.kb)) return launch_tiles<P8Tile<2, 4, 4>>(a, 256, st);
+    return launch_tiles<P8Tile<2, 2, 2>>(a, 512, st);
+  }
+  const double slabs = (double)((a.x_stride + 63) / 64);
+  if (big * (9.0 + 1.73 * slabs) < small * (5.0 + 1.07 * slabs)) return launch_exact<P8Exact<2, 4, 8>>(a, st);
+  return launch_exact<P8Exact<2, 2, 4>>(a, st);
 }
 
 namespace {
