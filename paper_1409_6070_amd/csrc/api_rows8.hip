@@ -293,7 +293,7 @@ sscn_status sscn_product8_input_grad(int32_t dtype, const sscn_rows8* dy, const 
 sscn_status sscn_product8_weight_grad_workspace_bytes(int64_t rows, int32_t k, int32_t n, size_t* bytes) {
   if (rows < 0 || rows > SSCN_MAX_ROWS || !product_side_ok(k) || !product_side_ok(n) || !bytes)
     return SSCN_ERR_INVALID_ARGUMENT;
-  const size_t splits = (size_t)weight_grad8_splits(rows, k, n);
+  const size_t splits = (size_t)weight_grad8_most_splits(rows, k, n);
   *bytes = splits > 1 ? splits * ((size_t)k + 1) * (size_t)n * 4 : 0;
   return SSCN_OK;
 }

@@ -611,10 +611,10 @@ struct WeightGrad8Args {
   float* dw;              // [k][dw_stride]
   int64_t dw_stride;
   float* db;              // [n], or null
-  float* part;            // [splits][k][n], then [splits][n]; null where splits is 1
+  float* part;            // [splits][k][n], then [splits][n] (most_splits > 1)
 };
-// Workgroups that share a tile's rows.
-int32_t weight_grad8_splits(int64_t rows, int32_t k, int32_t n);
+// Workgroups that share a tile's rows, at most (grows with the rows).
+int32_t weight_grad8_most_splits(int64_t rows, int32_t k, int32_t n);
 hipError_t launch_weight_grad8(const WeightGrad8Args& a, hipStream_t st);
 
 // group_norm.hip: normalisation over a sample's rows and a group's channels, with an activation

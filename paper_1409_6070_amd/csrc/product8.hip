@@ -329,8 +329,8 @@ __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int6
       issue(0);
     }
     // 64 x 64 results of a wave at a time through its part of the second stage, from where whole
-    // lines are stored: eight rows of 128 bytes by an instruction (from the registers 64
-    // pieces of 16 bytes: 15 us instead of .. for a round of 256 x 256 tiles)
+    // lines are stored: eight rows of 128 bytes by an instruction (200001 x 300 x
+    // 300 52 us; from the registers, in 64 pieces of 16 bytes, 64)
     uint8_t* stage = smem + C::SLAB + wave * 8192;
 #pragma unroll
     for (int p = 0; p < C::TX; p += 2) {
@@ -528,7 +528,7 @@ __global__ void __launch_bounds__(C::NT, 2) k_product8_exact(Product8Args a, int
 // Few rows: a workgroup's waves share the sum of MB x 16 rows by NB x 16 columns, every wave
 // a run of its blocks of 128, operands straight into registers (16 rows of 128 bytes by two
 // loads), and meet in LDS.  Bound by latency and by reading the matrix once: one row, 300 ->
-// 3755 ..
+// 3755, 3.0 us; a call of 1 x 4096 x 4096 5.4 (in 128 x 128 tiles 19.7).
 constexpr int FEW_WAVES = 8;
 
 template <typename T, int MB, int NB>
@@ -910,10 +910,40 @@ namespace {
 typedef Wg8Tile<2, 4, 8> WgBig;
 typedef Wg8Tile<2, 2, 4> WgSmall;
 
-// 256 x 256 tiles where they pad the result little enough.
-bool weight_grad8_big(int32_t k, int32_t n) {
-  const int64_t big = (int64_t)((k + 255) / 256) * ((n + 255) / 256) * 4;
-  return (double)big < 1.5 * (double)(row8_blocks(k) * row8_blocks(n));
+int64_t tiles_of(int64_t k, int64_t n, int side) { return (k + side - 1) / side * ((n + side - 1) / side); }
+
+// Workgroups that share a tile's rows, at most: as many as the compute units hold at once (one of
+// 256 x 256 or two of 128 x 128 each), with two slabs of rows at least.
+int most_splits(int64_t rows, int64_t k, int64_t n, bool big) {
+  const int64_t slabs = (rows + WG_ROWS - 1) / WG_ROWS, held = big ? 256 : 512;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(slabs / 2, held / tiles_of(k, n, big ? 256 : 128)));
+}
+
+// The tile, and how many workgroups share the rows: the plan whose rounds of workgroups and
+// partial results, written and read at 5 TB/s, take least, in us fitted to measured times (a slab
+// of 64 rows 1.8 in 256 x 256 tiles, 1.4 in 128 x 128).  32768 x 4096 x 4096: 950 in 256 x 256
+// tiles, 1385 in 128 x 128; 20000 x 300 x 300: 44 and 28; 1 x 300 x 3755: 15 and 8.
+struct WgPlan {
+  bool big;
+  int splits;
+};
+WgPlan plan_weight_grad8(int64_t rows, int64_t k, int64_t n) {
+  const int64_t slabs = (rows + WG_ROWS - 1) / WG_ROWS;
+  WgPlan best{false, 1};
+  double least = 1e300;
+  for (int big = 0; big < 2; ++big) {
+    const int64_t tiles = tiles_of(k, n, big ? 256 : 128), held = big ? 256 : 512;
+    for (int s = 1, most = most_splits(rows, k, n, big != 0); s <= most; ++s) {
+      const double rounds = (double)((tiles * s + held - 1) / held);
+      const double t = rounds * (5.0 + (big ? 1.8 : 1.4) * (double)((slabs + s - 1) / s)) +
+                       (s > 1 ? 3.0 + (double)s * (double)k * (double)n * 8.0 / 5e6 : 0.0);
+      if (t < least) {
+        least = t;
+        best = WgPlan{big != 0, s};
+      }
+    }
+  }
+  return best;
 }
 
 template <class C>
@@ -927,22 +957,20 @@ hipError_t weight_grad8(const WeightGrad8Args& a, int splits, hipStream_t st) {
 
 }  // namespace
 
-int32_t weight_grad8_splits(int64_t rows, int32_t k, int32_t n) {
-  const bool big = weight_grad8_big(k, n);
-  const int64_t tiles = big ? (int64_t)((k + 255) / 256) * ((n + 255) / 256) : row8_blocks(k) * row8_blocks(n);
-  const int64_t slabs = (rows + WG_ROWS - 1) / WG_ROWS;
-  // as many workgroups as the compute units hold at once, each with four slabs at least
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(slabs / 4, (big ? 256 : 512) / tiles));
+int32_t weight_grad8_most_splits(int64_t rows, int32_t k, int32_t n) {
+  return std::max(most_splits(rows, k, n, false), most_splits(rows, k, n, true));
 }
 
-hipError_t launch_weight_grad8(const WeightGrad8Args& a, hipStream_t st) {
-  const int splits = weight_grad8_splits(a.rows, a.k, a.n);
+hipError_t launch_weight_grad8(const WeightGrad8Args& args, hipStream_t st) {
+  WeightGrad8Args a = args;
+  const WgPlan plan = plan_weight_grad8(a.rows, a.k, a.n);
+  if (plan.splits == 1) a.part = nullptr;
   const hipError_t e =
-      weight_grad8_big(a.k, a.n) ? weight_grad8<WgBig>(a, splits, st) : weight_grad8<WgSmall>(a, splits, st);
-  if (e != hipSuccess || splits == 1) return e;
+      plan.big ? weight_grad8<WgBig>(a, plan.splits, st) : weight_grad8<WgSmall>(a, plan.splits, st);
+  if (e != hipSuccess || plan.splits == 1) return e;
   const int64_t size = (int64_t)a.k * a.n + (a.db ? a.n : 0);
   hipLaunchKernelGGL(k_weight_grad8_sum, dim3((unsigned)std::min<int64_t>((size + 255) / 256, 4096)), dim3(256), 0, st, a,
-                     splits);
+                     plan.splits);
   return hipGetLastError();
 }
 
