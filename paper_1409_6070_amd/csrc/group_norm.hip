@@ -428,7 +428,9 @@ __device__ inline Stats join_pieces(const GroupNormArgs& a, int64_t chunk, const
   return Stats{mean, 1.f / sqrtf(m2 / n + a.eps)};
 }
 
-// First launch: mean and summed squares of deviations of every piece and group.
+// First launch: mean and summed squares of deviations of every piece and group.  Bound by
+// reading x: 589824 rows of 256 in bf16 (302 MB) 50 us; where rows are few, by the chain of load,
+// sum and join: 200001 of 100 (40 MB) 13.
 template <typename T, int V, int NT>
 __global__ void __launch_bounds__(NT) k_group_norm_sums(GroupNormArgs a, int64_t chunk) {
   extern __shared__ float smem[];
@@ -501,7 +503,9 @@ __global__ void __launch_bounds__(256) k_group_norm_stats(GroupNormArgs a, int64
 }
 
 // Last launch: the rows.  JOIN: the statistics come from the pieces, and the workgroup with
-// a sample's first row stores them.
+// a sample's first row stores them (a launch less where samples have few pieces).  Bound by
+// memory: 589824 rows of 256 108 us, 5.6 TB/s with x partly from the last-level cache; 200001 of
+// 100 14, latency again.
 template <typename T, int V, int NT, bool SILU, bool JOIN>
 __global__ void __launch_bounds__(NT) k_group_norm_rows(GroupNormArgs a, int64_t chunk) {
   extern __shared__ float smem[];  // JOIN: [2][groups]
@@ -567,7 +571,8 @@ struct Slice {
   }
 };
 
-// Small samples: a thread's NV rows in registers.
+// Small samples: a thread's NV rows in registers, so that x is read once.  Bound by latency: one
+// character (150 rows of 10, f32) 6.3 to 6.8 us, of which a launch is 2.4.
 template <typename T, int V, int NT, int NV, bool SILU>
 __global__ void __launch_bounds__(NT) k_group_norm_small(GroupNormArgs a, int slice, int slices) {
   extern __shared__ float smem[];
@@ -710,7 +715,10 @@ __device__ inline BwdParts bwd_parts(const GroupNormArgs& a, int64_t parts) {
   return b;
 }
 
-// First launch: a piece's sums of dz and dz h for every column, and a chunk's.
+// First launch: a piece's sums of dz and dz h for every column, and a chunk's.  Bound by reading
+// dy and x: 43 us where x is in 8 bits in rows of 512 and the next launch takes 68, 4.4 to 4.7 TB/s
+// in both; by latency in smaller ones: 20011 rows of 300 in f32 16.5, one
+// sample of 200001 rows of 100 in bf16 18.9.
 template <typename T, int V, int NT, bool X8, bool SILU>
 __global__ void __launch_bounds__(NT) k_group_norm_bwd_sums(GroupNormArgs a, int64_t chunk) {
   extern __shared__ float smem[];
@@ -877,7 +885,9 @@ __global__ void __launch_bounds__(1024) k_group_norm_bwd_means(GroupNormArgs a, 
 }
 
 // Last launch: dx.  JOIN: the means come from the pieces, and the workgroups behind those of the
-// chunks sum the gain's and shift's gradients.
+// chunks sum the gain's and shift's gradients.  Reads dy and x again and writes dx: 20011 rows
+// of 300 in f32 24.7 us, one sample of 200001 of 100 in bf16 (means by a launch of their own,
+// 10.2) 23.3.
 template <typename T, int V, int NT, bool X8, bool SILU, bool JOIN>
 __global__ void __launch_bounds__(NT) k_group_norm_bwd_rows(GroupNormArgs a, int64_t chunk, int chunks) {
   extern __shared__ float smem[];  // JOIN: join_floats, then [2][groups]

@@ -159,7 +159,8 @@ struct P8Tile {
 // half's operands are read while the half before it is multiplied; a slab is loaded while
 // the one before it is, and one barrier a slab says that it has arrived and that the stage
 // of the one before is free.  Workgroups go on to further tiles, whose first slab is
-// loaded while the results of the last one are stored.
+// loaded while the results of the last one are stored.  Bound by the matrix cores' feed: 32768 x
+// 4096 x 4096 500 us, 2.2 PFLOP/s; 8192^3 403, 2.7 (the instructions alone, on registers, 3.9).
 template <class C>
 __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int64_t tiles, int64_t mt, int nt) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
@@ -678,7 +679,9 @@ struct Wg8Tile {
   static_assert(BK == BN && BK * 2 == NT, "a thread stages 32 codes of either operand");
 };
 
-// A tile of dw over a run of rows.
+// A tile of dw over a run of rows: slabs of 64 rows through two LDS stages.  Bound by reading the
+// transposed operands, which takes LDS about as long as the products take the matrix cores:
+// 32768 x 4096 x 4096 940 to 960 us, 1.15 PFLOP/s.
 template <class C>
 __global__ void __launch_bounds__(C::NT, 2) k_weight_grad8(WeightGrad8Args a, int kt, int nt, int splits) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];

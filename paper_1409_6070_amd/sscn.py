@@ -840,6 +840,7 @@ class Rows8:
         self.rows, self.cols = rows, cols
         cs, ss = sscn_rows8_strides(cols)
         self.device = _gpu_device(device) if codes is None else codes.device
+        _need(self.device.type == "cuda", "device: a GPU")
         if codes is None:
             codes = torch.empty((rows, cs), dtype=torch.uint8, device=self.device)
         if scales is None:
@@ -902,6 +903,7 @@ class GroupNorm:
         self.code, self.tdtype = _TYPES[dtype]
         self.ws_bytes = [sscn_group_norm_workspace_bytes(self.code, rows_max, cols, groups, batch_max, b) for b in (0, 1)]
         self.device = _gpu_device(device)
+        _need(self.device.type == "cuda", "device: a GPU")
         self.ws = [None, None]
         self.call = GroupNormCall(dtype=self.code, act=ACTIVATIONS.index(act), cols=cols, groups=groups, eps=eps)
 
@@ -1003,6 +1005,7 @@ class Product8:
         self.w8_bytes = sscn_weight8_bytes(k, n)
         self.ws_bytes = sscn_product8_weight_grad_workspace_bytes(rows_max, k, n)
         self.device = _gpu_device(device)
+        _need(self.device.type == "cuda", "device: a GPU")
         self.w8 = torch.empty(self.w8_bytes, dtype=torch.uint8, device=self.device)
         self.w8_ptr, self.ws, self._set = self.w8.data_ptr(), None, False
 

@@ -5,6 +5,7 @@ import ctypes
 import math
 
 import pytest
+import torch
 
 from paper_1409_6070_amd import sscn
 
@@ -199,3 +200,13 @@ def test_structures_match_the_header():
     assert ctypes.sizeof(c) == 96
     r = sscn.Rows8Call
     assert [getattr(r, f).offset for f, _ in r._fields_] == [0, 8, 16, 24] and ctypes.sizeof(r) == 32
+
+
+@pytest.mark.parametrize("device", ["cpu", "cpu:0"])
+def test_classes_refuse_the_host(device):
+    from paper_1409_6070_amd.sscn import GroupNorm, Product8, Rows8
+    codes, scales = torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(4, 4, dtype=torch.uint8)
+    for make in (lambda: Rows8(4, 50, device), lambda: Rows8(4, 50, codes=codes, scales=scales),
+                 lambda: GroupNorm(10, 2, 4, 1, device=device), lambda: Product8(10, 2, 4, device=device)):
+        with pytest.raises(ValueError):
+            make()
