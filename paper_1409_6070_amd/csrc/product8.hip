@@ -160,7 +160,8 @@ struct P8Tile {
 // the one before it is, and one barrier a slab says that it has arrived and that the stage
 // of the one before is free.  Workgroups go on to further tiles, whose first slab is
 // loaded while the results of the last one are stored.  Bound by the matrix cores' feed: 32768 x
-// 4096 x 4096 500 us, 2.2 PFLOP/s; 8192^3 403, 2.7 (the instructions alone, on registers, 3.9).
+// 4096 x 4096 450 to 535 us by the clock (2.1 to 2.4 PFLOP/s); 8192^3 403, 2.7 (the instructions
+// alone, on registers, 3.9).
 template <class C>
 __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int64_t tiles, int64_t mt, int nt) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
