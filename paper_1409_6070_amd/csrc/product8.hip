@@ -22,6 +22,7 @@
 #include "rows8.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace sscn {
@@ -682,7 +683,7 @@ struct Wg8Tile {
 
 // A tile of dw over a run of rows: slabs of 64 rows through two LDS stages.  Bound by reading the
 // transposed operands, which takes LDS about as long as the products take the matrix cores:
-// 32768 x 4096 x 4096 940 to 960 us, 1.15 PFLOP/s.
+// 32768 x 4096 x 4096 926 to 970 us, 1.13 to 1.19 PFLOP/s.
 template <class C>
 __global__ void __launch_bounds__(C::NT, 2) k_weight_grad8(WeightGrad8Args a, int kt, int nt, int splits) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
@@ -932,18 +933,21 @@ struct WgPlan {
   int splits;
 };
 WgPlan plan_weight_grad8(int64_t rows, int64_t k, int64_t n) {
-  const int64_t slabs = (rows + WG_ROWS - 1) / WG_ROWS;
+  const double slabs = (double)((rows + WG_ROWS - 1) / WG_ROWS), part = (double)k * (double)n * 8.0 / 5e6;
   WgPlan best{false, 1};
   double least = 1e300;
   for (int big = 0; big < 2; ++big) {
     const int64_t tiles = tiles_of(k, n, big ? 256 : 128), held = big ? 256 : 512;
-    for (int s = 1, most = most_splits(rows, k, n, big != 0); s <= most; ++s) {
-      const double rounds = (double)((tiles * s + held - 1) / held);
-      const double t = rounds * (5.0 + (big ? 1.8 : 1.4) * (double)((slabs + s - 1) / s)) +
-                       (s > 1 ? 3.0 + (double)s * (double)k * (double)n * 8.0 / 5e6 : 0.0);
+    const double slab = big ? 1.8 : 1.4;
+    // slab * slabs / s + part * s is least at this s; divided rows take one round
+    const int s = (int)std::lround(
+        std::min(std::max(std::sqrt(slab * slabs / part), 1.0), (double)most_splits(rows, k, n, big != 0)));
+    for (int splits : {1, s}) {
+      const double t = (double)((tiles * splits + held - 1) / held) * (5.0 + slab * std::ceil(slabs / splits)) +
+                       (splits > 1 ? 3.0 + part * splits : 0.0);
       if (t < least) {
         least = t;
-        best = WgPlan{big != 0, s};
+        best = WgPlan{big != 0, splits};
       }
     }
   }

@@ -290,6 +290,51 @@ def test_large_products_of_whole_numbers(rows, k, n):
     assert torch.equal(dw.double(), torch.mm(xd.t().contiguous(), dyd)) and torch.equal(db.double(), dyd.sum(0))
 
 
+@pytest.mark.parametrize("rows,k,n", [(0, 5, 3), (64, 128, 128), (65, 1, 1), (128, 257, 129), (129, 130, 1), (191, 1, 300),
+                                      (193, 256, 256), (65600, 1, 1), (70001, 128, 127), (33000, 256, 257), (5000, 1030, 700)])
+def test_rows_of_weight_gradients_are_divided(rows, k, n):
+    """From one workgroup a tile to hundreds, whose runs of rows are of unequal lengths: exact sums of whole numbers (a
+    column of at most 70001 x 1), nothing behind the workspace and beside the result, and the same with no bias gradient."""
+    from paper_1409_6070_amd import sscn
+    g = torch.Generator(device="cuda").manual_seed(rows + k)
+    x, dy = (torch.randint(-1, 2, (rows, c), generator=g, device="cuda").float() for c in (k, n))
+    x8, dy8 = sscn.Rows8(rows, k).store(x), sscn.Rows8(rows, n).store(dy)
+    need = sscn.sscn_product8_weight_grad_workspace_bytes(rows, k, n)
+    ws = torch.full((need + 4096,), 0x7f, dtype=torch.uint8, device="cuda")
+    want = torch.mm(x.double().t().contiguous(), dy.double())
+    st = torch.cuda.current_stream().cuda_stream
+    for with_db in (True, False):
+        buf = torch.full((k, n + 5), 7.0, device="cuda")
+        db = torch.full((n + 5,), 7.0, device="cuda")
+        sscn.sscn_product8_weight_grad(x8.call, dy8.call, buf.data_ptr(), n + 5, db.data_ptr() if with_db else None,
+                                       ws.data_ptr(), need, st)
+        torch.cuda.synchronize()
+        assert torch.equal(buf[:, :n].double(), want) and (buf[:, n:] == 7).all() and (ws[need:] == 0x7f).all()
+        assert (db[n:] == 7).all()
+        assert torch.equal(db[:n].double(), dy.double().sum(0)) if with_db else (db == 7).all()
+
+
+def test_two_plans_at_once():
+    """Each with its own workspace, on a stream of its own, over the same 8-bit rows."""
+    from paper_1409_6070_amd.sscn import Product8, Rows8
+    rows, k, n = 20000, 512, 300
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x8, dy8 = (Rows8(rows, c).store(torch.randn(rows, c, generator=g, device="cuda")) for c in (k, n))
+    ps = [Product8(k, n, rows, d).set_weights(torch.randn(k, n, generator=g, device="cuda")) for d in ("bf16", "f32")]
+    step = lambda p: (p.forward(x8), p.input_grad(dy8), *p.weight_grad(x8, dy8))
+    want = [step(p) for p in ps]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ps]
+    got = []
+    for _ in range(3):
+        for p, s in zip(ps, streams):
+            with torch.cuda.stream(s):
+                got.append(step(p))
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(g, want[i % 2]))
+
+
 @pytest.mark.parametrize("rows,cols", [(20000, 1024), (40001, 1000)])
 def test_large_loads(rows, cols):
     """Results that go past the caches, of whole lines and not."""
