@@ -412,6 +412,32 @@ def test_streams_and_graphs():
             torch.cuda.synchronize()
 
 
+def test_two_plans_at_once():
+    """Each with its own workspaces, on a stream of its own, over the same rows and parameters."""
+    from paper_1409_6070_amd.sscn import GroupNorm
+    rows, cols = 60001, 100
+    x, dy, gain, shift = (t.cuda() for t in _make(rows, cols, "bf16", 1))
+    b = torch.tensor(_begins(rows, 9, 2), dtype=torch.int32, device="cuda")
+    plans = [GroupNorm(cols, g, rows, 9, "bf16", a) for g, a in ((10, "leaky"), (4, "silu"))]
+
+    def step(plan):
+        y, stats = plan.forward(x, b, gain, shift, out=torch.zeros_like(x))
+        dx, dgain, dshift = plan.backward(dy, x, stats, b, gain, shift, dx=torch.zeros_like(x))
+        return y, stats, dx, dgain, dshift
+
+    want = [step(p) for p in plans]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in plans]
+    got = []
+    for _ in range(3):
+        for p, s in zip(plans, streams):
+            with torch.cuda.stream(s):
+                got.append(step(p))
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        assert all(torch.equal(p, q) for p, q in zip(g, want[i % 2]))
+
+
 def test_gradients_against_differences():
     """Central differences of sum(w * y) in float32 values nudged by 2^-7, against the formula's derivative."""
     from paper_1409_6070_amd.sscn import GroupNorm
