@@ -29,9 +29,8 @@
 #include "common.h"
 #include "kernels.h"
 #include "lanes.h"
+#include "norm_rules.h"
 #include "rows8.h"
-
-#include <type_traits>
 
 namespace sscn {
 
@@ -236,14 +235,13 @@ struct Place {
   int rl, rpb, col, skip, split, group[V];
   bool on;
   __device__ inline Place(int first, int width, int per, int nt) {
-    const int nvec = (width + V - 1) / V;
-    rpb = nt / nvec;
-    rl = threadIdx.x / nvec;
-    const int t = threadIdx.x - rl * nvec;
-    on = rl < rpb;
-    const int at = min(t * V, width - V);
+    const RowLane lane((int)threadIdx.x, (width + V - 1) / V, nt);
+    rpb = lane.rpb;
+    rl = lane.rl;
+    on = lane.on;
+    const int at = min(lane.t * V, width - V);
     col = first + at;
-    skip = t * V - at;
+    skip = lane.t * V - at;
     split = min(V, ROW8_BLOCK - (col & (ROW8_BLOCK - 1)));
     group[0] = col / per;
     int left = per - (col - group[0] * per);  // columns of the group from here on
@@ -349,48 +347,6 @@ __device__ inline float strided_sum(int first, int end, int step, Value&& value)
   }
   return s;
 }
-
-// The rows of a run of `count` that a thread takes: n of them, `all` that every thread has and
-// `most` that any has.  Threads without any stay at the run's last row.
-struct Share {
-  int rl, n, all, most;
-  __device__ inline Share(int count, int rl_, int rpb, bool on) {
-    rl = min(rl_, count - 1);
-    all = count / rpb;
-    most = all + (all * rpb < count ? 1 : 0);
-    n = on ? all + (rl_ < count - all * rpb ? 1 : 0) : 0;
-  }
-};
-
-// U of a thread's rows in flight.  take(q, k, valid) gets row k; `valid` is the constant true
-// where every thread has that many.
-template <class Q, int U>
-struct Stream {
-  Q q[U];
-  template <class F>
-  __device__ inline void fetch(const F& from, int i, int last) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) from.load(q[u], min(i + u, last));
-  }
-  // the first rows have been fetched
-  template <class F, class Take>
-  __device__ inline void run(const F& from, const Share& s, Take&& take) {
-    int i = 0;
-    for (; i + U <= s.all; i += U) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) take(q[u], i + u, std::true_type{});
-      if (i + 2 * U <= s.all) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) from.load(q[u], i + U + u);
-      } else if (i + U < s.most) {
-        fetch(from, i + U, max(s.n - 1, 0));
-      }
-    }
-    if (i < s.most)
-#pragma unroll
-      for (int u = 0; u < U; ++u) take(q[u], i + u, i + u < s.n);
-  }
-};
 
 // ---------------------------------------------------------------------------
 // forward
@@ -1037,38 +993,6 @@ __global__ void __launch_bounds__(NT) k_group_norm_bwd_small(GroupNormArgs a, in
 // ---------------------------------------------------------------------------
 // how work is dealt
 
-// Elements of a thread's vector: 16 bytes of x; in the backward pass 8 bytes of bf16, whose
-// values and parameters take twice the registers (200001 rows of 100 in bf16 take 1.3 times as
-// long with eight elements; forward, 589824 rows of 256 take 1.4 times as long with four).
-int vec_of(bool bf16, int cols, bool backward) {
-  const int ve = bf16 && !backward ? 8 : 4;
-  return cols < ve ? 1 : ve;
-}
-
-struct Deal {
-  int threads, rpb;
-  int64_t chunk;
-  int chunks, most;  // and a bound on them that grows with the rows
-  bool join;         // few pieces a sample: they are joined by the last launch
-};
-
-// Workgroups, and rows of one, at least.  131072 x 512 backward from 8 bits: 43 + 68 us with 1024
-// workgroups, with 512 56 + 77, with 2048 47 + 81; 60001 x 100 bf16 forward: 13 + 14 with 8 rows a
-// thread, with 4 16.6 + 15.9, with 16 16.0 + 16.6.
-Deal deal(bool bf16, int64_t rows, int32_t cols, int32_t batch, bool backward) {
-  const int v = vec_of(bf16, cols, backward), nvec = (cols + v - 1) / v;
-  Deal d;
-  d.threads = nvec <= 256 ? 256 : v == 8 ? 512 : 1024;
-  d.rpb = d.threads / nvec;
-  const int64_t most = 1024 * 256 / d.threads;  // workgroups that the compute units hold at once
-  const int64_t least = 8 * d.rpb;              // rows that pay for a workgroup's sums
-  d.chunk = std::max(least, (rows + most - 1) / most);
-  d.chunks = (int)((rows + d.chunk - 1) / d.chunk);
-  d.most = (int)std::min(most, (rows + least - 1) / least);
-  d.join = d.chunks <= 16 * (int64_t)batch;
-  return d;
-}
-
 // Small samples.
 constexpr int SMALL_PARTS = 1024;  // workgroups of a slice
 // rows of a thread in registers: 128 bytes of x, or 64 of x and 64 of dy, with 256 threads
@@ -1090,10 +1014,10 @@ Small small_of(bool bf16, int64_t rows, int32_t cols, int32_t groups, int32_t ba
   for (int want = std::min(most, std::max(1, (512 + batch - 1) / batch));; --want) {
     s.slice = (groups + want - 1) / want;
     s.slices = (groups + s.slice - 1) / s.slice;
-    if (s.slices == 1 || (groups - (s.slices - 1) * s.slice) * per >= vec_of(bf16, cols, backward)) break;
+    if (s.slices == 1 || (groups - (s.slices - 1) * s.slice) * per >= norm_vec(bf16, cols, backward)) break;
   }
   s.width = s.slice * per;
-  const int v = vec_of(bf16, s.width, backward), nvec = (s.width + v - 1) / v;
+  const int v = norm_vec(bf16, s.width, backward), nvec = (s.width + v - 1) / v;
   const double mean = (double)rows / batch;  // rows of a sample; the largest have several times as many
   if (nvec > 512) return s;
   s.threads = nvec <= 256 && 3.0 * mean <= 256 / nvec * small_rows(256, bf16, backward) ? 256 : 512;
@@ -1118,7 +1042,7 @@ int small_lds(const Small& s, const GroupNormArgs& a, int columns, int each) {
 }
 
 template <typename T, int V, int NT, bool SILU>
-hipError_t forward_large(const GroupNormArgs& a, const Deal& d, hipStream_t st) {
+hipError_t forward_large(const GroupNormArgs& a, const NormDeal& d, hipStream_t st) {
   hipError_t e = hipSuccess;
   if (a.rows > 0) {
     hipLaunchKernelGGL((k_group_norm_sums<T, V, NT>), dim3(d.chunks), dim3(NT), sum_lds(d.rpb, a.cols, a.groups), st, a,
@@ -1160,13 +1084,13 @@ hipError_t forward(const GroupNormArgs& a, hipStream_t st) {
     if (s.threads == 256) return scalar ? forward_small<T, 1, 256, SILU>(a, s, st) : forward_small<T, VE, 256, SILU>(a, s, st);
     return scalar ? forward_small<T, 1, 512, SILU>(a, s, st) : forward_small<T, VE, 512, SILU>(a, s, st);
   }
-  const Deal d = deal(bf16, a.rows, a.cols, a.batch, false);
+  const NormDeal d = norm_deal(bf16, a.rows, a.cols, a.batch, false);
   if (a.cols < VE) return forward_large<T, 1, 256, SILU>(a, d, st);
   return d.threads == 256 ? forward_large<T, VE, 256, SILU>(a, d, st) : forward_large<T, VE, WIDE, SILU>(a, d, st);
 }
 
 template <typename T, int V, int NT, bool X8, bool SILU>
-hipError_t backward_large(const GroupNormArgs& a, const Deal& d, hipStream_t st) {
+hipError_t backward_large(const GroupNormArgs& a, const NormDeal& d, hipStream_t st) {
   hipLaunchKernelGGL((k_group_norm_bwd_sums<T, V, NT, X8, SILU>), dim3(d.chunks), dim3(NT),
                      sum_lds(d.rpb, a.cols, 2 * a.cols), st, a, d.chunk);
   hipError_t e = hipGetLastError();
@@ -1216,7 +1140,7 @@ hipError_t backward(const GroupNormArgs& a, hipStream_t st) {
       return scalar ? backward_small<T, 1, 256, X8, SILU>(a, s, st) : backward_small<T, 4, 256, X8, SILU>(a, s, st);
     return scalar ? backward_small<T, 1, 512, X8, SILU>(a, s, st) : backward_small<T, 4, 512, X8, SILU>(a, s, st);
   }
-  const Deal d = deal(bf16, a.rows, a.cols, a.batch, true);
+  const NormDeal d = norm_deal(bf16, a.rows, a.cols, a.batch, true);
   if (a.cols < 4) return backward_large<T, 1, 256, X8, SILU>(a, d, st);
   return d.threads == 256 ? backward_large<T, 4, 256, X8, SILU>(a, d, st) : backward_large<T, 4, 1024, X8, SILU>(a, d, st);
 }
@@ -1226,7 +1150,7 @@ hipError_t backward(const GroupNormArgs& a, hipStream_t st) {
 // Either way of dealing: which one a call takes may differ with its rows.
 size_t group_norm_workspace(bool bf16, int64_t rows, int32_t cols, int32_t groups, int32_t batch, bool backward) {
   if (rows <= 0) return 0;
-  const Deal d = deal(bf16, rows, cols, batch, backward);
+  const NormDeal d = norm_deal(bf16, rows, cols, batch, backward);
   const size_t pieces = (size_t)d.most + (size_t)batch;
   if (!backward) return pieces * 2 * (size_t)groups * 4;
   const size_t large = ((pieces + (size_t)d.most) * 2 * (size_t)cols + 2 * (size_t)batch * (size_t)groups) * 4;
