@@ -757,7 +757,7 @@ __global__ void __launch_bounds__(1024) k_group_norm_params(GroupNormArgs a, int
 }
 
 // sum t / n and sum t h / n of a slice of a sample's groups, out of its pieces: done(k, group of
-// the slice, value) with k = 0 for the first.  smem: [2][max(1, NT / width)][width].
+// the slice, value) with k = 0 for the first.  smem: [2][join_lanes(NT, width)][width].
 template <int NT, class Done>
 __device__ inline void join_means(const GroupNormArgs& a, const float* piece, int64_t chunk, const Span& s, int first,
                                   int groups, int per, float* smem, Done&& done) {
@@ -765,7 +765,7 @@ __device__ inline void join_means(const GroupNormArgs& a, const float* piece, in
   const int64_t c0 = lo / chunk;
   const int pieces = (int)((hi - 1) / chunk - c0) + 1, step = 2 * a.cols;
   const float rn = 1.f / ((float)(int)(hi - lo) * (float)per);
-  const int width = groups * per, lanes = min(max(1, NT / width), pieces);
+  const int width = groups * per, lanes = min(join_lanes(NT, width), pieces);
   __syncthreads();  // (what smem held has been read)
   for (int i = threadIdx.x; i < lanes * width; i += NT) {
     const int l = i / width, col = first + i - l * width;
@@ -814,9 +814,6 @@ __device__ inline void join_means(const GroupNormArgs& a, const float* piece, in
                  },
                  [&](int g, float sum) { done(k, g, sum * rn); });
 }
-int join_floats(int nt, int width) { return 2 * std::max(1, nt / width) * width; }
-
-constexpr int BWD_COLS = 64;  // columns of a sample that a workgroup of the second launch sums
 
 // Where samples have many pieces, a launch of its own.  Its first `sample_blocks` workgroups: the means of
 // t and t h over the samples and some of their groups; the others: the gain's and shift's
@@ -849,7 +846,7 @@ __global__ void __launch_bounds__(NT) k_group_norm_bwd_rows(GroupNormArgs a, int
   extern __shared__ float smem[];  // JOIN: join_floats, then [2][groups]
   const BwdParts parts = bwd_parts(a, chunks);
   const int per = a.per;
-  float* joined = smem + 2 * max(1, NT / a.cols) * a.cols;
+  float* joined = smem + join_floats(NT, a.cols);
   if (JOIN && (int)blockIdx.x >= chunks) {
     param_sums<NT>(a, parts.chunk, chunks, (int)blockIdx.x - chunks, smem);
     return;
@@ -1103,13 +1100,9 @@ hipError_t backward_large(const GroupNormArgs& a, const NormDeal& d, hipStream_t
     hipLaunchKernelGGL(kernel, dim3(d.chunks + param_blocks<NT>(a.cols)), dim3(NT), lds, st, a, d.chunk, d.chunks);
     return hipGetLastError();
   }
-  const int per = a.per;
-  const int slice = (int)std::max<int64_t>(
-      1, std::min<int64_t>(BWD_COLS / per, (int64_t)a.batch * a.groups / 512));  // (enough workgroups first)
-  const int blocks = (int)std::min<int64_t>((int64_t)a.batch * ((a.groups + slice - 1) / slice), 1 << 16);
-  hipLaunchKernelGGL(k_group_norm_bwd_means, dim3((unsigned)(blocks + param_blocks<1024>(a.cols))), dim3(1024),
-                     std::max(1024, join_floats(1024, std::min(slice, a.groups) * per)) * 4, st, a, d.chunk, d.chunks,
-                     blocks, slice);
+  const NormMeans m = norm_means(a.batch, a.groups, a.per);
+  hipLaunchKernelGGL(k_group_norm_bwd_means, dim3((unsigned)(m.blocks + param_blocks<1024>(a.cols))), dim3(1024),
+                     m.floats * 4, st, a, d.chunk, d.chunks, m.blocks, m.slice);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((k_group_norm_bwd_rows<T, V, NT, X8, SILU, false>), dim3(d.chunks), dim3(NT), 0, st, a, d.chunk,

@@ -94,4 +94,24 @@ struct Stream {
   }
 };
 
+// Threads that share a column of `width` where a sample's pieces are joined, and the floats of LDS
+// that they fill: two sums of every column from each.
+constexpr inline int join_lanes(int nt, int width) { return nt / width > 1 ? nt / width : 1; }
+constexpr inline int join_floats(int nt, int width) { return 2 * join_lanes(nt, width) * width; }
+
+// The backward pass's means by a launch of their own, 1024 threads a workgroup: `slice` groups of a
+// sample at a time (64 columns, but enough workgroups first), `blocks` workgroups, and their LDS: as
+// much as any width up to the slice's fills, since the last slice may be narrower and its columns
+// have more threads (2 groups of 9 fill 2016 floats, 3 only 1998).
+struct NormMeans {
+  int slice, blocks, floats;
+};
+inline NormMeans norm_means(int32_t batch, int32_t groups, int per) {
+  NormMeans m;
+  m.slice = (int)std::max<int64_t>(1, std::min<int64_t>(64 / per, (int64_t)batch * groups / 512));
+  m.blocks = (int)std::min<int64_t>((int64_t)batch * ((groups + m.slice - 1) / m.slice), 1 << 16);
+  m.floats = 2 * std::max(1024, std::min(m.slice, groups) * per);
+  return m;
+}
+
 }  // namespace sscn

@@ -238,6 +238,14 @@ def test_many_rows(rows, cols, groups, batch, dtype):
     _check(rows, cols, groups, _begins(rows, batch, 5), dtype, "leaky", x8=batch % 2 == 1)
 
 
+@pytest.mark.parametrize("rows,cols,groups,batch,dtype", [(24001, 288, 32, 60, "f32"), (24001, 288, 32, 60, "bf16"),
+                                                          (1100, 3709, 3709, 8, "f32")])
+def test_joined_slices_of_unequal_width(rows, cols, groups, batch, dtype):
+    """One sample of nearly all rows among short ones, its pieces joined by a launch of their own in slices of groups
+    of which the last is narrower."""
+    _check(rows, cols, groups, [0] + list(range(rows - batch + 1, rows + 1)), dtype, "silu")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_small_samples(dtype):
     """One launch: slices of groups of unequal number, samples that fill the registers and ones that outgrow them."""

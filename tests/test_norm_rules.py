@@ -96,3 +96,33 @@ def test_rows_stay_in_their_piece(tmp_path):
     """Every load of every thread, also of those that have no row or no vector of one, over rows of 1 to 4096
     columns and runs around multiples of the rows in flight; every row is taken once."""
     assert int(run_host(tmp_path, ROWS)) > 100000
+
+
+MEANS = r"""
+#include "norm_rules.h"
+#include <cstdio>
+using namespace sscn;
+int main() {
+  long n = 0;
+  for (int per = 1; per <= 4096; ++per)
+    for (int groups = 1; groups * per <= 4096; groups = groups < 70 ? groups + 1 : groups + groups / 9)
+      for (int batch : {1, 2, 5, 8, 31, 60, 63, 100, 700, 5000}) {
+        const NormMeans m = norm_means(batch, groups, per);
+        if (m.slice < 1 || m.blocks < 1 || m.floats < 1024) return 1;  // (1024: the parameters' sums)
+        for (int g0 = 0; g0 < groups; g0 += m.slice) {  // the last slice may be narrower
+          const int width = std::min(m.slice, groups - g0) * per;
+          if (2 * std::max(1, 1024 / width) * width > m.floats) {
+            printf("%d groups of %d, batch %d: %d columns in %d floats\n", groups, per, batch, width, m.floats);
+            return 1;
+          }
+        }
+        ++n;
+      }
+  printf("%ld\n", n);
+}
+"""
+
+
+def test_joined_means_stay_in_their_lds(tmp_path):
+    """[2][lanes of a column][columns] floats of every slice of groups that a workgroup joins."""
+    assert int(run_host(tmp_path, MEANS)) > 100000
