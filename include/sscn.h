@@ -307,8 +307,8 @@ SSCN_API sscn_status sscn_layer_norm_backward(int32_t dtype, const void* d_dy, i
  * d_begin is a device array of batch + 1 int32, non-decreasing, within 0 .. rows, as
  * sscn_rulebook_build_grouped takes it; null: `batch` samples of rows / batch rows each
  * (rows must be a multiple of batch).  Rows before the first and behind the last
- * sample are neither read nor written, and a sample may have no rows.  With n the
- * values of a sample and group:
+ * sample are not written; they may be read, but no result depends on their values.
+ * A sample may have no rows.  With n the values of a sample and group:
  *   mean = sum x / n,  r = 1 / sqrt(sum (x - mean)^2 / n + eps),
  *   h = (x - mean) r,  z = h gain + shift,  y = act(z).
  * Offsets that decrease or lie outside 0 .. rows give undefined results within the

@@ -940,8 +940,8 @@ class GroupNorm:
 
     def forward(self, x: torch.Tensor, begin, gain: Optional[torch.Tensor] = None, shift: Optional[torch.Tensor] = None,
                 out: Optional[torch.Tensor] = None):
-        """(y, stats [2, batch, groups]: means and 1 / deviations); out may be x. Rows outside all samples are left
-        as they were (undefined in a new tensor)."""
+        """(y, stats [2, batch, groups]: means and 1 / deviations); out may be x. Rows outside all samples change no
+        result and are left as they were (undefined in a new tensor)."""
         rows, xs = self._rows(x, "x")
         batch, ws = self._prepare(rows, begin, gain, shift, 0)
         if out is None:

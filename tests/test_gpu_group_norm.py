@@ -309,6 +309,32 @@ def test_bad_values_stay_in_their_sample_and_group():
         assert dx[bad].isnan().all() and torch.equal(dx[~bad], cdx[~bad])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols,begin", [(300, 60, [40, 100, 100, 250]), (30000, 100, [5000, 5001, 28000]),
+                                             (5000, 12, [2000, 4000]), (40000, 16, [30000, 30000, 30001, 39999])])
+def test_rows_outside_the_samples_do_not_matter(rows, cols, begin, dtype):
+    """NaN, infinities and large values there: the samples' results are the same to the bit, and nothing is written."""
+    from paper_1409_6070_amd.sscn import GroupNorm, Rows8
+    x, dy, gain, shift = (t.cuda() for t in _make(rows, cols, dtype, 5))
+    b = torch.tensor(begin, dtype=torch.int32, device="cuda")
+    plan = GroupNorm(cols, 2, rows, len(begin) - 1, dtype, "leaky")
+    inside = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    inside[begin[0]: begin[-1]] = True
+
+    def results():
+        y, stats = plan.forward(x, b, gain, shift, out=torch.full_like(x, 3.0))
+        got = [y, stats]
+        for held in (x, Rows8(rows, cols).store(x)):
+            got += plan.backward(dy, held, stats, b, gain, shift, dx=torch.full_like(x, 3.0))
+        return got
+
+    want = results()
+    assert all((want[i][~inside] == 3).all() and want[i][inside].isfinite().all() for i in (0, 2, 5))
+    for value in (float("nan"), float("inf"), 1e30):
+        x[~inside], dy[~inside] = value, value
+        assert all(torch.equal(p, q) for p, q in zip(results(), want))
+
+
 def test_constant_groups():
     """No variance: r = 1 / sqrt(eps), h is zero or a rounding of the mean."""
     from paper_1409_6070_amd.sscn import GroupNorm
