@@ -321,6 +321,7 @@ typedef enum {
   SSCN_ACT_SILU = 3   /* z / (1 + exp(-z))                                 */
 } sscn_activation;
 #define SSCN_GROUP_NORM_MAX_COLS 4096
+#define SSCN_GROUP_NORM_MAX_BATCH 1073741824
 typedef struct {
   int32_t dtype;           /* of x, y, dy and dx; the arithmetic is float32            */
   int32_t act;             /* sscn_activation                                          */

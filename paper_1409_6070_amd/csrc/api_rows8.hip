@@ -38,7 +38,8 @@ bool product_side_ok(int32_t n) { return n >= 1 && n <= SSCN_PRODUCT8_MAX; }
 
 bool shape_ok(int32_t dtype, int64_t rows, int32_t cols, int32_t groups, int32_t batch) {
   return known_dtype(dtype) && rows >= 0 && rows <= SSCN_MAX_ROWS && cols >= 1 && cols <= SSCN_GROUP_NORM_MAX_COLS &&
-         groups >= 1 && cols % groups == 0 && batch >= 0;
+         groups >= 1 && cols % groups == 0 && batch >= 0 &&
+         batch <= SSCN_GROUP_NORM_MAX_BATCH;  // (sample numbers pass it by a grid's step in 32 bits)
 }
 
 sscn_status check_norm(const sscn_group_norm* n, bool backward) {

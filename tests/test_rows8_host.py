@@ -51,6 +51,16 @@ def test_group_norm_backward_refuses(bad):
     assert _bwd(_norm(**bad)) == INVALID
 
 
+@pytest.mark.parametrize("batch", [(1 << 30) + 1, (1 << 31) - 1024, (1 << 31) - 1])
+def test_group_norm_sample_numbers_stay_in_32_bits(batch):
+    """More samples than the kernels' counters, which go on by a grid's step, can pass."""
+    for backward in (0, 1):
+        with pytest.raises(sscn.SSCNError):
+            sscn.sscn_group_norm_workspace_bytes(1, 12, 8, 2, batch, backward)
+        assert sscn.sscn_group_norm_workspace_bytes(1, 12, 8, 2, 1 << 30, backward) > 0
+    assert _fwd(_norm(batch=batch)) == INVALID and _bwd(_norm(batch=batch)) == INVALID
+
+
 def test_group_norm_results_and_workspace():
     n = _norm()
     assert _fwd(None) == INVALID and _bwd(None) == INVALID
