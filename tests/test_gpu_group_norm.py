@@ -309,6 +309,48 @@ def test_bad_values_stay_in_their_sample_and_group():
         assert dx[bad].isnan().all() and torch.equal(dx[~bad], cdx[~bad])
 
 
+# samples in registers, pieces joined by the last launch and by a launch of their own, the longest rows
+PATHS = [(400, 60, 4, [0, 100, 100, 370]), (1500, 34, 17, list(range(0, 1501))), (30000, 100, 10, [0, 20000, 30000]),
+         (200001, 20, 2, [0, 200001]), (24001, 288, 32, [0] + list(range(24001 - 59, 24002))), (9, 4096, 8, [0, 9])]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols,groups,begin", PATHS)
+def test_workspaces_are_as_large_as_they_say(rows, cols, groups, begin, dtype):
+    """Exactly the bytes asked for, between bytes that have to stay as they were; results as from a plan, and as from
+    one for more rows and samples."""
+    from paper_1409_6070_amd import sscn
+    from paper_1409_6070_amd.sscn import GroupNorm
+    x, dy, gain, shift = (t.cuda() for t in _make(rows, cols, dtype, 7))
+    b = torch.tensor(begin, dtype=torch.int32, device="cuda")
+    batch, code = len(begin) - 1, int(dtype == "bf16")
+    want = None
+    for more in (0, 1, 5000):
+        plan = GroupNorm(cols, groups, rows + more, batch + more, dtype, "leaky", EPS)
+        y, stats = plan.forward(x, b, gain, shift, out=torch.zeros_like(x))
+        got = (y, stats) + plan.backward(dy, x, stats, b, gain, shift, dx=torch.zeros_like(x))
+        want = got if want is None else want
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+    call = sscn.GroupNormCall(dtype=code, act=2, rows=rows, cols=cols, groups=groups, batch=batch, eps=EPS,
+                              d_begin=b.data_ptr(), d_gain=gain.data_ptr(), d_shift=shift.data_ptr(), d_x=x.data_ptr(),
+                              x_stride=cols)
+    y, dx, stats = torch.zeros_like(x), torch.zeros_like(x), torch.zeros(2, batch, groups, device="cuda")
+    dgain, dshift = torch.empty(2, cols, device="cuda").unbind(0)
+    call.d_stats = stats.data_ptr()
+    stream = torch.cuda.current_stream().cuda_stream
+    for backward in (0, 1):
+        need = sscn.sscn_group_norm_workspace_bytes(code, rows, cols, groups, batch, backward)
+        ws = torch.full((need + 8192,), 0x5A, dtype=torch.uint8, device="cuda")
+        at = ws.data_ptr() + 4096
+        if backward:
+            sscn.sscn_group_norm_backward(call, dy.data_ptr(), cols, dx.data_ptr(), cols, dgain.data_ptr(), dshift.data_ptr(),
+                                          at, need, stream)
+        else:
+            sscn.sscn_group_norm_forward(call, y.data_ptr(), cols, at, need, stream)
+        assert (ws[:4096] == 0x5A).all() and (ws[4096 + need:] == 0x5A).all()
+    assert all(torch.equal(p, q) for p, q in zip((y, stats, dx, dgain, dshift), want))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,cols,begin", [(300, 60, [40, 100, 100, 250]), (30000, 100, [5000, 5001, 28000]),
                                              (5000, 12, [2000, 4000]), (40000, 16, [30000, 30000, 30001, 39999])])
