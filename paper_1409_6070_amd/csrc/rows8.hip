@@ -27,13 +27,13 @@ __device__ inline Run8<T> load_run(const T* p, int n) {
   return r;
 }
 
-// The bits of a run's largest magnitude; any that is not finite passes 0x7f800000 or counts
-// for nothing (a float32 NaN).
+// The bits of a run's largest magnitude, at least 0x7f800000 where one is not finite.  As integers:
+// a maximum of floats loses what it has at a signalling NaN.
 __device__ inline uint32_t largest(const Run8<float>& r) {
-  float m = 0.f;
+  uint32_t m = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(r.e[e]));
-  return __float_as_uint(m);
+  for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(r.e[e]) & 0x7fffffffu);
+  return m;
 }
 __device__ inline uint32_t largest(const Run8<__bf16>& r) {
   typedef uint16_t U16x2 __attribute__((ext_vector_type(2)));

@@ -165,6 +165,33 @@ def test_nan_and_infinities_stay_alone():
         assert (got[np.isfinite(want)] == want[np.isfinite(want)]).all()
 
 
+@pytest.mark.parametrize("bits", [0x7f800001, 0x7fa55555, 0x7fbfffff, 0x7fc00000, 0x7fffffff])
+def test_every_kind_of_nan_leaves_its_block_alone(bits):
+    """Signalling ones too, before, at and behind the place of the block's largest value."""
+    from paper_1409_6070_amd.sscn import Product8, Rows8
+    at = torch.arange(24)
+    for most in (0, 7, 9, 23):
+        for sign in (0, 1 << 31):
+            x = torch.ones(24, 130)
+            x[:, most] = 300.0
+            clean = _held(_np(x))[0]
+            v = np.array([bits | sign], dtype=np.uint32).view(np.int32)[0]
+            x.view(torch.int32)[at, at] = int(v)
+            for t in (x, (x.view(torch.int32) >> 16).to(torch.int16).view(torch.bfloat16)):
+                if not t.float().isnan()[at, at].all():
+                    continue  # (a NaN whose upper half is an infinity's)
+                got = _np(Rows8(24, 130).store(t.cuda()).load("f32"))
+                assert np.isnan(got[at, at]).all() and np.isnan(got).sum() == 24
+                assert (got == clean)[~np.isnan(got)].all()
+            w = x[most].clone()[None].repeat(130, 1)  # a column of NaN
+            w[0, 1] = 300.0                           # 288 in steps of 32
+            layer = Product8(130, 130, 1, "f32").set_weights(w.cuda())
+            e = torch.zeros(1, 130)
+            e[0, 0] = 1.0
+            y = _np(layer.forward(Rows8(1, 130).store(e.cuda())))[0]
+            assert np.isnan(y[most]) and np.isnan(y).sum() == 1 and y[1] == 288.0
+
+
 def test_offsets_past_32_bits():
     from paper_1409_6070_amd.sscn import Rows8
     rows, cols = (1 << 20) + 77, 4099  # codes 4.3e9 bytes, x 8.6e9
