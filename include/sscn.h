@@ -395,11 +395,11 @@ SSCN_API sscn_status sscn_weight8_store(int32_t dtype, const void* d_w, int64_t 
  *   y = xq wq + bias        x: rows of k columns, y [rows][n], bias [n] float32 or null;
  *   dx = dyq wq^T           dy: rows of n columns, dx [rows][k];
  *   dw = xq^T dyq,  db = sum over rows of dyq        float32, overwritten, db may be null.
- * y and dx have type dtype and are rounded once.  In float32 the products are exact and
- * their sums float32; in bf16 the matrix instructions drop, of every eight products, what
- * lies below 2^-13 of the largest: 1.5e-5 to 4e-5 of the result on values like a network's,
- * 8.5e-4 of the sum of the products' magnitudes at most.  dw and db do not depend on the
- * device's scheduling.  With no rows dw and db are zero.  The weight gradient's
+ * y and dx have type dtype and are rounded once.  In float32 the products are exact (held
+ * values under 2^-130 are taken in steps of 2^-133) and their sums float32, also dw's; in
+ * bf16 the matrix instructions drop, of every eight products, what lies below 2^-13 of the
+ * largest: 1.5e-5 to 4e-5 of the result on values like a network's, 8.5e-4 of the sum of the
+ * products' magnitudes at most.  dw and db do not depend on the device's scheduling.  With no rows dw and db are zero.  The weight gradient's
  * workspace grows with rows. */
 SSCN_API sscn_status sscn_product8_forward(int32_t dtype, const sscn_rows8* x, const void* d_weight8,
                                            size_t weight8_bytes, int32_t n, const float* d_bias, void* d_y,

@@ -369,7 +369,8 @@ __global__ void __launch_bounds__(C::NW * 64, 2) k_product8(Product8Args a, int6
   }
 }
 
-// Sixteen codes times a power of two as sixteen bf16 values.
+// Sixteen codes times a power of two as sixteen bf16 values: exact from 2^-130 on, where bf16's
+// smallest steps, 2^-133, are those of a code's four bits.
 struct Codes16 {
   u32x4 lo, hi;
 };

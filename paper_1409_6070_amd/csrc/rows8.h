@@ -35,7 +35,7 @@ __device__ inline bool is_finite(float x) { return (__float_as_uint(x) & 0x7f800
 typedef float row8_f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 row8_bf16x2 __attribute__((ext_vector_type(2)));
 
-// Four codes times a power of two, in float32 (exact) or bf16 (exact but for values under 2^-133).
+// Four codes times a power of two, in float32 (exact).
 __device__ inline void row8_values4(uint32_t w, float scale, float* f) {
   const row8_f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, false);
   const row8_f32x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, true);

@@ -409,6 +409,31 @@ def test_gradients_against_differences():
     assert torch.equal(db, dy.sum(0))
 
 
+def test_products_of_the_smallest_values():
+    """Held values from 2^-130 on are exact in float32 products, at every number of rows that takes another kernel; smaller
+    ones are taken in steps of 2^-133, each off by half a step at most."""
+    from paper_1409_6070_amd.sscn import Product8, Rows8
+    k, n = 300, 200
+    g = torch.Generator().manual_seed(3)
+    for rows in (1, 20, 60, 3000, 9000):
+        m, j, q = (torch.randint(-8, 9, s, generator=g).float() for s in ((rows, k), (k, n), (rows, n)))
+        for low in (0, 5):  # (x 2^-5: values under 2^-130 too)
+            x = (m.double() * 2.0 ** (-130 - low)).float()
+            p = Product8(k, n, rows, "f32").set_weights((j * 2.0 ** 60).cuda())
+            x8, dy8 = Rows8(rows, k).store(x.cuda()), Rows8(rows, n).store((q * 2.0 ** 60).cuda())
+            held = _np(x8.load("f32"))
+            assert low or (held == _np(x)).all()
+            w, dy = _np(j) * 2.0 ** 60, _np(q) * 2.0 ** 60
+            y, dw = _np(p.forward(x8)), _np(p.weight_grad(x8, dy8)[0])
+            if low == 0:  # whole numbers up to 64 * 9000 of 2^-70
+                assert (y == held @ w).all() and (dw == held.T @ dy).all()
+            else:
+                off = 2.0 ** -134 * (np.abs(held) < 2.0 ** -130)
+                for got, a, b, terms in ((y, held, w, k), (dw, held.T, dy, rows)):
+                    bound = (off if a is held else off.T) @ np.abs(b)
+                    assert (np.abs(got - a @ b) <= bound + (44 + terms / 32 + 520) * U * (np.abs(a) @ np.abs(b) + bound)).all()
+
+
 def test_a_nan_stays_in_its_row():
     from paper_1409_6070_amd.sscn import Product8, Rows8
     for dtype in ("f32", "bf16"):
