@@ -311,6 +311,10 @@ SSCN_API sscn_status sscn_layer_norm_backward(int32_t dtype, const void* d_dy, i
  * A sample may have no rows.  With n the values of a sample and group:
  *   mean = sum x / n,  r = 1 / sqrt(sum (x - mean)^2 / n + eps),
  *   h = (x - mean) r,  z = h gain + shift,  y = act(z).
+ * The work is dealt by the samples' mean length.  Where that is some hundreds of rows at
+ * most, a sample is the work of few workgroups however long it is (16 to 21 us for 1000 rows
+ * of 100 channels): batches of very unequal lengths take many times as long as equal ones.
+ * Where it is more, a sample that holds most rows makes a call 1.2 to 4 times as long.
  * Offsets that decrease or lie outside 0 .. rows give undefined results within the
  * call's arrays.  A NaN or an infinity makes its sample's group NaN and leaves the
  * others alone. */

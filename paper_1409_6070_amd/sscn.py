@@ -832,7 +832,8 @@ class LayerNorm:
 class Rows8:
     """Rows [rows, cols] held in 8 bits (e4m3 codes, a power of two for each row and 128 columns), through
     sscn_rows8_*: activations kept for the backward pass, and the operands of Product8. Allocates its two arrays, or
-    takes given ones: codes [rows, cols rounded up to 16] and scales [rows, blocks rounded up to 4], uint8, contiguous."""
+    takes given ones: codes [rows, cols rounded up to 16] and scales [rows, blocks rounded up to 4], uint8, contiguous,
+    zero behind the columns and blocks."""
 
     def __init__(self, rows: int, cols: int, device: str = "cuda", codes: Optional[torch.Tensor] = None,
                  scales: Optional[torch.Tensor] = None):

@@ -1,9 +1,5 @@
 """How group norm's kernels deal rows and LDS, compiled for the host: the addresses that they read, which no result
 shows (no GPU)."""
-import ctypes
-
-import pytest
-
 from tests.test_host_rules import run_host
 
 ROWS = r"""
